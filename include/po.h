@@ -528,6 +528,33 @@ po_status po_op_qkv_rope_fp8(const void* dev_a_codes, const float* dev_a_scales,
                              int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t K, float q_scale,
                              void* hip_stream);
 
+/* ---- FP8 linear layers with a scale per block of 128 (the other public convention of E4M3 checkpoints): an outlier then
+ * coarsens its own block only, not its whole row.  Activations have blocks of one row x 128 values of K, weights of
+ * 128 x 128.  A block with amax = max|x| becomes codes e4m3(x * (448 / amax)), round to nearest even, and the scale
+ * amax / 448, in single float32 operations, with amax raised to 448 * 2^-126 where it is below that and not zero (so that
+ * both quotients are normal numbers); amax == 0: codes 0, scale 1.  Finite inputs.
+ *
+ * po_op_quantize_blocks: codes [rows, K] (one byte each) and scales of the bf16 tensor x [rows, K], K % 128 == 0.
+ * block_rows 1: scales [K / 128][rows] (a block column's rows side by side, as the product reads them); block_rows 128:
+ * scales [ceil(rows / 128)][K / 128], the last row of blocks as high as the rows that are left.  dev_codes must not overlap
+ * dev_x. */
+po_status po_op_quantize_blocks(const void* dev_x, void* dev_codes, float* dev_scales, int64_t rows, int32_t K,
+                                int32_t block_rows, void* hip_stream);
+/* C[m][n] = sum over blocks b of a_scales[b][m] * w_scales[n / 128][b] * (product of the codes of block b), accumulated in
+ * fp32, result bf16.  Operands as po_op_quantize_blocks makes them (a: block_rows 1, w: block_rows 128).  Epilogues as in
+ * po_op_linear_fp8: 0: C [M, N]; 1: C = ... + residual [M, N] (may alias C); 2: w_codes in the interleaved gate/up order
+ * (po_op_pack_gate_up with PO_BF16 and K / 2 packs rows of K codes), w_scales [2][ceil(N / 256)][K / 128]: those of the gate
+ * matrix, then those of the up matrix, C [M, N/2] = silu(gate) * up.  K % 128 == 0, N % 64 == 0.
+ * dev_scratch (may be NULL; 16-byte aligned) lets a launch with few output tiles divide its reduction over K between
+ * workgroups, which it does where that is expected to take less time and its fp32 partial sums fit; they are added in a fixed
+ * order.  po_linear_fp8_block_bytes: the scratch that a shape can use (0: none; host only).  A row's result does not
+ * depend on the values of other rows; whether a launch is split, and so how its sums are rounded, depends on M, N, K and
+ * scratch_bytes. */
+po_status po_linear_fp8_block_bytes(int64_t M, int32_t N, int32_t K, size_t* scratch_bytes);
+po_status po_op_linear_fp8_block(int32_t epilogue, const void* dev_a_codes, const float* dev_a_scales, const void* dev_w_codes,
+                                 const float* dev_w_scales, void* dev_c, const void* dev_residual, void* dev_scratch,
+                                 size_t scratch_bytes, int64_t M, int32_t N, int32_t K, void* hip_stream);
+
 /* ---- Micro-peaks of the machine, for the benchmark to report beside the nominal peaks (measurement only; the
  * paper's claim that the workload is compute-bound, Section 2.3, is priced against what the board sustains).
  * po_op_mfma_peak: every wavefront of a chip-filling grid (1024 workgroups of 256 * waves_per_simd threads)

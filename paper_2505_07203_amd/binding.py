@@ -42,6 +42,7 @@ EXPORTS = [
     "po_op_attention_split_prefix", "po_attention_tile", "po_gemm_tile", "po_gemm_turns", "po_gemm_f32_tile", "po_op_linear_fp8_split",
     "po_sched_create", "po_sched_destroy", "po_sched_set_jct_model", "po_sched_fit_jct_model", "po_sched_push",
     "po_sched_size", "po_sched_pick", "po_sched_remove", "po_op_rope_static", "po_op_mfma_peak", "po_op_stream_copy",
+    "po_op_quantize_blocks", "po_linear_fp8_block_bytes", "po_op_linear_fp8_block",
 ]
 
 
@@ -142,6 +143,9 @@ def lib() -> C.CDLL:
     L.po_op_rmsnorm_quantize.argtypes = [vp, vp, vp, vp, i64, i32, f32, vp]
     L.po_op_linear_fp8.argtypes = [i32, vp, vp, vp, vp, vp, vp, i64, i32, i32, vp]
     L.po_op_qkv_rope_fp8.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, i64, i64, i32, i32, i32, i32, f32, vp]
+    L.po_op_quantize_blocks.argtypes = [vp, vp, vp, i64, i32, i32, vp]
+    L.po_linear_fp8_block_bytes.argtypes = [i64, i32, i32, C.POINTER(sz)]
+    L.po_op_linear_fp8_block.argtypes = [i32, vp, vp, vp, vp, vp, vp, vp, sz, i64, i32, i32, vp]
     f64 = C.c_double
     L.po_sched_create.argtypes = [f64, C.POINTER(vp)]
     L.po_sched_destroy.argtypes = [vp]
@@ -534,6 +538,73 @@ def po_op_linear_fp8_split(a_codes, a_scales, w_codes, w_scales, residual, scrat
                                        residual.data_ptr(), scratch.data_ptr(), scratch_bytes, M, N, K, _stream(), C.byref(n)))
     torch.cuda.synchronize()
     return (c if n.value > 1 else None), n.value
+
+
+def _operands(**tensors):
+    """checks what the library cannot: contiguous tensors of the named dtype on the current device, whose stream the call
+    uses.  name=(tensor or None, dtype name)"""
+    import torch
+    for name, (t, dtype) in tensors.items():
+        if t is None:
+            continue
+        if t.dtype != getattr(torch, dtype):
+            raise ValueError(f"{name}: {dtype} expected, got {t.dtype}")
+        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{name}: on {t.device}, not on the current GPU")
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: not contiguous")
+
+
+def _shape(name, t, shape):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
+
+
+def po_op_quantize_blocks(x, block_rows: int = 1):
+    """bf16 [rows, K] -> (uint8 codes [rows, K], float32 scales): block_rows 1: blocks of a row x 128, scales [K/128, rows];
+    block_rows 128: blocks of 128 x 128, scales [ceil(rows/128), K/128]"""
+    import torch
+    _operands(x=(x, "bfloat16"))
+    rows, K = x.shape
+    codes = torch.empty((rows, K), dtype=torch.uint8, device=x.device)
+    shape = (K // 128, rows) if block_rows == 1 else ((rows + 127) // 128, K // 128)
+    scales = torch.empty(shape, dtype=torch.float32, device=x.device)
+    check(lib().po_op_quantize_blocks(x.data_ptr(), codes.data_ptr(), scales.data_ptr(), rows, K, block_rows, _stream()))
+    return codes, scales
+
+
+def po_linear_fp8_block_bytes(M: int, N: int, K: int) -> int:
+    """bytes of scratch that po_op_linear_fp8_block can use at this shape (host only)"""
+    n = C.c_size_t(0)
+    check(lib().po_linear_fp8_block_bytes(M, N, K, C.byref(n)))
+    return n.value
+
+
+def po_op_linear_fp8_block(a_codes, a_scales, w_codes, w_scales, residual=None, out=None, silu_mul=False, scratch=None):
+    """a_codes [M, K], a_scales [K/128, M]; w_codes [N, K], w_scales [ceil(N/128), K/128] (silu_mul: gate and up rows interleaved
+    in blocks of 32, scales [2, ceil(N/256), K/128]) -> bf16 [M, N] (silu_mul: [M, N/2]).  scratch: a uint8 tensor to be used
+    instead of one of po_linear_fp8_block_bytes (an empty one: the reduction is not split)"""
+    import torch
+    M, K = a_codes.shape
+    N = w_codes.shape[0]
+    if silu_mul and residual is not None:
+        raise ValueError("residual: not with silu_mul")
+    epi = 2 if silu_mul else (1 if residual is not None else 0)
+    c = out if out is not None else torch.empty((M, N // 2 if silu_mul else N), dtype=torch.bfloat16, device=a_codes.device)
+    _operands(a_codes=(a_codes, "uint8"), a_scales=(a_scales, "float32"), w_codes=(w_codes, "uint8"), w_scales=(w_scales, "float32"),
+              residual=(residual, "bfloat16"), out=(c, "bfloat16"), scratch=(scratch, "uint8"))
+    _shape("w_codes", w_codes, (N, K))
+    _shape("a_scales", a_scales, (K // 128, M))
+    _shape("w_scales", w_scales, (2, (N + 255) // 256, K // 128) if silu_mul else ((N + 127) // 128, K // 128))
+    _shape("out", c, (M, N // 2 if silu_mul else N))
+    if residual is not None:
+        _shape("residual", residual, (M, N))
+    if scratch is None:
+        scratch = torch.empty(po_linear_fp8_block_bytes(M, N, K), dtype=torch.uint8, device=a_codes.device)
+    check(lib().po_op_linear_fp8_block(epi, a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(),
+                                       c.data_ptr(), None if residual is None else residual.data_ptr(),
+                                       scratch.data_ptr() if scratch.numel() else None, scratch.numel(), M, N, K, _stream()))
+    return c
 
 
 def attention_q_scale(head_dim: int) -> float:

@@ -1614,6 +1614,44 @@ po_status po_op_linear_fp8_split(const void* a_codes, const float* a_scales, con
     return PO_OK;
 }
 
+po_status po_op_quantize_blocks(const void* x, void* codes, float* scales, int64_t rows, int32_t K, int32_t block_rows, void* stream) {
+    if (!x || !codes || !scales || x == codes || rows <= 0 || K <= 0 || (block_rows != 1 && block_rows != 128)) return PO_ERR_INVALID_ARG;
+    if (K % 128) return PO_ERR_BAD_CONFIG;
+    if (rows > (int64_t)1 << 24) return PO_ERR_TOO_LONG;
+    launch_quant_blocks((const bf16_t*)x, (unsigned char*)codes, scales, rows, K, block_rows, (hipStream_t)stream);
+    PO_HIP(hipGetLastError());
+    return PO_OK;
+}
+
+// rows of a launch, whose tiles are addressed with 32-bit offsets of at most 256 rows of K codes
+static po_status fp8_block_shape(int64_t M, int32_t N, int32_t K) {
+    if (M <= 0 || N <= 0 || K <= 0) return PO_ERR_INVALID_ARG;
+    if (!gemm_fp8_block_supported(N, K)) return PO_ERR_BAD_CONFIG;
+    if (M > (int64_t)1 << 24 || K >= 1 << 23) return PO_ERR_TOO_LONG;
+    return PO_OK;
+}
+
+po_status po_linear_fp8_block_bytes(int64_t M, int32_t N, int32_t K, size_t* scratch_bytes) {
+    if (!scratch_bytes) return PO_ERR_INVALID_ARG;
+    const po_status st = fp8_block_shape(M, N, K);
+    if (st == PO_OK) *scratch_bytes = gemm_fp8_block_scratch(M, N, K);
+    return st;
+}
+
+po_status po_op_linear_fp8_block(int32_t epilogue, const void* a_codes, const float* a_scales, const void* w_codes,
+                                 const float* w_scales, void* cc, const void* residual, void* scratch, size_t scratch_bytes,
+                                 int64_t M, int32_t N, int32_t K, void* stream) {
+    if (!a_codes || !a_scales || !w_codes || !w_scales || !cc) return PO_ERR_INVALID_ARG;
+    if (epilogue != EPI_STORE && epilogue != EPI_RESIDUAL && epilogue != EPI_SILU_MUL) return PO_ERR_INVALID_ARG;
+    if (epilogue == EPI_RESIDUAL && !residual) return PO_ERR_INVALID_ARG;
+    const po_status st = fp8_block_shape(M, N, K);
+    if (st != PO_OK) return st;
+    launch_gemm_fp8_block(epilogue, (const unsigned char*)a_codes, a_scales, (const unsigned char*)w_codes, w_scales, (bf16_t*)cc,
+                          (const bf16_t*)residual, M, N, K, (float*)scratch, scratch ? scratch_bytes : 0, (hipStream_t)stream);
+    PO_HIP(hipGetLastError());
+    return PO_OK;
+}
+
 po_status po_op_qkv_rope_fp8(const void* a_codes, const float* a_scales, const void* w_codes, const float* w_scales,
                              const void* bqkv, void* q, void* k, void* vt, int64_t ldv, const float* cos_t,
                              const float* sin_t, int64_t pos0, int64_t M, int32_t Hq, int32_t Hkv, int32_t hd, int32_t K,

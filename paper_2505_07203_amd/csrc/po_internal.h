@@ -209,6 +209,18 @@ void launch_rmsnorm_quant(const bf16_t* x, const bf16_t* g, unsigned char* q, fl
                           float eps, hipStream_t s);
 bool attention_mfma_supported(int Hq, int Hkv, int hd);
 
+// ---- FP8 linear layers with a scale per block of 128 ------------------------------------------------
+// bf16 [rows, K] -> codes and scales: block_rows 1: blocks of a row x 128, scales [K / 128][rows]; block_rows 128: blocks of
+// 128 x 128, scales [ceil(rows / 128)][K / 128] (K % 128 == 0)
+void launch_quant_blocks(const bf16_t* x, unsigned char* q, float* scales, int64_t rows, int K, int block_rows, hipStream_t s);
+// C = sum over blocks of sa * sw * (Qa Qw^T) with the epilogues EPI_STORE, EPI_RESIDUAL, EPI_SILU_MUL (weight rows interleaved
+// gate / up in blocks of 32, scales of the gate rows then of the up rows); contiguous operands.  part (may be null): scratch for
+// launches of few tiles, which split the reduction with it; gemm_fp8_block_scratch: what that takes at most.
+bool gemm_fp8_block_supported(int N, int K);
+size_t gemm_fp8_block_scratch(int64_t M, int N, int K);
+void launch_gemm_fp8_block(int epi, const unsigned char* A, const float* sa, const unsigned char* W, const float* sw, bf16_t* C,
+                           const bf16_t* R, int64_t M, int N, int K, float* part, size_t part_bytes, hipStream_t s);
+
 // ---- micro-peaks (measurement only)
 double launch_mfma_peak(int kind, int waves_per_simd, int iters, const void* operands, size_t operand_bytes, float* sink,
                         hipStream_t s);

@@ -1,0 +1,41 @@
+"""What the entry points for batches behind one profile refuse (host logic: no call here reaches a launch)."""
+import ctypes as C
+
+import pytest
+
+from paper_2505_07203_amd import binding as B
+
+P = 0x1000            # stands for a device pointer: refused calls never look at it
+
+
+def test_quantize_blocks_refusals():
+    f = B.lib().po_op_quantize_blocks
+    ok = [P, 2 * P, 3 * P, 4, 256, 1, None]
+    for i, bad, status in ((0, None, 1), (1, None, 1), (2, None, 1), (1, P, 1), (3, 0, 1), (3, -1, 1), (4, 0, 1), (4, 200, 2), (4, 64, 2),
+                           (5, 0, 1), (5, 64, 1), (3, (1 << 24) + 1, 4)):
+        a = list(ok)
+        a[i] = bad
+        assert f(*a) == status, (i, bad)
+
+
+def test_linear_fp8_block_refusals():
+    f = B.lib().po_op_linear_fp8_block
+    ok = [0, P, P, P, P, P, None, None, 0, 4, 128, 256, None]
+    for i, bad, status in ((0, 3, 1), (0, -1, 1), (0, 1, 1), (1, None, 1), (2, None, 1), (3, None, 1), (4, None, 1), (5, None, 1),
+                           (9, 0, 1), (9, -3, 1), (9, (1 << 24) + 1, 4), (10, 0, 1), (10, 96, 2), (11, 0, 1), (11, 192, 2), (11, 1 << 23, 4)):
+        a = list(ok)
+        a[i] = bad
+        assert f(*a) == status, (i, bad)
+
+
+def test_linear_fp8_block_bytes():
+    n = C.c_size_t(7)
+    f = B.lib().po_linear_fp8_block_bytes
+    assert f(1, 4096, 4096, None) == 1 and f(0, 4096, 4096, C.byref(n)) == 1 and f(1, 100, 4096, C.byref(n)) == 2
+    assert n.value == 7                                          # nothing is written on error
+    for M, N, K in ((1, 64, 128), (150, 4096, 14336), (1, 4096, 4096), (8192, 28672, 4096)):
+        b = B.po_linear_fp8_block_bytes(M, N, K)
+        assert b % (4 * M * N) == 0 and b // (4 * M * N) <= 16 and b // (4 * M * N) != 1
+    assert B.po_linear_fp8_block_bytes(8192, 28672, 4096) == 0   # tiles enough
+    with pytest.raises(B.PoError):
+        B.po_linear_fp8_block_bytes(1, 4096, 100)
