@@ -572,6 +572,21 @@ po_status po_op_stream_copy(const void* dev_src, void* dev_dst, size_t bytes, vo
 po_status po_op_lm_head(int32_t dtype, const void* dev_x, const void* dev_w, float* dev_logits,
                         int32_t V, int32_t d, void* hip_stream);
 
+/* Draws one token per row from logits [rows][ld] (fp32, V <= ld of each row used), from one given random number u[row] in [0, 1)
+ * a row: the answer to a request as a token where po_prefill's log-probs are the answer as a distribution.  With m the row's largest
+ * logit, w_i = exp((l_i - m) / temperature).  Tokens are ordered by logit, the largest first, equal ones by index.  Kept is the
+ * beginning of that order of top_k tokens; of those the shortest beginning whose sum of w is at least top_p times the sum of the
+ * top_k; of those the tokens with w >= min_p; the first token always.  The token drawn is the first kept one, by INDEX, at which
+ * the running sum of kept w exceeds u times their whole sum; logprobs[row] (dev_logprobs may be NULL) = log(w / sum of kept w).
+ * Sums and comparisons are float64.
+ * The four settings are arrays [rows] on the device, each may be NULL (off; temperature 1).  temperature <= 0 or NaN: the first of
+ * the order, log-prob 0; top_k <= 0 or >= V, top_p >= 1 or NaN, min_p <= 0 or NaN: off.  u outside [0, 1) is moved to the nearest
+ * value inside, NaN to 0.  Logits of -infinity and NaN are never drawn; with +infinity among them only those are.  A row
+ * without any other than -infinity and NaN gives token -1, log-prob -infinity.  Every launch gives the same bits. */
+po_status po_op_sample(const float* dev_logits, int64_t ld, int64_t rows, int32_t V, const float* dev_u, const float* dev_temperature,
+                       const int32_t* dev_top_k, const float* dev_top_p, const float* dev_min_p, int32_t* dev_tokens,
+                       float* dev_logprobs, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

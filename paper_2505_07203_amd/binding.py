@@ -42,7 +42,7 @@ EXPORTS = [
     "po_op_attention_split_prefix", "po_attention_tile", "po_gemm_tile", "po_gemm_turns", "po_gemm_f32_tile", "po_op_linear_fp8_split",
     "po_sched_create", "po_sched_destroy", "po_sched_set_jct_model", "po_sched_fit_jct_model", "po_sched_push",
     "po_sched_size", "po_sched_pick", "po_sched_remove", "po_op_rope_static", "po_op_mfma_peak", "po_op_stream_copy",
-    "po_op_quantize_blocks", "po_linear_fp8_block_bytes", "po_op_linear_fp8_block",
+    "po_op_quantize_blocks", "po_linear_fp8_block_bytes", "po_op_linear_fp8_block", "po_op_sample",
 ]
 
 
@@ -146,6 +146,7 @@ def lib() -> C.CDLL:
     L.po_op_quantize_blocks.argtypes = [vp, vp, vp, i64, i32, i32, vp]
     L.po_linear_fp8_block_bytes.argtypes = [i64, i32, i32, C.POINTER(sz)]
     L.po_op_linear_fp8_block.argtypes = [i32, vp, vp, vp, vp, vp, vp, vp, sz, i64, i32, i32, vp]
+    L.po_op_sample.argtypes = [vp, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     f64 = C.c_double
     L.po_sched_create.argtypes = [f64, C.POINTER(vp)]
     L.po_sched_destroy.argtypes = [vp]
@@ -722,6 +723,26 @@ def po_op_lm_head(x, w):
     z = torch.empty(V, dtype=torch.float32, device=w.device)
     check(lib().po_op_lm_head(_dt(x), x.data_ptr(), w.data_ptr(), z.data_ptr(), V, d, _stream()))
     return z
+
+
+def po_op_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
+    """float32 logits [rows, V] (rows may have a pitch), u [rows] in [0, 1), settings [rows] each or None -> (int32 tokens [rows],
+    float32 log-probs [rows])"""
+    import torch
+    rows, V = logits.shape
+    if rows and V and logits.stride(1) != 1:
+        raise ValueError("logits: a row's values must lie side by side")
+    _operands(logits=(logits[:1], "float32"), u=(u, "float32"), temperature=(temperature, "float32"), top_k=(top_k, "int32"),
+              top_p=(top_p, "float32"), min_p=(min_p, "float32"))
+    for name, t in (("u", u), ("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
+        if t is not None:
+            _shape(name, t, (rows,))
+    tokens = torch.empty(rows, dtype=torch.int32, device=logits.device)
+    logprobs = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    p = lambda t: None if t is None else t.data_ptr()
+    check(lib().po_op_sample(logits.data_ptr(), logits.stride(0), rows, V, u.data_ptr(), p(temperature), p(top_k), p(top_p), p(min_p),
+                             tokens.data_ptr(), logprobs.data_ptr(), _stream()))
+    return tokens, logprobs
 
 
 def po_op_rope_table(n: int, head_dim: int, theta: float):

@@ -1693,5 +1693,14 @@ po_status po_op_lm_head(int32_t dtype, const void* x, const void* w, float* logi
     return PO_OK;
 }
 
+po_status po_op_sample(const float* logits, int64_t ld, int64_t rows, int32_t V, const float* u, const float* temperature,
+                       const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens, float* logprobs, void* stream) {
+    if (!logits || !u || !tokens || rows <= 0 || V <= 0 || ld < V) return PO_ERR_INVALID_ARG;
+    if (rows > 1 << 24 || V > 1 << 24) return PO_ERR_TOO_LONG;
+    launch_sample(logits, ld, (int)rows, V, u, temperature, top_k, top_p, min_p, tokens, logprobs, (hipStream_t)stream);
+    PO_HIP(hipGetLastError());
+    return PO_OK;
+}
+
 }  // extern "C"
 #pragma GCC visibility pop

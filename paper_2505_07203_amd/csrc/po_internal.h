@@ -221,6 +221,10 @@ size_t gemm_fp8_block_scratch(int64_t M, int N, int K);
 void launch_gemm_fp8_block(int epi, const unsigned char* A, const float* sa, const unsigned char* W, const float* sw, bf16_t* C,
                            const bf16_t* R, int64_t M, int N, int K, float* part, size_t part_bytes, hipStream_t s);
 
+// one token per row of logits (row pitch ld); the four settings may each be null; tokens -1 where a row has nothing to draw
+void launch_sample(const float* logits, int64_t ld, int rows, int V, const float* u, const float* temperature, const int* top_k,
+                   const float* top_p, const float* min_p, int* tokens, float* logprobs, hipStream_t s);
+
 // ---- micro-peaks (measurement only)
 double launch_mfma_peak(int kind, int waves_per_simd, int iters, const void* operands, size_t operand_bytes, float* sink,
                         hipStream_t s);

@@ -39,3 +39,15 @@ def test_linear_fp8_block_bytes():
     assert B.po_linear_fp8_block_bytes(8192, 28672, 4096) == 0   # tiles enough
     with pytest.raises(B.PoError):
         B.po_linear_fp8_block_bytes(1, 4096, 100)
+
+
+def test_sample_refusals():
+    f = B.lib().po_op_sample
+    ok = [P, 1000, 4, 1000, P, None, None, None, None, P, None, None]
+    for i, bad, status in ((0, None, 1), (1, 999, 1), (1, -1000, 1), (2, 0, 1), (2, -1, 1), (2, (1 << 24) + 1, 4), (3, 0, 1), (4, None, 1), (9, None, 1)):
+        a = list(ok)
+        a[i] = bad
+        assert f(*a) == status, (i, bad)
+    a = list(ok)
+    a[1] = a[3] = (1 << 24) + 1
+    assert f(*a) == 4
