@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpo.so")
 SOURCES = ["po_api.hip", "kernels_basic.hip", "gemm_mfma.hip", "attn_mfma.hip", "po_sched.hip", "fp8_kernels.hip",
-           "gemm_fp8_mfma.hip", "gemm_fp8_block.hip", "sample.hip", "peak_kernels.hip", "f32_mfma.hip"]
+           "gemm_fp8_mfma.hip", "gemm_fp8_block.hip", "sample.hip", "attn_shared.hip", "peak_kernels.hip", "f32_mfma.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-result"]
@@ -23,6 +23,7 @@ FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-fvisibility=hi
 # array indexed by its counter moves to scratch memory)
 # (the block-scaled GEMM's MFMA results go straight into vector arithmetic as well)
 EXTRA_FLAGS = {"gemm_fp8_block.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+               "attn_shared.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form=1"],
                "attn_mfma.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form=1",
                                  "-mllvm", "-pragma-unroll-threshold=1048576"]}
 

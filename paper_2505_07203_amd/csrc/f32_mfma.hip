@@ -5,6 +5,7 @@
 // fixed order that depends on nothing but its own row and column; speed only has to be enough for whole
 // configurations (32 layers x 32768 tokens) to run in seconds.
 #include "po_internal.h"
+#include "attn_shared.h"
 #include "slice_window.h"
 
 #include <algorithm>
@@ -274,6 +275,89 @@ bool launch_attention_f32_mfma(const float* q, const float* k, const float* v, f
     if (hd == 128) launch_attention_f32<128>(q, k, v, o, N, Hq, Hkv, q_row0, s);
     else launch_attention_f32<64>(q, k, v, o, N, Hq, Hkv, q_row0, s);
     return true;
+}
+
+// ------------------------------------------------------------------ attention of requests behind a shared prefix
+// Rows and keys as in attn_shared.hip, V in rows like K.  A workgroup is 32 rows of one request and KV head, all of the KV
+// head's query heads among them; its four wavefronts take every fourth tile of 32 keys, of the prefix and then of the request's own, and
+// meet at the end, in wavefront order.
+template <int HD>
+__global__ void __launch_bounds__(256, 2) attention_shared_f32_kernel(const SharedParams p, const SharedTable tab) {
+    constexpr int HH = HD / 2, NB = HD / 32;
+    __shared__ __attribute__((aligned(16))) float so[4 * HD * 32];       // [wave][hd][32 rows]
+    __shared__ float sm[128], sl[128];                                   // [wave][32] maxima, row sums
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const int c = (int)(blockIdx.x % (unsigned)p.Hkv), item = (int)(blockIdx.x / (unsigned)p.Hkv);
+    const int req = __builtin_amdgcn_readfirstlane(shared_request(tab, item));
+    const SharedSeq sq = tab.seq[req];
+    const int group = p.Hq / p.Hkv;
+    const int row0 = (item - tab.item0[req]) * 32, n_rows = sq.q_len * group;
+    const int vr = min(row0 + col, n_rows - 1);
+    const int pos = vr / group, h = c * group + vr - pos * group;
+    const int last = sq.kv_len - sq.q_len + pos;                         // the last own key this row sees (may be below 0)
+    const int last_max = sq.kv_len - sq.q_len + min(row0 + 31, n_rows - 1) / group;
+    const int last_min = sq.kv_len - sq.q_len + row0 / group;
+    const int64_t kvrow = (int64_t)p.Hkv * HD;
+    F32Rows<HD> st;
+    st.start((const float*)p.q, sq.q_row + pos, INT64_MAX, h, p.Hq, half);
+    // (positions past the last key are masked; their fragments come from the last key)
+    auto keys = [&](const float* k, const float* v, int n, int seen, int seen_min, int seen_max) {
+        for (int kv0 = wave * 32; kv0 <= seen_max; kv0 += 128) {
+            const float* kp = k + min(kv0 + col, n - 1) * kvrow + c * HD + half * HH;
+            float4 kf[HH / 4];
+#pragma unroll
+            for (int i = 0; i < HH / 4; ++i) kf[i] = *(const float4*)(kp + 4 * i);
+            const float* vp = v + c * HD + col;
+            st.tile(kv0, seen_min, seen, half, p.sc, [&](int i) { return kf[i]; },
+                    [&](int b, int r) { return vp[min(kv0 + 8 * (r / 4) + 4 * half + (r % 4), n - 1) * kvrow + 32 * b]; });
+        }
+    };
+    keys((const float*)p.k2, (const float*)p.v2, p.n2, p.n2 - 1, p.n2 - 1, p.n2 - 1);
+    keys((const float*)p.k + sq.kv_row * kvrow, (const float*)p.v + sq.kv_row * kvrow, sq.kv_len, last, last_min, last_max);
+    const float l = st.l + __shfl_xor(st.l, 32);
+    if (half == 0) {
+        sm[wave * 32 + col] = st.m;
+        sl[wave * 32 + col] = l;
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) so[(wave * HD + 32 * b + 8 * (r / 4) + 4 * half + (r % 4)) * 32 + col] = st.O[b][r];
+    __syncthreads();
+    float mx = sm[col], f[4], lt = 0.f;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) mx = fmaxf(mx, sm[w * 32 + col]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        f[w] = sm[w * 32 + col] == -INFINITY ? 0.f : expf(sm[w * 32 + col] - mx);      // (a wavefront that saw nothing)
+        lt += f[w] * sl[w * 32 + col];
+    }
+    if (row0 + col >= n_rows) return;
+    const float inv = lt > 0.f ? 1.0f / lt : 0.f;                        // (a row that sees nothing: 0)
+    float* op = (float*)p.o + ((int64_t)(sq.q_row + pos) * p.Hq + h) * HD;
+#pragma unroll
+    for (int x = 0; x < HD / 32; ++x) {
+        const int d0 = wave * (HD / 4) + half * (HD / 8) + 4 * x;
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float acc = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) acc += f[w] * so[(w * HD + d0 + e) * 32 + col];
+            y[e] = acc * inv;
+        }
+        *(float4*)(op + d0) = make_float4(y[0], y[1], y[2], y[3]);
+    }
+}
+
+void launch_attention_shared_f32(const SharedParams& p, const po_request_rows* seq, int n, int hd, hipStream_t s) {
+    for_tables(seq, n, p.Hq / p.Hkv, 32, [&](const SharedTable& tab, int items) {
+        const dim3 grid((unsigned)items * p.Hkv);
+        if (hd == 128) hipLaunchKernelGGL(attention_shared_f32_kernel<128>, grid, dim3(256), 0, s, p, tab);
+        else hipLaunchKernelGGL(attention_shared_f32_kernel<64>, grid, dim3(256), 0, s, p, tab);
+    });
 }
 
 // ------------------------------------------------------------------ GEMM

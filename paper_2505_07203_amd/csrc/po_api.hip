@@ -2,6 +2,7 @@
 // (layer loop, token-chunk loop, one HIP stream, no device<->host synchronisation inside
 // a request except the final one).
 #include "../../include/po.h"
+#include "attn_shared.h"
 #include "po_internal.h"
 
 #include <math.h>
@@ -1460,6 +1461,52 @@ po_status po_op_attention_split_prefix(const void* q, const void* k, const void*
                                                Hq, Hkv, hd, q_row0, (float*)scratch_part, part_bytes, true,
                                                n2 > 0 ? (const bf16_t*)k2 : nullptr, n2 > 0 ? (const bf16_t*)vt2 : nullptr, ldv2,
                                                n2, q_prescaled != 0, (hipStream_t)stream);
+    PO_HIP(hipGetLastError());
+    return PO_OK;
+}
+
+// q rows ascending and apart, sizes that the kernels' 32-bit numbers hold; -> own keys of all requests together
+static po_status shared_requests(const po_request_rows* req, int32_t n_req, int32_t Hq, int64_t ldv, bool vt, int64_t* keys) {
+    constexpr int64_t MAX = (int64_t)1 << 24;
+    int64_t row = 0, tiles = 0;
+    *keys = 0;
+    for (int32_t i = 0; i < n_req; ++i) {
+        const po_request_rows& r = req[i];
+        if (r.q_row < row || r.q_len < 0 || r.kv_row < 0 || r.kv_len < 0) return PO_ERR_INVALID_ARG;
+        if (r.q_len > MAX || r.kv_len > MAX || r.q_row > INT32_MAX - MAX || r.kv_row > INT32_MAX - MAX) return PO_ERR_TOO_LONG;
+        if (vt && (r.kv_row % 8 || r.kv_row + r.kv_len > ldv)) return PO_ERR_INVALID_ARG;
+        row = r.q_row + r.q_len;
+        tiles += (r.q_len * Hq + 31) / 32 + Hq;
+        if (r.q_len) *keys += r.kv_len;
+        if (tiles > INT32_MAX) return PO_ERR_TOO_LONG;
+    }
+    return PO_OK;
+}
+
+static inline bool misaligned16(const void* p) { return ((uintptr_t)p & 15) != 0; }
+
+po_status po_op_attention_shared(int32_t dtype, const void* q, const void* k, const void* v, int64_t ldv, void* o,
+                                 const po_request_rows* requests, int32_t n_req, const void* k2, const void* v2, int64_t ldv2,
+                                 int64_t n2, int32_t Hq, int32_t Hkv, int32_t hd, int32_t q_prescaled, void* stream) {
+    if (bad_dtype(dtype) || !q || !o || !requests || n_req <= 0 || n2 < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv) return PO_ERR_INVALID_ARG;
+    if ((q_prescaled != 0 && q_prescaled != 1) || (q_prescaled && dtype != PO_BF16)) return PO_ERR_INVALID_ARG;
+    const bool vt = dtype == PO_BF16;
+    if (n2 > 0 && (!k2 || !v2 || (vt && (ldv2 < n2 || ldv2 % 8)))) return PO_ERR_INVALID_ARG;
+    if (!attention_mfma_supported(Hq, Hkv, hd)) return PO_ERR_BAD_CONFIG;
+    // (a KV head's V^T and a row of all heads are addressed in bytes with 32 bits)
+    if (n2 > (int64_t)1 << 24 || ldv >= (int64_t)1 << 30 || ldv2 >= (int64_t)1 << 30 || (int64_t)Hq * hd >= (int64_t)1 << 23) return PO_ERR_TOO_LONG;
+    int64_t keys;
+    const po_status st = shared_requests(requests, n_req, Hq, ldv, vt, &keys);
+    if (st != PO_OK) return st;
+    if (keys > 0 && (!k || !v || (vt && ldv % 8))) return PO_ERR_INVALID_ARG;
+    if (misaligned16(q) || misaligned16(o) || misaligned16(k) || misaligned16(v) || misaligned16(k2) || misaligned16(v2)) return PO_ERR_INVALID_ARG;
+    SharedParams p{};
+    p.q = q; p.k = k; p.v = v; p.k2 = k2; p.v2 = v2; p.o = o;
+    p.ldv = ldv; p.ldv2 = ldv2;
+    p.n2 = (int)n2;
+    p.Hq = Hq; p.Hkv = Hkv;
+    p.sc = vt ? (q_prescaled ? 1.0f : attention_q_scale(hd)) : 1.0f / sqrtf((float)hd);
+    (vt ? launch_attention_shared_bf16 : launch_attention_shared_f32)(p, requests, n_req, hd, (hipStream_t)stream);
     PO_HIP(hipGetLastError());
     return PO_OK;
 }

@@ -51,3 +51,33 @@ def test_sample_refusals():
     a = list(ok)
     a[1] = a[3] = (1 << 24) + 1
     assert f(*a) == 4
+
+
+def rows(*requests):
+    return (C.c_int64 * (4 * len(requests)))(*[x for r in requests for x in r])
+
+
+def attention_args(**kw):
+    a = dict(dtype=1, q=P, k=P, v=P, ldv=640, o=P, requests=rows((0, 5, 0, 5), (5, 1, 64, 30)), n_req=2, k2=P, v2=P, ldv2=128, n2=100, Hq=8,
+             Hkv=2, hd=128, pre=1)
+    a.update(kw)
+    return a
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=2), 1), (dict(dtype=-1), 1), (dict(q=None), 1), (dict(o=None), 1), (dict(requests=None), 1), (dict(n_req=0), 1), (dict(n_req=-1), 1),
+    (dict(k=None), 1), (dict(v=None), 1), (dict(k2=None), 1), (dict(v2=None), 1), (dict(n2=-1), 1), (dict(ldv2=96), 1), (dict(ldv2=132), 1),
+    (dict(ldv=60), 1), (dict(ldv=637), 1), (dict(ldv=643), 1), (dict(Hq=0), 1), (dict(Hkv=0), 1), (dict(Hkv=3), 1), (dict(hd=96), 2), (dict(hd=256), 2), (dict(pre=2), 1),
+    (dict(dtype=0, pre=1), 1), (dict(q=P + 8), 1), (dict(k2=P + 2), 1), (dict(v=P + 4), 1), (dict(n2=(1 << 24) + 1, ldv2=1 << 25), 4), (dict(ldv=1 << 30), 4),
+    (dict(requests=rows((0, 5, 0, 5), (4, 1, 64, 30))), 1),            # rows of q overlap
+    (dict(requests=rows((5, 1, 64, 30), (0, 5, 0, 5))), 1),            # ... descend
+    (dict(requests=rows((0, -1, 0, 5), (5, 1, 64, 30))), 1), (dict(requests=rows((0, 5, 0, -5), (5, 1, 64, 30))), 1),
+    (dict(requests=rows((0, 5, -8, 5), (5, 1, 64, 30))), 1), (dict(requests=rows((-3, 2, 0, 5), (5, 1, 64, 30))), 1),
+    (dict(requests=rows((0, 5, 4, 5), (5, 1, 64, 30))), 1),            # V^T columns that no 16-byte load begins at
+    (dict(requests=rows((0, 5, 0, 5), (5, 1, 632, 30))), 1),           # ... beyond the pitch
+    (dict(requests=rows((0, (1 << 24) + 1, 0, 5), (1 << 25, 1, 64, 30))), 4), (dict(requests=rows((0, 5, 0, 5), (1 << 31, 1, 64, 30))), 4),
+    (dict(Hq=1 << 17, Hkv=1), 4),
+])
+def test_attention_shared_refusals(change, status):
+    a = attention_args(**change)
+    assert B.lib().po_op_attention_shared(*a.values(), None) == status
