@@ -438,10 +438,14 @@ po_status po_op_attention_split_prefix(const void* dev_q, const void* dev_k, con
  * as v; any n2, 0 = none (then they may be NULL).  What lies beyond a request's or the prefix's last key is not used, whatever it
  * holds.  head_dim 64 or 128; pointers 16-byte aligned; scores must be finite.  q_prescaled as in po_op_attention. */
 typedef struct { int64_t q_row, q_len, kv_row, kv_len; } po_request_rows;
+/* (dev_scratch may be NULL: then no call runs in parts.  po_attention_shared_bytes: the scratch that these requests can use; 0: none.
+ * Host only.) */
+po_status po_attention_shared_bytes(int32_t dtype, const po_request_rows* requests, int32_t n_req, int64_t n2, int32_t n_q_heads,
+                                    int32_t n_kv_heads, int32_t head_dim, size_t* scratch_bytes);
 po_status po_op_attention_shared(int32_t dtype, const void* dev_q, const void* dev_k, const void* dev_v, int64_t ldv, void* dev_o,
                                  const po_request_rows* requests, int32_t n_req, const void* dev_k2, const void* dev_v2,
                                  int64_t ldv2, int64_t n2, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
-                                 int32_t q_prescaled, void* hip_stream);
+                                 int32_t q_prescaled, void* dev_scratch, size_t scratch_bytes, void* hip_stream);
 
 /* The block tile (rows x columns of the output) that a launch of po_op_linear, po_op_gate_up_silu (N = 2 F) or
  * po_op_qkv_rope with contiguous operands takes, or of their FP8 forms with fp8 = 1.  *splits: 1 = a whole launch, more =

@@ -42,7 +42,7 @@ EXPORTS = [
     "po_op_attention_split_prefix", "po_attention_tile", "po_gemm_tile", "po_gemm_turns", "po_gemm_f32_tile", "po_op_linear_fp8_split",
     "po_sched_create", "po_sched_destroy", "po_sched_set_jct_model", "po_sched_fit_jct_model", "po_sched_push",
     "po_sched_size", "po_sched_pick", "po_sched_remove", "po_op_rope_static", "po_op_mfma_peak", "po_op_stream_copy",
-    "po_op_quantize_blocks", "po_linear_fp8_block_bytes", "po_op_linear_fp8_block", "po_op_sample", "po_op_attention_shared",
+    "po_op_quantize_blocks", "po_linear_fp8_block_bytes", "po_op_linear_fp8_block", "po_op_sample", "po_op_attention_shared", "po_attention_shared_bytes",
 ]
 
 
@@ -147,7 +147,8 @@ def lib() -> C.CDLL:
     L.po_linear_fp8_block_bytes.argtypes = [i64, i32, i32, C.POINTER(sz)]
     L.po_op_linear_fp8_block.argtypes = [i32, vp, vp, vp, vp, vp, vp, vp, sz, i64, i32, i32, vp]
     L.po_op_sample.argtypes = [vp, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp]
-    L.po_op_attention_shared.argtypes = [i32, vp, vp, vp, i64, vp, vp, i32, vp, vp, i64, i64, i32, i32, i32, i32, vp]
+    L.po_op_attention_shared.argtypes = [i32, vp, vp, vp, i64, vp, vp, i32, vp, vp, i64, i64, i32, i32, i32, i32, vp, sz, vp]
+    L.po_attention_shared_bytes.argtypes = [i32, vp, i32, i64, i32, i32, i32, C.POINTER(sz)]
     f64 = C.c_double
     L.po_sched_create.argtypes = [f64, C.POINTER(vp)]
     L.po_sched_destroy.argtypes = [vp]
@@ -692,10 +693,20 @@ def po_op_attention_split_prefix(q, k, v, q_row0: int, q_prescaled: bool = False
     return (o if n.value > 1 else None), n.value
 
 
-def po_op_attention_shared(q, k, v, requests, k2=None, v2=None, n2: int = 0, out=None, q_prescaled: bool = False):
+def po_attention_shared_bytes(dtype: int, requests, n2: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    """bytes of scratch that po_op_attention_shared can use for these requests (host only); dtype: PO_F32 or PO_BF16"""
+    r = np.ascontiguousarray(requests, dtype=np.int64)
+    _shape("requests", r, (len(r), 4))
+    n = C.c_size_t(0)
+    check(lib().po_attention_shared_bytes(dtype, r.ctypes.data, len(r), n2, n_q_heads, n_kv_heads, head_dim, C.byref(n)))
+    return n.value
+
+
+def po_op_attention_shared(q, k, v, requests, k2=None, v2=None, n2: int = 0, out=None, q_prescaled: bool = False, scratch=None):
     """requests: int64 [n, 4] on the host, (q_row, q_len, kv_row, kv_len) each, behind the shared prefix (k2, v2)[: n2]; q [rows, Hq, hd],
     k [rows, Hkv, hd], k2 [>= n2, Hkv, hd]; v, v2: transposed [Hkv*hd, ldv] for bfloat16, rows like k for float32 -> o like q
-    (out, which may be q itself; a fresh one is zero in rows of no request)"""
+    (out, which may be q itself; a fresh one is zero in rows of no request).  scratch: a uint8 tensor to be used instead of one of
+    po_attention_shared_bytes (an empty one: nothing runs in parts)"""
     import torch
     rows, Hq, hd = q.shape
     Hkv = k.shape[1]
@@ -704,7 +715,7 @@ def po_op_attention_shared(q, k, v, requests, k2=None, v2=None, n2: int = 0, out
     if n2 > 0 and (k2 is None or v2 is None):
         raise ValueError("k2, v2: expected with n2 > 0")
     o = torch.zeros_like(q) if out is None else out
-    _operands(q=(q, dt), k=(k, dt), v=(v, dt), k2=(k2, dt), v2=(v2, dt), out=(o, dt))
+    _operands(q=(q, dt), k=(k, dt), v=(v, dt), k2=(k2, dt), v2=(v2, dt), out=(o, dt), scratch=(scratch, "uint8"))
     _shape("k", k, (k.shape[0], Hkv, hd))
     _shape("out", o, (rows, Hq, hd))
     _shape("v", v, (Hkv * hd, v.shape[1]) if bf16 else k.shape)
@@ -720,9 +731,12 @@ def po_op_attention_shared(q, k, v, requests, k2=None, v2=None, n2: int = 0, out
         q_end, k_end = (int(r[0, 0] + r[0, 1]), int(r[0, 2] + r[0, 3])) if len(r) == 1 else (int(ends[0]), int(ends[1]))
         if q_end > rows or k_end > k.shape[0]:
             raise ValueError(f"requests: end at rows {q_end} of {rows} of q and {k_end} of {k.shape[0]} of k")
+    if scratch is None:
+        scratch = torch.empty(po_attention_shared_bytes(_dt(q), r, n2, Hq, Hkv, hd), dtype=torch.uint8, device=q.device)
     check(lib().po_op_attention_shared(_dt(q), q.data_ptr(), k.data_ptr(), v.data_ptr(), v.shape[1] if bf16 else 0, o.data_ptr(),
                                        r.ctypes.data, len(r), k2.data_ptr() if n2 else None, v2.data_ptr() if n2 else None,
-                                       v2.shape[1] if n2 and bf16 else 0, n2, Hq, Hkv, hd, 1 if q_prescaled else 0, _stream()))
+                                       v2.shape[1] if n2 and bf16 else 0, n2, Hq, Hkv, hd, 1 if q_prescaled else 0,
+                                       scratch.data_ptr() if scratch.numel() else None, scratch.numel(), _stream()))
     return o
 
 

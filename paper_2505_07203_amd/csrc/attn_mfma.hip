@@ -22,6 +22,7 @@
 // Scheduling: query tiles are issued longest-first; when n_q_heads is a multiple of 8 all
 // heads of one KV group are mapped to one XCD so that the group's K/V stream is shared in
 // that XCD's L2.
+#include "attn_shared.h"
 #include "po_internal.h"
 
 #include <algorithm>
@@ -435,11 +436,25 @@ struct SplitArgs {
     float *opart, *mlpart;        // [piece][row - q_row0][head][HD], [..][2]
     int q_row0, tiles2, n2, n, per;       // n: pieces
 };
+// SPLIT 3 (a batch of requests behind one shared prefix, attn_shared.h): the rows are those of all requests of a table, one behind the
+// other, and the pieces are of the prefix's tiles2 whole tiles (the second pair) alone, which every row sees in full: nothing is
+// masked in the pipeline.  Behind it the workgroups of the last piece go on, block by block from memory to registers, with what
+// is left of the prefix (n2 keys from tile tiles2 on) and the requests' own keys (the first pair); a wavefront's 64 rows
+// meet few requests, and their own keys are few beside the prefix.  With one piece the rows are then complete and are stored; no
+// partial result goes through memory.  [piece][row of the table][head][HD] otherwise.
+// own 0: the own keys are left to another launch (rows of many requests in a tile, each with keys of its own): always partial results.
+struct SharedSplitArgs : SplitArgs {
+    SharedTable tab;
+    int own;
+};
+template <int SPLIT> struct SplitArgsOf { typedef SplitArgs type; };
+template <> struct SplitArgsOf<3> { typedef SharedSplitArgs type; };
+
 template <bool PRE, int SPLIT, int QT>
 __global__ void __launch_bounds__(256) attn_fwd64_kernel(const bf16_t* q, const bf16_t* __restrict__ k,
                                                          const bf16_t* __restrict__ vt, int64_t ldv, bf16_t* o, int N,
                                                          int Hq, int Hkv, float sc_log2e, int nqt, int hpx, int* redo,
-                                                         const SplitArgs sp) {
+                                                         const typename SplitArgsOf<SPLIT>::type sp) {
     constexpr int HD = 128, KS = 8, HT = 4;
     constexpr bool LATE = PRE || SPLIT != 0;     // the row sums are looked at once, behind the last block
     constexpr int ROWS = 128 * QT;               // query rows of a workgroup
@@ -450,6 +465,8 @@ __global__ void __launch_bounds__(256) attn_fwd64_kernel(const bf16_t* q, const 
     int qtile, head, kvh, piece = 0, tile0 = 0, piece_tiles = 0;
     int tiles2 = 0, end = N;                // SPLIT: tiles of this piece in the second pair; positions from its first one on
     const int group = Hq / Hkv;
+    const bf16_t *const k_own = k, *const vt_own = vt;
+    const int64_t ldv_own = ldv;
     if (SPLIT) {
         kvh = blockIdx.x % Hkv;
         const int rest = blockIdx.x / Hkv;
@@ -457,7 +474,7 @@ __global__ void __launch_bounds__(256) attn_fwd64_kernel(const bf16_t* q, const 
         qtile = rest / sp.n;
         head = kvh * group;
         const int n_all = (N + 63) / 64;
-        const bool second = SPLIT == 1 && piece < sp.n2;       // (a piece of the second pair alone)
+        const bool second = SPLIT == 3 || (SPLIT == 1 && piece < sp.n2);       // (a piece of the second pair alone)
         tile0 = (SPLIT == 2 || second) ? piece * sp.per : sp.tiles2 + (piece - sp.n2) * sp.per;
         piece_tiles = min(sp.per, (second ? sp.tiles2 : n_all) - tile0);
         if (SPLIT == 2) tiles2 = max(0, min(sp.tiles2 - tile0, piece_tiles));
@@ -466,7 +483,7 @@ __global__ void __launch_bounds__(256) attn_fwd64_kernel(const bf16_t* q, const 
             vt = sp.vt2;
             ldv = sp.ldv2;
         }
-        end = (second ? sp.tiles2 * 64 : N) - tile0 * 64;
+        end = SPLIT == 3 ? piece_tiles * 64 : (second ? sp.tiles2 * 64 : N) - tile0 * 64;
         // everything below counts keys from this piece's first one
         k += (int64_t)tile0 * 64 * Hkv * HD;
         vt += tile0 * 64;
@@ -488,15 +505,21 @@ __global__ void __launch_bounds__(256) attn_fwd64_kernel(const bf16_t* q, const 
     const int n_tiles = SPLIT ? piece_tiles : blk_last / 64 + 1;       // 64-key tiles the workgroup streams
     const int nkb_w = (qw < N) ? (min(N, qw + 32 * QT) - 1) / 32 + 1 : 0;   // 32-key blocks this wavefront needs
     // SPLIT: this lane's query rows (position and head), clamped to the last one, and their positions in keys of this piece
+    // (SPLIT 3: N rows of the table; vreq: the request of a row, vq: its row of q; no key of the pieces is masked)
     const int n_virtual = SPLIT ? (N - sp.q_row0) * group : 0;
-    int vrow[2], vhead[2], vpos[2];
+    int vrow[2], vhead[2], vpos[2], vreq[2], vq[2];
     if (SPLIT) {
 #pragma unroll
         for (int qt = 0; qt < 2; ++qt) {
             const int vr = min(qw + qt * 32 + l31, n_virtual - 1);
             vrow[qt] = vr / group;
             vhead[qt] = head + vr - vrow[qt] * group;
-            vpos[qt] = sp.q_row0 + vrow[qt] - tile0 * 64;
+            vpos[qt] = SPLIT == 3 ? 1 << 30 : sp.q_row0 + vrow[qt] - tile0 * 64;
+            vq[qt] = sp.q_row0 + vrow[qt];
+            if constexpr (SPLIT == 3) {
+                vreq[qt] = shared_request_of_row(sp.tab, vrow[qt]);
+                vq[qt] = sp.tab.seq[vreq[qt]].q_row + vrow[qt] - sp.tab.row0[vreq[qt]];
+            }
         }
     }
 
@@ -504,7 +527,7 @@ __global__ void __launch_bounds__(256) attn_fwd64_kernel(const bf16_t* q, const 
     bf16x8 qf[QT][KS];
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
-        const int qrow = SPLIT ? sp.q_row0 + vrow[qt] : min(qw + qt * 32 + l31, N - 1);
+        const int qrow = SPLIT ? vq[qt] : min(qw + qt * 32 + l31, N - 1);
         const bf16_t* qp = q + ((int64_t)qrow * Hq + (SPLIT ? vhead[qt] : head)) * HD + lhi * 8;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
@@ -907,6 +930,106 @@ __global__ void __launch_bounds__(256) attn_fwd64_kernel(const bf16_t* q, const 
 #pragma unroll
     for (int e = 0; e < 4; ++e) lsum[0][e] = lsum[1][e] = 0.f;
     }   // attempt
+    if constexpr (SPLIT == 3) {
+        if (piece == sp.n - 1) {
+            // one source of keys: n_keys of them, of which a lane's rows see `see` and some row of the wavefront see_max
+            auto keys = [&](const bf16_t* kb, const bf16_t* vb, int64_t ld, int n_keys, int see0, int see1, int see_max) {
+                for (int key0 = 0; key0 < see_max; key0 += 32) {
+                    bf16x8 kf[KS], vf[2][HT];
+                    const bf16_t* const kr = kb + (int64_t)min(key0 + pk, n_keys - 1) * (Hkv * HD) + lhi * 8;
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) kf[ks] = __builtin_bit_cast(bf16x8, *(const uint4*)(kr + ks * 16));
+#pragma unroll
+                    for (int j2 = 0; j2 < 2; ++j2) load_vt_eight<HT>(vb, ld, key0 + 16 * j2 + 8 * lhi, n_keys, vf[j2]);
+                    f32x16 S[2];
+#pragma unroll
+                    for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) S[qt][r] = 0.f;
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                        for (int qt = 0; qt < 2; ++qt) S[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[qt][ks], S[qt], 0, 0, 0);
+                    float top[2];
+                    bool grew = false;
+#pragma unroll
+                    for (int qt = 0; qt < 2; ++qt) {
+                        const int see = (qt ? see1 : see0) - key0;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if ((r & 7) + 8 * lhi + 16 * (r >> 3) >= see) S[qt][r] = -INFINITY;
+                        PO_BLOCKMAX(S, qt, top[qt]);
+                        top[qt] *= sc_log2e;
+                        grew |= top[qt] > mb[qt] + 30.f;       // (below that probabilities of up to 2^30 do no harm)
+                    }
+                    if (__any(grew)) {
+                        PO_MFMA_END();
+#pragma unroll
+                        for (int qt = 0; qt < 2; ++qt) {
+                            const float m = fmaxf(mb[qt], top[qt]), a = __builtin_amdgcn_exp2f(mb[qt] - m);
+                            mb[qt] = m;
+                            lrow[qt] *= a;
+#pragma unroll
+                            for (int ht = 0; ht < HT; ++ht)
+#pragma unroll
+                                for (int r = 0; r < 16; ++r) oacc[ht][qt][r] *= a;
+                        }
+                    }
+                    bf16x8 pr[2][2];
+#pragma unroll
+                    for (int qt = 0; qt < 2; ++qt) {
+                        float sum = 0.f;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const float e = __builtin_amdgcn_exp2f(fmaf(S[qt][r], sc_log2e, -mb[qt]));
+                            sum += e;
+                            pr[qt][r >> 3][r & 7] = (__bf16)e;
+                        }
+                        lrow[qt] += sum;
+                    }
+#pragma unroll
+                    for (int j2 = 0; j2 < 2; ++j2)
+#pragma unroll
+                        for (int ht = 0; ht < HT; ++ht)
+#pragma unroll
+                            for (int qt = 0; qt < 2; ++qt) PO_MFMA_ACC_FRESH(oacc[ht][qt], vf[j2][ht], pr[qt][j2]);
+                }
+            };
+            if (sp.n2 > 0)
+                keys(sp.k2 + ((int64_t)sp.tiles2 * 64 * Hkv + kvh) * HD, sp.vt2 + ((int64_t)kvh * HD + l31) * sp.ldv2 + sp.tiles2 * 64, sp.ldv2,
+                     sp.n2, sp.n2, sp.n2, sp.n2);
+            if (sp.own && qw < n_virtual) {
+                const int r0 = __builtin_amdgcn_readfirstlane(vreq[0]), r1 = __builtin_amdgcn_readlane(vreq[1], 31);
+                const int last = min(qw + 63, n_virtual - 1) / group;                  // the wavefront's last row
+                for (int r = r0; r <= r1; ++r) {
+                    const SharedSeq sq = sp.tab.seq[r];
+                    const int first_row = sp.tab.row0[r];
+                    const int hidden = sq.kv_len - sq.q_len + 1 - first_row;           // row c of the table sees c + hidden keys
+                    keys(k_own + ((int64_t)sq.kv_row * Hkv + kvh) * HD, vt_own + ((int64_t)kvh * HD + l31) * ldv_own + sq.kv_row, ldv_own, sq.kv_len,
+                         vreq[0] == r ? vrow[0] + hidden : 0, vreq[1] == r ? vrow[1] + hidden : 0, min(last, first_row + sq.q_len - 1) + hidden);
+                }
+            }
+            PO_MFMA_END();
+        }
+        if (sp.own && sp.n == 1) {
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt) {
+                const float inv = 1.0f / half_swap_sum(lrow[qt]);
+                if (qw + qt * 32 + l31 >= n_virtual) continue;
+                bf16_t* op = o + ((int64_t)vq[qt] * Hq + vhead[qt]) * HD + 4 * lhi;
+#pragma unroll
+                for (int ht = 0; ht < HT; ++ht)
+#pragma unroll
+                    for (int rg = 0; rg < 4; ++rg) {
+                        uint2 w;
+                        w.x = (uint32_t)f2bf(oacc[ht][qt][rg * 4 + 0] * inv) | ((uint32_t)f2bf(oacc[ht][qt][rg * 4 + 1] * inv) << 16);
+                        w.y = (uint32_t)f2bf(oacc[ht][qt][rg * 4 + 2] * inv) | ((uint32_t)f2bf(oacc[ht][qt][rg * 4 + 3] * inv) << 16);
+                        *(uint2*)(op + ht * 32 + rg * 8) = w;
+                    }
+            }
+            return;
+        }
+    }
     if (SPLIT) {
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
@@ -1305,6 +1428,29 @@ int launch_split_fwd64(const bf16_t* q, const bf16_t* k, const bf16_t* vt, int64
 }
 
 }  // namespace
+
+// The tile kernel over the prefix's whole tiles and everything behind them, for the rows of one table, in `pieces` pieces of the
+// prefix (partial results in opart, mlpart when more than one or without the own keys, merged by the caller).
+int launch_attention_shared_tiles(const SharedParams& p, const SharedTable& tab, int pieces, bool own, float* opart, float* mlpart, hipStream_t s) {
+    constexpr int SMEM = 2 * A64_NSTAGE * A64_TILE + 16;
+    static OncePerDevice lds;
+    lds.run(current_device(), [] { allow_dynamic_lds((const void*)(attn_fwd64_kernel<false, 3, 2>), SMEM); });
+    const int rows = tab.row0[tab.n];
+    SharedSplitArgs sp;
+    sp.k2 = (const bf16_t*)p.k2; sp.vt2 = (const bf16_t*)p.v2; sp.ldv2 = p.ldv2;
+    sp.opart = opart; sp.mlpart = mlpart;
+    sp.q_row0 = 0;
+    sp.tiles2 = p.n2 / 64;
+    sp.n2 = p.n2 % 64;
+    sp.per = (sp.tiles2 + pieces - 1) / pieces;
+    sp.n = (sp.tiles2 + sp.per - 1) / sp.per;
+    sp.tab = tab;
+    sp.own = own;
+    const int nqt = (int)(((int64_t)rows * (p.Hq / p.Hkv) + 255) / 256);
+    hipLaunchKernelGGL((attn_fwd64_kernel<false, 3, 2>), dim3((unsigned)(p.Hkv * sp.n * nqt)), dim3(256), SMEM, s, (const bf16_t*)p.q,
+                       (const bf16_t*)p.k, (const bf16_t*)p.v, p.ldv, (bf16_t*)p.o, rows, p.Hq, p.Hkv, p.sc, nqt, 0, nullptr, sp);
+    return sp.n;
+}
 
 bool attention_mfma_supported(int Hq, int Hkv, int hd) {
     return (hd == 128 || hd == 64) && Hkv > 0 && Hq % Hkv == 0;

@@ -5,15 +5,16 @@
 // All query heads of a KV head are rows of one tile (a request of q_len positions has q_len * group of them), since they share
 // their keys.  A lane owns one row: S^T = K Q^T leaves it 16 of a block's 32 keys (its partner lane ^ 32 the others), the
 // softmax is per lane, and the probabilities are at once the operand of O^T += V^T P^T (K rows are read in an order that makes
-// the eight keys a lane feeds to an MFMA contiguous in V^T, as in attn_mfma.hip).  K and V^T go from memory to
-// registers: a wavefront's fragments are whole 16-byte pieces, and what several wavefronts read they find in the caches.
+// the eight keys a lane feeds to an MFMA contiguous in V^T, as in attn_mfma.hip).
 #include "attn_shared.h"
+
+#include <math.h>
 
 #include <algorithm>
 
 namespace po {
 
-typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef shared_bf16x8 bf16x8;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 
 namespace {
@@ -26,6 +27,8 @@ __device__ __forceinline__ float other_half_sum(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+
+__device__ __forceinline__ int swz8(int row) { return (row & 7) ^ ((row >> 3) & 1); }
 
 // 32 rows of a wavefront, a lane's column, and what has been summed for it
 template <int HD>
@@ -50,71 +53,72 @@ struct Rows {
         l = 0.f;
     }
 
-    // 32 keys; see: how many of them this lane's row sees (all of them unless `masked`)
-    __device__ __forceinline__ void block(const bf16x8 (&kf)[KS], const bf16x8 (&vf)[2][HT], bool masked, int see, int lhi, float sc) {
-        f32x16 s = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], s, 0, 0, 0);
+    // scores of N blocks of 32 keys -> their probabilities, as the operand of O^T += V^T P^T; see: how many of the keys this
+    // lane's row sees (all of them unless `masked`)
+    template <int N>
+    __device__ __forceinline__ void softmax(f32x16 (&s)[N], bf16x8 (&pf)[2 * N], bool masked, int see, int lhi, float sc) {
         if (masked) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if ((r & 7) + 8 * lhi + 16 * (r >> 3) >= see) s[r] = -INFINITY;
-        }
-        float top = s[0];
+            for (int a = 0; a < N; ++a)
 #pragma unroll
-        for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+                for (int r = 0; r < 16; ++r)
+                    if (a * 32 + (r & 7) + 8 * lhi + 16 * (r >> 3) >= see) s[a][r] = -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int a = 0; a < N; ++a)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[a][r]);
         top = fmaxf(m, other_half_max(top));
         const float ref = top == -INFINITY ? 0.f : top * sc;      // (nothing seen yet: all probabilities come out 0)
         if (__any(top > m)) {                                     // (else every factor is 1)
-            const float a = __builtin_amdgcn_exp2f(fmaf(m, sc, -ref));
-            l *= a;
+            const float f = __builtin_amdgcn_exp2f(fmaf(m, sc, -ref));
+            l *= f;
 #pragma unroll
             for (int ht = 0; ht < HT; ++ht)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[ht][r] *= a;
+                for (int r = 0; r < 16; ++r) acc[ht][r] *= f;
             m = top;
         }
-        bf16x8 pf[2];
-        float sum = 0.f;
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(s[r], sc, -ref));
-            sum += e;
-            pf[r >> 3][r & 7] = (__bf16)e;        // (the one rounding of a probability: the matrix instruction's operand)
-        }
-        l += sum;
+        for (int a = 0; a < N; ++a)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int ht = 0; ht < HT; ++ht) acc[ht] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j][ht], pf[j], acc[ht], 0, 0, 0);
+            for (int r = 0; r < 16; ++r) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[a][r], sc, -ref));
+                sum[r & 1] += e;
+                pf[2 * a + (r >> 3)][r & 7] = (__bf16)e;      // (the one rounding of a probability: the matrix instruction's operand)
+            }
+        l += sum[0] + sum[1];
     }
 };
 
-// One workgroup: a tile of rows of one request and KV head, all its keys.
-// SPLIT: the tile is 32 rows and the wavefronts take every NW-th block of keys each, meeting in LDS at the end (few rows, one
-// token of a request: what counts is how many keys are on their way at once); otherwise each wavefront has 32 rows of its own.
-template <int HD, int NW, bool SPLIT>
-__global__ void __launch_bounds__(NW * 64) attn_shared_kernel(const SharedParams p, const SharedTable tab) {
-    constexpr int KS = HD / 16, HT = HD / 32, ROWS = SPLIT ? 32 : 32 * NW;
-    extern __shared__ __attribute__((aligned(16))) float lds[];
+// o = y / l in bf16, 4 values; a row that sees nothing: 0
+__device__ __forceinline__ void store4(bf16_t* o, float a, float b, float c, float d, float inv) {
+    uint2 w;
+    w.x = (uint32_t)f2bf(a * inv) | ((uint32_t)f2bf(b * inv) << 16);
+    w.y = (uint32_t)f2bf(c * inv) | ((uint32_t)f2bf(d * inv) << 16);
+    *(uint2*)o = w;
+}
+
+// One workgroup: 128 rows of one request and KV head, 32 a wavefront, all their keys.  K and V^T come from memory to registers in
+// blocks of 32 keys; what several wavefronts read they find in the caches.
+template <int HD>
+__global__ void __launch_bounds__(256) attn_shared_rows_kernel(const SharedParams p, const SharedTable tab) {
+    constexpr int KS = HD / 16, HT = HD / 32;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l31 = lane & 31, lhi = lane >> 5;
-    const int kvh = (int)(blockIdx.x % (unsigned)p.Hkv), item = (int)(blockIdx.x / (unsigned)p.Hkv);
+    const int kvh = (int)(blockIdx.x % (unsigned)p.Hkv), item = (int)(blockIdx.x / (unsigned)p.Hkv), group = p.Hq / p.Hkv;
     const int req = __builtin_amdgcn_readfirstlane(shared_request(tab, item));
     const SharedSeq sq = tab.seq[req];
-    const int group = p.Hq / p.Hkv;
-    const int row0 = (item - tab.item0[req]) * ROWS + (SPLIT ? 0 : wave * 32);      // of this wavefront, in (position, head) order
-    const int n_rows = sq.q_len * group;
-    if (!SPLIT && row0 >= n_rows) return;
-    const int vr = min(row0 + l31, n_rows - 1);
-    const int pos = vr / group, head = kvh * group + vr - pos * group;
+    const int row0 = ((item - tab.item0[req]) * 4 + wave) * 32, n_rows = sq.q_len * group;      // (position, head) order
+    if (row0 >= n_rows) return;
+    const int vr = min(row0 + l31, n_rows - 1), pos = vr / group, head = kvh * group + vr - pos * group;
     const bool valid = row0 + l31 < n_rows;
     const int64_t orow = ((int64_t)(sq.q_row + pos) * p.Hq + head) * HD;
-    const int see = sq.kv_len - sq.q_len + pos + 1;            // own keys this row sees (may be below 0)
-    // own keys that any, and that every, row of the wavefront sees
-    const int see_max = max(0, sq.kv_len - sq.q_len + min(row0 + 31, n_rows - 1) / group + 1);
-    const int see_min = sq.kv_len - sq.q_len + row0 / group + 1;
+    const int hidden = sq.kv_len - sq.q_len + 1;               // position i of the request sees i + hidden own keys (may be below 0)
+    const int see_max = max(0, hidden + min(row0 + 31, n_rows - 1) / group), see_min = hidden + row0 / group;
 
     Rows<HD> st;
     st.start((const bf16_t*)p.q + orow + lhi * 8, valid);
@@ -127,135 +131,455 @@ __global__ void __launch_bounds__(NW * 64) attn_shared_kernel(const SharedParams
     const int nb2 = (p.n2 + 31) / 32, nb = nb2 + (see_max + 31) / 32;
     // K rows of block b; past the last key the last one (those scores are masked)
     auto load_k = [&](int b, bf16x8 (&kf)[KS]) {
-        const bool own = b >= nb2;
-        const int key = (own ? b - nb2 : b) * 32 + pk;
-        const bf16_t* const r = (own ? ko : kp) + (int64_t)min(key, (own ? sq.kv_len : p.n2) - 1) * krs;
+        const bf16_t* const r = (b < nb2 ? kp : ko) + (int64_t)min((b < nb2 ? b : b - nb2) * 32 + pk, (b < nb2 ? p.n2 : sq.kv_len) - 1) * krs;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) kf[ks] = __builtin_bit_cast(bf16x8, *(const uint4*)(r + ks * 16));
     };
-    // V^T of block b; columns past the last key count as 0, whatever they hold
-    auto load_v = [&](int b, bf16x8 (&vf)[2][HT]) {
-        const bool own = b >= nb2;
-        const int key0 = (own ? b - nb2 : b) * 32, end = own ? sq.kv_len : p.n2;
-        const bf16_t* const r = own ? vo : vp;
-        const int64_t ld = own ? p.ldv : p.ldv2;
-        if (key0 + 32 <= end) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int ht = 0; ht < HT; ++ht)
-                    vf[j][ht] = __builtin_bit_cast(bf16x8, *(const uint4*)(r + ht * 32 * ld + key0 + 16 * j + 8 * lhi));
-        } else {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int key = key0 + 16 * j + 8 * lhi, n = end - key;        // n of the eight are keys
-                uint32_t mask[4];
-#pragma unroll
-                for (int w = 0; w < 4; ++w) mask[w] = n >= 2 * w + 2 ? 0xffffffffu : n == 2 * w + 1 ? 0xffffu : 0u;
-#pragma unroll
-                for (int ht = 0; ht < HT; ++ht) {
-                    uint4 t = make_uint4(0, 0, 0, 0);
-                    if (n > 0) t = *(const uint4*)(r + ht * 32 * ld + key);
-                    t.x &= mask[0]; t.y &= mask[1]; t.z &= mask[2]; t.w &= mask[3];
-                    vf[j][ht] = __builtin_bit_cast(bf16x8, t);
-                }
-            }
-        }
-    };
-    const int step = SPLIT ? NW : 1;
-    bf16x8 kf[KS], kn[KS], vf[2][HT];
-    int b = SPLIT ? wave : 0;
-    if (b < nb) load_k(b, kf);
-    for (; b < nb; b += step) {
-        load_v(b, vf);
-        if (b + step < nb) load_k(b + step, kn);
+    bf16x8 kf[KS], kn[KS], vf[2][HT], pf[2];
+    if (nb > 0) load_k(0, kf);
+    for (int b = 0; b < nb; ++b) {
         const bool own = b >= nb2;
         const int key0 = (own ? b - nb2 : b) * 32;
-        st.block(kf, vf, key0 + 32 > (own ? see_min : p.n2), (own ? see : p.n2) - key0, lhi, p.sc);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            load_vt_eight<HT>(own ? vo : vp, own ? p.ldv : p.ldv2, key0 + 16 * j + 8 * lhi, own ? sq.kv_len : p.n2, vf[j]);
+        if (b + 1 < nb) load_k(b + 1, kn);
+        f32x16 s[1] = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], st.qf[ks], s[0], 0, 0, 0);
+        st.template softmax<1>(s, pf, key0 + 32 > (own ? see_min : p.n2), (own ? pos + hidden : p.n2) - key0, lhi, p.sc);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int ht = 0; ht < HT; ++ht) st.acc[ht] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j][ht], pf[j], st.acc[ht], 0, 0, 0);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) kf[ks] = kn[ks];
     }
-    bf16_t* const o = (bf16_t*)p.o;
     const float l = other_half_sum(st.l);
-    if (!SPLIT) {
-        if (!valid) return;
-        const float inv = l > 0.f ? 1.0f / l : 0.f;             // (a row that sees nothing: 0)
-#pragma unroll
-        for (int ht = 0; ht < HT; ++ht)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                uint2 w;
-                w.x = (uint32_t)f2bf(st.acc[ht][4 * g] * inv) | ((uint32_t)f2bf(st.acc[ht][4 * g + 1] * inv) << 16);
-                w.y = (uint32_t)f2bf(st.acc[ht][4 * g + 2] * inv) | ((uint32_t)f2bf(st.acc[ht][4 * g + 3] * inv) << 16);
-                *(uint2*)(o + orow + ht * 32 + 8 * g + 4 * lhi) = w;
-            }
-        return;
-    }
-    // SPLIT: [wave][row][HD + 4] accumulators, then [wave][row] maxima and sums, joined in wavefront order
-    constexpr int LD = HD + 4;
-    float* const sm = lds + NW * 32 * LD;
-    float* const sl = sm + NW * 32;
-    if (lhi == 0) { sm[wave * 32 + l31] = st.m; sl[wave * 32 + l31] = l; }
+    if (!valid) return;
+    const float inv = l > 0.f ? 1.0f / l : 0.f;
 #pragma unroll
     for (int ht = 0; ht < HT; ++ht)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-            *(float4*)(lds + (wave * 32 + l31) * LD + ht * 32 + 8 * g + 4 * lhi) =
-                make_float4(st.acc[ht][4 * g], st.acc[ht][4 * g + 1], st.acc[ht][4 * g + 2], st.acc[ht][4 * g + 3]);
-    __syncthreads();
-    constexpr int PER = NW * 64 / 32, DV = HD / PER;            // threads of a row, values of a thread
-    const int jr = tid / PER, d0 = tid % PER * DV;
-    const int jv = row0 + jr;
-    if (jv >= n_rows) return;
-    float top = sm[jr];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) top = fmaxf(top, sm[w * 32 + jr]);
-    float lt = 0.f, y[DV];
-#pragma unroll
-    for (int e = 0; e < DV; ++e) y[e] = 0.f;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-        const float mw = sm[w * 32 + jr];
-        const float f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw - top) * p.sc);
-        lt += f * sl[w * 32 + jr];
-#pragma unroll
-        for (int e = 0; e < DV; ++e) y[e] += f * lds[(w * 32 + jr) * LD + d0 + e];
+            store4((bf16_t*)p.o + orow + ht * 32 + 8 * g + 4 * lhi, st.acc[ht][4 * g], st.acc[ht][4 * g + 1], st.acc[ht][4 * g + 2],
+                   st.acc[ht][4 * g + 3], inv);
+}
+
+// How a launch of few rows is divided.  Partial results: opart [piece][row of the table][head][HD], mlpart [..][2] (maximum in
+// powers of 2, sum), the prefix's np pieces first, then those of a request's own keys.
+struct Parts {
+    float *opart, *mlpart;
+    int np, per;               // the prefix: pieces of `per` keys
+    int own_per;               // own keys: pieces of that many (0: their part is not among the pieces)
+    int prefix_items;          // workgroups of the prefix per KV head
+};
+
+// Few rows (one token a request): what counts is how many keys are on their way at once.  Every wavefront has 64 keys of its own in LDS
+// at a time, loaded by whole cache lines past the registers (K rows as they are, 128 bytes of each V^T row), no two wavefronts wait
+// for each other, and they meet at the end.  K of its next block is on its way as soon as the scores are there, V^T as soon as
+// the products are.  RT: tiles of 32 rows that go through the same keys.
+// WHOLE: a workgroup is 32 rows of one request, all keys they see; result in o.
+// PARTS: a workgroup is a piece of the prefix, which all requests share, with 32 RT rows of any requests; or a piece of a request's own keys
+// with 32 of its rows.  Partial results.
+enum { WHOLE, PARTS };
+template <int HD, int NW, int RT, int MODE>
+__global__ void __launch_bounds__(NW * 64, 1) attn_shared_tokens_kernel(const SharedParams p, const Parts parts, const SharedTable tab) {
+    constexpr int KS = HD / 16, HT = HD / 32;
+    constexpr int UNIT = 64 * HD * 2, N_DMA = UNIT / 1024;      // bytes of 64 keys of K or V^T; loads of a wavefront
+    constexpr int LPR = HD / 8;                                 // lanes (16 bytes each) of a K row
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l31 = lane & 31, lhi = lane >> 5;
+    const int kvh = (int)(blockIdx.x % (unsigned)p.Hkv), group = p.Hq / p.Hkv;
+    int item = (int)(blockIdx.x / (unsigned)p.Hkv);
+    const bool of_prefix = MODE == PARTS && item < parts.prefix_items;
+    if (MODE == PARTS && !of_prefix) item -= parts.prefix_items;
+    // rows in (position, head) order: of one request, or (a piece of the prefix) of the table
+    int req = 0, row0, n_rows, piece = 0;
+    SharedSeq sq = {0, 0, 0, 0};
+    if (of_prefix) {
+        piece = item % parts.np;
+        row0 = item / parts.np * (32 * RT);
+        n_rows = tab.row0[tab.n] * group;
+    } else {
+        req = __builtin_amdgcn_readfirstlane(shared_request(tab, item));
+        sq = tab.seq[req];
+        int tile = item - tab.item0[req];
+        if (MODE == PARTS) {
+            const int pieces = (sq.kv_len + parts.own_per - 1) / parts.own_per;
+            piece = tile % pieces;
+            tile /= pieces;
+        }
+        row0 = tile * 32;
+        n_rows = sq.q_len * group;
     }
-    const float inv = lt > 0.f ? 1.0f / lt : 0.f;
-    const int jp = jv / group;
-    bf16_t* const op = o + ((int64_t)(sq.q_row + jp) * p.Hq + kvh * group + jv - jp * group) * HD + d0;
+    const int n_rt = of_prefix ? min(RT, (n_rows - row0 + 31) / 32) : 1;
+    const int hidden = sq.kv_len - sq.q_len + 1;               // position i of the request sees i + hidden own keys (may be below 0)
+    const int see = min(row0 + l31, n_rows - 1) / group + hidden;
+    const int see_max = max(0, hidden + min(row0 + 31, n_rows - 1) / group), see_min = hidden + row0 / group;
+    // prefix keys [a0, a1), then own keys [b0, b1)
+    const int a0 = of_prefix ? piece * parts.per : 0;
+    const int a1 = MODE == WHOLE ? p.n2 : of_prefix ? min(a0 + parts.per, p.n2) : 0;
+    const int b0 = MODE == PARTS && !of_prefix ? piece * parts.own_per : 0;
+    const int b1 = MODE == WHOLE ? see_max : of_prefix ? 0 : min(b0 + parts.own_per, see_max);
+    const int nb2 = max(a1 - a0 + 63, 0) / 64, nb = nb2 + max(b1 - b0 + 63, 0) / 64;
+
+    Rows<HD> st[RT];
 #pragma unroll
-    for (int e = 0; e < DV; e += 4) {
-        uint2 w;
-        w.x = (uint32_t)f2bf(y[e] * inv) | ((uint32_t)f2bf(y[e + 1] * inv) << 16);
-        w.y = (uint32_t)f2bf(y[e + 2] * inv) | ((uint32_t)f2bf(y[e + 3] * inv) << 16);
-        *(uint2*)(op + e) = w;
+    for (int rt = 0; rt < RT; ++rt) {
+        const int vr = min(row0 + rt * 32 + l31, n_rows - 1), pos = vr / group;
+        int q_row = sq.q_row + pos;
+        if (of_prefix) {
+            const int r = shared_request_of_row(tab, pos);
+            q_row = tab.seq[r].q_row + pos - tab.row0[r];
+        }
+        st[rt].start((const bf16_t*)p.q + ((int64_t)q_row * p.Hq + kvh * group + vr - pos * group) * HD + lhi * 8, row0 + rt * 32 + l31 < n_rows);
+    }
+    const int64_t krs = (int64_t)p.Hkv * HD;
+    const bf16_t* const ko = (const bf16_t*)p.k + (int64_t)sq.kv_row * krs + kvh * HD;
+    const bf16_t* const kp = (const bf16_t*)p.k2 + kvh * HD;
+    const bf16_t* const vo = (const bf16_t*)p.v + (int64_t)kvh * HD * p.ldv + sq.kv_row;
+    const bf16_t* const vp = (const bf16_t*)p.v2 + (int64_t)kvh * HD * p.ldv2;
+    unsigned char* const sk = smem + wave * (2 * UNIT);
+    unsigned char* const sv = sk + UNIT;
+    auto first_key = [&](int b) { return b < nb2 ? a0 + b * 64 : b0 + (b - nb2) * 64; };
+    // Block b's K, and V^T, into this wavefront's LDS, 16-byte segments swizzled with the row on the global side; from block nb on nothing
+    // (an empty descriptor: the number of loads in flight stays known).  K rows past the last key read as 0; V^T columns past it
+    // hold anything, the last row's up to the eight that hold the last key.
+    auto dma_k = [&](int b) {
+        const int key0 = first_key(b), end = b < nb2 ? p.n2 : sq.kv_len;
+        const int n = b < nb ? min(64, end - key0) : 0;
+        const bf16_t* const base = (b < nb2 ? kp : ko) + (b < nb ? key0 * krs : 0);
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, n > 0 ? (int)((uint32_t)(n - 1) * (uint32_t)(krs * 2) + HD * 2) : 0, 0x00020000);
+#pragma unroll
+        for (int j = 0; j < N_DMA; ++j) {
+            const int row = j * (64 / LPR) + lane / LPR, seg = lane % LPR;
+            const int sw = LPR == 16 ? seg ^ (row & 15) : seg ^ swz8(row);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(sk + j * 1024), 16,
+                                                     (uint32_t)row * (uint32_t)(krs * 2) + (uint32_t)(sw << 4), 0, 0, 0);
+        }
+    };
+    auto dma_v = [&](int b) {
+        const int key0 = first_key(b), end = b < nb2 ? p.n2 : sq.kv_len;
+        const uint32_t ld2 = (uint32_t)((b < nb2 ? p.ldv2 : p.ldv) * 2);
+        const bf16_t* const base = (b < nb2 ? vp : vo) + (b < nb ? key0 : 0);
+        const uint32_t bytes = b < nb ? (HD - 1) * ld2 + (uint32_t)min(64, (end - key0 + 7) & ~7) * 2 : 0u;
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
+#pragma unroll
+        for (int j = 0; j < N_DMA; ++j) {
+            const int row = j * 8 + (lane >> 3);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(sv + j * 1024), 16,
+                                                     (uint32_t)row * ld2 + (uint32_t)(((lane & 7) ^ swz8(row)) << 4), 0, 0, 0);
+        }
+    };
+    // fragments: K row pi(i) of a 32-key half (bits 2, 3 swapped: the eight keys a lane feeds to an MFMA are then side by side in
+    // V^T), V^T row i of a 32-row tile
+    const int pk = (l31 & 0x13) | ((l31 & 4) << 1) | ((l31 & 8) >> 1);
+    const int k_sw = LPR == 16 ? (pk & 15) : swz8(pk), v_sw = swz8(l31);
+    int b = wave;
+    dma_k(b);
+    dma_v(b);
+#pragma unroll 1
+    for (; b < nb; b += NW) {
+        const bool own = b >= nb2;
+        const int key0 = first_key(b), end = own ? sq.kv_len : p.n2;
+        const bool masked = key0 + 64 > (own ? see_min : a1);
+        const int n_v = end - key0;                            // V^T columns that are keys
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            if (rt >= n_rt) break;
+            if (rt == 0) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N_DMA) : "memory");        // K is there, V^T may be on its way
+            f32x16 s[2];
+            bf16x8 pf[4];
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[a][r] = 0.f;
+            bf16x8 kf[KS][2];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int a = 0; a < 2; ++a) kf[ks][a] = *(const bf16x8*)(sk + (a * 32 + pk) * (HD * 2) + (((ks * 2 + lhi) ^ k_sw) << 4));
+            if (rt == n_rt - 1) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                // (the fragments are in registers)
+                dma_k(b + NW);
+            }
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int a = 0; a < 2; ++a) s[a] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks][a], st[rt].qf[ks], s[a], 0, 0, 0);
+            st[rt].template softmax<2>(s, pf, masked, (own ? see : a1) - key0, lhi, p.sc);
+            if (rt == 0) {                                                        // V^T is there (K of the next block may be on its way)
+                if (n_rt == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N_DMA) : "memory");
+                else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int ht = 0; ht < HT; ++ht) {
+                    uint4 v = *(const uint4*)(sv + (ht * 32 + l31) * 128 + (((j * 2 + lhi) ^ v_sw) << 4));
+                    if (n_v < 64) {                                               // columns past the last key count as 0, whatever they hold
+                        const int n = n_v - (16 * j + 8 * lhi);
+                        v.x &= n >= 2 ? 0xffffffffu : n == 1 ? 0xffffu : 0u;
+                        v.y &= n >= 4 ? 0xffffffffu : n == 3 ? 0xffffu : 0u;
+                        v.z &= n >= 6 ? 0xffffffffu : n == 5 ? 0xffffu : 0u;
+                        v.w &= n >= 8 ? 0xffffffffu : n == 7 ? 0xffffu : 0u;
+                    }
+                    st[rt].acc[ht] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pf[j], st[rt].acc[ht], 0, 0, 0);
+                }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        dma_v(b + NW);
+    }
+    // ---- the wavefronts' parts, a row tile at a time: [wave][row][HD + 4] sums, then [wave][row] maxima and sums of p, joined in
+    // wavefront order (what the loads still on their way write is out of use)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    constexpr int LD = HD + 4, DV = HD / 4;                    // 4 values a thread and turn
+    float* const lds = (float*)smem;
+    float* const sm = lds + NW * 32 * LD;
+    float* const sl = sm + NW * 32;
+    const int64_t plane = (int64_t)tab.row0[tab.n] * p.Hq;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        if (rt >= n_rt) break;
+        const float l = other_half_sum(st[rt].l);
+        __syncthreads();
+        // (maxima in powers of 2 from here on)
+        if (lhi == 0) { sm[wave * 32 + l31] = st[rt].m == -INFINITY ? -1.0e30f : st[rt].m * p.sc; sl[wave * 32 + l31] = l; }
+#pragma unroll
+        for (int ht = 0; ht < HT; ++ht)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *(float4*)(lds + (wave * 32 + l31) * LD + ht * 32 + 8 * g + 4 * lhi) =
+                    make_float4(st[rt].acc[ht][4 * g], st[rt].acc[ht][4 * g + 1], st[rt].acc[ht][4 * g + 2], st[rt].acc[ht][4 * g + 3]);
+        __syncthreads();
+        const int rows_here = min(32, n_rows - row0 - rt * 32);
+        for (int i = tid; i < rows_here * DV; i += NW * 64) {
+            const int jr = i / DV, d = i % DV * 4, jv = row0 + rt * 32 + jr, jp = jv / group, jh = kvh * group + jv - jp * group;
+            const int64_t rh = (of_prefix ? jp : tab.row0[req] + jp) * (int64_t)p.Hq + jh;
+            float top = sm[jr];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) top = fmaxf(top, sm[w * 32 + jr]);
+            float lt = 0.f;
+            float4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float f = __builtin_amdgcn_exp2f(sm[w * 32 + jr] - top);
+                const float4 v = *(const float4*)(lds + (w * 32 + jr) * LD + d);
+                lt += f * sl[w * 32 + jr];
+                y.x += f * v.x; y.y += f * v.y; y.z += f * v.z; y.w += f * v.w;
+            }
+            if (MODE == PARTS) {
+                const int64_t slot = (of_prefix ? piece : parts.np + piece) * plane + rh;
+                *(float4*)(parts.opart + slot * HD + d) = y;
+                if (d == 0) *(float2*)(parts.mlpart + slot * 2) = make_float2(top, lt);
+                continue;
+            }
+            store4((bf16_t*)p.o + ((int64_t)(sq.q_row + jp) * p.Hq + jh) * HD + d, y.x, y.y, y.z, y.w, lt > 0.f ? 1.0f / lt : 0.f);
+        }
     }
 }
 
+// The pieces of every row, in their order: o = sum of 2^(m - top) O / sum of 2^(m - top) l; HD / 4 threads a row and head.
 template <int HD>
-void launch_t(const SharedParams& p, const po_request_rows* seq, int n, hipStream_t s) {
-    constexpr int SPLIT_LDS = (8 * 32 * (HD + 4) + 2 * 8 * 32) * 4;
+__global__ void __launch_bounds__(256) attn_shared_join_kernel(const SharedParams p, const Parts parts, const SharedTable tab) {
+    constexpr int PER = HD / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int rows = tab.row0[tab.n];
+    const int64_t plane = (int64_t)rows * p.Hq;
+    if (i >= plane * PER) return;
+    const int64_t rh = i / PER;
+    const int c = (int)(rh / p.Hq), head = (int)(rh - (int64_t)c * p.Hq), f = (int)(i - rh * PER) * 4;
+    const int req = shared_request_of_row(tab, c);
+    const SharedSeq sq = tab.seq[req];
+    const int n = parts.np + (parts.own_per ? (sq.kv_len + parts.own_per - 1) / parts.own_per : 0);
+    const int lane = threadIdx.x & (PER - 1);
+    float top = -1.0e30f;
+    for (int s = lane; s < n; s += PER) top = fmaxf(top, parts.mlpart[(s * plane + rh) * 2]);
+#pragma unroll
+    for (int off = PER / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, PER));
+    float4 acc = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+    for (int s0 = 0; s0 < n; s0 += PER) {
+        const float2 ml = *(const float2*)(parts.mlpart + (min(s0 + lane, n - 1) * plane + rh) * 2);
+        const float wl = s0 + lane < n ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
+        for (int e0 = 0; e0 < min(PER, n - s0); e0 += 4) {              // (pieces past the last one: the last one, weight 0)
+            float4 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = *(const float4*)(parts.opart + (min(s0 + e0 + u, n - 1) * plane + rh) * HD + f);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float w = __shfl(wl, e0 + u, PER);
+                acc.x += w * v[u].x; acc.y += w * v[u].y; acc.z += w * v[u].z; acc.w += w * v[u].w;
+                l += w * __shfl(ml.y, e0 + u, PER);
+            }
+        }
+    }
+    const float inv = l > 0.f ? 1.0f / l : 0.f;
+    uint2 w2;
+    w2.x = (uint32_t)f2bf(acc.x * inv) | ((uint32_t)f2bf(acc.y * inv) << 16);
+    w2.y = (uint32_t)f2bf(acc.z * inv) | ((uint32_t)f2bf(acc.w * inv) << 16);
+    *(uint2*)((bf16_t*)p.o + ((int64_t)(sq.q_row + c - tab.row0[req]) * p.Hq + head) * HD + f) = w2;
+}
+
+// How the requests of a table run.
+//   TOKENS       one launch, 32 rows of a request and all their keys a workgroup
+//   ROWS         one launch, 128 rows of a request and all their keys a workgroup
+//   TILES        256 rows of any requests a workgroup of attn_mfma.hip's tile kernel, the prefix in np pieces; joined when np > 1
+//   SPLIT        the prefix in np pieces with 32 rt rows of any requests, own keys in pieces of own_per, joined
+//   TILES_SPLIT  the prefix by the tile kernel, own keys in pieces, joined
+enum Mode { TOKENS, ROWS, TILES, SPLIT, TILES_SPLIT };
+struct Plan {
+    Mode mode;
+    int np, per, own_per, rt, slots;     // slots: partial results of a row at most
+};
+
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+// The one expected to take the least time (microseconds) with the scratch there is.
+Plan plan(const SharedTable& t, int Hq, int Hkv, int hd, int n2, size_t scratch_bytes) {
+    const int group = Hq / Hkv, rows = t.row0[t.n], tiles2 = n2 / 64;
+    const int64_t vr = (int64_t)rows * group;
+    const double row_us = (double)rows * Hq * (hd + 2) * 4.0 * 2.0 / 4.5e6;          // a slot of every row, written and read
+    const double row_bytes = (double)rows * Hq * (hd + 2) * 4.0, hd_part = hd / 128.0;
+    int own_max = 0;
+    int64_t own_sum = 0, tiles32 = 0, tiles128 = 0;
+    for (int i = 0; i < t.n; ++i) {
+        const SharedSeq& q = t.seq[i];
+        own_max = std::max(own_max, q.kv_len);
+        own_sum += q.kv_len;
+        tiles32 += ceil_div((int64_t)q.q_len * group, 32);
+        tiles128 += ceil_div((int64_t)q.q_len * group, 128);
+    }
+    Plan best{TOKENS, 0, 0, 0, 1, 0};
+    // a wavefront's block of 64 keys costs 1.9 us alone on its compute unit, 2.4 with another workgroup beside it
+    const int64_t wg32 = tiles32 * Hkv;
+    const double keys_mean = n2 + (double)own_sum / t.n, keys_max = n2 + own_max;
+    double t_best = wg32 <= 256 ? 6.0 + 1.9 * hd_part * std::ceil(keys_max / 256)
+                                : 6.0 + 2.4 * hd_part * std::max(std::ceil(keys_max / 128), wg32 / 512.0 * std::ceil(keys_mean / 128));
+    const auto take = [&](const Plan& p, double us) {
+        if (us < t_best && p.slots * row_bytes <= (double)scratch_bytes) { best = p; t_best = us; }
+    };
+    // 32 keys of a wavefront: 1.4 us, 1.8 with two workgroups a compute unit
+    const int64_t wg128 = tiles128 * Hkv;
+    take({ROWS, 0, 0, 0, 1, 0}, 5.0 + hd_part * (wg128 <= 256 ? 1.4 * std::ceil(keys_max / 32) : 1.8 * std::max(std::ceil(keys_max / 32), wg128 / 256.0 * keys_mean / 32)));
+    if (n2 == 0 && own_max == 0) return best;
+    // own keys by pieces, and the join
+    const int own_per = (int)std::min<int64_t>(2048, std::max<int64_t>(512, (own_sum * Hkv / 256 + 255) / 256 * 256));
+    const int own_slots = ceil_div(own_max, own_per);
+    int64_t own_wgs = 0;
+    for (int i = 0; i < t.n; ++i) own_wgs += (int64_t)ceil_div((int64_t)t.seq[i].q_len * group, 32) * ceil_div(t.seq[i].kv_len, own_per) * Hkv;
+    const double own_blocks = std::ceil(std::min<double>(own_per, own_max) / 256);
+    const double own_us = own_wgs ? hd_part * 1.9 * std::max(own_blocks, own_wgs / 256.0 * std::max(1.0, (double)own_sum / t.n / 256 / std::max(1, own_slots))) : 0.0;
+    // the prefix by the tile kernel: a tile of 64 keys 1.35 us, 5 of them for its beginning and end
+    if (hd == 128 && tiles2 > 0) {
+        const int64_t wgs = (vr + 255) / 256 * Hkv;
+        // own keys in the tile: a wavefront goes through those of all requests that its 64 rows meet, 32 keys a microsecond
+        const double meets = std::min<double>(t.n, std::ceil(64.0 / group / ((double)rows / t.n)) + 1);
+        const double in_tile = meets * std::ceil((double)own_sum / t.n / 32) * 0.8;
+        for (int np = 1; np <= std::min(tiles2, 64); ++np) {
+            const int per = ceil_div(tiles2, np);
+            if (ceil_div(tiles2, per) != np || (uint64_t)per * 64 * (uint64_t)Hkv * 256 >= (1ull << 32)) continue;
+            const double us = 6.0 + ceil_div(wgs * np, 256) * (per + 5) * 1.35;
+            take({TILES, np, 0, 0, 1, np > 1 ? np : 0}, us + in_tile + (np > 1 ? 5.0 + np * row_us : 0.0));
+            take({TILES_SPLIT, np, 0, own_per, 1, np + own_slots}, us + 4.0 + own_us + 5.0 + (np + own_slots) * row_us);
+        }
+    }
+    // the prefix like the own keys, with 32 or 64 rows of any requests
+    const int rt = vr <= 32 ? 1 : 2;
+    const int64_t groups = (vr + 32 * rt - 1) / (32 * rt) * Hkv;
+    for (int np = n2 > 0 ? 1 : 0; np <= 64; ++np) {
+        const int per = np ? std::max(256, ceil_div(ceil_div(n2, np), 64) * 64) : 0;
+        if (np && ceil_div(n2, per) != np) continue;
+        const double pre = np ? hd_part * (rt == 1 ? 1.9 : 3.0) * std::ceil(per / 256.0) : 0.0;
+        take({SPLIT, np, per, own_per, rt, np + own_slots},
+             6.0 + std::max({pre, own_us, (groups * np + own_wgs) / 256.0 * std::max(pre, own_wgs ? 1.9 * own_blocks : 0.0)}) + 6.0 + (np + own_slots) * row_us);
+        if (np == 0) break;
+    }
+    return best;
+}
+
+template <int HD, int NW, int RT, int MODE>
+void launch_tokens(const SharedParams& p, const Parts& parts, const SharedTable& tab, unsigned items, hipStream_t s) {
+    constexpr int RING = NW * 2 * 64 * HD * 2, JOIN = (NW * 32 * (HD + 4) + 2 * NW * 32) * 4, LDS = RING > JOIN ? RING : JOIN;
     static OncePerDevice lds;
-    lds.run(current_device(), [] { allow_dynamic_lds((const void*)(attn_shared_kernel<HD, 8, true>), SPLIT_LDS); });
+    lds.run(current_device(), [] { allow_dynamic_lds((const void*)(attn_shared_tokens_kernel<HD, NW, RT, MODE>), LDS); });
+    hipLaunchKernelGGL((attn_shared_tokens_kernel<HD, NW, RT, MODE>), dim3(items * p.Hkv), dim3(NW * 64), LDS, s, p, parts, tab);
+}
+
+template <int HD>
+void launch_t(const SharedParams& p, const po_request_rows* seq, int n, float* scratch, size_t scratch_bytes, hipStream_t s) {
     const int group = p.Hq / p.Hkv;
-    int64_t longest = 0;
-    for (int i = 0; i < n; ++i) longest = std::max<int64_t>(longest, seq[i].q_len);
-    if (longest * group <= 32)
-        for_tables(seq, n, group, 32, [&](const SharedTable& tab, int items) {
-            hipLaunchKernelGGL((attn_shared_kernel<HD, 8, true>), dim3((unsigned)items * p.Hkv), dim3(512), SPLIT_LDS, s, p, tab);
-        });
-    else
-        for_tables(seq, n, group, 128, [&](const SharedTable& tab, int items) {
-            hipLaunchKernelGGL((attn_shared_kernel<HD, 4, false>), dim3((unsigned)items * p.Hkv), dim3(256), 0, s, p, tab);
-        });
+    for (int i = 0; i < n;) {
+        SharedTable tab;
+        const int i0 = i;
+        i = fill_table(tab, seq, i0, n, [](const SharedSeq&) { return 0; });
+        if (tab.n == 0) continue;
+        const Plan t = plan(tab, p.Hq, p.Hkv, HD, p.n2, scratch ? scratch_bytes : 0);
+        const int rows = tab.row0[tab.n];
+        Parts parts{};
+        parts.np = t.np;
+        parts.per = t.per;
+        parts.own_per = t.own_per;
+        parts.opart = scratch;
+        parts.mlpart = scratch + (size_t)t.slots * rows * p.Hq * HD;
+        const auto items = [&](int tile) {
+            fill_table(tab, seq, i0, n, [&](const SharedSeq& q) {
+                return ceil_div((int64_t)q.q_len * group, tile) * (t.own_per ? ceil_div(q.kv_len, t.own_per) : 1);
+            });
+            return (unsigned)tab.item0[tab.n];
+        };
+        unsigned n_items;
+        switch (t.mode) {
+            case TOKENS:
+                n_items = items(32);
+                // (two wavefronts, two workgroups a compute unit, where there are enough of them)
+                if (n_items * p.Hkv > 256) launch_tokens<HD, 2, 1, WHOLE>(p, parts, tab, n_items, s);
+                else launch_tokens<HD, 4, 1, WHOLE>(p, parts, tab, n_items, s);
+                break;
+            case ROWS:
+                n_items = items(128);
+                hipLaunchKernelGGL(attn_shared_rows_kernel<HD>, dim3(n_items * p.Hkv), dim3(256), 0, s, p, tab);
+                break;
+            case TILES:
+                launch_attention_shared_tiles(p, tab, t.np, true, parts.opart, parts.mlpart, s);
+                break;
+            case TILES_SPLIT:
+                launch_attention_shared_tiles(p, tab, t.np, false, parts.opart, parts.mlpart, s);
+                n_items = items(32);
+                if (n_items) launch_tokens<HD, 4, 1, PARTS>(p, parts, tab, n_items, s);
+                break;
+            case SPLIT:
+                parts.prefix_items = ceil_div((int64_t)rows * group, 32 * t.rt) * t.np;
+                n_items = items(32) + parts.prefix_items;
+                if (t.rt == 1) launch_tokens<HD, 4, 1, PARTS>(p, parts, tab, n_items, s);
+                else launch_tokens<HD, 4, 2, PARTS>(p, parts, tab, n_items, s);
+                break;
+        }
+        if (t.slots > 0)
+            hipLaunchKernelGGL(attn_shared_join_kernel<HD>, dim3((unsigned)(((int64_t)rows * p.Hq * (HD / 4) + 255) / 256)), dim3(256), 0, s, p,
+                               parts, tab);
+    }
 }
 
 }  // namespace
 
-void launch_attention_shared_bf16(const SharedParams& p, const po_request_rows* seq, int n, int hd, hipStream_t s) {
-    if (hd == 128) launch_t<128>(p, seq, n, s);
-    else launch_t<64>(p, seq, n, s);
+size_t attention_shared_scratch(const po_request_rows* seq, int n, int Hq, int Hkv, int hd, int64_t n2) {
+    size_t most = 0;
+    for (int i = 0; i < n;) {
+        SharedTable tab;
+        i = fill_table(tab, seq, i, n, [](const SharedSeq&) { return 0; });
+        if (tab.n) most = std::max(most, (size_t)plan(tab, Hq, Hkv, hd, (int)n2, SIZE_MAX).slots * tab.row0[tab.n] * Hq * (hd + 2) * sizeof(float));
+    }
+    return most;
+}
+
+void launch_attention_shared_bf16(const SharedParams& p, const po_request_rows* seq, int n, int hd, float* scratch, size_t scratch_bytes,
+                                  hipStream_t s) {
+    if (hd == 128) launch_t<128>(p, seq, n, scratch, scratch_bytes, s);
+    else launch_t<64>(p, seq, n, scratch, scratch_bytes, s);
 }
 
 }  // namespace po

@@ -353,11 +353,15 @@ __global__ void __launch_bounds__(256, 2) attention_shared_f32_kernel(const Shar
 }
 
 void launch_attention_shared_f32(const SharedParams& p, const po_request_rows* seq, int n, int hd, hipStream_t s) {
-    for_tables(seq, n, p.Hq / p.Hkv, 32, [&](const SharedTable& tab, int items) {
-        const dim3 grid((unsigned)items * p.Hkv);
+    const int group = p.Hq / p.Hkv;
+    for (int i = 0; i < n;) {
+        SharedTable tab;
+        i = fill_table(tab, seq, i, n, [&](const SharedSeq& q) { return (q.q_len * group + 31) / 32; });
+        if (tab.n == 0) continue;
+        const dim3 grid((unsigned)tab.item0[tab.n] * p.Hkv);
         if (hd == 128) hipLaunchKernelGGL(attention_shared_f32_kernel<128>, grid, dim3(256), 0, s, p, tab);
         else hipLaunchKernelGGL(attention_shared_f32_kernel<64>, grid, dim3(256), 0, s, p, tab);
-    });
+    }
 }
 
 // ------------------------------------------------------------------ GEMM

@@ -1485,28 +1485,44 @@ static po_status shared_requests(const po_request_rows* req, int32_t n_req, int3
 
 static inline bool misaligned16(const void* p) { return ((uintptr_t)p & 15) != 0; }
 
+po_status po_attention_shared_bytes(int32_t dtype, const po_request_rows* requests, int32_t n_req, int64_t n2, int32_t Hq, int32_t Hkv,
+                                    int32_t hd, size_t* scratch_bytes) {
+    if (bad_dtype(dtype) || !requests || n_req <= 0 || n2 < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || !scratch_bytes) return PO_ERR_INVALID_ARG;
+    if (!attention_mfma_supported(Hq, Hkv, hd)) return PO_ERR_BAD_CONFIG;
+    if (n2 > (int64_t)1 << 24 || (int64_t)Hq * hd >= (int64_t)1 << 23) return PO_ERR_TOO_LONG;
+    int64_t keys;
+    const po_status st = shared_requests(requests, n_req, Hq, 0, false, &keys);
+    if (st == PO_OK) *scratch_bytes = dtype == PO_BF16 ? attention_shared_scratch(requests, n_req, Hq, Hkv, hd, n2) : 0;
+    return st;
+}
+
 po_status po_op_attention_shared(int32_t dtype, const void* q, const void* k, const void* v, int64_t ldv, void* o,
                                  const po_request_rows* requests, int32_t n_req, const void* k2, const void* v2, int64_t ldv2,
-                                 int64_t n2, int32_t Hq, int32_t Hkv, int32_t hd, int32_t q_prescaled, void* stream) {
+                                 int64_t n2, int32_t Hq, int32_t Hkv, int32_t hd, int32_t q_prescaled, void* scratch,
+                                 size_t scratch_bytes, void* stream) {
     if (bad_dtype(dtype) || !q || !o || !requests || n_req <= 0 || n2 < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv) return PO_ERR_INVALID_ARG;
     if ((q_prescaled != 0 && q_prescaled != 1) || (q_prescaled && dtype != PO_BF16)) return PO_ERR_INVALID_ARG;
     const bool vt = dtype == PO_BF16;
     if (n2 > 0 && (!k2 || !v2 || (vt && (ldv2 < n2 || ldv2 % 8)))) return PO_ERR_INVALID_ARG;
     if (!attention_mfma_supported(Hq, Hkv, hd)) return PO_ERR_BAD_CONFIG;
-    // (a KV head's V^T and a row of all heads are addressed in bytes with 32 bits)
-    if (n2 > (int64_t)1 << 24 || ldv >= (int64_t)1 << 30 || ldv2 >= (int64_t)1 << 30 || (int64_t)Hq * hd >= (int64_t)1 << 23) return PO_ERR_TOO_LONG;
+    // (a KV head's V^T and 64 rows of all heads are addressed in bytes with 32 bits)
+    if (n2 > (int64_t)1 << 24 || (int64_t)Hq * hd >= (int64_t)1 << 23 || (vt && (ldv >= ((int64_t)1 << 24) - 64 || ldv2 >= ((int64_t)1 << 24) - 64)))
+        return PO_ERR_TOO_LONG;
     int64_t keys;
     const po_status st = shared_requests(requests, n_req, Hq, ldv, vt, &keys);
     if (st != PO_OK) return st;
     if (keys > 0 && (!k || !v || (vt && ldv % 8))) return PO_ERR_INVALID_ARG;
-    if (misaligned16(q) || misaligned16(o) || misaligned16(k) || misaligned16(v) || misaligned16(k2) || misaligned16(v2)) return PO_ERR_INVALID_ARG;
+    if (misaligned16(q) || misaligned16(o) || misaligned16(k) || misaligned16(v) || misaligned16(k2) || misaligned16(v2) ||
+        misaligned16(scratch))
+        return PO_ERR_INVALID_ARG;
     SharedParams p{};
     p.q = q; p.k = k; p.v = v; p.k2 = k2; p.v2 = v2; p.o = o;
     p.ldv = ldv; p.ldv2 = ldv2;
     p.n2 = (int)n2;
     p.Hq = Hq; p.Hkv = Hkv;
     p.sc = vt ? (q_prescaled ? 1.0f : attention_q_scale(hd)) : 1.0f / sqrtf((float)hd);
-    (vt ? launch_attention_shared_bf16 : launch_attention_shared_f32)(p, requests, n_req, hd, (hipStream_t)stream);
+    if (vt) launch_attention_shared_bf16(p, requests, n_req, hd, (float*)scratch, scratch_bytes, (hipStream_t)stream);
+    else launch_attention_shared_f32(p, requests, n_req, hd, (hipStream_t)stream);
     PO_HIP(hipGetLastError());
     return PO_OK;
 }

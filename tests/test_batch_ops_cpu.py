@@ -68,7 +68,7 @@ def attention_args(**kw):
     (dict(dtype=2), 1), (dict(dtype=-1), 1), (dict(q=None), 1), (dict(o=None), 1), (dict(requests=None), 1), (dict(n_req=0), 1), (dict(n_req=-1), 1),
     (dict(k=None), 1), (dict(v=None), 1), (dict(k2=None), 1), (dict(v2=None), 1), (dict(n2=-1), 1), (dict(ldv2=96), 1), (dict(ldv2=132), 1),
     (dict(ldv=60), 1), (dict(ldv=637), 1), (dict(ldv=643), 1), (dict(Hq=0), 1), (dict(Hkv=0), 1), (dict(Hkv=3), 1), (dict(hd=96), 2), (dict(hd=256), 2), (dict(pre=2), 1),
-    (dict(dtype=0, pre=1), 1), (dict(q=P + 8), 1), (dict(k2=P + 2), 1), (dict(v=P + 4), 1), (dict(n2=(1 << 24) + 1, ldv2=1 << 25), 4), (dict(ldv=1 << 30), 4),
+    (dict(dtype=0, pre=1), 1), (dict(q=P + 8), 1), (dict(k2=P + 2), 1), (dict(v=P + 4), 1), (dict(n2=(1 << 24) + 1, ldv2=1 << 25), 4), (dict(ldv2=1 << 24), 4), (dict(ldv=1 << 24), 4),
     (dict(requests=rows((0, 5, 0, 5), (4, 1, 64, 30))), 1),            # rows of q overlap
     (dict(requests=rows((5, 1, 64, 30), (0, 5, 0, 5))), 1),            # ... descend
     (dict(requests=rows((0, -1, 0, 5), (5, 1, 64, 30))), 1), (dict(requests=rows((0, 5, 0, -5), (5, 1, 64, 30))), 1),
@@ -80,4 +80,4 @@ def attention_args(**kw):
 ])
 def test_attention_shared_refusals(change, status):
     a = attention_args(**change)
-    assert B.lib().po_op_attention_shared(*a.values(), None) == status
+    assert B.lib().po_op_attention_shared(*a.values(), None, 0, None) == status
