@@ -432,9 +432,9 @@ po_status po_op_attention_split_prefix(const void* dev_q, const void* dev_k, con
  * token of a request with a history: q_len 1).  A row that sees no key gives zeros.  Rows of o of no request are left as they are.
  * requests: HOST array, read before the call returns (a captured call keeps it); rows of q ascending and apart, q_len and kv_len
  * may be 0, rows of k may be shared.
- * Layouts as po_op_qkv_rope and a prefix-cache entry have them: q, o [rows, Hq, hd] (o may be q), k [rows, Hkv, hd]; PO_BF16:
+ * Layouts as po_op_qkv_rope and a prefix-cache entry have them: q, o [q_rows, Hq, hd] (o may be q), k [kv_rows, Hkv, hd]; PO_BF16:
  * v transposed, [Hkv*hd][ldv] with column j the V of row j of k, ldv and kv_row multiples of 8, kv_row + kv_len <= ldv; PO_F32: v
- * [rows, Hkv, hd] (ldv, ldv2 unused).  dev_k2 [n2, Hkv, hd], dev_v2: the prefix, [Hkv*hd][ldv2] (ldv2 >= n2 a multiple of 8) or rows
+ * [kv_rows, Hkv, hd] (ldv, ldv2 unused).  dev_k2 [n2, Hkv, hd], dev_v2: the prefix, [Hkv*hd][ldv2] (ldv2 >= n2 a multiple of 8) or rows
  * as v; any n2, 0 = none (then they may be NULL).  What lies beyond a request's or the prefix's last key is not used, whatever it
  * holds.  head_dim 64 or 128; pointers 16-byte aligned; scores must be finite.  q_prescaled as in po_op_attention. */
 typedef struct { int64_t q_row, q_len, kv_row, kv_len; } po_request_rows;
@@ -442,9 +442,9 @@ typedef struct { int64_t q_row, q_len, kv_row, kv_len; } po_request_rows;
  * Host only.) */
 po_status po_attention_shared_bytes(int32_t dtype, const po_request_rows* requests, int32_t n_req, int64_t n2, int32_t n_q_heads,
                                     int32_t n_kv_heads, int32_t head_dim, size_t* scratch_bytes);
-po_status po_op_attention_shared(int32_t dtype, const void* dev_q, const void* dev_k, const void* dev_v, int64_t ldv, void* dev_o,
-                                 const po_request_rows* requests, int32_t n_req, const void* dev_k2, const void* dev_v2,
-                                 int64_t ldv2, int64_t n2, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+po_status po_op_attention_shared(int32_t dtype, const void* dev_q, int64_t q_rows, const void* dev_k, const void* dev_v,
+                                 int64_t kv_rows, int64_t ldv, void* dev_o, const po_request_rows* requests, int32_t n_req,
+                                 const void* dev_k2, const void* dev_v2, int64_t ldv2, int64_t n2, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                  int32_t q_prescaled, void* dev_scratch, size_t scratch_bytes, void* hip_stream);
 
 /* The block tile (rows x columns of the output) that a launch of po_op_linear, po_op_gate_up_silu (N = 2 F) or

@@ -147,7 +147,7 @@ def lib() -> C.CDLL:
     L.po_linear_fp8_block_bytes.argtypes = [i64, i32, i32, C.POINTER(sz)]
     L.po_op_linear_fp8_block.argtypes = [i32, vp, vp, vp, vp, vp, vp, vp, sz, i64, i32, i32, vp]
     L.po_op_sample.argtypes = [vp, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp]
-    L.po_op_attention_shared.argtypes = [i32, vp, vp, vp, i64, vp, vp, i32, vp, vp, i64, i64, i32, i32, i32, i32, vp, sz, vp]
+    L.po_op_attention_shared.argtypes = [i32, vp, i64, vp, vp, i64, i64, vp, vp, i32, vp, vp, i64, i64, i32, i32, i32, i32, vp, sz, vp]
     L.po_attention_shared_bytes.argtypes = [i32, vp, i32, i64, i32, i32, i32, C.POINTER(sz)]
     f64 = C.c_double
     L.po_sched_create.argtypes = [f64, C.POINTER(vp)]
@@ -543,36 +543,35 @@ def po_op_linear_fp8_split(a_codes, a_scales, w_codes, w_scales, residual, scrat
     return (c if n.value > 1 else None), n.value
 
 
-def _operands(**tensors):
-    """checks what the library cannot: contiguous tensors of the named dtype on the current device, whose stream the call
-    uses.  name=(tensor or None, dtype name)"""
+def _operands(*named):
+    """checks what the library cannot see: each (name, tensor or None, dtype) contiguous, of that dtype and on the current device, on
+    whose current stream the call runs (-> its handle; the raw form, since a torch.cuda.Stream costs as much as a small launch)"""
     import torch
-    for name, (t, dtype) in tensors.items():
-        if t is None:
+    device = torch.cuda.current_device()
+    for name, t, dtype in named:
+        if t is None or (t.dtype is dtype and t.get_device() == device and t.is_contiguous()):
             continue
-        if t.dtype != getattr(torch, dtype):
+        if t.dtype is not dtype:
             raise ValueError(f"{name}: {dtype} expected, got {t.dtype}")
-        if not t.is_cuda or t.device.index != torch.cuda.current_device():
-            raise ValueError(f"{name}: on {t.device}, not on the current GPU")
-        if not t.is_contiguous():
-            raise ValueError(f"{name}: not contiguous")
+        raise ValueError(f"{name}: not contiguous" if t.get_device() == device else f"{name}: on {t.device}, not on the current GPU")
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
-def _shape(name, t, shape):
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
+def _shape(name, t, *shape):
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {shape} expected, got {tuple(t.shape)}")
 
 
 def po_op_quantize_blocks(x, block_rows: int = 1):
     """bf16 [rows, K] -> (uint8 codes [rows, K], float32 scales): block_rows 1: blocks of a row x 128, scales [K/128, rows];
     block_rows 128: blocks of 128 x 128, scales [ceil(rows/128), K/128]"""
     import torch
-    _operands(x=(x, "bfloat16"))
+    stream = _operands(("x", x, torch.bfloat16))
     rows, K = x.shape
     codes = torch.empty((rows, K), dtype=torch.uint8, device=x.device)
     shape = (K // 128, rows) if block_rows == 1 else ((rows + 127) // 128, K // 128)
     scales = torch.empty(shape, dtype=torch.float32, device=x.device)
-    check(lib().po_op_quantize_blocks(x.data_ptr(), codes.data_ptr(), scales.data_ptr(), rows, K, block_rows, _stream()))
+    check(lib().po_op_quantize_blocks(x.data_ptr(), codes.data_ptr(), scales.data_ptr(), rows, K, block_rows, stream))
     return codes, scales
 
 
@@ -592,21 +591,24 @@ def po_op_linear_fp8_block(a_codes, a_scales, w_codes, w_scales, residual=None, 
     N = w_codes.shape[0]
     if silu_mul and residual is not None:
         raise ValueError("residual: not with silu_mul")
-    epi = 2 if silu_mul else (1 if residual is not None else 0)
-    c = out if out is not None else torch.empty((M, N // 2 if silu_mul else N), dtype=torch.bfloat16, device=a_codes.device)
-    _operands(a_codes=(a_codes, "uint8"), a_scales=(a_scales, "float32"), w_codes=(w_codes, "uint8"), w_scales=(w_scales, "float32"),
-              residual=(residual, "bfloat16"), out=(c, "bfloat16"), scratch=(scratch, "uint8"))
-    _shape("w_codes", w_codes, (N, K))
-    _shape("a_scales", a_scales, (K // 128, M))
-    _shape("w_scales", w_scales, (2, (N + 255) // 256, K // 128) if silu_mul else ((N + 127) // 128, K // 128))
-    _shape("out", c, (M, N // 2 if silu_mul else N))
+    epi, cols = (2, N // 2) if silu_mul else (1 if residual is not None else 0, N)
+    c = out if out is not None else torch.empty((M, cols), dtype=torch.bfloat16, device=a_codes.device)
+    stream = _operands(("a_codes", a_codes, torch.uint8), ("a_scales", a_scales, torch.float32), ("w_codes", w_codes, torch.uint8),
+                       ("w_scales", w_scales, torch.float32), ("residual", residual, torch.bfloat16), ("out", c, torch.bfloat16),
+                       ("scratch", scratch, torch.uint8))
+    _shape("w_codes", w_codes, N, K)
+    _shape("a_scales", a_scales, K // 128, M)
+    _shape("w_scales", w_scales, *((2, (N + 255) // 256, K // 128) if silu_mul else ((N + 127) // 128, K // 128)))
+    _shape("out", c, M, cols)
     if residual is not None:
-        _shape("residual", residual, (M, N))
+        _shape("residual", residual, M, N)
     if scratch is None:
-        scratch = torch.empty(po_linear_fp8_block_bytes(M, N, K), dtype=torch.uint8, device=a_codes.device)
+        need = po_linear_fp8_block_bytes(M, N, K)
+        scratch = torch.empty(need, dtype=torch.uint8, device=a_codes.device) if need else None
+    n = 0 if scratch is None else scratch.numel()
     check(lib().po_op_linear_fp8_block(epi, a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(),
-                                       c.data_ptr(), None if residual is None else residual.data_ptr(),
-                                       scratch.data_ptr() if scratch.numel() else None, scratch.numel(), M, N, K, _stream()))
+                                       c.data_ptr(), None if residual is None else residual.data_ptr(), scratch.data_ptr() if n else None,
+                                       n, M, N, K, stream))
     return c
 
 
@@ -693,10 +695,16 @@ def po_op_attention_split_prefix(q, k, v, q_row0: int, q_prescaled: bool = False
     return (o if n.value > 1 else None), n.value
 
 
+def _requests(requests):
+    r = np.ascontiguousarray(requests, dtype=np.int64)
+    if r.ndim != 2 or r.shape[1] != 4:
+        raise ValueError(f"requests: shape (n, 4) expected, got {r.shape}")
+    return r
+
+
 def po_attention_shared_bytes(dtype: int, requests, n2: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
     """bytes of scratch that po_op_attention_shared can use for these requests (host only); dtype: PO_F32 or PO_BF16"""
-    r = np.ascontiguousarray(requests, dtype=np.int64)
-    _shape("requests", r, (len(r), 4))
+    r = _requests(requests)
     n = C.c_size_t(0)
     check(lib().po_attention_shared_bytes(dtype, r.ctypes.data, len(r), n2, n_q_heads, n_kv_heads, head_dim, C.byref(n)))
     return n.value
@@ -709,34 +717,31 @@ def po_op_attention_shared(q, k, v, requests, k2=None, v2=None, n2: int = 0, out
     po_attention_shared_bytes (an empty one: nothing runs in parts)"""
     import torch
     rows, Hq, hd = q.shape
-    Hkv = k.shape[1]
-    bf16 = q.dtype == torch.bfloat16
-    dt = "bfloat16" if bf16 else "float32"
+    keys, Hkv = k.shape[:2]
+    dt = q.dtype
+    bf16 = dt is torch.bfloat16
     if n2 > 0 and (k2 is None or v2 is None):
         raise ValueError("k2, v2: expected with n2 > 0")
     o = torch.zeros_like(q) if out is None else out
-    _operands(q=(q, dt), k=(k, dt), v=(v, dt), k2=(k2, dt), v2=(v2, dt), out=(o, dt), scratch=(scratch, "uint8"))
-    _shape("k", k, (k.shape[0], Hkv, hd))
-    _shape("out", o, (rows, Hq, hd))
-    _shape("v", v, (Hkv * hd, v.shape[1]) if bf16 else k.shape)
+    stream = _operands(("q", q, dt), ("k", k, dt), ("v", v, dt), ("k2", k2, dt), ("v2", v2, dt), ("out", o, dt), ("scratch", scratch, torch.uint8))
+    _shape("k", k, keys, Hkv, hd)
+    _shape("out", o, rows, Hq, hd)
+    _shape("v", v, *((Hkv * hd, v.shape[-1]) if bf16 else (keys, Hkv, hd)))
     if n2 > 0:
-        _shape("k2", k2, (k2.shape[0], Hkv, hd))
-        _shape("v2", v2, (Hkv * hd, v2.shape[1]) if bf16 else k2.shape)
+        _shape("k2", k2, k2.shape[0], Hkv, hd)
+        _shape("v2", v2, *((Hkv * hd, v2.shape[-1]) if bf16 else k2.shape))
         if n2 > k2.shape[0]:
             raise ValueError(f"k2: {n2} rows expected, got {k2.shape[0]}")
-    r = np.ascontiguousarray(requests, dtype=np.int64)
-    _shape("requests", r, (len(r), 4))
-    if len(r):
-        ends = r.sum(0) if len(r) == 1 else (r[:, 0::2] + r[:, 1::2]).max(0)
-        q_end, k_end = (int(r[0, 0] + r[0, 1]), int(r[0, 2] + r[0, 3])) if len(r) == 1 else (int(ends[0]), int(ends[1]))
-        if q_end > rows or k_end > k.shape[0]:
-            raise ValueError(f"requests: end at rows {q_end} of {rows} of q and {k_end} of {k.shape[0]} of k")
+    r = _requests(requests)
+    n, host = len(r), r.ctypes.data
     if scratch is None:
-        scratch = torch.empty(po_attention_shared_bytes(_dt(q), r, n2, Hq, Hkv, hd), dtype=torch.uint8, device=q.device)
-    check(lib().po_op_attention_shared(_dt(q), q.data_ptr(), k.data_ptr(), v.data_ptr(), v.shape[1] if bf16 else 0, o.data_ptr(),
-                                       r.ctypes.data, len(r), k2.data_ptr() if n2 else None, v2.data_ptr() if n2 else None,
-                                       v2.shape[1] if n2 and bf16 else 0, n2, Hq, Hkv, hd, 1 if q_prescaled else 0,
-                                       scratch.data_ptr() if scratch.numel() else None, scratch.numel(), _stream()))
+        need = C.c_size_t(0)
+        check(lib().po_attention_shared_bytes(_dt(q), host, n, n2, Hq, Hkv, hd, C.byref(need)))
+        scratch = torch.empty(need.value, dtype=torch.uint8, device=q.device) if need.value else None
+    size = 0 if scratch is None else scratch.numel()
+    check(lib().po_op_attention_shared(_dt(q), q.data_ptr(), rows, k.data_ptr(), v.data_ptr(), keys, v.shape[1] if bf16 else 0, o.data_ptr(), host,
+                                       n, k2.data_ptr() if n2 else None, v2.data_ptr() if n2 else None, v2.shape[1] if n2 and bf16 else 0,
+                                       n2, Hq, Hkv, hd, 1 if q_prescaled else 0, scratch.data_ptr() if size else None, size, stream))
     return o
 
 
@@ -779,18 +784,20 @@ def po_op_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None
     float32 log-probs [rows])"""
     import torch
     rows, V = logits.shape
+    ld = logits.stride(0)
     if rows and V and logits.stride(1) != 1:
         raise ValueError("logits: a row's values must lie side by side")
-    _operands(logits=(logits[:1], "float32"), u=(u, "float32"), temperature=(temperature, "float32"), top_k=(top_k, "int32"),
-              top_p=(top_p, "float32"), min_p=(min_p, "float32"))
+    f32 = torch.float32
+    stream = _operands(("logits", logits[:1], f32), ("u", u, f32), ("temperature", temperature, f32), ("top_k", top_k, torch.int32),
+                       ("top_p", top_p, f32), ("min_p", min_p, f32))
+    settings = []
     for name, t in (("u", u), ("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
         if t is not None:
-            _shape(name, t, (rows,))
+            _shape(name, t, rows)
+        settings.append(None if t is None else t.data_ptr())
     tokens = torch.empty(rows, dtype=torch.int32, device=logits.device)
-    logprobs = torch.empty(rows, dtype=torch.float32, device=logits.device)
-    p = lambda t: None if t is None else t.data_ptr()
-    check(lib().po_op_sample(logits.data_ptr(), logits.stride(0), rows, V, u.data_ptr(), p(temperature), p(top_k), p(top_p), p(min_p),
-                             tokens.data_ptr(), logprobs.data_ptr(), _stream()))
+    logprobs = torch.empty(rows, dtype=f32, device=logits.device)
+    check(lib().po_op_sample(logits.data_ptr(), ld, rows, V, *settings, tokens.data_ptr(), logprobs.data_ptr(), stream))
     return tokens, logprobs
 
 

@@ -1465,8 +1465,9 @@ po_status po_op_attention_split_prefix(const void* q, const void* k, const void*
     return PO_OK;
 }
 
-// q rows ascending and apart, sizes that the kernels' 32-bit numbers hold; -> own keys of all requests together
-static po_status shared_requests(const po_request_rows* req, int32_t n_req, int32_t Hq, int64_t ldv, bool vt, int64_t* keys) {
+// q rows ascending and apart, everything within q_rows and kv_rows, sizes that the kernels' 32-bit numbers hold; -> own keys of all
+// requests together
+static po_status shared_requests(const po_request_rows* req, int32_t n_req, int32_t Hq, int64_t q_rows, int64_t kv_rows, bool vt, int64_t* keys) {
     constexpr int64_t MAX = (int64_t)1 << 24;
     int64_t row = 0, tiles = 0;
     *keys = 0;
@@ -1474,7 +1475,7 @@ static po_status shared_requests(const po_request_rows* req, int32_t n_req, int3
         const po_request_rows& r = req[i];
         if (r.q_row < row || r.q_len < 0 || r.kv_row < 0 || r.kv_len < 0) return PO_ERR_INVALID_ARG;
         if (r.q_len > MAX || r.kv_len > MAX || r.q_row > INT32_MAX - MAX || r.kv_row > INT32_MAX - MAX) return PO_ERR_TOO_LONG;
-        if (vt && (r.kv_row % 8 || r.kv_row + r.kv_len > ldv)) return PO_ERR_INVALID_ARG;
+        if (r.q_row + r.q_len > q_rows || r.kv_row + r.kv_len > kv_rows || (vt && r.kv_row % 8)) return PO_ERR_INVALID_ARG;
         row = r.q_row + r.q_len;
         tiles += (r.q_len * Hq + 31) / 32 + Hq;
         if (r.q_len) *keys += r.kv_len;
@@ -1491,16 +1492,16 @@ po_status po_attention_shared_bytes(int32_t dtype, const po_request_rows* reques
     if (!attention_mfma_supported(Hq, Hkv, hd)) return PO_ERR_BAD_CONFIG;
     if (n2 > (int64_t)1 << 24 || (int64_t)Hq * hd >= (int64_t)1 << 23) return PO_ERR_TOO_LONG;
     int64_t keys;
-    const po_status st = shared_requests(requests, n_req, Hq, 0, false, &keys);
+    const po_status st = shared_requests(requests, n_req, Hq, INT64_MAX, INT64_MAX, false, &keys);
     if (st == PO_OK) *scratch_bytes = dtype == PO_BF16 ? attention_shared_scratch(requests, n_req, Hq, Hkv, hd, n2) : 0;
     return st;
 }
 
-po_status po_op_attention_shared(int32_t dtype, const void* q, const void* k, const void* v, int64_t ldv, void* o,
-                                 const po_request_rows* requests, int32_t n_req, const void* k2, const void* v2, int64_t ldv2,
+po_status po_op_attention_shared(int32_t dtype, const void* q, int64_t q_rows, const void* k, const void* v, int64_t kv_rows, int64_t ldv,
+                                 void* o, const po_request_rows* requests, int32_t n_req, const void* k2, const void* v2, int64_t ldv2,
                                  int64_t n2, int32_t Hq, int32_t Hkv, int32_t hd, int32_t q_prescaled, void* scratch,
                                  size_t scratch_bytes, void* stream) {
-    if (bad_dtype(dtype) || !q || !o || !requests || n_req <= 0 || n2 < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv) return PO_ERR_INVALID_ARG;
+    if (bad_dtype(dtype) || !q || !o || !requests || n_req <= 0 || q_rows < 0 || kv_rows < 0 || n2 < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv) return PO_ERR_INVALID_ARG;
     if ((q_prescaled != 0 && q_prescaled != 1) || (q_prescaled && dtype != PO_BF16)) return PO_ERR_INVALID_ARG;
     const bool vt = dtype == PO_BF16;
     if (n2 > 0 && (!k2 || !v2 || (vt && (ldv2 < n2 || ldv2 % 8)))) return PO_ERR_INVALID_ARG;
@@ -1509,7 +1510,7 @@ po_status po_op_attention_shared(int32_t dtype, const void* q, const void* k, co
     if (n2 > (int64_t)1 << 24 || (int64_t)Hq * hd >= (int64_t)1 << 23 || (vt && (ldv >= ((int64_t)1 << 24) - 64 || ldv2 >= ((int64_t)1 << 24) - 64)))
         return PO_ERR_TOO_LONG;
     int64_t keys;
-    const po_status st = shared_requests(requests, n_req, Hq, ldv, vt, &keys);
+    const po_status st = shared_requests(requests, n_req, Hq, q_rows, vt ? std::min(kv_rows, ldv) : kv_rows, vt, &keys);
     if (st != PO_OK) return st;
     if (keys > 0 && (!k || !v || (vt && ldv % 8))) return PO_ERR_INVALID_ARG;
     if (misaligned16(q) || misaligned16(o) || misaligned16(k) || misaligned16(v) || misaligned16(k2) || misaligned16(v2) ||

@@ -58,7 +58,7 @@ def rows(*requests):
 
 
 def attention_args(**kw):
-    a = dict(dtype=1, q=P, k=P, v=P, ldv=640, o=P, requests=rows((0, 5, 0, 5), (5, 1, 64, 30)), n_req=2, k2=P, v2=P, ldv2=128, n2=100, Hq=8,
+    a = dict(dtype=1, q=P, q_rows=6, k=P, v=P, kv_rows=700, ldv=640, o=P, requests=rows((0, 5, 0, 5), (5, 1, 64, 30)), n_req=2, k2=P, v2=P, ldv2=128, n2=100, Hq=8,
              Hkv=2, hd=128, pre=1)
     a.update(kw)
     return a
@@ -76,7 +76,8 @@ def attention_args(**kw):
     (dict(requests=rows((0, 5, 4, 5), (5, 1, 64, 30))), 1),            # V^T columns that no 16-byte load begins at
     (dict(requests=rows((0, 5, 0, 5), (5, 1, 632, 30))), 1),           # ... beyond the pitch
     (dict(requests=rows((0, (1 << 24) + 1, 0, 5), (1 << 25, 1, 64, 30))), 4), (dict(requests=rows((0, 5, 0, 5), (1 << 31, 1, 64, 30))), 4),
-    (dict(Hq=1 << 17, Hkv=1), 4),
+    (dict(Hq=1 << 17, Hkv=1), 4), (dict(q_rows=5), 1), (dict(q_rows=-1), 1), (dict(kv_rows=93), 1), (dict(kv_rows=-1), 1),
+    (dict(dtype=0, pre=0, kv_rows=93), 1),
 ])
 def test_attention_shared_refusals(change, status):
     a = attention_args(**change)

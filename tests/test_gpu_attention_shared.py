@@ -244,12 +244,11 @@ def test_binding_refuses_what_the_library_cannot_see():
     b = Batch(15, "bf16", 8, 2, 128, posts([50, 9]), 100)
     q, k, v, k2, v2 = b.device()
     f = B.po_op_attention_shared
-    for args, kw in (((q, k, v, [(0, q.shape[0] + 1, 0, 5)]), {}), ((q, k, v, [(0, 5, 0, k.shape[0] + 1)]), {}),
-                     ((q, k.float(), v, b.req), {}), ((q, k, v.t(), b.req), {}), ((q.cpu(), k, v, b.req), {}),
+    for args, kw in (((q, k.float(), v, b.req), {}), ((q, k, v.t(), b.req), {}), ((q.cpu(), k, v, b.req), {}),
                      ((q, k, v, b.req), {"k2": k2, "v2": v2, "n2": k2.shape[0] + 1}), ((q, k, v, b.req), {"n2": 10}),
                      ((q, k, v, b.req[:, :3]), {}), ((q[:, :, :64].contiguous(), k, v, b.req), {})):
         with pytest.raises(ValueError):
             f(*args, **kw)
-    for bad in ([(5, 5, 0, 5), (0, 5, 8, 5)], [(0, 5, 0, 5), (4, 5, 8, 5)], [(0, 5, 4, 5)], [(0, -1, 0, 5)], [(-1, 5, 0, 5)], np.zeros((0, 4))):
+    for bad in ([(0, q.shape[0] + 1, 0, 5)], [(0, 5, 0, k.shape[0] + 1)], [(5, 5, 0, 5), (0, 5, 8, 5)], [(0, 5, 0, 5), (4, 5, 8, 5)], [(0, 5, 4, 5)], [(0, -1, 0, 5)], [(-1, 5, 0, 5)], np.zeros((0, 4))):
         with pytest.raises(B.PoError):
             f(q, k, v, np.array(bad, dtype=np.int64).reshape(-1, 4))
