@@ -298,6 +298,96 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_block_kernel(const BlockParam
     if (col_base < p.N) tile_epilogue<EPI, MR, 2>(q, acc, smem + wave * 8192, row_base, col_base, lane);
 }
 
+// Up to 16 rows, where only how fast the weights arrive counts: strips of 16 weight rows (SiLU: 16 gate rows and their up rows), a
+// workgroup each and the whole of K in one launch, the slices from wavefront to wavefront.  A fragment is 32 bytes a lane, so
+// that four lanes read a 128-byte line of a row, straight into registers; a slice is one MFMA 16 x 16 x 128, and the four
+// values a lane gets of it (features 4 (lane / 16) .. of token lane % 16) are scaled and added.  Two slices of a wavefront are on
+// their way while the two before are multiplied, and up to four workgroups share a compute unit (eight wavefronts, or four
+// slices at a time, or both, take 4 to 40 % longer).  Wavefronts meet in LDS, in their order.
+// One row (us, in brackets in tiles with the reduction split): 4096 x 4096 6.4 (10.4), 4096 x 14336 14.2 (17.6), gate / up 28672 x
+// 4096 28.0 (31.2), 7168 x 5120 10.1 (13.3); 16 rows 7.6 (10.5), 17.6 (18.4), 33.4 (31.4), 13.8 (13.4).
+template <int EPI>
+__global__ void __launch_bounds__(256, 4) gemm_fp8_block_strip_kernel(const BlockParams bp) {
+    const GemmParams& p = bp.g;
+    constexpr int NS = EPI == EPI_SILU_MUL ? 2 : 1;                  // weight fragments of a slice
+    constexpr int NW = 4, U = 2;
+    __shared__ __attribute__((aligned(16))) f32x4 part[NW][NS][64];
+    const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, lq = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int f0 = (int)blockIdx.x * 16;                             // first output feature
+    const int n0 = EPI == EPI_SILU_MUL ? (f0 >> 5) * 64 + (f0 & 31) : f0;
+    const int slices = p.K / BKB;
+    const int row = min(l15, p.M - 1);
+    const unsigned char* const w = (const unsigned char*)p.W + (int64_t)(n0 + l15) * p.ldw + lq * 32;
+    const unsigned char* const a = (const unsigned char*)p.A + (int64_t)row * p.lda + lq * 32;
+    const float* const sa = p.sa + row;
+    scale_t* const psw = (scale_t*)p.sw + (int64_t)(f0 / 128) * slices;
+    i32x8 wf[2][U][NS], af[2][U];
+    float sx[2][U], sw[2][U][NS];
+    f32x4 acc[NS];
+#pragma unroll
+    for (int n = 0; n < NS; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const auto frag = [](const unsigned char* q) {
+        return __builtin_shufflevector(*(const i32x4*)q, *(const i32x4*)(q + 16), 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    const auto load = [&](int s0, int h) {                           // (slices past the last: the last one, not added)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int s = min(s0 + u * NW, slices - 1);
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+                wf[h][u][n] = frag(w + n * 32 * p.ldw + (int64_t)s * BKB);
+                sw[h][u][n] = psw[s + (n ? bp.sw_up : 0)];
+            }
+            af[h][u] = frag(a + (int64_t)s * BKB);
+            sx[h][u] = sa[(int64_t)s * p.M];
+        }
+    };
+    const auto multiply = [&](int s0, int h) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (s0 + u * NW >= slices) break;
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+                const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+                const f32x4 v = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf[h][u][n], af[h][u], zero, 0, 0, 0, 0x7F7F7F7F, 0, 0x7F7F7F7F);
+                const float f = sx[h][u] * sw[h][u][n];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[n][r] = fmaf(v[r], f, acc[n][r]);
+            }
+        }
+    };
+    load(wave, 0);
+#pragma unroll 1
+    for (int s = wave; s < slices; s += 2 * U * NW) {
+        load(s + U * NW, 1);
+        multiply(s, 0);
+        load(s + 2 * U * NW, 0);
+        multiply(s + U * NW, 1);
+    }
+#pragma unroll
+    for (int n = 0; n < NS; ++n) part[wave][n][lane] = acc[n];
+    __syncthreads();
+    if (wave != 0 || l15 >= p.M) return;
+    f32x4 v = part[0][0][lane], up = part[0][NS - 1][lane];
+#pragma unroll
+    for (int x = 1; x < NW; ++x) {
+        v += part[x][0][lane];
+        if (NS == 2) up += part[x][NS - 1][lane];
+    }
+    const int col = f0 + 4 * lq;
+    if (EPI == EPI_SILU_MUL) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = silu_f(v[r]) * up[r];
+    }
+    if (EPI == EPI_RESIDUAL) {
+        const uint2 r = *(const uint2*)(p.R + (int64_t)l15 * p.ldr + col);
+        v[0] += __uint_as_float(r.x << 16); v[1] += __uint_as_float(r.x & 0xffff0000u);
+        v[2] += __uint_as_float(r.y << 16); v[3] += __uint_as_float(r.y & 0xffff0000u);
+    }
+    *(uint2*)(p.dst + (int64_t)l15 * p.ld + col) = pack4(v[0], v[1], v[2], v[3]);
+}
+
 // C = epilogue(sum over splits, in their order, of part[split][M][N]); a thread makes eight outputs of a row.
 template <int EPI>
 __global__ void __launch_bounds__(256) block_reduce_kernel(const float* __restrict__ part, int splits, const bf16_t* R, bf16_t* C,
@@ -355,13 +445,21 @@ void launch_rows(int mr, const BlockParams& bp, int splits, hipStream_t s) {
     }
 }
 
-// Tile height 64 mr and K slices per split of a launch, by expected time: rounds of workgroups over the 256 compute units,
-// each the slices of a split long, and the second kernel of a split launch.
+template <int EPI>
+void launch_strips(const BlockParams& bp, hipStream_t s) {
+    hipLaunchKernelGGL(gemm_fp8_block_strip_kernel<EPI>, dim3((unsigned)(bp.g.N / (EPI == EPI_SILU_MUL ? 32 : 16))), dim3(256), 0, s, bp);
+}
+
+// Tile height 64 mr and K slices per split of a launch, by expected time (microseconds): rounds of workgroups over the 256 compute
+// units, each US and the slices of a split long, a slice between LO (few workgroups) and HI (256); no less than the
+// weights take from memory; and the second kernel of a split launch.  Fitted to 28 shapes (1 .. 3000 rows; 4096 x 14336,
+// 4096 x 4096, 28672 x 4096, 7168 x 5120), every height and 1 .. 16 splits: the pick is 1.4 % off the fastest on average, 7 % at most.
+// Strips (mr 0) where those are expected to take less: a compute unit takes in 23 KB of its strips a microsecond, less with more rows.
 struct Plan {
     int mr, per;
 };
-Plan plan(int64_t M, int N, int K, size_t scratch_bytes) {
-    constexpr double US = 4.0, SLICE[5] = {0, 0.33, 0.42, 0.55, 0.68};
+Plan plan(int epi, int64_t M, int N, int K, size_t scratch_bytes) {
+    constexpr double US = 3.4, LO[5] = {0, 0.44, 0.50, 0.55, 0.67}, HI[5] = {0, 0.40, 0.58, 0.71, 0.88};
     const int slices = K / BKB;
     Plan best{1, slices};
     double t_best = 1e30;
@@ -370,11 +468,17 @@ Plan plan(int64_t M, int N, int K, size_t scratch_bytes) {
         for (int splits = 1; splits <= 16 && 2 * splits <= std::max(slices, 2); ++splits) {
             const int per = (slices + splits - 1) / splits, n = (slices + per - 1) / per;
             const double bytes = (double)n * (double)M * N * 4.0;
-            if (n > 1 && (bytes > (double)scratch_bytes || tiles * n > 512)) continue;
-            const double rounds = (double)((tiles * n + 255) / 256);
-            const double t = rounds * (US + per * SLICE[mr]) + (n > 1 ? 3.0 + bytes * 2.0 / 4.0e6 : 0.0);
+            if (n != splits || (n > 1 && (bytes > (double)scratch_bytes || tiles * n > 600))) continue;
+            const int64_t full = tiles * n / 256, rest = tiles * n % 256;
+            double t = full * (US + per * HI[mr]) + (rest ? US + per * (LO[mr] + (HI[mr] - LO[mr]) * rest / 256.0) : 0.0);
+            t = std::max(t, 3.0 + (double)N * K / 5.0e6) + (n > 1 ? 3.9 + 2.0 * bytes / 4.8e6 : 0.0);
             if (t < t_best) { t_best = t; best = {mr, per}; }
         }
+    }
+    if (M <= 16) {
+        const int rows = epi == EPI_SILU_MUL ? 32 : 16, strips = N / rows;
+        const double turns = strips <= 768 ? (strips + 255) / 256 : strips / 256.0;        // (then several share a compute unit)
+        if (3.9 + turns * rows * (double)K * (1.0 + 0.023 * M) / 23.0e3 < t_best) best = {0, slices};
     }
     return best;
 }
@@ -395,7 +499,9 @@ void launch_quant_blocks(const bf16_t* x, unsigned char* q, float* scales, int64
 }
 
 size_t gemm_fp8_block_scratch(int64_t M, int N, int K) {
-    const Plan t = plan(M, N, K, SIZE_MAX);
+    // (over the epilogues: which of them it will be is not known here)
+    Plan t = plan(EPI_STORE, M, N, K, SIZE_MAX);
+    if (t.mr == 0) t = plan(EPI_SILU_MUL, M, N, K, SIZE_MAX);
     const int splits = (K / 128 + t.per - 1) / t.per;
     return splits > 1 ? (size_t)splits * (size_t)M * (size_t)N * sizeof(float) : 0;
 }
@@ -412,9 +518,17 @@ void launch_gemm_fp8_block(int epi, const unsigned char* A, const float* sa, con
     p.R = R; p.ldr = N;
     p.dst = C; p.ld = epi == EPI_SILU_MUL ? N / 2 : N;
     bp.sw_up = epi == EPI_SILU_MUL ? ((N / 2 + 127) / 128) * (K / 128) : 0;
-    const Plan t = plan(M, N, K, part ? part_bytes : 0);
+    const Plan t = plan(epi, M, N, K, part ? part_bytes : 0);
     bp.per = t.per;
     const int splits = (K / 128 + t.per - 1) / t.per;
+    if (t.mr == 0) {
+        switch (epi) {
+            case EPI_STORE: launch_strips<EPI_STORE>(bp, s); break;
+            case EPI_RESIDUAL: launch_strips<EPI_RESIDUAL>(bp, s); break;
+            default: launch_strips<EPI_SILU_MUL>(bp, s); break;
+        }
+        return;
+    }
     if (splits == 1) {
         switch (epi) {
             case EPI_STORE: launch_rows<EPI_STORE>(t.mr, bp, 1, s); break;
