@@ -14,27 +14,29 @@
 
 #include <float.h>
 
-#include <algorithm>
-
 namespace po {
 namespace {
 
 constexpr int NT = 1024;            // threads of a workgroup: one row
 constexpr int NWAVE = NT / 64;
-constexpr int BINS = 2048;
+constexpr int BINS = 4096;
+constexpr int PER = BINS / NT;      // bins of a thread
 constexpr int CAP = 4096;           // entries that are ordered in LDS
 constexpr int MAX_TILES = 1024;
+constexpr int SUB = 1024;           // logits that a wavefront reads at once, 16 a lane
 
 struct Shared {
     double table[64];
     double part[NWAVE];
     int ipart[NWAVE];
+    unsigned long long wave_best[NWAVE];
     double scan_w[NT];
     int scan_n[NT];
     unsigned long long weight[BINS];        // of a bin, as a multiple of 2^(its reference exponent - fix)
     int count[BINS];
     unsigned long long list[CAP];           // key << 32 | ~index: descending order is the order of the tokens
     double tile[MAX_TILES];
+    float tile_top[MAX_TILES];
     int n_list;
     // answers of a search, written by the one thread that finds them
     int found;
@@ -75,6 +77,31 @@ struct Row {
         return ldexp(fma(t * r, p, t), i >> 6);
     }
 };
+
+// the SUB logits from i0 on, lane l the ones at i0 + l, + 64, ..; -inf past the end
+__device__ __forceinline__ void read_sub(const Row& r, int i0, float (&v)[16]) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        const int i = i0 + j * 64 + lane;
+        const float x = r.z[min(i, r.V - 1)];
+        v[j] = i < r.V ? x : -INFINITY;
+    }
+}
+// f(logit, its index) for all logits of the row, a wavefront SUB of them at a time
+template <typename F>
+__device__ __forceinline__ void for_each(const Row& r, F f) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float v[16], next[16];
+    if (wave * SUB < r.V) read_sub(r, wave * SUB, next);
+    for (int i0 = wave * SUB; i0 < r.V; i0 += NWAVE * SUB) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = next[j];
+        if (i0 + NWAVE * SUB < r.V) read_sub(r, i0 + NWAVE * SUB, next);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) f(v[j], i0 + j * 64 + lane);
+    }
+}
 
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
@@ -122,22 +149,37 @@ __device__ __forceinline__ int first_thread(Shared& sh, bool yes, bool before) {
 // The bin of sh.count / sh.weight (bin 0 first, base_n / base_w in front of it) in which the goal is reached, the last one with
 // a token where rounding leaves it a little out of reach; sh.above_n / above_w: what is in front of it; sh.total_w: all of it.
 // ref(b): a bin's reference exponent.
-template <typename Ref>
+template <bool weights, typename Ref>
 __device__ int find_bin(Shared& sh, const Goal& goal, int base_n, double base_w, int fix, Ref ref) {
-    const int t = threadIdx.x, b0 = 2 * t, b1 = b0 + 1;
-    const int n0 = sh.count[b0], n1 = sh.count[b1];
-    const double w0 = ldexp((double)sh.weight[b0], ref(b0) - fix), w1 = ldexp((double)sh.weight[b1], ref(b1) - fix);
-    block_scan(sh, n0 + n1, w0 + w1);
-    const int all = sh.scan_n[NT - 1], bn = t ? sh.scan_n[t - 1] : 0;
-    const double bw = base_w + (t ? sh.scan_w[t - 1] : 0.0);
+    const int t = threadIdx.x;
+    int n[PER], sum_n = 0;
+    double w[PER], sum_w = 0.0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        n[j] = sh.count[t * PER + j];
+        w[j] = weights ? ldexp((double)sh.weight[t * PER + j], ref(t * PER + j) - fix) : 0.0;
+        sum_n += n[j];
+        sum_w += w[j];
+    }
+    block_scan(sh, sum_n, sum_w);
+    const int all = sh.scan_n[NT - 1];
+    int bn = t ? sh.scan_n[t - 1] : 0;
+    double bw = base_w + (t ? sh.scan_w[t - 1] : 0.0);
     const bool yes = sh.scan_n[t] == all || goal.reached(base_n + sh.scan_n[t], base_w + sh.scan_w[t]);
     const bool before = t && (bn == all || goal.reached(base_n + bn, bw));
-    const int f = first_thread(sh, yes, before);
-    if (t == f) {
-        const bool first = n1 == 0 || (n0 > 0 && goal.reached(base_n + bn + n0, bw + w0));
-        sh.found = first ? b0 : b1;
-        sh.above_n = base_n + (first ? bn : bn + n0);
-        sh.above_w = first ? bw : bw + w0;
+    if (t == first_thread(sh, yes, before)) {
+        int j = 0, at = -1;
+        int at_n = 0;
+        double at_w = 0.0;
+#pragma unroll
+        for (j = 0; j < PER; ++j) {                   // the first of its bins that reaches it, else its last one with a token
+            if (n[j] && (at < 0 || !goal.reached(base_n + bn, bw))) { at = j; at_n = bn; at_w = bw; }
+            bn += n[j];
+            bw += w[j];
+        }
+        sh.found = t * PER + max(at, 0);
+        sh.above_n = base_n + at_n;
+        sh.above_w = at < 0 ? bw : at_w;
         sh.total_w = sh.scan_w[NT - 1];
     }
     __syncthreads();
@@ -213,14 +255,13 @@ __device__ void find_in_row(Shared& sh, const Row& r, const Goal& goal, int fix)
         const double wh = r.weight(value_of(high), sh.table);
         const int ref = wh > 0.0 ? ilogb(wh) + 1 : -1000;
         clear_bins(sh);
-        for (int i = threadIdx.x; i < r.V; i += NT) {
-            const float l = r.z[i];
+        for_each(r, [&](float l, int) {
             const uint32_t key = key_of(l);
             if (key && (key & upper) == prefix)
                 add_to_bin(sh, (1 << bits) - 1 - (int)((key >> shift) & ((1u << bits) - 1)), r.weight(l, sh.table), fix - ref);
-        }
+        });
         __syncthreads();
-        const int b = find_bin(sh, goal, base_n, base_w, fix, [&](int) { return ref; });
+        const int b = find_bin<true>(sh, goal, base_n, base_w, fix, [&](int) { return ref; });
         prefix |= (uint32_t)((1 << bits) - 1 - b) << shift;
         base_n = sh.above_n;
         base_w = sh.above_w;
@@ -260,143 +301,117 @@ __device__ void find_in_row(Shared& sh, const Row& r, const Goal& goal, int fix)
     __syncthreads();
 }
 
-__global__ void __launch_bounds__(NT) sample_kernel(const float* __restrict__ logits, int64_t ld, int V, int ts, int fix,
-                                                    const float* __restrict__ u, const float* __restrict__ temperature,
-                                                    const int* __restrict__ top_k, const float* __restrict__ top_p,
-                                                    const float* __restrict__ min_p, int* __restrict__ tokens,
-                                                    float* __restrict__ logprobs) {
-    __shared__ Shared sh;
-    const int row = blockIdx.x, t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    Row r;
-    r.z = logits + (int64_t)row * ld;
-    r.V = V;
-    r.ts = ts;
-    r.tiles = (V + ts - 1) / ts;
-    if (t < 64) sh.table[t] = exp2((double)t / 64.0);
-    // ---- the first of the largest logits, the smallest that may be drawn
-    unsigned long long best = 0;
-    uint32_t least = 0xffffffffu;
-    for (int i = t; i < V; i += NT) {
-        const uint32_t key = key_of(r.z[i]);
+// The first of the largest logits, as an entry of a list (0: there is none), and the lowest key of what may be drawn.
+struct Extremes {
+    unsigned long long best;
+    uint32_t least;
+    __device__ __forceinline__ void see(float l, int i) {
+        const uint32_t key = key_of(l);
         const unsigned long long e = (unsigned long long)key << 32 | (uint32_t)~i;
         if (key) { best = e > best ? e : best; least = min(least, key); }
     }
-    for (int off = 32; off > 0; off >>= 1) {
-        const unsigned long long o = __shfl_xor(best, off);
-        best = o > best ? o : best;
-        least = min(least, (uint32_t)__shfl_xor((int)least, off));
-    }
-    if (lane == 0) { sh.list[wave] = best; sh.ipart[wave] = (int)least; }
-    __syncthreads();
-    for (int i = 0; i < NWAVE; ++i) {
-        best = sh.list[i] > best ? sh.list[i] : best;
-        least = min(least, (uint32_t)sh.ipart[i]);
-    }
-    __syncthreads();
-    const float T = temperature ? temperature[row] : 1.0f;
-    if (best == 0 || !(T > 0.0f)) {                           // nothing to draw; or the most likely token
-        if (t == 0) {
-            tokens[row] = best ? (int)~(uint32_t)best : -1;
-            if (logprobs) logprobs[row] = best ? 0.0f : -INFINITY;
+    __device__ void join(Shared& sh) {
+        for (int off = 32; off > 0; off >>= 1) {
+            const unsigned long long o = __shfl_xor(best, off);
+            best = o > best ? o : best;
+            least = min(least, (uint32_t)__shfl_xor((int)least, off));
         }
-        return;
-    }
-    r.top = value_of((uint32_t)(best >> 32));
-    r.rate = 1.4426950408889634074 / (double)T;
-    const int k = top_k ? top_k[row] : 0;
-    const float p = top_p ? top_p[row] : 1.0f;
-    const double floor_w = min_p && min_p[row] > 0.0f ? (double)min_p[row] : 0.0;      // (NaN: off)
-    unsigned long long cut = 0;                               // the last token of the kept beginning (0: all)
-    const bool by_k = k > 0 && k < V, by_p = p < 1.0f;
-    if (by_k || by_p) {
-        // ---- tokens and weight in 2048 equal steps of the logit below the largest: over all logits, or down to where no
-        // weight counts any more (the last bin takes the rest)
-        const double span = fmin((double)r.top - (double)value_of(least), 64.0 * fmax((double)T, 1.0));
-        const float scale = span > 0.0 && r.top < INFINITY ? (float)(BINS / span) : 0.0f;
-        const double step = scale > 0.0f ? r.rate / (double)scale : 0.0;
-        // no weight in a bin is above that of its upper edge; 1 for what the steps' own rounding moves across edges
-        const auto ref = [&](int b) { return (int)fmax(ceil(-(double)b * step), -1000.0) + 1; };
-        const auto bin = [&](float l) {
-            const float x = (r.top - l) * scale;
-            return x < (float)(BINS - 1) ? (int)x : BINS - 1;
-        };
-        const auto fill = [&] {
-            clear_bins(sh);
-            for (int i = t; i < V; i += NT) {
-                const float l = r.z[i];
-                if (key_of(l)) {
-                    const int b = bin(l);
-                    add_to_bin(sh, b, r.weight(l, sh.table), fix - ref(b));
-                }
-            }
-            __syncthreads();
-        };
-        // -> whether the bins still are what fill made
-        const auto search = [&](const Goal& goal) {
-            const int b = find_bin(sh, goal, 0, 0.0, fix, ref), n = sh.count[b], base_n = sh.above_n;
-            const double base_w = sh.above_w;
-            if (n > CAP) {
-                find_in_row(sh, r, goal, fix);
-                return false;
-            }
-            if (t == 0) sh.n_list = 0;
-            __syncthreads();
-            for (int i = t; i < V; i += NT) {
-                const float l = r.z[i];
-                const uint32_t key = key_of(l);
-                if (key && bin(l) == b) sh.list[atomicAdd(&sh.n_list, 1)] = (unsigned long long)key << 32 | (uint32_t)~i;
-            }
-            __syncthreads();
-            sort_list(sh, n);
-            find_in_list(sh, r, goal, n, base_n, base_w);
-            return true;
-        };
-        fill();
-        double sum;
-        if (by_k) {
-            const bool whole = search(Goal{k, 0.0});
-            cut = sh.cut;
-            sum = sh.cut_sum;
-            __syncthreads();
-            if (by_p && !whole) fill();
-        } else {
-            find_bin(sh, Goal{1, 0.0}, 0, 0.0, fix, ref);
-            sum = sh.total_w;
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) { sh.wave_best[threadIdx.x >> 6] = best; sh.ipart[threadIdx.x >> 6] = (int)least; }
+        __syncthreads();
+        for (int i = 0; i < NWAVE; ++i) {
+            best = sh.wave_best[i] > best ? sh.wave_best[i] : best;
+            least = min(least, (uint32_t)sh.ipart[i]);
         }
-        if (by_p) {           // (above 0, so that no sum of nothing reaches it)
-            search(Goal{0, fmax((double)p * sum, DBL_MIN)});
-            cut = sh.cut > cut ? sh.cut : cut;
-            __syncthreads();
-        }
+        __syncthreads();
     }
-    // ---- the kept weight of every tile, a wavefront each; the tile, then the token, in which the running sum passes u
-    const auto kept = [&](float l, int i) {
-        const uint32_t key = key_of(l);
-        const unsigned long long e = (unsigned long long)key << 32 | (uint32_t)~i;
-        if (!key || e < cut) return 0.0;
-        const double w = r.weight(l, sh.table);
-        return w >= floor_w || e == best ? w : 0.0;
-    };
-    for (int a = wave; a < r.tiles; a += NWAVE) {
-        const int i1 = min(V, (a + 1) * ts);
+};
+
+struct Answer {
+    int* token;
+    float* logprob;
+    __device__ __forceinline__ void give(int t, double lp) const {
+        *token = t;
+        if (logprob) *logprob = (float)lp;
+    }
+};
+
+__device__ __forceinline__ double target_of(float u, double all) {
+    return (double)(u > 0.0f ? fminf(u, 1.0f - 0x1p-24f) : 0.0f) * all;      // (NaN: 0)
+}
+
+// The rest of the way when the n tokens at the head of the order are in sh.list: by_k: the first k of them, otherwise `total` is
+// what top_p is a part of.
+__device__ void finish_list(Shared& sh, const Row& r, int n, bool by_k, int k, bool by_p, double p, double total, double floor_w, float u,
+                            const Answer& answer) {
+    const int t = threadIdx.x;
+    const auto weight = [&](uint32_t key) { return r.weight(value_of(key), sh.table); };
+    sort_list(sh, n);
+    const int nk = by_k ? min(k, n) : n, per = (nk + NT - 1) / NT, i0 = t * per, i1 = min(i0 + per, nk);
+    int keep = nk;
+    if (by_p) {
         double w = 0.0;
-        for (int i = a * ts + lane; i < i1; i += 64) w += kept(r.z[i], i);
-        w = wave_sum(w);
-        if (lane == 0) sh.tile[a] = w;
+        for (int i = i0; i < i1; ++i) w += weight((uint32_t)(sh.list[i] >> 32));
+        block_scan(sh, max(i1 - i0, 0), w);
+        const double goal = fmax(p * (by_k ? sh.scan_w[NT - 1] : total), DBL_MIN);       // (above 0: no sum of nothing reaches it)
+        const bool yes = sh.scan_n[t] == nk || sh.scan_w[t] >= goal;
+        const bool before = t && (sh.scan_n[t - 1] == nk || sh.scan_w[t - 1] >= goal);
+        if (t == first_thread(sh, yes, before)) {
+            double c = t ? sh.scan_w[t - 1] : 0.0;
+            int i = i0;
+            for (;; ++i) {
+                c += weight((uint32_t)(sh.list[i] >> 32));
+                if (i == i1 - 1 || c >= goal) break;
+            }
+            sh.above_n = i + 1;
+        }
+        __syncthreads();
+        keep = sh.above_n;
+    }
+    // by index: ~index << 32 | key, what is not kept at the end
+    for (int i = t; i < n; i += NT) {
+        const unsigned long long e = sh.list[i];
+        const uint32_t key = (uint32_t)(e >> 32);
+        const bool kept = i < keep && (i == 0 || floor_w <= 0.0 || weight(key) >= floor_w);
+        sh.list[i] = kept ? (unsigned long long)(uint32_t)e << 32 | key : 0;
     }
     __syncthreads();
+    sort_list(sh, keep);
+    const int per2 = (keep + NT - 1) / NT, j0 = t * per2, j1 = min(j0 + per2, keep);
+    double w = 0.0;
+    int some = 0;
+    for (int i = j0; i < j1; ++i)
+        if (sh.list[i]) { w += weight((uint32_t)sh.list[i]); ++some; }
+    block_scan(sh, some, w);
+    const int kept = sh.scan_n[NT - 1];
+    const double all = sh.scan_w[NT - 1], target = target_of(u, all);
+    const bool yes = sh.scan_n[t] == kept || sh.scan_w[t] > target;
+    const bool before = t && (sh.scan_n[t - 1] == kept || sh.scan_w[t - 1] > target);
+    if (t == first_thread(sh, yes, before)) {
+        double c = t ? sh.scan_w[t - 1] : 0.0, wi = 0.0;
+        int i = j0;
+        for (;; ++i) {
+            wi = weight((uint32_t)sh.list[i]);
+            c += wi;
+            if (i == j0 + some - 1 || (wi > 0.0 && c > target)) break;
+        }
+        answer.give((int)~(uint32_t)(sh.list[i] >> 32), log(wi / all));
+    }
+}
+
+// The token once sh.tile holds the kept weight of every tile.  kept(logit, index): its weight, or 0.
+template <typename F>
+__device__ void finish_tiles(Shared& sh, const Row& r, float u, int best, const Answer& answer, F kept) {
+    const int t = threadIdx.x, lane = t & 63;
     block_scan(sh, 0, t < r.tiles ? sh.tile[t] : 0.0);
-    const double all = sh.scan_w[r.tiles - 1];
-    const float uu = u[row];
-    const double target = (double)(uu > 0.0f ? fminf(uu, 1.0f - 0x1p-24f) : 0.0f) * all;
-    const bool yes = t == r.tiles - 1 || sh.scan_w[t] > target, before = t && sh.scan_w[t - 1] > target;
-    const int a = first_thread(sh, yes, before);
-    if (wave != 0) return;
+    const double all = sh.scan_w[r.tiles - 1], target = target_of(u, all);
+    const int a = first_thread(sh, t == r.tiles - 1 || sh.scan_w[t] > target, t && (t - 1 == r.tiles - 1 || sh.scan_w[t - 1] > target));
+    if (t >= 64) return;
     double run = a ? sh.scan_w[a - 1] : 0.0, w_last = 1.0;
-    int token = -1;
-    for (int i0 = a * ts; i0 < min(V, (a + 1) * ts); i0 += 64) {
+    int token = best;
+    for (int i0 = a * r.ts; i0 < min(r.V, (a + 1) * r.ts); i0 += 64) {
         const int i = i0 + lane;
-        const double w = i < min(V, (a + 1) * ts) ? kept(r.z[i], i) : 0.0;
+        const double w = i < min(r.V, (a + 1) * r.ts) ? kept(r.z[i], i) : 0.0;
         double c = w;
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
@@ -413,10 +428,215 @@ __global__ void __launch_bounds__(NT) sample_kernel(const float* __restrict__ lo
         if (past) break;
         run += __shfl(c, 63);
     }
-    if (lane == 0) {
-        tokens[row] = token >= 0 ? token : (int)~(uint32_t)best;
-        if (logprobs) logprobs[row] = (float)log(w_last / all);
+    if (lane == 0) answer.give(token, log(w_last / all));
+}
+
+// A row, a workgroup.  What it takes by settings: nothing but a temperature, one pass over the logits; top_k (up to half a list), one
+// pass that counts keys by their leading bits and one that gathers the head of the order; top_p alone, a pass for the extremes, one
+// that adds weights by steps of the logit, one that gathers; where the head is longer than a list holds, passes that find
+// the last kept token and one that adds up what is kept.
+__global__ void __launch_bounds__(NT) sample_kernel(const float* __restrict__ logits, int64_t ld, int V, int ts, int fix,
+                                                    const float* __restrict__ u, const float* __restrict__ temperature,
+                                                    const int* __restrict__ top_k, const float* __restrict__ top_p,
+                                                    const float* __restrict__ min_p, int* __restrict__ tokens,
+                                                    float* __restrict__ logprobs) {
+    __shared__ Shared sh;
+    const int row = blockIdx.x, t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    Row r;
+    r.z = logits + (int64_t)row * ld;
+    r.V = V;
+    r.ts = ts;
+    r.tiles = (V + ts - 1) / ts;
+    r.top = 0.f;
+    if (t < 64) sh.table[t] = exp2((double)t / 64.0);
+    const Answer answer = {tokens + row, logprobs ? logprobs + row : nullptr};
+    const float T = temperature ? temperature[row] : 1.0f, uu = u[row];
+    const int k = top_k ? top_k[row] : 0;
+    const float p = top_p ? top_p[row] : 1.0f;
+    const double floor_w = min_p && min_p[row] > 0.0f ? (double)min_p[row] : 0.0;      // (NaN: off)
+    const bool greedy = !(T > 0.0f), by_k = k > 0 && k < V, by_p = p < 1.0f;
+    r.rate = 1.4426950408889634074 / (double)T;
+    Extremes ext = {0ull, 0xffffffffu};
+
+    if (!greedy && !by_k && !by_p && floor_w == 0.0) {
+        // ---- nothing is left out: each tile's weight with the tile's own largest logit for reference
+        __syncthreads();
+        for (int a = wave; a < r.tiles; a += NWAVE) {
+            Row q = r;
+            q.top = -INFINITY;
+            double w = 0.0;
+            for (int i0 = a * ts; i0 < min(V, (a + 1) * ts); i0 += SUB) {
+                float v[16], m = -INFINITY;
+                read_sub(r, i0, v);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    if (!key_of(v[j])) v[j] = -INFINITY;
+                    m = fmaxf(m, v[j]);
+                }
+                for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+                if (m == -INFINITY) continue;
+                if (m > q.top) {
+                    const float old = q.top;
+                    q.top = m;
+                    w *= old == -INFINITY ? 0.0 : q.weight(old, sh.table);
+                }
+#pragma unroll
+                for (int j = 0; j < 16; ++j) w += v[j] == -INFINITY ? 0.0 : q.weight(v[j], sh.table);
+            }
+            w = wave_sum(w);
+            if (lane == 0) { sh.tile[a] = w; sh.tile_top[a] = q.top; }
+        }
+        __syncthreads();
+        float m = t < r.tiles ? sh.tile_top[t] : -INFINITY;
+        for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+        if (lane == 0) sh.part[wave] = m;
+        __syncthreads();
+        for (int i = 0; i < NWAVE; ++i) m = fmaxf(m, (float)sh.part[i]);
+        __syncthreads();
+        if (m == -INFINITY) {
+            if (t == 0) answer.give(-1, -INFINITY);
+            return;
+        }
+        r.top = m;
+        if (t < r.tiles) sh.tile[t] *= sh.tile_top[t] == -INFINITY ? 0.0 : r.weight(sh.tile_top[t], sh.table);
+        finish_tiles(sh, r, uu, 0, answer, [&](float l, int) { return key_of(l) ? r.weight(l, sh.table) : 0.0; });
+        return;
     }
+    const bool counts = !greedy && by_k && k <= CAP / 2;
+    if (counts) {
+        // ---- tokens by the leading 12 bits of their key; once 16 K logits have been seen only what can be among the first k
+        clear_bins(sh);
+        uint32_t low = 1;
+        bool first = true;
+        float v[16];
+        for (int i0 = wave * SUB; i0 - wave * SUB < V; i0 += NWAVE * SUB) {
+            if (i0 < V) {
+                read_sub(r, i0, v);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    ext.see(v[j], i0 + j * 64 + lane);
+                    const uint32_t key = key_of(v[j]);
+                    if (key >= low) atomicAdd(&sh.count[BINS - 1 - (key >> 20)], 1);
+                }
+            }
+            if (first && V > 2 * NWAVE * SUB) {
+                __syncthreads();
+                const int b = find_bin<false>(sh, Goal{k, 0.0}, 0, 0.0, 0, [](int) { return 0; });
+                if (sh.scan_n[NT - 1] >= k) low = (uint32_t)(BINS - 1 - b) << 20;
+                low = max(low, 1u);
+                __syncthreads();
+            }
+            first = false;
+        }
+    } else {
+        for_each(r, [&](float l, int i) { ext.see(l, i); });
+    }
+    ext.join(sh);
+    if (ext.best == 0 || greedy) {                            // nothing to draw; or the most likely token
+        if (t == 0) answer.give(ext.best ? (int)~(uint32_t)ext.best : -1, ext.best ? 0.0 : -INFINITY);
+        return;
+    }
+    r.top = value_of((uint32_t)(ext.best >> 32));
+    const auto gather = [&](auto take) {
+        if (t == 0) sh.n_list = 0;
+        __syncthreads();
+        for_each(r, [&](float l, int i) {
+            const uint32_t key = key_of(l);
+            if (key && take(l, key)) sh.list[atomicAdd(&sh.n_list, 1)] = (unsigned long long)key << 32 | (uint32_t)~i;
+        });
+        __syncthreads();
+    };
+    if (counts) {
+        const int b = find_bin<false>(sh, Goal{k, 0.0}, 0, 0.0, 0, [](int) { return 0; }), n = sh.above_n + sh.count[b];
+        if (n <= CAP) {
+            const uint32_t low = (uint32_t)(BINS - 1 - b) << 20;
+            gather([&](float, uint32_t key) { return key >= low; });
+            finish_list(sh, r, n, true, k, by_p, p, 0.0, floor_w, uu, answer);
+            return;
+        }
+    }
+    unsigned long long cut = 0;                               // the last token of the kept beginning (0: all)
+    if (by_k || by_p) {
+        // ---- tokens and weight in equal steps of the logit below the largest: over all logits, or down to where no weight
+        // counts any more (the last bin takes the rest)
+        const double span = fmin((double)r.top - (double)value_of(ext.least), 64.0 * fmax((double)T, 1.0));
+        const float scale = span > 0.0 && r.top < INFINITY ? (float)(BINS / span) : 0.0f;
+        const double step = scale > 0.0f ? r.rate / (double)scale : 0.0;
+        // no weight in a bin is above that of its upper edge; 1 for what the steps' own rounding moves across edges
+        const auto ref = [&](int b) { return (int)fmax(ceil(-(double)b * step), -1000.0) + 1; };
+        const auto bin = [&](float l) {
+            const float x = (r.top - l) * scale;
+            return x < (float)(BINS - 1) ? (int)x : BINS - 1;
+        };
+        const auto fill = [&] {
+            clear_bins(sh);
+            for_each(r, [&](float l, int) {
+                if (key_of(l)) {
+                    const int b = bin(l);
+                    add_to_bin(sh, b, r.weight(l, sh.table), fix - ref(b));
+                }
+            });
+            __syncthreads();
+        };
+        // -> whether the bins still are what fill made
+        const auto search = [&](const Goal& goal) {
+            const int b = find_bin<true>(sh, goal, 0, 0.0, fix, ref), n = sh.count[b], base_n = sh.above_n;
+            const double base_w = sh.above_w;
+            if (n > CAP) {
+                find_in_row(sh, r, goal, fix);
+                return false;
+            }
+            gather([&](float l, uint32_t) { return bin(l) == b; });
+            sort_list(sh, n);
+            find_in_list(sh, r, goal, n, base_n, base_w);
+            return true;
+        };
+        fill();
+        double sum;
+        if (by_k) {
+            const bool whole = search(Goal{k, 0.0});
+            cut = sh.cut;
+            sum = sh.cut_sum;
+            __syncthreads();
+            if (by_p && !whole) fill();
+        } else {
+            find_bin<true>(sh, Goal{1, 0.0}, 0, 0.0, fix, ref);
+            sum = sh.total_w;
+            __syncthreads();
+            const int b = find_bin<true>(sh, Goal{0, fmax((double)p * sum, DBL_MIN)}, 0, 0.0, fix, ref), n = sh.above_n + sh.count[b];
+            if (n <= CAP) {
+                gather([&](float l, uint32_t) { return bin(l) <= b; });
+                finish_list(sh, r, n, false, 0, true, p, sum, floor_w, uu, answer);
+                return;
+            }
+        }
+        if (by_p) {           // (above 0, so that no sum of nothing reaches it)
+            search(Goal{0, fmax((double)p * sum, DBL_MIN)});
+            cut = sh.cut > cut ? sh.cut : cut;
+            __syncthreads();
+        }
+    }
+    // ---- the kept weight of every tile, a wavefront each
+    const auto kept = [&](float l, int i) {
+        const uint32_t key = key_of(l);
+        const unsigned long long e = (unsigned long long)key << 32 | (uint32_t)~i;
+        if (!key || e < cut) return 0.0;
+        const double w = r.weight(l, sh.table);
+        return w >= floor_w || e == ext.best ? w : 0.0;
+    };
+    for (int a = wave; a < r.tiles; a += NWAVE) {
+        double w = 0.0;
+        for (int i0 = a * ts; i0 < min(V, (a + 1) * ts); i0 += SUB) {
+            float v[16];
+            read_sub(r, i0, v);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) w += kept(v[j], i0 + j * 64 + lane);
+        }
+        w = wave_sum(w);
+        if (lane == 0) sh.tile[a] = w;
+    }
+    __syncthreads();
+    finish_tiles(sh, r, uu, (int)~(uint32_t)ext.best, answer, kept);
 }
 
 }  // namespace
@@ -424,9 +644,8 @@ __global__ void __launch_bounds__(NT) sample_kernel(const float* __restrict__ lo
 void launch_sample(const float* logits, int64_t ld, int rows, int V, const float* u, const float* temperature, const int* top_k,
                    const float* top_p, const float* min_p, int* tokens, float* logprobs, hipStream_t s) {
     if (rows <= 0) return;
-    // at most 1024 tiles, not so short that adding up a wavefront's parts costs more than the parts; histogram weights of as
-    // many digits as V of them may add up
-    const int ts = (int)std::max<int64_t>(round_up64((V + MAX_TILES - 1) / MAX_TILES, 64), 512);
+    // at most MAX_TILES tiles of whole SUBs; histogram weights of as many digits as V of them may add up
+    const int ts = (int)round_up64((V + MAX_TILES - 1) / MAX_TILES, SUB);
     int fix = 62;
     while (fix > 0 && ((int64_t)V << fix) > ((int64_t)1 << 62)) --fix;
     fix = fix < 44 ? fix : 44;
