@@ -603,10 +603,13 @@ po_status po_op_lm_head(int32_t dtype, const void* dev_x, const void* dev_w, flo
  * The four settings are arrays [rows] on the device, each may be NULL (off; temperature 1).  temperature <= 0 or NaN: the first of
  * the order, log-prob 0; top_k <= 0 or >= V, top_p >= 1 or NaN, min_p <= 0 or NaN: off.  u outside [0, 1) is moved to the nearest
  * value inside, NaN to 0.  Logits of -infinity and NaN are never drawn; with +infinity among them only those are.  A row
- * without any other than -infinity and NaN gives token -1, log-prob -infinity.  Every launch gives the same bits. */
+ * without any other than -infinity and NaN gives token -1, log-prob -infinity.  Every call gives the same bits.
+ * dev_scratch (256-byte aligned): po_sample_bytes of what the call is given (with_top_k, with_top_p: 0 where that array is NULL;
+ * host only), nothing in it is expected or left; calls that may run at the same time need one each. */
+po_status po_sample_bytes(int64_t rows, int32_t V, int32_t with_top_k, int32_t with_top_p, size_t* scratch_bytes);
 po_status po_op_sample(const float* dev_logits, int64_t ld, int64_t rows, int32_t V, const float* dev_u, const float* dev_temperature,
                        const int32_t* dev_top_k, const float* dev_top_p, const float* dev_min_p, int32_t* dev_tokens,
-                       float* dev_logprobs, void* hip_stream);
+                       float* dev_logprobs, void* dev_scratch, size_t scratch_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -42,7 +42,7 @@ EXPORTS = [
     "po_op_attention_split_prefix", "po_attention_tile", "po_gemm_tile", "po_gemm_turns", "po_gemm_f32_tile", "po_op_linear_fp8_split",
     "po_sched_create", "po_sched_destroy", "po_sched_set_jct_model", "po_sched_fit_jct_model", "po_sched_push",
     "po_sched_size", "po_sched_pick", "po_sched_remove", "po_op_rope_static", "po_op_mfma_peak", "po_op_stream_copy",
-    "po_op_quantize_blocks", "po_linear_fp8_block_bytes", "po_op_linear_fp8_block", "po_op_sample", "po_op_attention_shared", "po_attention_shared_bytes",
+    "po_op_quantize_blocks", "po_linear_fp8_block_bytes", "po_op_linear_fp8_block", "po_op_sample", "po_op_attention_shared", "po_attention_shared_bytes", "po_sample_bytes",
 ]
 
 
@@ -146,7 +146,8 @@ def lib() -> C.CDLL:
     L.po_op_quantize_blocks.argtypes = [vp, vp, vp, i64, i32, i32, vp]
     L.po_linear_fp8_block_bytes.argtypes = [i64, i32, i32, C.POINTER(sz)]
     L.po_op_linear_fp8_block.argtypes = [i32, vp, vp, vp, vp, vp, vp, vp, sz, i64, i32, i32, vp]
-    L.po_op_sample.argtypes = [vp, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.po_op_sample.argtypes = [vp, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.po_sample_bytes.argtypes = [i64, i32, i32, i32, C.POINTER(sz)]
     L.po_op_attention_shared.argtypes = [i32, vp, i64, vp, vp, i64, i64, vp, vp, i32, vp, vp, i64, i64, i32, i32, i32, i32, vp, sz, vp]
     L.po_attention_shared_bytes.argtypes = [i32, vp, i32, i64, i32, i32, i32, C.POINTER(sz)]
     f64 = C.c_double
@@ -779,6 +780,13 @@ def po_op_lm_head(x, w):
     return z
 
 
+def po_sample_bytes(rows: int, V: int, with_top_k: bool = True, with_top_p: bool = True) -> int:
+    """bytes of scratch that po_op_sample needs (host only)"""
+    n = C.c_size_t(0)
+    check(lib().po_sample_bytes(rows, V, 1 if with_top_k else 0, 1 if with_top_p else 0, C.byref(n)))
+    return n.value
+
+
 def po_op_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
     """float32 logits [rows, V] (rows may have a pitch), u [rows] in [0, 1), settings [rows] each or None -> (int32 tokens [rows],
     float32 log-probs [rows])"""
@@ -797,7 +805,10 @@ def po_op_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None
         settings.append(None if t is None else t.data_ptr())
     tokens = torch.empty(rows, dtype=torch.int32, device=logits.device)
     logprobs = torch.empty(rows, dtype=f32, device=logits.device)
-    check(lib().po_op_sample(logits.data_ptr(), ld, rows, V, *settings, tokens.data_ptr(), logprobs.data_ptr(), stream))
+    need = po_sample_bytes(rows, V, top_k is not None, top_p is not None)
+    scratch = torch.empty(need, dtype=torch.uint8, device=logits.device)
+    check(lib().po_op_sample(logits.data_ptr(), ld, rows, V, *settings, tokens.data_ptr(), logprobs.data_ptr(), scratch.data_ptr(), need,
+                             stream))
     return tokens, logprobs
 
 

@@ -1757,11 +1757,26 @@ po_status po_op_lm_head(int32_t dtype, const void* x, const void* w, float* logi
     return PO_OK;
 }
 
+static po_status sample_shape(int64_t rows, int32_t V) {
+    if (rows <= 0 || V <= 0) return PO_ERR_INVALID_ARG;
+    return rows > 1 << 20 || V > 1 << 24 ? PO_ERR_TOO_LONG : PO_OK;
+}
+
+po_status po_sample_bytes(int64_t rows, int32_t V, int32_t with_top_k, int32_t with_top_p, size_t* scratch_bytes) {
+    if (!scratch_bytes) return PO_ERR_INVALID_ARG;
+    const po_status st = sample_shape(rows, V);
+    if (st == PO_OK) *scratch_bytes = sample_scratch(rows, V, with_top_k != 0, with_top_p != 0);
+    return st;
+}
+
 po_status po_op_sample(const float* logits, int64_t ld, int64_t rows, int32_t V, const float* u, const float* temperature,
-                       const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens, float* logprobs, void* stream) {
-    if (!logits || !u || !tokens || rows <= 0 || V <= 0 || ld < V) return PO_ERR_INVALID_ARG;
-    if (rows > 1 << 24 || V > 1 << 24) return PO_ERR_TOO_LONG;
-    launch_sample(logits, ld, (int)rows, V, u, temperature, top_k, top_p, min_p, tokens, logprobs, (hipStream_t)stream);
+                       const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens, float* logprobs,
+                       void* scratch, size_t scratch_bytes, void* stream) {
+    if (!logits || !u || !tokens || !scratch || ((uintptr_t)scratch & 255) || ld < V) return PO_ERR_INVALID_ARG;
+    const po_status st = sample_shape(rows, V);
+    if (st != PO_OK) return st;
+    if (scratch_bytes < sample_scratch(rows, V, top_k != nullptr, top_p != nullptr)) return PO_ERR_WORKSPACE_TOO_SMALL;
+    launch_sample(logits, ld, (int)rows, V, u, temperature, top_k, top_p, min_p, tokens, logprobs, scratch, (hipStream_t)stream);
     PO_HIP(hipGetLastError());
     return PO_OK;
 }

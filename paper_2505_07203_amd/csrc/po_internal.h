@@ -223,7 +223,9 @@ void launch_gemm_fp8_block(int epi, const unsigned char* A, const float* sa, con
 
 // one token per row of logits (row pitch ld); the four settings may each be null; tokens -1 where a row has nothing to draw
 void launch_sample(const float* logits, int64_t ld, int rows, int V, const float* u, const float* temperature, const int* top_k,
-                   const float* top_p, const float* min_p, int* tokens, float* logprobs, hipStream_t s);
+                   const float* top_p, const float* min_p, int* tokens, float* logprobs, void* scratch, hipStream_t s);
+// bytes of scratch (256-byte aligned) that it needs, by which settings are given
+size_t sample_scratch(int64_t rows, int V, bool top_k, bool top_p);
 
 // ---- micro-peaks (measurement only)
 double launch_mfma_peak(int kind, int waves_per_simd, int iters, const void* operands, size_t operand_bytes, float* sink,

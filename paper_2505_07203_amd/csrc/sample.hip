@@ -8,11 +8,23 @@
 //
 // Whole numbers come out, so sums and comparisons are float64 throughout: an error of 1e-7 in a running sum over 10^5 tokens
 // would move a draw to its neighbour once in a hundred.  The exponential is the only costly part (a float64 operation takes a
-// compute unit a cycle per wavefront): 2^y by a table of 64 values of 2^(j / 64) in LDS and a polynomial of degree 5, relative
-// error below 1e-15, about 12 operations.
+// compute unit a cycle per wavefront): 2^y by a table of 256 values of 2^(j / 256) in LDS and a polynomial of degree 4, relative
+// error below 1e-15, about 16 operations.
+//
+// A row is cut into parts, a workgroup each, so that few rows use many compute units, and goes through up to four launches:
+//   1  parts: nothing but a temperature: every tile's weight (SUB logits), its own largest logit for reference.  top_k up to
+//      K_MAX: the part's own first top_k, found by counting leading bits of keys; the row's are among the parts'.  Otherwise
+//      the part's extremes.
+//   2  parts, where top_p (or a larger top_k) decides: tokens and weight in 4096 equal steps of the logit below the row's largest.
+//   3  rows: the head of the order that holds everything kept, gathered and sorted in LDS, and the draw; or, where that is longer
+//      than a list, the last kept token.
+//   4  parts, for those rows: every tile's kept weight; the last workgroup of a row to finish draws.
 #include "po_internal.h"
 
 #include <float.h>
+
+#include <algorithm>
+#include <type_traits>
 
 namespace po {
 namespace {
@@ -24,20 +36,24 @@ constexpr int PER = BINS / NT;      // bins of a thread
 constexpr int CAP = 4096;           // entries that are ordered in LDS
 constexpr int MAX_TILES = 1024;
 constexpr int SUB = 1024;           // logits that a wavefront reads at once, 16 a lane
+constexpr int K_MAX = 1024;         // top_k up to which parts list their own first
+constexpr int PART_CAP = 2048;      // tokens that a part may list
+constexpr int MAX_PARTS = 16;
 
 struct Shared {
-    double table[64];
+    double table[256];
     double part[NWAVE];
     int ipart[NWAVE];
     unsigned long long wave_best[NWAVE];
     double scan_w[NT];
     int scan_n[NT];
     unsigned long long weight[BINS];        // of a bin, as a multiple of 2^(its reference exponent - fix)
-    int count[BINS];
+    alignas(16) int count[BINS];
     unsigned long long list[CAP];           // key << 32 | ~index: descending order is the order of the tokens
     double tile[MAX_TILES];
     float tile_top[MAX_TILES];
     int n_list;
+    int part_end[16];
     // answers of a search, written by the one thread that finds them
     int found;
     int above_n;
@@ -59,22 +75,21 @@ struct Row {
     const float* z;
     int V, ts, tiles;               // a tile: ts consecutive logits, a wavefront's
     float top;                      // the largest logit
-    double rate;                    // log2(e) / T
+    double rate;                    // 256 log2(e) / T
 
-    // 2^((l - top) rate) of a logit that may be drawn
+    // exp((l - top) / T) of a logit that may be drawn
     __device__ __forceinline__ double weight(float l, const double* table) const {
-        if (l == top) return 1.0;
-        const double y = ((double)l - (double)top) * rate;
-        if (!(y > -1000.0)) return 0.0;              // (what is left of it no sum holds; -inf, and -inf * 0)
-        const double n = rint(y * 64.0);
-        const double r = fma(n, -1.0 / 64.0, y) * 0.69314718055994530942;
-        double p = fma(r, 1.0 / 120.0, 1.0 / 24.0);
-        p = fma(p, r, 1.0 / 6.0);
-        p = fma(p, r, 0.5);
-        p = fma(p, r, 1.0);
+        if (top == INFINITY) return l == top ? 1.0 : 0.0;                     // (wavefront-uniform)
+        // 256 log2 of it; what is left below 2^-1090 is 0 (also where the product is no number)
+        const double y = fmax(((double)l - (double)top) * rate, -280000.0);
+        const double n = rint(y), f = y - n;                                  // 2^(f / 256), |f| <= 1/2: c = ln 2 / 256
+        constexpr double c = 0.69314718055994530942 / 256.0;
+        double q = fma(f, c * c * c * c / 24.0, c * c * c / 6.0);
+        q = fma(q, f, c * c / 2.0);
+        q = fma(q, f, c);
         const int i = (int)n;
-        const double t = table[i & 63];
-        return ldexp(fma(t * r, p, t), i >> 6);
+        const double t = table[i & 255];
+        return ldexp(fma(t * f, q, t), i >> 8);
     }
 };
 
@@ -88,19 +103,31 @@ __device__ __forceinline__ void read_sub(const Row& r, int i0, float (&v)[16]) {
         v[j] = i < r.V ? x : -INFINITY;
     }
 }
-// f(logit, its index) for all logits of the row, a wavefront SUB of them at a time
-template <typename F>
-__device__ __forceinline__ void for_each(const Row& r, F f) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// f(first index, the 16 logits of this lane) for every SUB of the logits [i0, i1) of the row (i0 a multiple of SUB), one after the other by
+// each wavefront, AHEAD: the next one's logits on their way
+template <bool AHEAD = true, typename F>
+__device__ __forceinline__ void for_each_sub(const Row& r, int i0, int i1, F f) {
+    i0 += (threadIdx.x >> 6) * SUB;
     float v[16], next[16];
-    if (wave * SUB < r.V) read_sub(r, wave * SUB, next);
-    for (int i0 = wave * SUB; i0 < r.V; i0 += NWAVE * SUB) {
+    if (AHEAD && i0 < i1) read_sub(r, i0, next);
+    for (; i0 < i1; i0 += NWAVE * SUB) {
+        if (AHEAD) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = next[j];
-        if (i0 + NWAVE * SUB < r.V) read_sub(r, i0 + NWAVE * SUB, next);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) f(v[j], i0 + j * 64 + lane);
+            for (int j = 0; j < 16; ++j) v[j] = next[j];
+            if (i0 + NWAVE * SUB < i1) read_sub(r, i0 + NWAVE * SUB, next);
+        } else {
+            read_sub(r, i0, v);
+        }
+        f(i0, v);
     }
+}
+// f(logit, its index)
+template <bool AHEAD = true, typename F>
+__device__ __forceinline__ void for_each(const Row& r, int i0, int i1, F f) {
+    for_each_sub<AHEAD>(r, i0, i1, [&](int i, const float (&v)[16]) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) f(v[j], i + j * 64 + (int)(threadIdx.x & 63));
+    });
 }
 
 __device__ __forceinline__ double wave_sum(double v) {
@@ -199,15 +226,31 @@ __device__ __forceinline__ void add_to_bin(Shared& sh, int b, double w, int digi
     if (f) atomicAdd(&sh.weight[b], f);
 }
 
-// sh.list[0 .. n) in descending order (n <= CAP)
+// sh.list[0 .. n) in descending order (n <= CAP; entries that are not 0 differ)
 __device__ void sort_list(Shared& sh, int n) {
-    int m = 2;
+    const int t = threadIdx.x;
+    if (n <= 512) {                        // every entry's place is the number of larger ones (and of equal ones in front)
+        unsigned long long e = 0;
+        int place = 0;
+        if (t < n) {
+            e = sh.list[t];
+            for (int i = 0; i < n; ++i) {
+                const unsigned long long o = sh.list[i];
+                place += o > e || (o == e && i < t);
+            }
+        }
+        __syncthreads();
+        if (t < n) sh.list[place] = e;
+        __syncthreads();
+        return;
+    }
+    int m = 1024;
     while (m < n) m <<= 1;
-    for (int i = n + threadIdx.x; i < m; i += NT) sh.list[i] = 0;
+    for (int i = n + t; i < m; i += NT) sh.list[i] = 0;
     __syncthreads();
     for (int size = 2; size <= m; size <<= 1)
         for (int half = size >> 1; half > 0; half >>= 1) {
-            for (int i = threadIdx.x; i < m / 2; i += NT) {
+            for (int i = t; i < m / 2; i += NT) {
                 const int lo = 2 * i - (i & (half - 1)), hi = lo + half;
                 const bool down = (lo & size) == 0;
                 const unsigned long long a = sh.list[lo], b = sh.list[hi];
@@ -255,7 +298,7 @@ __device__ void find_in_row(Shared& sh, const Row& r, const Goal& goal, int fix)
         const double wh = r.weight(value_of(high), sh.table);
         const int ref = wh > 0.0 ? ilogb(wh) + 1 : -1000;
         clear_bins(sh);
-        for_each(r, [&](float l, int) {
+        for_each<false>(r, 0, r.V, [&](float l, int) {
             const uint32_t key = key_of(l);
             if (key && (key & upper) == prefix)
                 add_to_bin(sh, (1 << bits) - 1 - (int)((key >> shift) & ((1u << bits) - 1)), r.weight(l, sh.table), fix - ref);
@@ -300,32 +343,6 @@ __device__ void find_in_row(Shared& sh, const Row& r, const Goal& goal, int fix)
     }
     __syncthreads();
 }
-
-// The first of the largest logits, as an entry of a list (0: there is none), and the lowest key of what may be drawn.
-struct Extremes {
-    unsigned long long best;
-    uint32_t least;
-    __device__ __forceinline__ void see(float l, int i) {
-        const uint32_t key = key_of(l);
-        const unsigned long long e = (unsigned long long)key << 32 | (uint32_t)~i;
-        if (key) { best = e > best ? e : best; least = min(least, key); }
-    }
-    __device__ void join(Shared& sh) {
-        for (int off = 32; off > 0; off >>= 1) {
-            const unsigned long long o = __shfl_xor(best, off);
-            best = o > best ? o : best;
-            least = min(least, (uint32_t)__shfl_xor((int)least, off));
-        }
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) { sh.wave_best[threadIdx.x >> 6] = best; sh.ipart[threadIdx.x >> 6] = (int)least; }
-        __syncthreads();
-        for (int i = 0; i < NWAVE; ++i) {
-            best = sh.wave_best[i] > best ? sh.wave_best[i] : best;
-            least = min(least, (uint32_t)sh.ipart[i]);
-        }
-        __syncthreads();
-    }
-};
 
 struct Answer {
     int* token;
@@ -399,95 +416,319 @@ __device__ void finish_list(Shared& sh, const Row& r, int n, bool by_k, int k, b
     }
 }
 
-// The token once sh.tile holds the kept weight of every tile.  kept(logit, index): its weight, or 0.
-template <typename F>
-__device__ void finish_tiles(Shared& sh, const Row& r, float u, int best, const Answer& answer, F kept) {
-    const int t = threadIdx.x, lane = t & 63;
-    block_scan(sh, 0, t < r.tiles ? sh.tile[t] : 0.0);
-    const double all = sh.scan_w[r.tiles - 1], target = target_of(u, all);
-    const int a = first_thread(sh, t == r.tiles - 1 || sh.scan_w[t] > target, t && (t - 1 == r.tiles - 1 || sh.scan_w[t - 1] > target));
-    if (t >= 64) return;
-    double run = a ? sh.scan_w[a - 1] : 0.0, w_last = 1.0;
-    int token = best;
-    for (int i0 = a * r.ts; i0 < min(r.V, (a + 1) * r.ts); i0 += 64) {
-        const int i = i0 + lane;
-        const double w = i < min(r.V, (a + 1) * r.ts) ? kept(r.z[i], i) : 0.0;
-        double c = w;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const double o = __shfl_up(c, off);
-            if (lane >= off) c += o;
-        }
-        // (the last kept token so far stands in where rounding leaves the target out of reach at the very end)
-        const unsigned long long some = __ballot(w > 0.0), past = __ballot(w > 0.0 && run + c > target);
-        if (some) {
-            const int pick = past ? __ffsll(past) - 1 : 63 - __clzll(some);
-            token = i0 + pick;
-            w_last = __shfl(w, pick);
-        }
-        if (past) break;
-        run += __shfl(c, 63);
-    }
-    if (lane == 0) answer.give(token, log(w_last / all));
+// Of the threads with a weight (w > 0, at least one), scanned by block_scan(sh, w > 0, w), the first at which the sum, `run` in
+// front of it, exceeds target, or the last where none does (*past).  (Sums of neighbours are added up in different orders: one
+// without a weight may seem to be past the target a rounding early.)
+__device__ __forceinline__ int first_past(Shared& sh, bool has, double run, double target, bool* past) {
+    const int t = threadIdx.x, some = sh.scan_n[NT - 1];
+    const bool yes = sh.scan_n[t] == some || run + sh.scan_w[t] > target;
+    const bool before = t && (sh.scan_n[t - 1] == some || run + sh.scan_w[t - 1] > target);
+    const int f = first_thread(sh, yes, before);
+    *past = run + sh.scan_w[f] > target;
+    const int in_front = f ? sh.scan_n[f - 1] : 0;
+    return first_thread(sh, t >= f && has, t > f && sh.scan_n[t - 1] > in_front);
 }
 
-// A row, a workgroup.  What it takes by settings: nothing but a temperature, one pass over the logits; top_k (up to half a list), one
-// pass that counts keys by their leading bits and one that gathers the head of the order; top_p alone, a pass for the extremes, one
-// that adds weights by steps of the logit, one that gathers; where the head is longer than a list holds, passes that find
-// the last kept token and one that adds up what is kept.
-__global__ void __launch_bounds__(NT) sample_kernel(const float* __restrict__ logits, int64_t ld, int V, int ts, int fix,
-                                                    const float* __restrict__ u, const float* __restrict__ temperature,
-                                                    const int* __restrict__ top_k, const float* __restrict__ top_p,
-                                                    const float* __restrict__ min_p, int* __restrict__ tokens,
-                                                    float* __restrict__ logprobs) {
-    __shared__ Shared sh;
-    const int row = blockIdx.x, t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    Row r;
-    r.z = logits + (int64_t)row * ld;
-    r.V = V;
-    r.ts = ts;
-    r.tiles = (V + ts - 1) / ts;
-    r.top = 0.f;
-    if (t < 64) sh.table[t] = exp2((double)t / 64.0);
-    const Answer answer = {tokens + row, logprobs ? logprobs + row : nullptr};
-    const float T = temperature ? temperature[row] : 1.0f, uu = u[row];
-    const int k = top_k ? top_k[row] : 0;
-    const float p = top_p ? top_p[row] : 1.0f;
-    const double floor_w = min_p && min_p[row] > 0.0f ? (double)min_p[row] : 0.0;      // (NaN: off)
-    const bool greedy = !(T > 0.0f), by_k = k > 0 && k < V, by_p = p < 1.0f;
-    r.rate = 1.4426950408889634074 / (double)T;
-    Extremes ext = {0ull, 0xffffffffu};
+// The token once sh.tile holds the kept weight of every tile (not all of them 0).  kept(logit, index): its weight, or 0.
+template <typename F>
+__device__ void finish_tiles(Shared& sh, const Row& r, float u, const Answer& answer, F kept) {
+    const int t = threadIdx.x;
+    const double mine = t < r.tiles ? sh.tile[t] : 0.0;
+    block_scan(sh, mine > 0.0, mine);
+    const double all = sh.scan_w[NT - 1], target = target_of(u, all);
+    bool past;
+    const int a = first_past(sh, mine > 0.0, 0.0, target, &past);
+    double run = a ? sh.scan_w[a - 1] : 0.0, w_last = 1.0;
+    int token = -1;                                      // (the last kept one so far stands in where rounding leaves the target out of reach)
+    __syncthreads();
+    for (int i0 = a * r.ts; i0 < min(r.V, (a + 1) * r.ts); i0 += NT) {
+        const int i = i0 + t;
+        const double w = i < r.V ? kept(r.z[i], i) : 0.0;
+        block_scan(sh, w > 0.0, w);
+        const double end = sh.scan_w[NT - 1];
+        if (sh.scan_n[NT - 1]) {
+            const int f = first_past(sh, w > 0.0, run, target, &past);
+            if (t == f) { sh.above_n = i; sh.above_w = w; }
+            __syncthreads();
+            token = sh.above_n;
+            w_last = sh.above_w;
+            __syncthreads();
+            if (past) break;
+        }
+        run += end;
+    }
+    if (t == 0) answer.give(token, log(w_last / all));
+}
 
-    if (!greedy && !by_k && !by_p && floor_w == 0.0) {
-        // ---- nothing is left out: each tile's weight with the tile's own largest logit for reference
-        __syncthreads();
-        for (int a = wave; a < r.tiles; a += NWAVE) {
-            Row q = r;
+// What the launches hand on, in the caller's scratch; arrays of a row one behind the other.
+struct Handover {
+    unsigned long long* best;        // [row][part] the part's first token (an entry of a list; 0: none)
+    uint32_t* least;                 // [row][part] lowest key of what may be drawn
+    int* listed;                     // [row][part] tokens of list, PART_CAP + 1: more than it holds
+    unsigned long long* list;        // [row][part][PART_CAP]
+    double* tile;                    // [row][MAX_TILES] weight of a tile
+    float* tile_top;                 // [row][MAX_TILES]
+    int* count;                      // [row][part][BINS]
+    unsigned long long* weight;      // [row][part][BINS]
+    unsigned long long* first;       // [row] the row's first token where the fourth launch has to see to it, else 0
+    unsigned long long* cut;         // [row] ... and the last kept one (0: all)
+    int* finished;                   // [row][2] parts that have finished the third, and the fourth, launch
+};
+struct Call {
+    const float* logits;
+    int64_t ld;
+    int V, ts, fix, parts, part_len;
+    const float *u, *temperature;
+    const int* top_k;
+    const float *top_p, *min_p;
+    int* tokens;
+    float* logprobs;
+    Handover h;
+};
+
+enum How { GREEDY, FREE, COUNT, WEIGH, KEEP };      // KEEP: min_p alone
+struct Settings {
+    float T, p, u;
+    int k;
+    double floor_w;
+    bool by_k, by_p;
+    How how;
+    __device__ Settings(const Call& c, int row) {
+        T = c.temperature ? c.temperature[row] : 1.0f;
+        k = c.top_k ? c.top_k[row] : 0;
+        p = c.top_p ? c.top_p[row] : 1.0f;
+        u = c.u[row];
+        floor_w = c.min_p && c.min_p[row] > 0.0f ? (double)c.min_p[row] : 0.0;      // (NaN: off)
+        by_k = k > 0 && k < c.V;
+        by_p = p < 1.0f;
+        how = !(T > 0.0f) ? GREEDY : by_k && k <= K_MAX ? COUNT : by_k || by_p ? WEIGH : floor_w > 0.0 ? KEEP : FREE;
+    }
+};
+
+__device__ __forceinline__ Row row_of(const Call& c, int row, const Settings& s) {
+    Row r;
+    r.z = c.logits + (int64_t)row * c.ld;
+    r.V = c.V;
+    r.ts = c.ts;
+    r.tiles = (c.V + c.ts - 1) / c.ts;
+    r.top = 0.f;
+    r.rate = fmin(256.0 * 1.4426950408889634074 / (double)s.T, 1e300);        // (0 * infinity would be none)
+    return r;
+}
+
+__device__ __forceinline__ Answer answer_of(const Call& c, int row) { return {c.tokens + row, c.logprobs ? c.logprobs + row : nullptr}; }
+
+__device__ __forceinline__ void fill_table(Shared& sh) {
+    if (threadIdx.x < 256) sh.table[threadIdx.x] = exp2((double)threadIdx.x / 256.0);
+    __syncthreads();
+}
+
+// the largest of a workgroup's values
+__device__ __forceinline__ unsigned long long block_max(Shared& sh, unsigned long long v) {
+    for (int off = 32; off > 0; off >>= 1) {
+        const unsigned long long o = __shfl_xor(v, off);
+        v = o > v ? o : v;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh.wave_best[threadIdx.x >> 6] = v;
+    __syncthreads();
+    for (int i = 0; i < NWAVE; ++i) v = sh.wave_best[i] > v ? sh.wave_best[i] : v;
+    return v;
+}
+
+// Between the workgroups of a row within a launch: what one writes for another goes past the caches (hand / handed), each wavefront
+// waits until its own has arrived, and one thread counts the workgroup in.  -> whether it is the last, which then finds everything.
+__device__ __forceinline__ void hand(unsigned long long* p, unsigned long long v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void hand(int* p, int v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void hand(double* p, double v) { hand((unsigned long long*)p, (unsigned long long)__double_as_longlong(v)); }
+template <typename V>
+__device__ __forceinline__ V handed(V* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ bool last_to_finish(Shared& sh, int* counter, int parts) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) sh.found = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    const bool last = sh.found == parts - 1;
+    __syncthreads();
+    return last;
+}
+
+// ---- launch 1
+__global__ void __launch_bounds__(NT) sample_parts_kernel(const Call c) {
+    __shared__ Shared sh;
+    const int row = blockIdx.x / c.parts, part = blockIdx.x - row * c.parts, t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const Settings s(c, row);
+    const Row r = row_of(c, row, s);
+    const int c0 = part * c.part_len, c1 = min(c.V, c0 + c.part_len);
+    const int64_t at = (int64_t)row * c.parts + part;
+    if (part == 0 && t < 2) c.h.finished[row * 2 + t] = 0;
+    if (part == 0 && t == 0) c.h.first[row] = 0;             // (until it is known that the fourth launch has to see to this row)
+    if (s.how == FREE) {
+        fill_table(sh);
+        // a SUB's weight with its own largest logit for reference, added to its tile's (of one SUB, up to 2^20 logits)
+        const auto weigh = [&](const float (&v)[16], Row& q, double& w) {
+            float m = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) m = fmaxf(m, v[j]);                       // (of a NaN and a number the number)
+            for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+            if (m == -INFINITY) return;
+            if (m > q.top) {
+                const float old = q.top;
+                q.top = m;
+                w *= old == -INFINITY ? 0.0 : q.weight(old, sh.table);
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) w += v[j] > -INFINITY ? q.weight(v[j], sh.table) : 0.0;
+        };
+        const auto put = [&](int a, const Row& q, double w) {
+            w = wave_sum(w);
+            if (lane == 0) { c.h.tile[(int64_t)row * MAX_TILES + a] = w; c.h.tile_top[(int64_t)row * MAX_TILES + a] = q.top; }
+        };
+        Row q = r;
+        if (c.ts == SUB) {
+            for_each_sub(r, c0, c1, [&](int i0, const float (&v)[16]) {
+                q.top = -INFINITY;
+                double w = 0.0;
+                weigh(v, q, w);
+                put(i0 / SUB, q, w);
+            });
+            return;
+        }
+        for (int a = c0 / c.ts + wave; a * c.ts < c1; a += NWAVE) {
             q.top = -INFINITY;
             double w = 0.0;
-            for (int i0 = a * ts; i0 < min(V, (a + 1) * ts); i0 += SUB) {
-                float v[16], m = -INFINITY;
+            for (int i0 = a * c.ts; i0 < min(c.V, (a + 1) * c.ts); i0 += SUB) {
+                float v[16];
                 read_sub(r, i0, v);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    if (!key_of(v[j])) v[j] = -INFINITY;
-                    m = fmaxf(m, v[j]);
-                }
-                for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
-                if (m == -INFINITY) continue;
-                if (m > q.top) {
-                    const float old = q.top;
-                    q.top = m;
-                    w *= old == -INFINITY ? 0.0 : q.weight(old, sh.table);
-                }
-#pragma unroll
-                for (int j = 0; j < 16; ++j) w += v[j] == -INFINITY ? 0.0 : q.weight(v[j], sh.table);
+                weigh(v, q, w);
             }
-            w = wave_sum(w);
-            if (lane == 0) { sh.tile[a] = w; sh.tile_top[a] = q.top; }
+            put(a, q, w);
         }
+        return;
+    }
+    // the largest logit of a thread, and the SUB it is in; the lowest that may be drawn
+    float m = -INFINITY, low = INFINITY;
+    int where = 0;
+    if (s.how == COUNT) clear_bins(sh);
+    for_each_sub(r, c0, c1, [&](int i0, const float (&v)[16]) {
+        float mi = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) mi = fmaxf(mi, v[j]);
+        if (mi > m) { m = mi; where = i0; }
+        if (s.how == WEIGH) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) low = fminf(low, v[j] > -INFINITY ? v[j] : INFINITY);
+        } else if (s.how == COUNT) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const uint32_t key = key_of(v[j]);
+                if (key) atomicAdd(&sh.count[BINS - 1 - (key >> 20)], 1);
+            }
+        }
+    });
+    unsigned long long best = 0;
+    if (m > -INFINITY) {
+        int i = where + lane;                                    // (one of the 16 of this thread in that SUB)
+        for (int j = 0; j < 15 && r.z[min(i, c.V - 1)] != m; ++j) i += 64;
+        best = (unsigned long long)key_of(m) << 32 | (uint32_t)~i;
+    }
+    best = block_max(sh, best);
+    if (t == 0) c.h.best[at] = best;
+    if (s.how == WEIGH) {
+        // (all of a thread's may be +inf: m; or none be there)
+        const unsigned long long l = block_max(sh, m > -INFINITY ? (unsigned long long)~key_of(low == INFINITY ? m : low) : 0ull);
+        if (t == 0) c.h.least[at] = best ? ~(uint32_t)l : 0xffffffffu;
+    }
+    if (s.how != COUNT) return;
+    const int b = find_bin<false>(sh, Goal{s.k, 0.0}, 0, 0.0, 0, [](int) { return 0; }), n = sh.above_n + sh.count[b];
+    if (n <= PART_CAP && best) {
+        const uint32_t lowest = (uint32_t)(BINS - 1 - b) << 20;
+        if (t == 0) sh.n_list = 0;
         __syncthreads();
-        float m = t < r.tiles ? sh.tile_top[t] : -INFINITY;
+        for_each(r, c0, c1, [&](float l, int i) {
+            const uint32_t key = key_of(l);
+            if (key && key >= lowest) c.h.list[at * PART_CAP + atomicAdd(&sh.n_list, 1)] = (unsigned long long)key << 32 | (uint32_t)~i;
+        });
+    }
+    if (t == 0) c.h.listed[at] = best == 0 ? 0 : n <= PART_CAP ? n : PART_CAP + 1;
+}
+
+// ---- the row's first token, and the steps of logits that its weights are counted in
+static_assert(MAX_PARTS <= 16, "a lane each");
+__device__ __forceinline__ unsigned long long first_of(const Call& c, int row) {
+    const int lane = threadIdx.x & 15;
+    unsigned long long best = lane < c.parts ? c.h.best[(int64_t)row * c.parts + lane] : 0;
+#pragma unroll
+    for (int off = 8; off > 0; off >>= 1) {
+        const unsigned long long o = __shfl_xor(best, off, 16);
+        best = o > best ? o : best;
+    }
+    return best;
+}
+// Over all logits, or down to where no weight counts any more (the last bin takes the rest).
+struct Steps {
+    float top, scale;
+    double step;
+    __device__ Steps(const Call& c, int row, const Row& r, float T) {
+        const int lane = threadIdx.x & 15;
+        uint32_t least = lane < c.parts ? c.h.least[(int64_t)row * c.parts + lane] : 0xffffffffu;
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) least = min(least, (uint32_t)__shfl_xor((int)least, off, 16));
+        top = r.top;
+        const double span = fmin((double)top - (double)value_of(least), 64.0 * fmax((double)T, 1.0));
+        scale = span > 0.0 && top < INFINITY ? (float)(BINS / span) : 0.0f;
+        step = scale > 0.0f ? r.rate / 256.0 / (double)scale : 0.0;
+    }
+    __device__ __forceinline__ int bin(float l) const {
+        const float x = (top - l) * scale;
+        return x < (float)(BINS - 1) ? (int)x : BINS - 1;
+    }
+    // no weight in a bin is above that of its upper edge; 1 for what the steps' own rounding moves across edges
+    __device__ __forceinline__ int ref(int b) const { return (int)fmax(ceil(-(double)b * step), -1000.0) + 1; }
+};
+
+template <bool AHEAD>
+__device__ void fill_bins(Shared& sh, const Row& r, const Steps& st, int c0, int c1, int fix) {
+    clear_bins(sh);
+    for_each<AHEAD>(r, c0, c1, [&](float l, int) {
+        if (l > -INFINITY) {
+            const int b = st.bin(l);
+            add_to_bin(sh, b, r.weight(l, sh.table), fix - st.ref(b));
+        }
+    });
+    __syncthreads();
+}
+
+// ---- launch 2
+__global__ void __launch_bounds__(NT) sample_weigh_kernel(const Call c) {
+    __shared__ Shared sh;
+    const int row = blockIdx.x / c.parts, part = blockIdx.x - row * c.parts;
+    const Settings s(c, row);
+    if (s.how != WEIGH) return;
+    Row r = row_of(c, row, s);
+    const unsigned long long best = first_of(c, row);
+    if (best == 0) return;
+    r.top = value_of((uint32_t)(best >> 32));
+    fill_table(sh);
+    const Steps st(c, row, r, s.T);
+    const int c0 = part * c.part_len;
+    fill_bins<true>(sh, r, st, c0, min(c.V, c0 + c.part_len), c.fix);
+    const int64_t at = ((int64_t)row * c.parts + part) * BINS;
+    for (int b = threadIdx.x; b < BINS; b += NT) { c.h.count[at + b] = sh.count[b]; c.h.weight[at + b] = sh.weight[b]; }
+}
+
+// ---- launch 3
+__global__ void __launch_bounds__(NT) sample_pick_kernel(const Call c) {
+    __shared__ Shared sh;
+    const int row = blockIdx.x / c.parts, part = blockIdx.x - row * c.parts, t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const Settings s(c, row);
+    if (part != 0 && !(s.how == WEIGH && !s.by_k)) return;   // (only top_p alone has work for more than one)
+    Row r = row_of(c, row, s);
+    const Answer answer = answer_of(c, row);
+    fill_table(sh);
+    if (s.how == FREE) {
+        const float mine = t < r.tiles ? c.h.tile_top[(int64_t)row * MAX_TILES + t] : -INFINITY;
+        float m = mine;
         for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
         if (lane == 0) sh.part[wave] = m;
         __syncthreads();
@@ -498,159 +739,280 @@ __global__ void __launch_bounds__(NT) sample_kernel(const float* __restrict__ lo
             return;
         }
         r.top = m;
-        if (t < r.tiles) sh.tile[t] *= sh.tile_top[t] == -INFINITY ? 0.0 : r.weight(sh.tile_top[t], sh.table);
-        finish_tiles(sh, r, uu, 0, answer, [&](float l, int) { return key_of(l) ? r.weight(l, sh.table) : 0.0; });
+        if (t < r.tiles) sh.tile[t] = mine == -INFINITY ? 0.0 : c.h.tile[(int64_t)row * MAX_TILES + t] * r.weight(mine, sh.table);
+        __syncthreads();
+        finish_tiles(sh, r, s.u, answer, [&](float l, int) { return l > -INFINITY ? r.weight(l, sh.table) : 0.0; });
         return;
     }
-    const bool counts = !greedy && by_k && k <= CAP / 2;
-    if (counts) {
-        // ---- tokens by the leading 12 bits of their key; once 16 K logits have been seen only what can be among the first k
-        clear_bins(sh);
-        uint32_t low = 1;
-        bool first = true;
-        float v[16];
-        for (int i0 = wave * SUB; i0 - wave * SUB < V; i0 += NWAVE * SUB) {
-            if (i0 < V) {
-                read_sub(r, i0, v);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    ext.see(v[j], i0 + j * 64 + lane);
-                    const uint32_t key = key_of(v[j]);
-                    if (key >= low) atomicAdd(&sh.count[BINS - 1 - (key >> 20)], 1);
-                }
-            }
-            if (first && V > 2 * NWAVE * SUB) {
-                __syncthreads();
-                const int b = find_bin<false>(sh, Goal{k, 0.0}, 0, 0.0, 0, [](int) { return 0; });
-                if (sh.scan_n[NT - 1] >= k) low = (uint32_t)(BINS - 1 - b) << 20;
-                low = max(low, 1u);
-                __syncthreads();
-            }
-            first = false;
-        }
-    } else {
-        for_each(r, [&](float l, int i) { ext.see(l, i); });
-    }
-    ext.join(sh);
-    if (ext.best == 0 || greedy) {                            // nothing to draw; or the most likely token
-        if (t == 0) answer.give(ext.best ? (int)~(uint32_t)ext.best : -1, ext.best ? 0.0 : -INFINITY);
+    const unsigned long long best = first_of(c, row);
+    if (best == 0 || s.how == GREEDY) {                      // nothing to draw; or the most likely token
+        if (part == 0 && t == 0) answer.give(best ? (int)~(uint32_t)best : -1, best ? 0.0 : -INFINITY);
         return;
     }
-    r.top = value_of((uint32_t)(ext.best >> 32));
-    const auto gather = [&](auto take) {
-        if (t == 0) sh.n_list = 0;
-        __syncthreads();
-        for_each(r, [&](float l, int i) {
-            const uint32_t key = key_of(l);
-            if (key && take(l, key)) sh.list[atomicAdd(&sh.n_list, 1)] = (unsigned long long)key << 32 | (uint32_t)~i;
-        });
-        __syncthreads();
+    r.top = value_of((uint32_t)(best >> 32));
+    const auto leave = [&](unsigned long long cut) {         // to the fourth launch
+        if (t == 0) { hand(c.h.cut + row, cut); hand(c.h.first + row, best); }
     };
-    if (counts) {
-        const int b = find_bin<false>(sh, Goal{k, 0.0}, 0, 0.0, 0, [](int) { return 0; }), n = sh.above_n + sh.count[b];
-        if (n <= CAP) {
-            const uint32_t low = (uint32_t)(BINS - 1 - b) << 20;
-            gather([&](float, uint32_t key) { return key >= low; });
-            finish_list(sh, r, n, true, k, by_p, p, 0.0, floor_w, uu, answer);
-            return;
-        }
+    if (s.how == KEEP) {
+        leave(0);
+        return;
     }
-    unsigned long long cut = 0;                               // the last token of the kept beginning (0: all)
-    if (by_k || by_p) {
-        // ---- tokens and weight in equal steps of the logit below the largest: over all logits, or down to where no weight
-        // counts any more (the last bin takes the rest)
-        const double span = fmin((double)r.top - (double)value_of(ext.least), 64.0 * fmax((double)T, 1.0));
-        const float scale = span > 0.0 && r.top < INFINITY ? (float)(BINS / span) : 0.0f;
-        const double step = scale > 0.0f ? r.rate / (double)scale : 0.0;
-        // no weight in a bin is above that of its upper edge; 1 for what the steps' own rounding moves across edges
-        const auto ref = [&](int b) { return (int)fmax(ceil(-(double)b * step), -1000.0) + 1; };
-        const auto bin = [&](float l) {
-            const float x = (r.top - l) * scale;
-            return x < (float)(BINS - 1) ? (int)x : BINS - 1;
+    if (s.how == COUNT) {
+        // the parts' lists, one behind the other: entry e of all
+        int n_part = (lane & 15) < c.parts ? c.h.listed[(int64_t)row * c.parts + (lane & 15)] : 0;
+        const bool whole = !__any(n_part > PART_CAP);
+        if (wave == 0 && lane < 16) sh.part_end[lane] = n_part;
+        __syncthreads();
+        int total = 0;
+        for (int i = 0; i < c.parts; ++i) total += sh.part_end[i];
+        const auto listed = [&](auto f) {
+            for (int e = t; e < total; e += NT) {
+                int i = 0, x = e;
+                while (x >= sh.part_end[i]) x -= sh.part_end[i++];
+                f(c.h.list[((int64_t)row * c.parts + i) * PART_CAP + x]);
+            }
         };
-        const auto fill = [&] {
+        if (whole) {
+            // what can be among the first k of them, by equal steps of keys between the lowest and the highest
+            const uint32_t top = (uint32_t)(best >> 32);
+            unsigned long long low = 0;
+            listed([&](unsigned long long x) { low = max(low, (unsigned long long)~(uint32_t)(x >> 32)); });
+            low = block_max(sh, low);
+            const uint32_t lowest = ~(uint32_t)low;
+            int shift = 0;
+            while ((top - lowest) >> shift >= BINS) ++shift;
             clear_bins(sh);
-            for_each(r, [&](float l, int) {
-                if (key_of(l)) {
-                    const int b = bin(l);
-                    add_to_bin(sh, b, r.weight(l, sh.table), fix - ref(b));
-                }
-            });
+            listed([&](unsigned long long x) { atomicAdd(&sh.count[(top - (uint32_t)(x >> 32)) >> shift], 1); });
             __syncthreads();
-        };
-        // -> whether the bins still are what fill made
+            const int b = find_bin<false>(sh, Goal{s.k, 0.0}, 0, 0.0, 0, [](int) { return 0; }), n = sh.above_n + sh.count[b];
+            if (n <= CAP) {
+                if (t == 0) sh.n_list = 0;
+                __syncthreads();
+                listed([&](unsigned long long x) {
+                    if ((int)((top - (uint32_t)(x >> 32)) >> shift) <= b) sh.list[atomicAdd(&sh.n_list, 1)] = x;
+                });
+                __syncthreads();
+                finish_list(sh, r, n, true, s.k, s.by_p, s.p, 0.0, s.floor_w, s.u, answer);
+                return;
+            }
+        }
+        // (thousands of keys with the same leading bits) the k-th and, in its place, the last one that top_p leaves, from the row
+        find_in_row(sh, r, Goal{s.k, 0.0}, c.fix);
+        unsigned long long cut = sh.cut;
+        const double sum = sh.cut_sum;
+        __syncthreads();
+        if (s.by_p) {
+            find_in_row(sh, r, Goal{0, fmax((double)s.p * sum, DBL_MIN)}, c.fix);
+            cut = sh.cut > cut ? sh.cut : cut;
+        }
+        leave(cut);
+        return;
+    }
+    // ---- WEIGH: the parts' bins added up
+    const Steps st(c, row, r, s.T);
+    const auto ref = [&](int b) { return st.ref(b); };
+    {
+        static_assert(PER == 4, "a thread's bins are one and two 16-byte loads");
+        int4 n = {0, 0, 0, 0};
+        unsigned long long w[4] = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int i = 0; i < c.parts; ++i) {
+            const int64_t at = ((int64_t)row * c.parts + i) * BINS + t * 4;
+            const int4 x = *(const int4*)(c.h.count + at);
+            const ulonglong2 a = *(const ulonglong2*)(c.h.weight + at), b = *(const ulonglong2*)(c.h.weight + at + 2);
+            n.x += x.x; n.y += x.y; n.z += x.z; n.w += x.w;
+            w[0] += a.x; w[1] += a.y; w[2] += b.x; w[3] += b.y;
+        }
+        *(int4*)(sh.count + t * 4) = n;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sh.weight[t * 4 + j] = w[j];
+    }
+    __syncthreads();
+    if (s.by_k) {
+        // (more than K_MAX tokens) one workgroup; -> whether the bins still are there
         const auto search = [&](const Goal& goal) {
-            const int b = find_bin<true>(sh, goal, 0, 0.0, fix, ref), n = sh.count[b], base_n = sh.above_n;
+            const int b = find_bin<true>(sh, goal, 0, 0.0, c.fix, ref), n = sh.count[b], base_n = sh.above_n;
             const double base_w = sh.above_w;
             if (n > CAP) {
-                find_in_row(sh, r, goal, fix);
+                find_in_row(sh, r, goal, c.fix);
                 return false;
             }
-            gather([&](float l, uint32_t) { return bin(l) == b; });
+            if (t == 0) sh.n_list = 0;
+            __syncthreads();
+            for_each<false>(r, 0, c.V, [&](float l, int i) {
+                if (l > -INFINITY && st.bin(l) == b) sh.list[atomicAdd(&sh.n_list, 1)] = (unsigned long long)key_of(l) << 32 | (uint32_t)~i;
+            });
+            __syncthreads();
             sort_list(sh, n);
             find_in_list(sh, r, goal, n, base_n, base_w);
             return true;
         };
-        fill();
-        double sum;
-        if (by_k) {
-            const bool whole = search(Goal{k, 0.0});
-            cut = sh.cut;
-            sum = sh.cut_sum;
-            __syncthreads();
-            if (by_p && !whole) fill();
-        } else {
-            find_bin<true>(sh, Goal{1, 0.0}, 0, 0.0, fix, ref);
-            sum = sh.total_w;
-            __syncthreads();
-            const int b = find_bin<true>(sh, Goal{0, fmax((double)p * sum, DBL_MIN)}, 0, 0.0, fix, ref), n = sh.above_n + sh.count[b];
-            if (n <= CAP) {
-                gather([&](float l, uint32_t) { return bin(l) <= b; });
-                finish_list(sh, r, n, false, 0, true, p, sum, floor_w, uu, answer);
-                return;
-            }
-        }
-        if (by_p) {           // (above 0, so that no sum of nothing reaches it)
-            search(Goal{0, fmax((double)p * sum, DBL_MIN)});
+        const bool still = search(Goal{s.k, 0.0});
+        unsigned long long cut = sh.cut;
+        const double sum = sh.cut_sum;
+        __syncthreads();
+        if (s.by_p) {
+            if (!still) fill_bins<false>(sh, r, st, 0, c.V, c.fix);
+            search(Goal{0, fmax((double)s.p * sum, DBL_MIN)});
             cut = sh.cut > cut ? sh.cut : cut;
-            __syncthreads();
         }
+        leave(cut);
+        return;
     }
-    // ---- the kept weight of every tile, a wavefront each
-    const auto kept = [&](float l, int i) {
-        const uint32_t key = key_of(l);
-        const unsigned long long e = (unsigned long long)key << 32 | (uint32_t)~i;
-        if (!key || e < cut) return 0.0;
-        const double w = r.weight(l, sh.table);
-        return w >= floor_w || e == ext.best ? w : 0.0;
-    };
-    for (int a = wave; a < r.tiles; a += NWAVE) {
-        double w = 0.0;
-        for (int i0 = a * ts; i0 < min(V, (a + 1) * ts); i0 += SUB) {
-            float v[16];
-            read_sub(r, i0, v);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) w += kept(v[j], i0 + j * 64 + lane);
-        }
-        w = wave_sum(w);
-        if (lane == 0) sh.tile[a] = w;
+    // top_p alone: every part's workgroup finds the bin in which it ends (goal above 0, so that no sum of nothing reaches it) and lists
+    // its part's tokens of that bin, or, if they are few, of all up to it; the last one takes them together
+    find_bin<true>(sh, Goal{1, 0.0}, 0, 0.0, c.fix, ref);
+    const double sum = sh.total_w;
+    __syncthreads();
+    const Goal goal = {0, fmax((double)s.p * sum, DBL_MIN)};
+    const int b = find_bin<true>(sh, goal, 0, 0.0, c.fix, ref), n_bin = sh.count[b], above_n = sh.above_n;
+    const double above_w = sh.above_w;
+    __syncthreads();
+    if (n_bin > PART_CAP) {
+        if (part != 0) return;
+        find_in_row(sh, r, goal, c.fix);
+        leave(sh.cut);
+        return;
+    }
+    const bool all = above_n + n_bin <= 512;
+    const int64_t at = (int64_t)row * c.parts + part;
+    const int c0 = part * c.part_len;
+    if (t == 0) sh.n_list = 0;
+    __syncthreads();
+    for_each(r, c0, min(c.V, c0 + c.part_len), [&](float l, int i) {
+        if (!(l > -INFINITY)) return;
+        const int x = st.bin(l);
+        if (x == b || (all && x < b)) hand(c.h.list + at * PART_CAP + atomicAdd(&sh.n_list, 1), (unsigned long long)key_of(l) << 32 | (uint32_t)~i);
+    });
+    __syncthreads();
+    if (t == 0) hand(c.h.listed + at, sh.n_list);
+    if (!last_to_finish(sh, c.h.finished + row * 2, c.parts)) return;
+    int n = 0;
+    for (int i = 0; i < c.parts; ++i) {
+        const int64_t from = (int64_t)row * c.parts + i;
+        const int ni = handed(c.h.listed + from);
+        for (int e = t; e < ni; e += NT) sh.list[n + e] = handed(c.h.list + from * PART_CAP + e);
+        n += ni;
     }
     __syncthreads();
-    finish_tiles(sh, r, uu, (int)~(uint32_t)ext.best, answer, kept);
+    if (all) {
+        finish_list(sh, r, n, false, 0, true, s.p, sum, s.floor_w, s.u, answer);
+        return;
+    }
+    sort_list(sh, n);
+    find_in_list(sh, r, goal, n, above_n, above_w);
+    leave(sh.cut);
+}
+
+// ---- launch 4
+__global__ void __launch_bounds__(NT) sample_keep_kernel(const Call c) {
+    __shared__ Shared sh;
+    const int row = blockIdx.x / c.parts, part = blockIdx.x - row * c.parts, t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const unsigned long long best = c.h.first[row];
+    if (best == 0) return;
+    const Settings s(c, row);
+    Row r = row_of(c, row, s);
+    r.top = value_of((uint32_t)(best >> 32));
+    fill_table(sh);
+    const unsigned long long cut = c.h.cut[row];
+    const float lowest = cut ? value_of((uint32_t)(cut >> 32)) : -INFINITY;
+    const auto kept = [&](float l, int i) {
+        if (!(l > -INFINITY) || l < lowest) return 0.0;
+        const unsigned long long e = (unsigned long long)key_of(l) << 32 | (uint32_t)~i;
+        if (e < cut) return 0.0;
+        const double w = r.weight(l, sh.table);
+        return w >= s.floor_w || e == best ? w : 0.0;
+    };
+    const int c0 = part * c.part_len, c1 = min(c.V, c0 + c.part_len);
+    double* const tile = c.h.tile + (int64_t)row * MAX_TILES;
+    const auto weigh = [&](int i0, const float (&v)[16]) {
+        double w = 0.0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) w += kept(v[j], i0 + j * 64 + lane);
+        return w;
+    };
+    const auto put = [&](int a, double w) {
+        w = wave_sum(w);
+        if (lane == 0) hand(tile + a, w);
+    };
+    if (c.ts == SUB) {
+        for_each_sub(r, c0, c1, [&](int i0, const float (&v)[16]) { put(i0 / SUB, weigh(i0, v)); });
+    } else {
+        for (int a = c0 / c.ts + wave; a * c.ts < c1; a += NWAVE) {
+            double w = 0.0;
+            for (int i0 = a * c.ts; i0 < min(c.V, (a + 1) * c.ts); i0 += SUB) {
+                float v[16];
+                read_sub(r, i0, v);
+                w += weigh(i0, v);
+            }
+            put(a, w);
+        }
+    }
+    if (!last_to_finish(sh, c.h.finished + row * 2 + 1, c.parts)) return;
+    if (t < r.tiles) sh.tile[t] = handed(tile + t);
+    __syncthreads();
+    finish_tiles(sh, r, s.u, answer_of(c, row), kept);
+}
+
+// parts of a row: as many as fill the card with all rows, of whole tiles, not so short that a thread has less than a SUB's 16 logits
+int parts_of(int64_t rows, int V, int ts, int* part_len) {
+    const int64_t most = std::min<int64_t>(MAX_PARTS, std::max<int64_t>(1, 256 / rows));
+    const int64_t unit = std::max<int64_t>(ts, NWAVE * SUB) / ts * ts;
+    *part_len = (int)round_up64(std::max<int64_t>((V + most - 1) / most, 1), unit);
+    return (V + *part_len - 1) / *part_len;
+}
+int tile_of(int V) { return (int)round_up64((V + MAX_TILES - 1) / MAX_TILES, SUB); }
+
+// the arrays of a Handover, in `base` if there is one; -> bytes
+size_t lay_out(Handover* h, unsigned char* base, int64_t rows, int parts, bool listed, bool weighed) {
+    size_t at = 0;
+    const auto place = [&](auto*& p, size_t n) {
+        p = (std::remove_reference_t<decltype(p)>)(base + at);
+        at += (n * sizeof(*p) + 255) / 256 * 256;
+    };
+    const size_t rp = (size_t)rows * parts;
+    place(h->best, rp);
+    place(h->least, rp);
+    place(h->listed, rp);
+    place(h->cut, rows);
+    place(h->first, rows);
+    place(h->finished, 2 * rows);
+    place(h->tile, (size_t)rows * MAX_TILES);
+    place(h->tile_top, (size_t)rows * MAX_TILES);
+    place(h->list, listed || weighed ? rp * PART_CAP : 0);
+    place(h->count, weighed ? rp * BINS : 0);
+    place(h->weight, weighed ? rp * BINS : 0);
+    return at;
 }
 
 }  // namespace
 
+size_t sample_scratch(int64_t rows, int V, bool top_k, bool top_p) {
+    Handover h;
+    int part_len;
+    const int parts = parts_of(rows, V, tile_of(V), &part_len);
+    return lay_out(&h, nullptr, rows, parts, top_k, top_k || top_p);
+}
+
 void launch_sample(const float* logits, int64_t ld, int rows, int V, const float* u, const float* temperature, const int* top_k,
-                   const float* top_p, const float* min_p, int* tokens, float* logprobs, hipStream_t s) {
+                   const float* top_p, const float* min_p, int* tokens, float* logprobs, void* scratch, hipStream_t s) {
     if (rows <= 0) return;
+    Call c;
+    c.logits = logits; c.ld = ld; c.V = V;
+    c.u = u; c.temperature = temperature; c.top_k = top_k; c.top_p = top_p; c.min_p = min_p;
+    c.tokens = tokens; c.logprobs = logprobs;
     // at most MAX_TILES tiles of whole SUBs; histogram weights of as many digits as V of them may add up
-    const int ts = (int)round_up64((V + MAX_TILES - 1) / MAX_TILES, SUB);
-    int fix = 62;
-    while (fix > 0 && ((int64_t)V << fix) > ((int64_t)1 << 62)) --fix;
-    fix = fix < 44 ? fix : 44;
-    hipLaunchKernelGGL(sample_kernel, dim3((unsigned)rows), dim3(NT), 0, s, logits, ld, V, ts, fix, u, temperature, top_k, top_p, min_p,
-                       tokens, logprobs);
+    c.ts = tile_of(V);
+    c.fix = 62;
+    while (c.fix > 0 && ((int64_t)V << c.fix) > ((int64_t)1 << 62)) --c.fix;
+    c.fix = std::min(c.fix, 44);
+    c.parts = parts_of(rows, V, c.ts, &c.part_len);
+    lay_out(&c.h, (unsigned char*)scratch, rows, c.parts, top_k != nullptr, top_k || top_p);
+    const dim3 parts((unsigned)((int64_t)rows * c.parts)), block(NT);
+    hipLaunchKernelGGL(sample_parts_kernel, parts, block, 0, s, c);
+    if (top_k || top_p) hipLaunchKernelGGL(sample_weigh_kernel, parts, block, 0, s, c);
+    hipLaunchKernelGGL(sample_pick_kernel, parts, block, 0, s, c);
+    if (top_k || top_p || min_p) hipLaunchKernelGGL(sample_keep_kernel, parts, block, 0, s, c);
 }
 
 }  // namespace po

@@ -43,14 +43,30 @@ def test_linear_fp8_block_bytes():
 
 def test_sample_refusals():
     f = B.lib().po_op_sample
-    ok = [P, 1000, 4, 1000, P, None, None, None, None, P, None, None]
-    for i, bad, status in ((0, None, 1), (1, 999, 1), (1, -1000, 1), (2, 0, 1), (2, -1, 1), (2, (1 << 24) + 1, 4), (3, 0, 1), (4, None, 1), (9, None, 1)):
+    ok = [P, 1000, 4, 1000, P, None, None, None, None, P, None, P, 1 << 30, None]
+    for i, bad, status in ((0, None, 1), (1, 999, 1), (1, -1000, 1), (2, 0, 1), (2, -1, 1), (2, (1 << 20) + 1, 4), (3, 0, 1), (4, None, 1), (9, None, 1),
+                           (11, None, 1), (11, P + 64, 1), (12, 0, 6), (12, B.po_sample_bytes(4, 1000, False, False) - 1, 6)):
         a = list(ok)
         a[i] = bad
         assert f(*a) == status, (i, bad)
     a = list(ok)
     a[1] = a[3] = (1 << 24) + 1
     assert f(*a) == 4
+    a = list(ok)
+    a[12] = B.po_sample_bytes(4, 1000, False, False)
+    a[6] = P                                                     # a setting that needs more of it
+    assert f(*a) == 6
+
+
+def test_sample_bytes():
+    n = C.c_size_t(7)
+    f = B.lib().po_sample_bytes
+    assert f(4, 1000, 0, 0, None) == 1 and f(0, 1000, 0, 0, C.byref(n)) == 1 and f(4, 0, 0, 0, C.byref(n)) == 1 and f(4, 1 << 25, 0, 0, C.byref(n)) == 4
+    assert n.value == 7
+    for rows in (1, 3, 64, 256, 1000):
+        for V in (1, 1000, 128256, 1 << 24):
+            none, p, k = (B.po_sample_bytes(rows, V, *w) for w in ((False, False), (False, True), (True, True)))
+            assert 0 < none < p < k
 
 
 def rows(*requests):
