@@ -787,9 +787,9 @@ def po_sample_bytes(rows: int, V: int, with_top_k: bool = True, with_top_p: bool
     return n.value
 
 
-def po_op_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
+def po_op_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, scratch=None):
     """float32 logits [rows, V] (rows may have a pitch), u [rows] in [0, 1), settings [rows] each or None -> (int32 tokens [rows],
-    float32 log-probs [rows])"""
+    float32 log-probs [rows]).  scratch: uint8 of at least po_sample_bytes; allocated if None"""
     import torch
     rows, V = logits.shape
     ld = logits.stride(0)
@@ -797,7 +797,7 @@ def po_op_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None
         raise ValueError("logits: a row's values must lie side by side")
     f32 = torch.float32
     stream = _operands(("logits", logits[:1], f32), ("u", u, f32), ("temperature", temperature, f32), ("top_k", top_k, torch.int32),
-                       ("top_p", top_p, f32), ("min_p", min_p, f32))
+                       ("top_p", top_p, f32), ("min_p", min_p, f32), ("scratch", scratch, torch.uint8))
     settings = []
     for name, t in (("u", u), ("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
         if t is not None:
@@ -805,10 +805,10 @@ def po_op_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None
         settings.append(None if t is None else t.data_ptr())
     tokens = torch.empty(rows, dtype=torch.int32, device=logits.device)
     logprobs = torch.empty(rows, dtype=f32, device=logits.device)
-    need = po_sample_bytes(rows, V, top_k is not None, top_p is not None)
-    scratch = torch.empty(need, dtype=torch.uint8, device=logits.device)
-    check(lib().po_op_sample(logits.data_ptr(), ld, rows, V, *settings, tokens.data_ptr(), logprobs.data_ptr(), scratch.data_ptr(), need,
-                             stream))
+    if scratch is None:
+        scratch = torch.empty(po_sample_bytes(rows, V, top_k is not None, top_p is not None), dtype=torch.uint8, device=logits.device)
+    check(lib().po_op_sample(logits.data_ptr(), ld, rows, V, *settings, tokens.data_ptr(), logprobs.data_ptr(), scratch.data_ptr(),
+                             scratch.numel(), stream))
     return tokens, logprobs
 
 

@@ -155,10 +155,12 @@ __device__ void block_scan(Shared& sh, int n, double w) {
     __syncthreads();
 }
 
-// What a search is after: the k-th token of an order (k > 0), or the first at which the running sum reaches `sum`.
+// What a search is after: the k-th token of an order (k > 0), or the first at which the running sum reaches `sum`, which is above 0
+// so that no sum of nothing reaches it.
 struct Goal {
     int k;
     double sum;
+    __device__ __forceinline__ static Goal share(double p, double all) { return {0, fmax(p * all, DBL_MIN)}; }
     __device__ __forceinline__ bool reached(int n, double w) const { return k > 0 ? n >= k : w >= sum; }
 };
 
@@ -175,9 +177,9 @@ __device__ __forceinline__ int first_thread(Shared& sh, bool yes, bool before) {
 
 // The bin of sh.count / sh.weight (bin 0 first, base_n / base_w in front of it) in which the goal is reached, the last one with
 // a token where rounding leaves it a little out of reach; sh.above_n / above_w: what is in front of it; sh.total_w: all of it.
-// ref(b): a bin's reference exponent.
-template <bool weights, typename Ref>
-__device__ int find_bin(Shared& sh, const Goal& goal, int base_n, double base_w, int fix, Ref ref) {
+// goal(sum of the bins): a Goal; ref(b): a bin's reference exponent.
+template <bool weights, typename G, typename Ref>
+__device__ int find_bin(Shared& sh, G goal_of, int base_n, double base_w, int fix, Ref ref) {
     const int t = threadIdx.x;
     int n[PER], sum_n = 0;
     double w[PER], sum_w = 0.0;
@@ -190,6 +192,7 @@ __device__ int find_bin(Shared& sh, const Goal& goal, int base_n, double base_w,
     }
     block_scan(sh, sum_n, sum_w);
     const int all = sh.scan_n[NT - 1];
+    const Goal goal = goal_of(sh.scan_w[NT - 1]);
     int bn = t ? sh.scan_n[t - 1] : 0;
     double bw = base_w + (t ? sh.scan_w[t - 1] : 0.0);
     const bool yes = sh.scan_n[t] == all || goal.reached(base_n + sh.scan_n[t], base_w + sh.scan_w[t]);
@@ -226,39 +229,67 @@ __device__ __forceinline__ void add_to_bin(Shared& sh, int b, double w, int digi
     if (f) atomicAdd(&sh.weight[b], f);
 }
 
-// sh.list[0 .. n) in descending order (n <= CAP; entries that are not 0 differ)
-__device__ void sort_list(Shared& sh, int n) {
+// sh.list[0 .. n) in descending order, n <= E * NT (entries that are not 0 differ).  A bitonic order of m entries, a power of two: E
+// in a thread's registers, entry e * NT + t the e-th of thread t, so that steps within a wavefront are shuffles, steps of NT and more
+// need no exchange, and only those between wavefronts (10 of 55 at 1024 entries) go through LDS.
+template <int E>
+__device__ void sort_registers(Shared& sh, int n, int m) {
     const int t = threadIdx.x;
-    if (n <= 512) {                        // every entry's place is the number of larger ones (and of equal ones in front)
-        unsigned long long e = 0;
-        int place = 0;
-        if (t < n) {
-            e = sh.list[t];
-            for (int i = 0; i < n; ++i) {
-                const unsigned long long o = sh.list[i];
-                place += o > e || (o == e && i < t);
-            }
-        }
-        __syncthreads();
-        if (t < n) sh.list[place] = e;
-        __syncthreads();
-        return;
-    }
-    int m = 1024;
-    while (m < n) m <<= 1;
-    for (int i = n + t; i < m; i += NT) sh.list[i] = 0;
+    unsigned long long x[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = e * NT + t < n ? sh.list[e * NT + t] : 0;
     __syncthreads();
-    for (int size = 2; size <= m; size <<= 1)
-        for (int half = size >> 1; half > 0; half >>= 1) {
-            for (int i = t; i < m / 2; i += NT) {
-                const int lo = 2 * i - (i & (half - 1)), hi = lo + half;
-                const bool down = (lo & size) == 0;
-                const unsigned long long a = sh.list[lo], b = sh.list[hi];
-                if ((a < b) == down) { sh.list[lo] = b; sh.list[hi] = a; }
-            }
+    const auto settle = [&](int e, unsigned long long o, int size, int half) {
+        const int i = e * NT + t;
+        const bool larger = ((i & half) == 0) == ((i & size) == 0);
+        if ((o > x[e]) == larger) x[e] = o;
+    };
+    for (int size = 2; size <= m; size <<= 1) {
+        if constexpr (E > 1) {
+#pragma unroll
+            for (int step = E / 2; step > 0; step >>= 1)
+                if (step * NT < size) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (!(e & step)) {
+                            const unsigned long long lo = x[e], hi = x[e | step];
+                            settle(e, hi, size, step * NT);
+                            settle(e | step, lo, size, step * NT);
+                        }
+                }
+        }
+        for (int half = min(size, NT) >> 1; half >= 64; half >>= 1) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (t < m) sh.list[e * NT + t] = x[e];
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (t < m) settle(e, sh.list[e * NT + (t ^ half)], size, half);
             __syncthreads();
         }
+        if (t < m) {
+#pragma unroll
+            for (int half = 32; half > 0; half >>= 1)
+                if (half < size) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) settle(e, __shfl_xor(x[e], half), size, half);
+                }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (e * NT + t < n) sh.list[e * NT + t] = x[e];
+    __syncthreads();
 }
+__device__ void sort_list(Shared& sh, int n) {
+    int m = 64;
+    while (m < n) m <<= 1;
+    if (m <= NT) sort_registers<1>(sh, n, m);
+    else if (m == 2 * NT) sort_registers<2>(sh, n, m);
+    else sort_registers<4>(sh, n, m);
+}
+static_assert(CAP == 4 * NT, "what sort_list orders");
 
 // The token of the sorted sh.list[0 .. n) at which the goal is reached (base_n / base_w in front of the first; the last one where
 // rounding leaves it out of reach): sh.cut, and sh.cut_sum, the running sum up to it.
@@ -304,7 +335,7 @@ __device__ void find_in_row(Shared& sh, const Row& r, const Goal& goal, int fix)
                 add_to_bin(sh, (1 << bits) - 1 - (int)((key >> shift) & ((1u << bits) - 1)), r.weight(l, sh.table), fix - ref);
         });
         __syncthreads();
-        const int b = find_bin<true>(sh, goal, base_n, base_w, fix, [&](int) { return ref; });
+        const int b = find_bin<true>(sh, [&](double) { return goal; }, base_n, base_w, fix, [&](int) { return ref; });
         prefix |= (uint32_t)((1 << bits) - 1 - b) << shift;
         base_n = sh.above_n;
         base_w = sh.above_w;
@@ -640,9 +671,28 @@ __global__ void __launch_bounds__(NT) sample_parts_kernel(const Call c) {
         if (t == 0) c.h.least[at] = best ? ~(uint32_t)l : 0xffffffffu;
     }
     if (s.how != COUNT) return;
-    const int b = find_bin<false>(sh, Goal{s.k, 0.0}, 0, 0.0, 0, [](int) { return 0; }), n = sh.above_n + sh.count[b];
+    // the bin of the part's k-th token, and, where the part's first up to that bin are too many for its list (all but a few logits
+    // close together), the same by the next 12 bits of the key
+    const auto kth = [&](int in_front) {
+        return find_bin<false>(sh, [&](double) { return Goal{s.k, 0.0}; }, in_front, 0.0, 0, [](int) { return 0; });
+    };
+    const uint32_t high = BINS - 1 - kth(0);
+    uint32_t lowest = high << 20;
+    int in_front = sh.above_n, n = in_front + sh.count[BINS - 1 - high];
+    __syncthreads();
+    if (n > PART_CAP) {
+        clear_bins(sh);
+        for_each(r, c0, c1, [&](float l, int) {
+            const uint32_t key = key_of(l);
+            if (key && key >> 20 == high) atomicAdd(&sh.count[BINS - 1 - (key >> 8 & (BINS - 1))], 1);
+        });
+        __syncthreads();
+        const int b = kth(in_front);
+        lowest |= (uint32_t)(BINS - 1 - b) << 8;
+        n = sh.above_n + sh.count[b];
+        __syncthreads();
+    }
     if (n <= PART_CAP && best) {
-        const uint32_t lowest = (uint32_t)(BINS - 1 - b) << 20;
         if (t == 0) sh.n_list = 0;
         __syncthreads();
         for_each(r, c0, c1, [&](float l, int i) {
@@ -784,7 +834,7 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(const Call c) {
             clear_bins(sh);
             listed([&](unsigned long long x) { atomicAdd(&sh.count[(top - (uint32_t)(x >> 32)) >> shift], 1); });
             __syncthreads();
-            const int b = find_bin<false>(sh, Goal{s.k, 0.0}, 0, 0.0, 0, [](int) { return 0; }), n = sh.above_n + sh.count[b];
+            const int b = find_bin<false>(sh, [&](double) { return Goal{s.k, 0.0}; }, 0, 0.0, 0, [](int) { return 0; }), n = sh.above_n + sh.count[b];
             if (n <= CAP) {
                 if (t == 0) sh.n_list = 0;
                 __syncthreads();
@@ -802,7 +852,7 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(const Call c) {
         const double sum = sh.cut_sum;
         __syncthreads();
         if (s.by_p) {
-            find_in_row(sh, r, Goal{0, fmax((double)s.p * sum, DBL_MIN)}, c.fix);
+            find_in_row(sh, r, Goal::share(s.p, sum), c.fix);
             cut = sh.cut > cut ? sh.cut : cut;
         }
         leave(cut);
@@ -831,7 +881,7 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(const Call c) {
     if (s.by_k) {
         // (more than K_MAX tokens) one workgroup; -> whether the bins still are there
         const auto search = [&](const Goal& goal) {
-            const int b = find_bin<true>(sh, goal, 0, 0.0, c.fix, ref), n = sh.count[b], base_n = sh.above_n;
+            const int b = find_bin<true>(sh, [&](double) { return goal; }, 0, 0.0, c.fix, ref), n = sh.count[b], base_n = sh.above_n;
             const double base_w = sh.above_w;
             if (n > CAP) {
                 find_in_row(sh, r, goal, c.fix);
@@ -853,20 +903,18 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(const Call c) {
         __syncthreads();
         if (s.by_p) {
             if (!still) fill_bins<false>(sh, r, st, 0, c.V, c.fix);
-            search(Goal{0, fmax((double)s.p * sum, DBL_MIN)});
+            search(Goal::share(s.p, sum));
             cut = sh.cut > cut ? sh.cut : cut;
         }
         leave(cut);
         return;
     }
-    // top_p alone: every part's workgroup finds the bin in which it ends (goal above 0, so that no sum of nothing reaches it) and lists
-    // its part's tokens of that bin, or, if they are few, of all up to it; the last one takes them together
-    find_bin<true>(sh, Goal{1, 0.0}, 0, 0.0, c.fix, ref);
-    const double sum = sh.total_w;
-    __syncthreads();
-    const Goal goal = {0, fmax((double)s.p * sum, DBL_MIN)};
-    const int b = find_bin<true>(sh, goal, 0, 0.0, c.fix, ref), n_bin = sh.count[b], above_n = sh.above_n;
-    const double above_w = sh.above_w;
+    // top_p alone: every part's workgroup finds the bin in which it ends and lists its part's tokens of that bin, or, if they are
+    // few, of all up to it; the last one takes them together
+    const int b = find_bin<true>(sh, [&](double all) { return Goal::share(s.p, all); }, 0, 0.0, c.fix, ref);
+    const int n_bin = sh.count[b], above_n = sh.above_n;
+    const double above_w = sh.above_w, sum = sh.total_w;
+    const Goal goal = Goal::share(s.p, sum);
     __syncthreads();
     if (n_bin > PART_CAP) {
         if (part != 0) return;
@@ -874,7 +922,7 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(const Call c) {
         leave(sh.cut);
         return;
     }
-    const bool all = above_n + n_bin <= 512;
+    const bool all = above_n + n_bin <= NT;
     const int64_t at = (int64_t)row * c.parts + part;
     const int c0 = part * c.part_len;
     if (t == 0) sh.n_list = 0;
