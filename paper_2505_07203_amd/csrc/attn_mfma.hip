@@ -934,11 +934,14 @@ __global__ void __launch_bounds__(256) attn_fwd64_kernel(const bf16_t* q, const 
         if (piece == sp.n - 1) {
             // one source of keys: n_keys of them, of which a lane's rows see `see` and some row of the wavefront see_max
             auto keys = [&](const bf16_t* kb, const bf16_t* vb, int64_t ld, int n_keys, int see0, int see1, int see_max) {
-                for (int key0 = 0; key0 < see_max; key0 += 32) {
-                    bf16x8 kf[KS], vf[2][HT];
+                bf16x8 kf[KS], vf[2][HT];
+                auto load_k = [&](int key0) {
                     const bf16_t* const kr = kb + (int64_t)min(key0 + pk, n_keys - 1) * (Hkv * HD) + lhi * 8;
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) kf[ks] = __builtin_bit_cast(bf16x8, *(const uint4*)(kr + ks * 16));
+                };
+                if (see_max > 0) load_k(0);
+                for (int key0 = 0; key0 < see_max; key0 += 32) {
 #pragma unroll
                     for (int j2 = 0; j2 < 2; ++j2) load_vt_eight<HT>(vb, ld, key0 + 16 * j2 + 8 * lhi, n_keys, vf[j2]);
                     f32x16 S[2];
@@ -950,6 +953,7 @@ __global__ void __launch_bounds__(256) attn_fwd64_kernel(const bf16_t* q, const 
                     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
                         for (int qt = 0; qt < 2; ++qt) S[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[qt][ks], S[qt], 0, 0, 0);
+                    if (key0 + 32 < see_max) load_k(key0 + 32);        // (on their way through the softmax)
                     float top[2];
                     bool grew = false;
 #pragma unroll

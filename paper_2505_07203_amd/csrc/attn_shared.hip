@@ -11,6 +11,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace po {
 
@@ -101,69 +102,151 @@ __device__ __forceinline__ void store4(bf16_t* o, float a, float b, float c, flo
     *(uint2*)o = w;
 }
 
-// One workgroup: 128 rows of one request and KV head, 32 a wavefront, all their keys.  K and V^T come from memory to registers in
-// blocks of 32 keys; what several wavefronts read they find in the caches.
+// 64 keys of K (rows as they are) or V^T (128 bytes of each row) of one KV head in LDS, 16-byte segments swizzled with the row; the
+// loads (1 KB each) by whole cache lines past the registers, the swizzle on the global side.  Loads j0 .. j0 + N.
+// n: keys of it that there are (<= 0: nothing is read, though as many loads are on their way).  K rows from n on read as 0; V^T
+// columns from there on hold anything, the last row's up to the eight that hold the last key.
+template <int HD, int N>
+__device__ __forceinline__ void dma_k_tile(unsigned char* lds, const bf16_t* k, int64_t krs, int n, int lane, int j0) {
+    constexpr int LPR = HD / 8;                                 // lanes (16 bytes each) of a row
+    n = min(n, 64);
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc((void*)k, 0, n > 0 ? (int)((uint32_t)(n - 1) * (uint32_t)(krs * 2) + HD * 2) : 0, 0x00020000);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int row = (j0 + j) * (64 / LPR) + lane / LPR, seg = lane % LPR;
+        const int sw = LPR == 16 ? seg ^ (row & 15) : seg ^ swz8(row);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (j0 + j) * 1024), 16,
+                                                 (uint32_t)row * (uint32_t)(krs * 2) + (uint32_t)(sw << 4), 0, 0, 0);
+    }
+}
+template <int HD, int N>
+__device__ __forceinline__ void dma_vt_tile(unsigned char* lds, const bf16_t* v, int64_t ld, int n, int lane, int j0) {
+    const uint32_t ld2 = (uint32_t)(ld * 2);
+    const uint32_t bytes = n > 0 ? (HD - 1) * ld2 + (uint32_t)min(64, (n + 7) & ~7) * 2 : 0u;
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)v, 0, (int)bytes, 0x00020000);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int row = (j0 + j) * 8 + (lane >> 3);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (j0 + j) * 1024), 16,
+                                                 (uint32_t)row * ld2 + (uint32_t)(((lane & 7) ^ swz8(row)) << 4), 0, 0, 0);
+    }
+}
+// columns from n on (of the eight keys 16 j + 8 lhi ..) as 0, whatever they hold: a probability of 0 times a NaN would be one
+__device__ __forceinline__ void clear_columns(uint4& v, int n) {
+    v.x &= n >= 2 ? 0xffffffffu : n == 1 ? 0xffffu : 0u;
+    v.y &= n >= 4 ? 0xffffffffu : n == 3 ? 0xffffu : 0u;
+    v.z &= n >= 6 ? 0xffffffffu : n == 5 ? 0xffffu : 0u;
+    v.w &= n >= 8 ? 0xffffffffu : n == 7 ? 0xffffu : 0u;
+}
+
+// One workgroup: 128 rows of one request and KV head, 32 a wavefront, all their keys, 64 at a time in LDS for all four; the next 64
+// are on their way while these are worked on, and one barrier a step says both that they are there and that the last ones are
+// out of use.
 template <int HD>
-__global__ void __launch_bounds__(256) attn_shared_rows_kernel(const SharedParams p, const SharedTable tab) {
+__global__ void __launch_bounds__(256, 2) attn_shared_rows_kernel(const SharedParams p, const SharedTable tab) {
     constexpr int KS = HD / 16, HT = HD / 32;
+    constexpr int UNIT = 64 * HD * 2, N_DMA = UNIT / 1024 / 4;  // bytes of 64 keys of K or V^T; loads of a wavefront
+    __shared__ __attribute__((aligned(16))) unsigned char smem[2][2][UNIT];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l31 = lane & 31, lhi = lane >> 5;
     const int kvh = (int)(blockIdx.x % (unsigned)p.Hkv), item = (int)(blockIdx.x / (unsigned)p.Hkv), group = p.Hq / p.Hkv;
     const int req = __builtin_amdgcn_readfirstlane(shared_request(tab, item));
     const SharedSeq sq = tab.seq[req];
-    const int row0 = ((item - tab.item0[req]) * 4 + wave) * 32, n_rows = sq.q_len * group;      // (position, head) order
-    if (row0 >= n_rows) return;
+    const int n_rows = sq.q_len * group, wg0 = (item - tab.item0[req]) * 128, row0 = wg0 + wave * 32;      // (position, head) order
     const int vr = min(row0 + l31, n_rows - 1), pos = vr / group, head = kvh * group + vr - pos * group;
     const bool valid = row0 + l31 < n_rows;
     const int64_t orow = ((int64_t)(sq.q_row + pos) * p.Hq + head) * HD;
     const int hidden = sq.kv_len - sq.q_len + 1;               // position i of the request sees i + hidden own keys (may be below 0)
-    const int see_max = max(0, hidden + min(row0 + 31, n_rows - 1) / group), see_min = hidden + row0 / group;
+    const int see_max = row0 < n_rows ? max(0, hidden + min(row0 + 31, n_rows - 1) / group) : 0, see_min = hidden + min(row0, n_rows - 1) / group;
+    const int wg_max = max(0, hidden + min(wg0 + 127, n_rows - 1) / group);
 
     Rows<HD> st;
     st.start((const bf16_t*)p.q + orow + lhi * 8, valid);
-    const int pk = (l31 & 0x13) | ((l31 & 4) << 1) | ((l31 & 8) >> 1);       // MFMA row i holds key pi(i): bits 2, 3 swapped
     const int64_t krs = (int64_t)p.Hkv * HD;
-    const bf16_t* const ko = (const bf16_t*)p.k + (int64_t)sq.kv_row * krs + kvh * HD + lhi * 8;
-    const bf16_t* const kp = (const bf16_t*)p.k2 + kvh * HD + lhi * 8;
-    const bf16_t* const vo = (const bf16_t*)p.v + ((int64_t)kvh * HD + l31) * p.ldv + sq.kv_row;
-    const bf16_t* const vp = (const bf16_t*)p.v2 + ((int64_t)kvh * HD + l31) * p.ldv2;
-    const int nb2 = (p.n2 + 31) / 32, nb = nb2 + (see_max + 31) / 32;
-    // K rows of block b; past the last key the last one (those scores are masked)
-    auto load_k = [&](int b, bf16x8 (&kf)[KS]) {
-        const bf16_t* const r = (b < nb2 ? kp : ko) + (int64_t)min((b < nb2 ? b : b - nb2) * 32 + pk, (b < nb2 ? p.n2 : sq.kv_len) - 1) * krs;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) kf[ks] = __builtin_bit_cast(bf16x8, *(const uint4*)(r + ks * 16));
+    const bf16_t* const ko = (const bf16_t*)p.k + (int64_t)sq.kv_row * krs + kvh * HD;
+    const bf16_t* const kp = (const bf16_t*)p.k2 + kvh * HD;
+    const bf16_t* const vo = (const bf16_t*)p.v + (int64_t)kvh * HD * p.ldv + sq.kv_row;
+    const bf16_t* const vp = (const bf16_t*)p.v2 + (int64_t)kvh * HD * p.ldv2;
+    const int nb2 = (p.n2 + 63) / 64, nb = nb2 + (wg_max + 63) / 64;
+    auto dma = [&](int b) {
+        if (b >= nb) return;
+        const bool own = b >= nb2;
+        const int key0 = (own ? b - nb2 : b) * 64, n = (own ? sq.kv_len : p.n2) - key0;
+        dma_k_tile<HD, N_DMA>(smem[b & 1][0], (own ? ko : kp) + key0 * krs, krs, n, lane, wave * N_DMA);
+        dma_vt_tile<HD, N_DMA>(smem[b & 1][1], (own ? vo : vp) + key0, own ? p.ldv : p.ldv2, n, lane, wave * N_DMA);
     };
-    bf16x8 kf[KS], kn[KS], vf[2][HT], pf[2];
-    if (nb > 0) load_k(0, kf);
+    const int pk = (l31 & 0x13) | ((l31 & 4) << 1) | ((l31 & 8) >> 1);       // MFMA row i holds key pi(i): bits 2, 3 swapped
+    const int k_sw = HD == 128 ? (pk & 15) : swz8(pk), v_sw = swz8(l31);
+    dma(0);
+#pragma unroll 1
     for (int b = 0; b < nb; ++b) {
         const bool own = b >= nb2;
-        const int key0 = (own ? b - nb2 : b) * 32;
+        const int key0 = (own ? b - nb2 : b) * 64;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        dma(b + 1);
+        if (key0 >= (own ? see_max : row0 < n_rows ? p.n2 : 0)) continue;      // (wavefront-uniform)
+        const unsigned char *const sk = smem[b & 1][0], *const sv = smem[b & 1][1];
+        const int n_v = (own ? sq.kv_len : p.n2) - key0;       // V^T columns that are keys
+        f32x16 s[2];
+        bf16x8 pf[4];
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-            load_vt_eight<HT>(own ? vo : vp, own ? p.ldv : p.ldv2, key0 + 16 * j + 8 * lhi, own ? sq.kv_len : p.n2, vf[j]);
-        if (b + 1 < nb) load_k(b + 1, kn);
-        f32x16 s[1] = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+        for (int a = 0; a < 2; ++a)
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], st.qf[ks], s[0], 0, 0, 0);
-        st.template softmax<1>(s, pf, key0 + 32 > (own ? see_min : p.n2), (own ? pos + hidden : p.n2) - key0, lhi, p.sc);
+            for (int r = 0; r < 16; ++r) s[a][r] = 0.f;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-            for (int ht = 0; ht < HT; ++ht) st.acc[ht] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j][ht], pf[j], st.acc[ht], 0, 0, 0);
+            for (int a = 0; a < 2; ++a) {
+                const bf16x8 kf = *(const bf16x8*)(sk + (a * 32 + pk) * (HD * 2) + (((ks * 2 + lhi) ^ k_sw) << 4));
+                s[a] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, st.qf[ks], s[a], 0, 0, 0);
+            }
+        uint4 v[2][HT];
+        const auto read_v = [&](int j0) {                       // V^T of 32 keys
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) kf[ks] = kn[ks];
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int ht = 0; ht < HT; ++ht) v[j][ht] = *(const uint4*)(sv + (ht * 32 + l31) * 128 + ((((j0 + j) * 2 + lhi) ^ v_sw) << 4));
+            if (n_v < 64) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int ht = 0; ht < HT; ++ht) clear_columns(v[j][ht], n_v - (16 * (j0 + j) + 8 * lhi));
+            }
+        };
+        read_v(0);
+        st.template softmax<2>(s, pf, key0 + 64 > (own ? see_min : p.n2), (own ? pos + hidden : p.n2) - key0, lhi, p.sc);
+#pragma unroll
+        for (int j0 = 0; j0 < 4; j0 += 2) {
+            if (j0) read_v(j0);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int ht = 0; ht < HT; ++ht)
+                    st.acc[ht] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[j][ht]), pf[j0 + j], st.acc[ht], 0, 0, 0);
+        }
     }
-    const float l = other_half_sum(st.l);
-    if (!valid) return;
-    const float inv = l > 0.f ? 1.0f / l : 0.f;
+    // through LDS, so that whole rows are written side by side (16 bytes of 32 rows at a time took 6.5 us for 16 MB more)
+    constexpr int PITCH = HD * 2 + 16, LPR = HD / 8;           // lanes (16 bytes each) of a row
+    const float l = other_half_sum(st.l), inv = l > 0.f ? 1.0f / l : 0.f;
+    __syncthreads();
+    unsigned char* const so = &smem[0][0][0] + wave * 32 * PITCH;
 #pragma unroll
     for (int ht = 0; ht < HT; ++ht)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-            store4((bf16_t*)p.o + orow + ht * 32 + 8 * g + 4 * lhi, st.acc[ht][4 * g], st.acc[ht][4 * g + 1], st.acc[ht][4 * g + 2],
+            store4((bf16_t*)(so + l31 * PITCH) + ht * 32 + 8 * g + 4 * lhi, st.acc[ht][4 * g], st.acc[ht][4 * g + 1], st.acc[ht][4 * g + 2],
                    st.acc[ht][4 * g + 3], inv);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // (a wavefront's own rows: no barrier)
+#pragma unroll
+    for (int i = 0; i < 32 * LPR / 64; ++i) {
+        const int row = i * (64 / LPR) + lane / LPR;
+        const uint4 x = *(const uint4*)(so + row * PITCH + lane % LPR * 16);
+        const int64_t at = __shfl(orow, row);
+        if (row0 + row < n_rows) *(uint4*)((bf16_t*)p.o + at + lane % LPR * 8) = x;
+    }
 }
 
 // How a launch of few rows is divided.  Partial results: opart [piece][row of the table][head][HD], mlpart [..][2] (maximum in
@@ -182,12 +265,12 @@ struct Parts {
 // WHOLE: a workgroup is 32 rows of one request, all keys they see; result in o.
 // PARTS: a workgroup is a piece of the prefix, which all requests share, with 32 RT rows of any requests; or a piece of a request's own keys
 // with 32 of its rows.  Partial results.
-enum { WHOLE, PARTS };
+// FINISH: a workgroup is 32 rows of one request, the own keys they see, joined with the prefix's np pieces of these rows; result in o.
+enum { WHOLE, PARTS, FINISH };
 template <int HD, int NW, int RT, int MODE>
 __global__ void __launch_bounds__(NW * 64, 1) attn_shared_tokens_kernel(const SharedParams p, const Parts parts, const SharedTable tab) {
     constexpr int KS = HD / 16, HT = HD / 32;
     constexpr int UNIT = 64 * HD * 2, N_DMA = UNIT / 1024;      // bytes of 64 keys of K or V^T; loads of a wavefront
-    constexpr int LPR = HD / 8;                                 // lanes (16 bytes each) of a K row
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -223,7 +306,7 @@ __global__ void __launch_bounds__(NW * 64, 1) attn_shared_tokens_kernel(const Sh
     const int a0 = of_prefix ? piece * parts.per : 0;
     const int a1 = MODE == WHOLE ? p.n2 : of_prefix ? min(a0 + parts.per, p.n2) : 0;
     const int b0 = MODE == PARTS && !of_prefix ? piece * parts.own_per : 0;
-    const int b1 = MODE == WHOLE ? see_max : of_prefix ? 0 : min(b0 + parts.own_per, see_max);
+    const int b1 = MODE != PARTS ? see_max : of_prefix ? 0 : min(b0 + parts.own_per, see_max);
     const int nb2 = max(a1 - a0 + 63, 0) / 64, nb = nb2 + max(b1 - b0 + 63, 0) / 64;
 
     Rows<HD> st[RT];
@@ -245,39 +328,19 @@ __global__ void __launch_bounds__(NW * 64, 1) attn_shared_tokens_kernel(const Sh
     unsigned char* const sk = smem + wave * (2 * UNIT);
     unsigned char* const sv = sk + UNIT;
     auto first_key = [&](int b) { return b < nb2 ? a0 + b * 64 : b0 + (b - nb2) * 64; };
-    // Block b's K, and V^T, into this wavefront's LDS, 16-byte segments swizzled with the row on the global side; from block nb on nothing
-    // (an empty descriptor: the number of loads in flight stays known).  K rows past the last key read as 0; V^T columns past it
-    // hold anything, the last row's up to the eight that hold the last key.
+    // Block b's K, and V^T, into this wavefront's LDS; from block nb on nothing (the number of loads in flight stays known).
     auto dma_k = [&](int b) {
         const int key0 = first_key(b), end = b < nb2 ? p.n2 : sq.kv_len;
-        const int n = b < nb ? min(64, end - key0) : 0;
-        const bf16_t* const base = (b < nb2 ? kp : ko) + (b < nb ? key0 * krs : 0);
-        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, n > 0 ? (int)((uint32_t)(n - 1) * (uint32_t)(krs * 2) + HD * 2) : 0, 0x00020000);
-#pragma unroll
-        for (int j = 0; j < N_DMA; ++j) {
-            const int row = j * (64 / LPR) + lane / LPR, seg = lane % LPR;
-            const int sw = LPR == 16 ? seg ^ (row & 15) : seg ^ swz8(row);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(sk + j * 1024), 16,
-                                                     (uint32_t)row * (uint32_t)(krs * 2) + (uint32_t)(sw << 4), 0, 0, 0);
-        }
+        dma_k_tile<HD, N_DMA>(sk, (b < nb2 ? kp : ko) + (b < nb ? key0 * krs : 0), krs, b < nb ? end - key0 : 0, lane, 0);
     };
     auto dma_v = [&](int b) {
         const int key0 = first_key(b), end = b < nb2 ? p.n2 : sq.kv_len;
-        const uint32_t ld2 = (uint32_t)((b < nb2 ? p.ldv2 : p.ldv) * 2);
-        const bf16_t* const base = (b < nb2 ? vp : vo) + (b < nb ? key0 : 0);
-        const uint32_t bytes = b < nb ? (HD - 1) * ld2 + (uint32_t)min(64, (end - key0 + 7) & ~7) * 2 : 0u;
-        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
-#pragma unroll
-        for (int j = 0; j < N_DMA; ++j) {
-            const int row = j * 8 + (lane >> 3);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(sv + j * 1024), 16,
-                                                     (uint32_t)row * ld2 + (uint32_t)(((lane & 7) ^ swz8(row)) << 4), 0, 0, 0);
-        }
+        dma_vt_tile<HD, N_DMA>(sv, (b < nb2 ? vp : vo) + (b < nb ? key0 : 0), b < nb2 ? p.ldv2 : p.ldv, b < nb ? end - key0 : 0, lane, 0);
     };
     // fragments: K row pi(i) of a 32-key half (bits 2, 3 swapped: the eight keys a lane feeds to an MFMA are then side by side in
     // V^T), V^T row i of a 32-row tile
     const int pk = (l31 & 0x13) | ((l31 & 4) << 1) | ((l31 & 8) >> 1);
-    const int k_sw = LPR == 16 ? (pk & 15) : swz8(pk), v_sw = swz8(l31);
+    const int k_sw = HD == 128 ? (pk & 15) : swz8(pk), v_sw = swz8(l31);
     int b = wave;
     dma_k(b);
     dma_v(b);
@@ -320,13 +383,7 @@ __global__ void __launch_bounds__(NW * 64, 1) attn_shared_tokens_kernel(const Sh
 #pragma unroll
                 for (int ht = 0; ht < HT; ++ht) {
                     uint4 v = *(const uint4*)(sv + (ht * 32 + l31) * 128 + (((j * 2 + lhi) ^ v_sw) << 4));
-                    if (n_v < 64) {                                               // columns past the last key count as 0, whatever they hold
-                        const int n = n_v - (16 * j + 8 * lhi);
-                        v.x &= n >= 2 ? 0xffffffffu : n == 1 ? 0xffffu : 0u;
-                        v.y &= n >= 4 ? 0xffffffffu : n == 3 ? 0xffffu : 0u;
-                        v.z &= n >= 6 ? 0xffffffffu : n == 5 ? 0xffffu : 0u;
-                        v.w &= n >= 8 ? 0xffffffffu : n == 7 ? 0xffffu : 0u;
-                    }
+                    if (n_v < 64) clear_columns(v, n_v - (16 * j + 8 * lhi));
                     st[rt].acc[ht] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pf[j], st[rt].acc[ht], 0, 0, 0);
                 }
         }
@@ -376,6 +433,23 @@ __global__ void __launch_bounds__(NW * 64, 1) attn_shared_tokens_kernel(const Sh
                 *(float4*)(parts.opart + slot * HD + d) = y;
                 if (d == 0) *(float2*)(parts.mlpart + slot * 2) = make_float2(top, lt);
                 continue;
+            }
+            if (MODE == FINISH) {
+                const float* const ml = parts.mlpart + rh * 2;
+                float all = top;
+#pragma unroll 8
+                for (int e = 0; e < parts.np; ++e) all = fmaxf(all, ml[e * plane * 2]);
+                const float f = __builtin_amdgcn_exp2f(top - all);
+                lt *= f;
+                y.x *= f; y.y *= f; y.z *= f; y.w *= f;
+#pragma unroll 8
+                for (int e = 0; e < parts.np; ++e) {
+                    const float2 m2 = *(const float2*)(ml + e * plane * 2);
+                    const float4 v = *(const float4*)(parts.opart + (e * plane + rh) * HD + d);
+                    const float w = __builtin_amdgcn_exp2f(m2.x - all);
+                    lt += w * m2.y;
+                    y.x += w * v.x; y.y += w * v.y; y.z += w * v.z; y.w += w * v.w;
+                }
             }
             store4((bf16_t*)p.o + ((int64_t)(sq.q_row + jp) * p.Hq + jh) * HD + d, y.x, y.y, y.z, y.w, lt > 0.f ? 1.0f / lt : 0.f);
         }
@@ -430,7 +504,8 @@ __global__ void __launch_bounds__(256) attn_shared_join_kernel(const SharedParam
 //   TILES        256 rows of any requests a workgroup of attn_mfma.hip's tile kernel, the prefix in np pieces; joined when np > 1
 //   SPLIT        the prefix in np pieces with 32 rt rows of any requests, own keys in pieces of own_per, joined
 //   TILES_SPLIT  the prefix by the tile kernel, own keys in pieces, joined
-enum Mode { TOKENS, ROWS, TILES, SPLIT, TILES_SPLIT };
+//   TILES_FINISH the prefix by the tile kernel, own keys whole, which joins both
+enum Mode { TOKENS, ROWS, TILES, SPLIT, TILES_SPLIT, TILES_FINISH };
 struct Plan {
     Mode mode;
     int np, per, own_per, rt, slots;     // slots: partial results of a row at most
@@ -438,64 +513,79 @@ struct Plan {
 
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// The one expected to take the least time (microseconds) with the scratch there is.
+// The one expected to take the least time (microseconds) with the scratch there is.  Every form's time is what one workgroup takes
+// times how often the card is filled with them, and no less than its bytes at what memory gives.
 Plan plan(const SharedTable& t, int Hq, int Hkv, int hd, int n2, size_t scratch_bytes) {
     const int group = Hq / Hkv, rows = t.row0[t.n], tiles2 = n2 / 64;
     const int64_t vr = (int64_t)rows * group;
-    const double row_us = (double)rows * Hq * (hd + 2) * 4.0 * 2.0 / 4.5e6;          // a slot of every row, written and read
-    const double row_bytes = (double)rows * Hq * (hd + 2) * 4.0, hd_part = hd / 128.0;
+    const double row_bytes = (double)rows * Hq * (hd + 2) * 4.0, slot_us = row_bytes * 2.0 / 6.0e6;      // a slot of every row, written and read
+    const double narrow = hd / 128.0, key_bytes = Hkv * hd * 4.0;
     int own_max = 0;
     int64_t own_sum = 0, tiles32 = 0, tiles128 = 0;
+    double seen = 0.0;                                        // own keys of all rows
     for (int i = 0; i < t.n; ++i) {
         const SharedSeq& q = t.seq[i];
         own_max = std::max(own_max, q.kv_len);
         own_sum += q.kv_len;
+        seen += q.q_len * std::max(0.0, q.kv_len - 0.5 * q.q_len);
         tiles32 += ceil_div((int64_t)q.q_len * group, 32);
         tiles128 += ceil_div((int64_t)q.q_len * group, 128);
     }
+    seen /= rows;
     Plan best{TOKENS, 0, 0, 0, 1, 0};
-    // a wavefront's block of 64 keys costs 1.9 us alone on its compute unit, 2.4 with another workgroup beside it
-    const int64_t wg32 = tiles32 * Hkv;
-    const double keys_mean = n2 + (double)own_sum / t.n, keys_max = n2 + own_max;
-    double t_best = wg32 <= 256 ? 6.0 + 1.9 * hd_part * std::ceil(keys_max / 256)
-                                : 6.0 + 2.4 * hd_part * std::max(std::ceil(keys_max / 128), wg32 / 512.0 * std::ceil(keys_mean / 128));
+    // 32 rows a workgroup; two wavefronts, and two workgroups a compute unit, where there are more than 256.  A wavefront's block of
+    // 64 keys: 1.9 us alone on its compute unit, 2.2 to 2.4 with another workgroup beside it
+    const auto tokens_us = [&](double wgs, double most, double mean, double keys_read) {
+        const double us = wgs <= 256 ? 1.9 * (std::ceil(most / 256) + 1.0)
+                                     : std::max(2.4 * (std::ceil(most / 128) + 1.0), 2.2 * wgs / 512.0 * (mean / 128 + 2.0));
+        return std::max(us * narrow, keys_read * key_bytes / 4.2e6);
+    };
+    double t_best = 5.0 + tokens_us((double)tiles32 * Hkv, n2 + own_max, n2 + seen, (double)n2 + own_sum);
     const auto take = [&](const Plan& p, double us) {
         if (us < t_best && p.slots * row_bytes <= (double)scratch_bytes) { best = p; t_best = us; }
     };
-    // 32 keys of a wavefront: 1.4 us, 1.8 with two workgroups a compute unit
-    const int64_t wg128 = tiles128 * Hkv;
-    take({ROWS, 0, 0, 0, 1, 0}, 5.0 + hd_part * (wg128 <= 256 ? 1.4 * std::ceil(keys_max / 32) : 1.8 * std::max(std::ceil(keys_max / 32), wg128 / 256.0 * keys_mean / 32)));
+    // 128 rows a workgroup: 64 keys 1.3 us alone, 0.85 a workgroup with two on a compute unit, 6 more for its beginning and end
+    const double wg128 = (double)tiles128 * Hkv, c1 = hd == 128 ? 1.3 : 0.9, c2 = hd == 128 ? 0.85 : 0.65;
+    take({ROWS, 0, 0, 0, 1, 0}, 5.0 + std::max((wg128 <= 256 ? c1 : 2.0 * c2) * (std::ceil((n2 + own_max) / 64.0) + 2.0),
+                                              std::max(wg128 / 256.0 * c2 * ((n2 + seen) / 64.0 + 6.0), ((double)n2 + own_sum) * key_bytes / 3.6e6)));
     if (n2 == 0 && own_max == 0) return best;
     // own keys by pieces, and the join
     const int own_per = (int)std::min<int64_t>(2048, std::max<int64_t>(512, (own_sum * Hkv / 256 + 255) / 256 * 256));
     const int own_slots = ceil_div(own_max, own_per);
     int64_t own_wgs = 0;
     for (int i = 0; i < t.n; ++i) own_wgs += (int64_t)ceil_div((int64_t)t.seq[i].q_len * group, 32) * ceil_div(t.seq[i].kv_len, own_per) * Hkv;
-    const double own_blocks = std::ceil(std::min<double>(own_per, own_max) / 256);
-    const double own_us = own_wgs ? hd_part * 1.9 * std::max(own_blocks, own_wgs / 256.0 * std::max(1.0, (double)own_sum / t.n / 256 / std::max(1, own_slots))) : 0.0;
     // the prefix by the tile kernel: a tile of 64 keys 1.35 us, 5 of them for its beginning and end
     if (hd == 128 && tiles2 > 0) {
         const int64_t wgs = (vr + 255) / 256 * Hkv;
-        // own keys in the tile: a wavefront goes through those of all requests that its 64 rows meet, 32 keys a microsecond
-        const double meets = std::min<double>(t.n, std::ceil(64.0 / group / ((double)rows / t.n)) + 1);
-        const double in_tile = meets * std::ceil((double)own_sum / t.n / 32) * 0.8;
+        // own keys in the tile: a wavefront goes through those of all requests that its 64 rows meet, 32 keys in 3 us
+        const double meets = std::min<double>(t.n, std::ceil(64.0 / group / ((double)rows / t.n)) + 0.5);
+        const double in_tile = own_sum ? 3.0 * meets * std::ceil(seen / 32) : 0.0;
+        const double finish_rows = std::ceil((double)vr / (double)tiles32 / 4.0);        // (128 threads: four rows at once)
         for (int np = 1; np <= std::min(tiles2, 64); ++np) {
             const int per = ceil_div(tiles2, np);
             if (ceil_div(tiles2, per) != np || (uint64_t)per * 64 * (uint64_t)Hkv * 256 >= (1ull << 32)) continue;
             const double us = 6.0 + ceil_div(wgs * np, 256) * (per + 5) * 1.35;
-            take({TILES, np, 0, 0, 1, np > 1 ? np : 0}, us + in_tile + (np > 1 ? 5.0 + np * row_us : 0.0));
-            take({TILES_SPLIT, np, 0, own_per, 1, np + own_slots}, us + 4.0 + own_us + 5.0 + (np + own_slots) * row_us);
+            take({TILES, np, 0, 0, 1, np > 1 ? np : 0}, us + ceil_div(wgs, 256) * in_tile + (np > 1 ? 4.0 + np * slot_us : 0.0));
+            if (!own_wgs) continue;
+            take({TILES_SPLIT, np, 0, own_per, 1, np + own_slots},
+                 us + 3.0 + tokens_us((double)own_wgs, std::min(own_per, own_max), seen / own_slots, (double)own_sum) + 7.0 + (np + own_slots) * slot_us);
+            take({TILES_FINISH, np, 0, 0, 1, np}, us + 1.0 + tokens_us((double)tiles32 * Hkv, own_max, seen, (double)own_sum) +
+                                                      (1.5 + 0.1 * np) * finish_rows * std::max(1.0, tiles32 * Hkv / 512.0) + np * slot_us);
         }
     }
-    // the prefix like the own keys, with 32 or 64 rows of any requests
+    // the prefix like the own keys, with 32 or 64 rows of any requests: 256 keys of a workgroup 1.9 or 5 us, 3 or 10 for its beginning and end
     const int rt = vr <= 32 ? 1 : 2;
     const int64_t groups = (vr + 32 * rt - 1) / (32 * rt) * Hkv;
+    const double own_us = own_wgs ? (3.0 + 1.9 * std::ceil(std::min<double>(own_per, seen) / 256)) * narrow : 0.0;
+    const double own_most = own_wgs ? (3.0 + 1.9 * std::ceil(std::min(own_per, own_max) / 256.0)) * narrow : 0.0;
+    const double read_us = ((double)n2 + own_sum) * key_bytes / 4.8e6;
     for (int np = n2 > 0 ? 1 : 0; np <= 64; ++np) {
         const int per = np ? std::max(256, ceil_div(ceil_div(n2, np), 64) * 64) : 0;
         if (np && ceil_div(n2, per) != np) continue;
-        const double pre = np ? hd_part * (rt == 1 ? 1.9 : 3.0) * std::ceil(per / 256.0) : 0.0;
+        const double pre = np ? (rt == 1 ? 3.0 + 1.9 * std::ceil(per / 256.0) : 10.0 + 5.0 * std::ceil(per / 256.0)) * narrow : 0.0;
+        const int64_t wgs = groups * np;
         take({SPLIT, np, per, own_per, rt, np + own_slots},
-             6.0 + std::max({pre, own_us, (groups * np + own_wgs) / 256.0 * std::max(pre, own_wgs ? 1.9 * own_blocks : 0.0)}) + 6.0 + (np + own_slots) * row_us);
+             3.0 + std::max({wgs > 256 && wgs <= 512 ? 2.0 * pre : pre, own_most, (wgs * pre + own_wgs * own_us) / 256.0, read_us}) + 3.0 + (np + own_slots) * slot_us);
         if (np == 0) break;
     }
     return best;
@@ -507,6 +597,13 @@ void launch_tokens(const SharedParams& p, const Parts& parts, const SharedTable&
     static OncePerDevice lds;
     lds.run(current_device(), [] { allow_dynamic_lds((const void*)(attn_shared_tokens_kernel<HD, NW, RT, MODE>), LDS); });
     hipLaunchKernelGGL((attn_shared_tokens_kernel<HD, NW, RT, MODE>), dim3(items * p.Hkv), dim3(NW * 64), LDS, s, p, parts, tab);
+}
+
+// (two wavefronts, two workgroups a compute unit, where there are enough of them)
+template <int HD, int MODE>
+void launch_tokens(const SharedParams& p, const Parts& parts, const SharedTable& tab, unsigned items, hipStream_t s) {
+    if (items * p.Hkv > 256) launch_tokens<HD, 2, 1, MODE>(p, parts, tab, items, s);
+    else launch_tokens<HD, 4, 1, MODE>(p, parts, tab, items, s);
 }
 
 template <int HD>
@@ -534,10 +631,7 @@ void launch_t(const SharedParams& p, const po_request_rows* seq, int n, float* s
         unsigned n_items;
         switch (t.mode) {
             case TOKENS:
-                n_items = items(32);
-                // (two wavefronts, two workgroups a compute unit, where there are enough of them)
-                if (n_items * p.Hkv > 256) launch_tokens<HD, 2, 1, WHOLE>(p, parts, tab, n_items, s);
-                else launch_tokens<HD, 4, 1, WHOLE>(p, parts, tab, n_items, s);
+                launch_tokens<HD, WHOLE>(p, parts, tab, items(32), s);
                 break;
             case ROWS:
                 n_items = items(128);
@@ -549,7 +643,11 @@ void launch_t(const SharedParams& p, const po_request_rows* seq, int n, float* s
             case TILES_SPLIT:
                 launch_attention_shared_tiles(p, tab, t.np, false, parts.opart, parts.mlpart, s);
                 n_items = items(32);
-                if (n_items) launch_tokens<HD, 4, 1, PARTS>(p, parts, tab, n_items, s);
+                if (n_items) launch_tokens<HD, PARTS>(p, parts, tab, n_items, s);
+                break;
+            case TILES_FINISH:
+                launch_attention_shared_tiles(p, tab, t.np, false, parts.opart, parts.mlpart, s);
+                launch_tokens<HD, FINISH>(p, parts, tab, items(32), s);
                 break;
             case SPLIT:
                 parts.prefix_items = ceil_div((int64_t)rows * group, 32 * t.rt) * t.np;
@@ -558,7 +656,7 @@ void launch_t(const SharedParams& p, const po_request_rows* seq, int n, float* s
                 else launch_tokens<HD, 4, 2, PARTS>(p, parts, tab, n_items, s);
                 break;
         }
-        if (t.slots > 0)
+        if (t.slots > 0 && t.mode != TILES_FINISH)
             hipLaunchKernelGGL(attn_shared_join_kernel<HD>, dim3((unsigned)(((int64_t)rows * p.Hq * (HD / 4) + 255) / 256)), dim3(256), 0, s, p,
                                parts, tab);
     }
