@@ -442,6 +442,18 @@ typedef struct { int64_t q_row, q_len, kv_row, kv_len; } po_request_rows;
  * Host only.) */
 po_status po_attention_shared_bytes(int32_t dtype, const po_request_rows* requests, int32_t n_req, int64_t n2, int32_t n_q_heads,
                                     int32_t n_kv_heads, int32_t head_dim, size_t* scratch_bytes);
+/* How the bf16 op runs the first 128 of these requests that have a row, given this much scratch.  Host only.  prefix_pieces: into how
+ * many the prefix is divided (0: it is not divided from the own keys). */
+enum {
+    PO_SHARED_TOKENS = 0,        /* 32 rows of a request and all their keys a workgroup */
+    PO_SHARED_ROWS = 1,          /* 128 rows of a request and all their keys a workgroup */
+    PO_SHARED_TILES = 2,         /* 256 rows of any requests a workgroup (head_dim 128) */
+    PO_SHARED_SPLIT = 3,         /* the prefix with rows of any requests, and own keys, in pieces */
+    PO_SHARED_TILES_SPLIT = 4,   /* the prefix as TILES, own keys in pieces */
+    PO_SHARED_TILES_FINISH = 5   /* the prefix as TILES, own keys whole by the workgroups that join all pieces */
+};
+po_status po_attention_shared_form(const po_request_rows* requests, int32_t n_req, int64_t n2, int32_t n_q_heads, int32_t n_kv_heads,
+                                   int32_t head_dim, size_t scratch_bytes, int32_t* form, int32_t* prefix_pieces);
 po_status po_op_attention_shared(int32_t dtype, const void* dev_q, int64_t q_rows, const void* dev_k, const void* dev_v,
                                  int64_t kv_rows, int64_t ldv, void* dev_o, const po_request_rows* requests, int32_t n_req,
                                  const void* dev_k2, const void* dev_v2, int64_t ldv2, int64_t n2, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,

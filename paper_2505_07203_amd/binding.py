@@ -42,7 +42,7 @@ EXPORTS = [
     "po_op_attention_split_prefix", "po_attention_tile", "po_gemm_tile", "po_gemm_turns", "po_gemm_f32_tile", "po_op_linear_fp8_split",
     "po_sched_create", "po_sched_destroy", "po_sched_set_jct_model", "po_sched_fit_jct_model", "po_sched_push",
     "po_sched_size", "po_sched_pick", "po_sched_remove", "po_op_rope_static", "po_op_mfma_peak", "po_op_stream_copy",
-    "po_op_quantize_blocks", "po_linear_fp8_block_bytes", "po_op_linear_fp8_block", "po_op_sample", "po_op_attention_shared", "po_attention_shared_bytes", "po_sample_bytes",
+    "po_op_quantize_blocks", "po_linear_fp8_block_bytes", "po_op_linear_fp8_block", "po_op_sample", "po_op_attention_shared", "po_attention_shared_bytes", "po_attention_shared_form", "po_sample_bytes",
 ]
 
 
@@ -149,6 +149,7 @@ def lib() -> C.CDLL:
     L.po_op_sample.argtypes = [vp, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.po_sample_bytes.argtypes = [i64, i32, i32, i32, C.POINTER(sz)]
     L.po_op_attention_shared.argtypes = [i32, vp, i64, vp, vp, i64, i64, vp, vp, i32, vp, vp, i64, i64, i32, i32, i32, i32, vp, sz, vp]
+    L.po_attention_shared_form.argtypes = [vp, i32, i64, i32, i32, i32, sz, C.POINTER(i32), C.POINTER(i32)]
     L.po_attention_shared_bytes.argtypes = [i32, vp, i32, i64, i32, i32, i32, C.POINTER(sz)]
     f64 = C.c_double
     L.po_sched_create.argtypes = [f64, C.POINTER(vp)]
@@ -709,6 +710,17 @@ def po_attention_shared_bytes(dtype: int, requests, n2: int, n_q_heads: int, n_k
     n = C.c_size_t(0)
     check(lib().po_attention_shared_bytes(dtype, r.ctypes.data, len(r), n2, n_q_heads, n_kv_heads, head_dim, C.byref(n)))
     return n.value
+
+
+SHARED_FORMS = ("TOKENS", "ROWS", "TILES", "SPLIT", "TILES_SPLIT", "TILES_FINISH")
+
+
+def po_attention_shared_form(requests, n2: int, n_q_heads: int, n_kv_heads: int, head_dim: int, scratch_bytes: int = 1 << 62):
+    """how the bf16 op runs the first 128 of these requests that have a row -> (one of SHARED_FORMS, pieces of the prefix); needs no GPU"""
+    r = _requests(requests)
+    form, pieces = C.c_int32(0), C.c_int32(0)
+    check(lib().po_attention_shared_form(r.ctypes.data, len(r), n2, n_q_heads, n_kv_heads, head_dim, scratch_bytes, C.byref(form), C.byref(pieces)))
+    return SHARED_FORMS[form.value], pieces.value
 
 
 def po_op_attention_shared(q, k, v, requests, k2=None, v2=None, n2: int = 0, out=None, q_prescaled: bool = False, scratch=None):

@@ -93,6 +93,8 @@ int fill_table(SharedTable& tab, const po_request_rows* seq, int i, int n, F ite
 int launch_attention_shared_tiles(const SharedParams& p, const SharedTable& tab, int pieces, bool own, float* opart, float* mlpart, hipStream_t s);
 // scratch (may be null): for partial results; attention_shared_scratch: how much of it the requests can use
 size_t attention_shared_scratch(const po_request_rows* seq, int n, int Hq, int Hkv, int hd, int64_t n2);
+// how the first table of them runs with that much, as the public enumeration has it
+void attention_shared_form(const po_request_rows* seq, int n, int Hq, int Hkv, int hd, int64_t n2, size_t scratch_bytes, int* form, int* pieces);
 void launch_attention_shared_bf16(const SharedParams& p, const po_request_rows* seq, int n, int hd, float* scratch, size_t scratch_bytes,
                                   hipStream_t s);
 void launch_attention_shared_f32(const SharedParams& p, const po_request_rows* seq, int n, int hd, hipStream_t s);

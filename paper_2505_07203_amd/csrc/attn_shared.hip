@@ -505,7 +505,7 @@ __global__ void __launch_bounds__(256) attn_shared_join_kernel(const SharedParam
 //   SPLIT        the prefix in np pieces with 32 rt rows of any requests, own keys in pieces of own_per, joined
 //   TILES_SPLIT  the prefix by the tile kernel, own keys in pieces, joined
 //   TILES_FINISH the prefix by the tile kernel, own keys whole, which joins both
-enum Mode { TOKENS, ROWS, TILES, SPLIT, TILES_SPLIT, TILES_FINISH };
+enum Mode { TOKENS = PO_SHARED_TOKENS, ROWS = PO_SHARED_ROWS, TILES = PO_SHARED_TILES, SPLIT = PO_SHARED_SPLIT, TILES_SPLIT = PO_SHARED_TILES_SPLIT, TILES_FINISH = PO_SHARED_TILES_FINISH };
 struct Plan {
     Mode mode;
     int np, per, own_per, rt, slots;     // slots: partial results of a row at most
@@ -672,6 +672,14 @@ size_t attention_shared_scratch(const po_request_rows* seq, int n, int Hq, int H
         if (tab.n) most = std::max(most, (size_t)plan(tab, Hq, Hkv, hd, (int)n2, SIZE_MAX).slots * tab.row0[tab.n] * Hq * (hd + 2) * sizeof(float));
     }
     return most;
+}
+
+void attention_shared_form(const po_request_rows* seq, int n, int Hq, int Hkv, int hd, int64_t n2, size_t scratch_bytes, int* form, int* pieces) {
+    SharedTable tab;
+    fill_table(tab, seq, 0, n, [](const SharedSeq&) { return 0; });
+    const Plan p = tab.n ? plan(tab, Hq, Hkv, hd, (int)n2, scratch_bytes) : Plan{TOKENS, 0, 0, 0, 1, 0};
+    *form = p.mode;
+    *pieces = p.np;
 }
 
 void launch_attention_shared_bf16(const SharedParams& p, const po_request_rows* seq, int n, int hd, float* scratch, size_t scratch_bytes,

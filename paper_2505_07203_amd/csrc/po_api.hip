@@ -1497,6 +1497,15 @@ po_status po_attention_shared_bytes(int32_t dtype, const po_request_rows* reques
     return st;
 }
 
+po_status po_attention_shared_form(const po_request_rows* requests, int32_t n_req, int64_t n2, int32_t Hq, int32_t Hkv, int32_t hd,
+                                   size_t scratch_bytes, int32_t* form, int32_t* prefix_pieces) {
+    size_t need;
+    if (!form || !prefix_pieces) return PO_ERR_INVALID_ARG;
+    const po_status st = po_attention_shared_bytes(PO_BF16, requests, n_req, n2, Hq, Hkv, hd, &need);
+    if (st == PO_OK) attention_shared_form(requests, n_req, Hq, Hkv, hd, n2, scratch_bytes, form, prefix_pieces);
+    return st;
+}
+
 po_status po_op_attention_shared(int32_t dtype, const void* q, int64_t q_rows, const void* k, const void* v, int64_t kv_rows, int64_t ldv,
                                  void* o, const po_request_rows* requests, int32_t n_req, const void* k2, const void* v2, int64_t ldv2,
                                  int64_t n2, int32_t Hq, int32_t Hkv, int32_t hd, int32_t q_prescaled, void* scratch,

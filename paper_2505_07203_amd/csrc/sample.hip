@@ -1012,7 +1012,7 @@ int parts_of(int64_t rows, int V, int ts, int* part_len) {
 int tile_of(int V) { return (int)round_up64((V + MAX_TILES - 1) / MAX_TILES, SUB); }
 
 // the arrays of a Handover, in `base` if there is one; -> bytes
-size_t lay_out(Handover* h, unsigned char* base, int64_t rows, int parts, bool listed, bool weighed) {
+size_t lay_out(Handover* h, unsigned char* base, int64_t rows, int parts, bool filtered) {
     size_t at = 0;
     const auto place = [&](auto*& p, size_t n) {
         p = (std::remove_reference_t<decltype(p)>)(base + at);
@@ -1027,9 +1027,9 @@ size_t lay_out(Handover* h, unsigned char* base, int64_t rows, int parts, bool l
     place(h->finished, 2 * rows);
     place(h->tile, (size_t)rows * MAX_TILES);
     place(h->tile_top, (size_t)rows * MAX_TILES);
-    place(h->list, listed || weighed ? rp * PART_CAP : 0);
-    place(h->count, weighed ? rp * BINS : 0);
-    place(h->weight, weighed ? rp * BINS : 0);
+    place(h->list, filtered ? rp * PART_CAP : 0);
+    place(h->count, filtered ? rp * BINS : 0);
+    place(h->weight, filtered ? rp * BINS : 0);
     return at;
 }
 
@@ -1039,7 +1039,7 @@ size_t sample_scratch(int64_t rows, int V, bool top_k, bool top_p) {
     Handover h;
     int part_len;
     const int parts = parts_of(rows, V, tile_of(V), &part_len);
-    return lay_out(&h, nullptr, rows, parts, top_k, top_k || top_p);
+    return lay_out(&h, nullptr, rows, parts, top_k || top_p);
 }
 
 void launch_sample(const float* logits, int64_t ld, int rows, int V, const float* u, const float* temperature, const int* top_k,
@@ -1055,7 +1055,7 @@ void launch_sample(const float* logits, int64_t ld, int rows, int V, const float
     while (c.fix > 0 && ((int64_t)V << c.fix) > ((int64_t)1 << 62)) --c.fix;
     c.fix = std::min(c.fix, 44);
     c.parts = parts_of(rows, V, c.ts, &c.part_len);
-    lay_out(&c.h, (unsigned char*)scratch, rows, c.parts, top_k != nullptr, top_k || top_p);
+    lay_out(&c.h, (unsigned char*)scratch, rows, c.parts, top_k || top_p);
     const dim3 parts((unsigned)((int64_t)rows * c.parts)), block(NT);
     hipLaunchKernelGGL(sample_parts_kernel, parts, block, 0, s, c);
     if (top_k || top_p) hipLaunchKernelGGL(sample_weigh_kernel, parts, block, 0, s, c);
