@@ -549,6 +549,7 @@ Plan plan(const SharedTable& t, int Hq, int Hkv, int hd, int n2, size_t scratch_
     take({ROWS, 0, 0, 0, 1, 0}, 5.0 + std::max((wg128 <= 256 ? c1 : 2.0 * c2) * (std::ceil((n2 + own_max) / 64.0) + 2.0),
                                               std::max(wg128 / 256.0 * c2 * ((n2 + seen) / 64.0 + 6.0), ((double)n2 + own_sum) * key_bytes / 3.6e6)));
     if (n2 == 0 && own_max == 0) return best;
+    constexpr int64_t MOST = 1 << 24;                         // workgroups of a form with pieces: far beyond where pieces help
     // own keys by pieces, and the join
     const int own_per = (int)std::min<int64_t>(2048, std::max<int64_t>(512, (own_sum * Hkv / 256 + 255) / 256 * 256));
     const int own_slots = ceil_div(own_max, own_per);
@@ -566,7 +567,7 @@ Plan plan(const SharedTable& t, int Hq, int Hkv, int hd, int n2, size_t scratch_
             if (ceil_div(tiles2, per) != np || (uint64_t)per * 64 * (uint64_t)Hkv * 256 >= (1ull << 32)) continue;
             const double us = 6.0 + ceil_div(wgs * np, 256) * (per + 5) * 1.35;
             take({TILES, np, 0, 0, 1, np > 1 ? np : 0}, us + ceil_div(wgs, 256) * in_tile + (np > 1 ? 4.0 + np * slot_us : 0.0));
-            if (!own_wgs) continue;
+            if (!own_wgs || own_wgs > MOST) continue;
             take({TILES_SPLIT, np, 0, own_per, 1, np + own_slots},
                  us + 3.0 + tokens_us((double)own_wgs, std::min(own_per, own_max), seen / own_slots, (double)own_sum) + 7.0 + (np + own_slots) * slot_us);
             take({TILES_FINISH, np, 0, 0, 1, np}, us + 1.0 + tokens_us((double)tiles32 * Hkv, own_max, seen, (double)own_sum) +
@@ -584,6 +585,7 @@ Plan plan(const SharedTable& t, int Hq, int Hkv, int hd, int n2, size_t scratch_
         if (np && ceil_div(n2, per) != np) continue;
         const double pre = np ? (rt == 1 ? 3.0 + 1.9 * std::ceil(per / 256.0) : 10.0 + 5.0 * std::ceil(per / 256.0)) * narrow : 0.0;
         const int64_t wgs = groups * np;
+        if (wgs + own_wgs > MOST) break;
         take({SPLIT, np, per, own_per, rt, np + own_slots},
              3.0 + std::max({wgs > 256 && wgs <= 512 ? 2.0 * pre : pre, own_most, (wgs * pre + own_wgs * own_us) / 256.0, read_us}) + 3.0 + (np + own_slots) * slot_us);
         if (np == 0) break;

@@ -1469,7 +1469,7 @@ po_status po_op_attention_split_prefix(const void* q, const void* k, const void*
 // requests together
 static po_status shared_requests(const po_request_rows* req, int32_t n_req, int32_t Hq, int64_t q_rows, int64_t kv_rows, bool vt, int64_t* keys) {
     constexpr int64_t MAX = (int64_t)1 << 24;
-    int64_t row = 0, tiles = 0;
+    int64_t row = 0, heads = 0;
     *keys = 0;
     for (int32_t i = 0; i < n_req; ++i) {
         const po_request_rows& r = req[i];
@@ -1477,9 +1477,9 @@ static po_status shared_requests(const po_request_rows* req, int32_t n_req, int3
         if (r.q_len > MAX || r.kv_len > MAX || r.q_row > INT32_MAX - MAX || r.kv_row > INT32_MAX - MAX) return PO_ERR_TOO_LONG;
         if (r.q_row + r.q_len > q_rows || r.kv_row + r.kv_len > kv_rows || (vt && r.kv_row % 8)) return PO_ERR_INVALID_ARG;
         row = r.q_row + r.q_len;
-        tiles += (r.q_len * Hq + 31) / 32 + Hq;
+        heads += (r.q_len + 1) * Hq;                          // (rows and heads, and their tiles, are counted with 32 bits)
         if (r.q_len) *keys += r.kv_len;
-        if (tiles > INT32_MAX) return PO_ERR_TOO_LONG;
+        if (heads > INT32_MAX - 4096) return PO_ERR_TOO_LONG;
     }
     return PO_OK;
 }

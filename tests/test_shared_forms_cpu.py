@@ -44,5 +44,10 @@ def test_refusals():
         assert ask(**kw) == B.PO_ERR_INVALID_ARG, kw
     assert ask(hd=96) == B.PO_ERR_BAD_CONFIG
     assert ask(n2=(1 << 24) + 1) == B.PO_ERR_TOO_LONG
+    for rows in ([(0, 1 << 24, 0, 0)], [(i << 19, 1 << 19, 0, 0) for i in range(128)]):           # more rows and heads than 32 bits count
+        many = np.array(rows, dtype=np.int64)
+        assert ask(r=many.ctypes.data, n=len(many), hq=4096, hkv=1, hd=64) == B.PO_ERR_TOO_LONG
+    long = np.array([(0, 1 << 20, 0, 1 << 24)], dtype=np.int64)                                  # ... and more pieces than a launch has
+    assert ask(r=long.ctypes.data, hq=32, hkv=8, n2=0) == B.PO_OK and B.SHARED_FORMS[f.value] in ("TOKENS", "ROWS")
     bad = np.array([(0, 2, 0, 5), (1, 1, 0, 5)], dtype=np.int64)                       # rows of q that meet
     assert ask(r=bad.ctypes.data, n=2) == B.PO_ERR_INVALID_ARG
