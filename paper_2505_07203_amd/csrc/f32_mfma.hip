@@ -352,15 +352,120 @@ __global__ void __launch_bounds__(256, 2) attention_shared_f32_kernel(const Shar
     }
 }
 
+// The same with 128 rows of a request a workgroup, 32 a wavefront: tiles of 32 keys in LDS for all four, the next one on its way, as
+// in the kernel for one sequence above.
+template <int HD>
+__global__ void __launch_bounds__(256, 2) attention_shared_f32_rows_kernel(const SharedParams p, const SharedTable tab) {
+    constexpr int NB = HD / 32, ROWB = HD * 4, TB = 32 * ROWB;           // bytes of a K / V row and of a tile
+    constexpr int RPL = 1024 / ROWB, LPW = 32 / RPL / 4, SEGS = ROWB / 16;   // rows per 1 KiB load; loads per wavefront, operand and tile
+    __shared__ __attribute__((aligned(16))) unsigned char smem[4 * TB];  // [stage][K, V]
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const int c = (int)(blockIdx.x % (unsigned)p.Hkv), item = (int)(blockIdx.x / (unsigned)p.Hkv);
+    const int req = __builtin_amdgcn_readfirstlane(shared_request(tab, item));
+    const SharedSeq sq = tab.seq[req];
+    const int group = p.Hq / p.Hkv, n_rows = sq.q_len * group;
+    const int wg0 = (item - tab.item0[req]) * 128, row0 = wg0 + wave * 32;
+    const bool any = row0 < n_rows;
+    const int vr = min(row0 + col, n_rows - 1), pos = vr / group, h = c * group + vr - pos * group;
+    const int first = sq.kv_len - sq.q_len;                              // own keys 0 .. first + position are seen
+    const int last = first + pos, last_min = first + min(row0, n_rows - 1) / group;
+    const int last_max = any ? first + min(row0 + 31, n_rows - 1) / group : -1, wg_last = first + min(wg0 + 127, n_rows - 1) / group;
+    const int64_t kvrow = (int64_t)p.Hkv * HD;
+    F32Rows<HD> st;
+    st.start((const float*)p.q, sq.q_row + pos, INT64_MAX, h, p.Hq, half);
+    uint32_t vok[4], vov[4];                                             // (LPW entries used)
+#pragma unroll
+    for (int jj = 0; jj < LPW; ++jj) {
+        const int row = (wave * LPW + jj) * RPL + lane / SEGS, seg = lane % SEGS;
+        vok[jj] = (uint32_t)row * (uint32_t)(kvrow * 4) + (uint32_t)((seg ^ (row & 15)) << 4);
+        vov[jj] = (uint32_t)row * (uint32_t)(kvrow * 4) + (uint32_t)(seg << 4);
+    }
+    const float* const ko = (const float*)p.k + sq.kv_row * kvrow + c * HD;
+    const float* const vo = (const float*)p.v + sq.kv_row * kvrow + c * HD;
+    const float *const kp = (const float*)p.k2 + c * HD, *const vp = (const float*)p.v2 + c * HD;
+    const int nb2 = (p.n2 + 31) / 32, nb = nb2 + max(wg_last + 32, 0) / 32;
+    auto load_tile = [&](int b) {                                        // (rows past the last key read as zero)
+        if (b >= nb) return;
+        const bool own = b >= nb2;
+        const int kv0 = (own ? b - nb2 : b) * 32, rows = min(32, (own ? sq.kv_len : p.n2) - kv0);
+        const int bytes = (int)((rows - 1) * kvrow * 4) + ROWB;
+        const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void*)((own ? ko : kp) + kv0 * kvrow), 0, bytes, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)((own ? vo : vp) + kv0 * kvrow), 0, bytes, 0x00020000);
+        unsigned char* dst = smem + (b & 1) * 2 * TB + wave * LPW * 1024;
+#pragma unroll
+        for (int jj = 0; jj < LPW; ++jj) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (__attribute__((address_space(3))) void*)(dst + jj * 1024), 16, vok[jj], 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (__attribute__((address_space(3))) void*)(dst + TB + jj * 1024), 16, vov[jj], 0, 0, 0);
+        }
+    };
+    load_tile(0);
+    for (int b = 0; b < nb; ++b) {
+        // this tile has landed; everybody is done with the other stage
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        load_tile(b + 1);
+        const bool own = b >= nb2;
+        const int kv0 = (own ? b - nb2 : b) * 32;
+        if (!any || (own && kv0 > last_max)) continue;                   // (wavefront-uniform)
+        const unsigned char* ks = smem + (b & 1) * 2 * TB + col * ROWB;
+        const float* vs = (const float*)(smem + (b & 1) * 2 * TB + TB) + (4 * half) * HD + col;
+        st.tile(kv0, own ? last_min : p.n2 - 1, own ? last : p.n2 - 1, half, p.sc,
+                [&](int i) { return *(const float4*)(ks + (((half * (SEGS / 2) + i) ^ (col & 15)) << 4)); },
+                [&](int b2, int r) { return vs[(8 * (r / 4) + (r % 4)) * HD + 32 * b2]; });
+    }
+    const float l = st.l + __shfl_xor(st.l, 32);
+    if (row0 + col >= n_rows) return;
+    const float inv = l > 0.f ? 1.0f / l : 0.f;                          // (a row that sees nothing: 0)
+    float* op = (float*)p.o + ((int64_t)(sq.q_row + pos) * p.Hq + h) * HD;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *(float4*)(op + 32 * b + 8 * g + 4 * half) =
+                make_float4(st.O[b][4 * g] * inv, st.O[b][4 * g + 1] * inv, st.O[b][4 * g + 2] * inv, st.O[b][4 * g + 3] * inv);
+}
+
+// Which of the two, by expected time (us): 512 workgroups at once, two a compute unit, each as many tiles of 32 keys long as its
+// wavefronts go through.  A tile of 128 rows 5.8 with a compute unit to itself, 9.4 beside another one; four tiles at once of 32 rows 15 (in
+// part 8.5), but a fourth of them in turn.  Measured (32 heads on 8 KV heads of 128; 32 rows / 128 rows): 8 requests of 100 rows
+// behind 2000 keys 457 / 390, 16 behind 1000 406 / 324, 40 of 150 behind 200 628 / 343; one of 300 alone 47 / 55, 64 of one row
+// behind 2000 214 / 323, two of 600 behind 2000 639 / 688.
+static bool shared_f32_rows128(const SharedTable& t, int group, int Hkv, int hd, int n2) {
+    int64_t wg32 = 0, wg128 = 0, own_max = 0;
+    double seen = 0.0, rows = t.row0[t.n];
+    for (int i = 0; i < t.n; ++i) {
+        const SharedSeq& q = t.seq[i];
+        wg32 += ((int64_t)q.q_len * group + 31) / 32 * Hkv;
+        wg128 += ((int64_t)q.q_len * group + 127) / 128 * Hkv;
+        own_max = std::max<int64_t>(own_max, q.kv_len);
+        seen += q.q_len * std::max(0.0, q.kv_len - 0.5 * q.q_len);
+    }
+    const bool narrow = hd == 64;
+    const double most = (double)((n2 + 31) / 32 + (own_max + 31) / 32), mean = (n2 + seen / rows) / 32 + 0.5;
+    const double alone = narrow ? 3.0 : 5.8, beside = narrow ? 5.4 : 9.4, four = narrow ? 6.0 : 15.0, four_alone = narrow ? 4.0 : 8.5;
+    const double t128 = wg128 <= 256 ? alone * most : beside * std::max(most, std::ceil(wg128 / 512.0) * mean);
+    const double t32 = wg32 <= 256 ? four_alone * std::ceil(most / 4) : four * std::max(std::ceil(most / 4), wg32 / 512.0 * (mean / 4 + 0.5));
+    return t128 < t32;
+}
+
 void launch_attention_shared_f32(const SharedParams& p, const po_request_rows* seq, int n, int hd, hipStream_t s) {
     const int group = p.Hq / p.Hkv;
     for (int i = 0; i < n;) {
         SharedTable tab;
-        i = fill_table(tab, seq, i, n, [&](const SharedSeq& q) { return (q.q_len * group + 31) / 32; });
+        const int i0 = i;
+        i = fill_table(tab, seq, i0, n, [&](const SharedSeq& q) { return (q.q_len * group + 31) / 32; });
         if (tab.n == 0) continue;
-        const dim3 grid((unsigned)tab.item0[tab.n] * p.Hkv);
-        if (hd == 128) hipLaunchKernelGGL(attention_shared_f32_kernel<128>, grid, dim3(256), 0, s, p, tab);
-        else hipLaunchKernelGGL(attention_shared_f32_kernel<64>, grid, dim3(256), 0, s, p, tab);
+        const bool rows128 = shared_f32_rows128(tab, group, p.Hkv, hd, p.n2);
+        if (rows128) fill_table(tab, seq, i0, n, [&](const SharedSeq& q) { return (q.q_len * group + 127) / 128; });
+        const dim3 grid((unsigned)tab.item0[tab.n] * p.Hkv), block(256);
+        if (rows128) {
+            if (hd == 128) hipLaunchKernelGGL(attention_shared_f32_rows_kernel<128>, grid, block, 0, s, p, tab);
+            else hipLaunchKernelGGL(attention_shared_f32_rows_kernel<64>, grid, block, 0, s, p, tab);
+        } else {
+            if (hd == 128) hipLaunchKernelGGL(attention_shared_f32_kernel<128>, grid, block, 0, s, p, tab);
+            else hipLaunchKernelGGL(attention_shared_f32_kernel<64>, grid, block, 0, s, p, tab);
+        }
     }
 }
 

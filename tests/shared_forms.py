@@ -29,6 +29,13 @@ FORMS = {
     "a little scratch": ("SPLIT", 1, SMALL, [(1, 1, 700)], 1500, 12500),
 }
 
+# float32: 128 rows a workgroup, for either head dimension
+WIDE_F32 = {
+    "128": (LLAMA, [(3, 150, 150), (6, 100, 130), (2, 1, 1), (4, 97, 40), (1, 64, 0)], 517),
+    "128, no prefix": (LLAMA, [(7, 150, 150), (6, 100, 130), (2, 1, 1), (4, 97, 40), (1, 64, 0)], 0),
+    "64": ((16, 4, 64), [(40, 150, 150), (6, 100, 130), (2, 1, 1), (12, 97, 40), (1, 64, 0)], 33),
+}
+
 
 def requests_of(spec):
     out, row, key = [], 0, 0

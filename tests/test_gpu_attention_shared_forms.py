@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2505_07203_amd import binding as B
-from tests.shared_forms import FORMS, requests_of
+from tests.shared_forms import FORMS, WIDE_F32, requests_of
 from tests.test_gpu_attention_shared import Batch
 
 pytestmark = pytest.mark.gpu
@@ -40,6 +40,18 @@ def test_a_form(name):
         B.po_op_attention_shared(q, k, v, b.req, k2, v2, n2, out=out, q_prescaled=b.pre, scratch=scratch[:size])
         compare(b, out, mark)
     assert bool((scratch[size:] == 0xff).all())                                           # (nothing behind it)
+
+
+@pytest.mark.parametrize("name", WIDE_F32)
+def test_float32_with_128_rows_a_workgroup(name):
+    (hq, hkv, hd), spec, n2 = WIDE_F32[name]
+    b = Batch(len(name), "f32", hq, hkv, hd, requests_of(spec), n2)
+    q, k, v, k2, v2 = b.device()
+    for in_place in (False, True):
+        out = q if in_place else torch.full_like(q, 777.0)
+        mark = out.clone()
+        B.po_op_attention_shared(q, k, v, b.req, k2, v2, n2, out=out)
+        compare(b, out, mark)
 
 
 def test_scores_that_grow_along_the_keys():
