@@ -1434,7 +1434,9 @@ int launch_split_fwd64(const bf16_t* q, const bf16_t* k, const bf16_t* vt, int64
 }  // namespace
 
 // The tile kernel over the prefix's whole tiles and everything behind them, for the rows of one table, in `pieces` pieces of the
-// prefix (partial results in opart, mlpart when more than one or without the own keys, merged by the caller).
+// prefix (partial results in opart, mlpart when more than one or without the own keys, merged by the caller).  The prefix's tiles
+// go as in one long sequence, without a mask; own keys, which differ between the rows of a tile, from memory to registers, 32 in
+// about 3 us.  50 requests of 150 rows behind 14000 keys 1.38 ms, 1.26 PFLOP/s of the 1.40 that one sequence reaches.
 int launch_attention_shared_tiles(const SharedParams& p, const SharedTable& tab, int pieces, bool own, float* opart, float* mlpart, hipStream_t s) {
     constexpr int SMEM = 2 * A64_NSTAGE * A64_TILE + 16;
     static OncePerDevice lds;

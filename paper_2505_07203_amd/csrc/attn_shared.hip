@@ -143,6 +143,11 @@ __device__ __forceinline__ void clear_columns(uint4& v, int n) {
 // One workgroup: 128 rows of one request and KV head, 32 a wavefront, all their keys, 64 at a time in LDS for all four; the next 64
 // are on their way while these are worked on, and one barrier a step says both that they are there and that the last ones are
 // out of use.
+// What bounds it: with two workgroups a compute unit 0.85 to 1.1 us for 128 rows and 64 keys, where the matrix instructions take 0.45;
+// without the copies a sixth less, without the softmax a sixth less: two wavefronts a SIMD wait for one another's LDS reads and
+// vector instructions.  (64 rows a wavefront halve the LDS reads, but one wavefront a SIMD then has nobody to hide behind: 2.7 us.)
+// Measured (us, 32 heads on 8 KV heads): 20 requests of 500 rows alone 84, 60 of 500 behind 1000 keys 770 (0.8 PFLOP/s), 27 of 161
+// behind 45 37; head dimension 64, 20 of 150 behind 4000 87.
 template <int HD>
 __global__ void __launch_bounds__(256, 2) attn_shared_rows_kernel(const SharedParams p, const SharedTable tab) {
     constexpr int KS = HD / 16, HT = HD / 32;
@@ -262,6 +267,8 @@ struct Parts {
 // at a time, loaded by whole cache lines past the registers (K rows as they are, 128 bytes of each V^T row), no two wavefronts wait
 // for each other, and they meet at the end.  K of its next block is on its way as soon as the scores are there, V^T as soon as
 // the products are.  RT: tiles of 32 rows that go through the same keys.
+// What bounds it: reading the keys, 4.2 to 4.8 TB/s where there are many (128 tokens with 3000 keys each: 1.6 GB in 307 us), else the
+// chain of a launch, a first block, the meeting in LDS and the join: one token behind 14000 keys 22 us, two behind 500 10.
 // WHOLE: a workgroup is 32 rows of one request, all keys they see; result in o.
 // PARTS: a workgroup is a piece of the prefix, which all requests share, with 32 RT rows of any requests; or a piece of a request's own keys
 // with 32 of its rows.  Partial results.
@@ -514,7 +521,18 @@ struct Plan {
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // The one expected to take the least time (microseconds) with the scratch there is.  Every form's time is what one workgroup takes
-// times how often the card is filled with them, and no less than its bytes at what memory gives.
+// times how often the card is filled with them, and no less than its bytes at what memory gives.  Measured (us, 32 heads on 8 KV heads
+// of 128; requests x rows / prefix):        TOKENS  ROWS  TILES  SPLIT  TILES_SPLIT  TILES_FINISH
+//   3 x 161 / 45                                13    12      -     41            -             -
+//   20 x 500 / 0                               200    83      -      -            -             -
+//   20 x 20 / 2000                              52    49     41     67           50            52
+//   4 x 150 / 14000                            447   288    148    355          160           172
+//   60 x 500 / 1000                           1608   768    823      -         1605          1633
+//   1 x 1, 300 own keys / 14000                110   278     26     22           34            29
+//   1 x 40, 3000 own / 14000                   153   355    165     50           45            69
+//   64 x 1, 300 own / 14000                    275   304    341     70           62            57
+//   20 x 1, 9000 own / 14000                   309   740   7120    170          198           229
+//   128 x 1, 3000 own / 2000                   378   435   4097    309          327           341
 Plan plan(const SharedTable& t, int Hq, int Hkv, int hd, int n2, size_t scratch_bytes) {
     const int group = Hq / Hkv, rows = t.row0[t.n], tiles2 = n2 / 64;
     const int64_t vr = (int64_t)rows * group;
