@@ -570,14 +570,15 @@ po_status po_op_qkv_rope_fp8(const void* dev_a_codes, const float* dev_a_scales,
  * po_op_quantize_blocks: codes [rows, K] (one byte each) and scales of the bf16 tensor x [rows, K], K % 128 == 0.
  * block_rows 1: scales [K / 128][rows] (a block column's rows side by side, as the product reads them); block_rows 128:
  * scales [ceil(rows / 128)][K / 128], the last row of blocks as high as the rows that are left.  dev_codes must not overlap
- * dev_x. */
+ * dev_x; both 16-byte aligned. */
 po_status po_op_quantize_blocks(const void* dev_x, void* dev_codes, float* dev_scales, int64_t rows, int32_t K,
                                 int32_t block_rows, void* hip_stream);
 /* C[m][n] = sum over blocks b of a_scales[b][m] * w_scales[n / 128][b] * (product of the codes of block b), accumulated in
  * fp32, result bf16.  Operands as po_op_quantize_blocks makes them (a: block_rows 1, w: block_rows 128).  Epilogues as in
  * po_op_linear_fp8: 0: C [M, N]; 1: C = ... + residual [M, N] (may alias C); 2: w_codes in the interleaved gate/up order
  * (po_op_pack_gate_up with PO_BF16 and K / 2 packs rows of K codes), w_scales [2][ceil(N / 256)][K / 128]: those of the gate
- * matrix, then those of the up matrix, C [M, N/2] = silu(gate) * up.  K % 128 == 0, N % 64 == 0.
+ * matrix, then those of the up matrix, C [M, N/2] = silu(gate) * up.  K % 128 == 0, N % 64 == 0; codes, C and residual 16-byte
+ * aligned.
  * dev_scratch (may be NULL; 16-byte aligned) lets a launch with few output tiles divide its reduction over K between
  * workgroups, which it does where that is expected to take less time and its fp32 partial sums fit; they are added in a fixed
  * order.  po_linear_fp8_block_bytes: the scratch that a shape can use (0: none; host only).  A row's result does not

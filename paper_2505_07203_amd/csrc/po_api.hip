@@ -1689,8 +1689,9 @@ po_status po_op_linear_fp8_split(const void* a_codes, const float* a_scales, con
 
 po_status po_op_quantize_blocks(const void* x, void* codes, float* scales, int64_t rows, int32_t K, int32_t block_rows, void* stream) {
     if (!x || !codes || !scales || x == codes || rows <= 0 || K <= 0 || (block_rows != 1 && block_rows != 128)) return PO_ERR_INVALID_ARG;
+    if (misaligned16(x) || misaligned16(codes)) return PO_ERR_INVALID_ARG;
     if (K % 128) return PO_ERR_BAD_CONFIG;
-    if (rows > (int64_t)1 << 24) return PO_ERR_TOO_LONG;
+    if (rows > (int64_t)1 << 24 || rows * K > (int64_t)1 << 40) return PO_ERR_TOO_LONG;
     launch_quant_blocks((const bf16_t*)x, (unsigned char*)codes, scales, rows, K, block_rows, (hipStream_t)stream);
     PO_HIP(hipGetLastError());
     return PO_OK;
@@ -1700,7 +1701,7 @@ po_status po_op_quantize_blocks(const void* x, void* codes, float* scales, int64
 static po_status fp8_block_shape(int64_t M, int32_t N, int32_t K) {
     if (M <= 0 || N <= 0 || K <= 0) return PO_ERR_INVALID_ARG;
     if (!gemm_fp8_block_supported(N, K)) return PO_ERR_BAD_CONFIG;
-    if (M > (int64_t)1 << 24 || K >= 1 << 23) return PO_ERR_TOO_LONG;
+    if (M > (int64_t)1 << 24 || K >= 1 << 23 || M * N > (int64_t)1 << 40) return PO_ERR_TOO_LONG;
     return PO_OK;
 }
 
@@ -1717,6 +1718,7 @@ po_status po_op_linear_fp8_block(int32_t epilogue, const void* a_codes, const fl
     if (!a_codes || !a_scales || !w_codes || !w_scales || !cc) return PO_ERR_INVALID_ARG;
     if (epilogue != EPI_STORE && epilogue != EPI_RESIDUAL && epilogue != EPI_SILU_MUL) return PO_ERR_INVALID_ARG;
     if (epilogue == EPI_RESIDUAL && !residual) return PO_ERR_INVALID_ARG;
+    if (misaligned16(a_codes) || misaligned16(w_codes) || misaligned16(cc) || misaligned16(residual) || misaligned16(scratch)) return PO_ERR_INVALID_ARG;
     const po_status st = fp8_block_shape(M, N, K);
     if (st != PO_OK) return st;
     launch_gemm_fp8_block(epilogue, (const unsigned char*)a_codes, a_scales, (const unsigned char*)w_codes, w_scales, (bf16_t*)cc,

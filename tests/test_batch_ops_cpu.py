@@ -28,6 +28,25 @@ def test_linear_fp8_block_refusals():
         assert f(*a) == status, (i, bad)
 
 
+def test_fp8_block_sizes_beyond_a_launch():
+    assert B.lib().po_op_quantize_blocks(P, 2 * P, 3 * P, 1 << 24, 1 << 17, 1, None) == 4
+    n = C.c_size_t(0)
+    assert B.lib().po_linear_fp8_block_bytes(1 << 24, 1 << 17, 128, C.byref(n)) == 4
+
+
+def test_fp8_block_operands_lie_on_16_bytes():
+    f = B.lib().po_op_quantize_blocks
+    for i in (0, 1):
+        a = [P, 2 * P, 3 * P, 4, 256, 1, None]
+        a[i] += 8
+        assert f(*a) == 1
+    f = B.lib().po_op_linear_fp8_block
+    for i in (1, 3, 5, 6, 7):
+        a = [1, P, P, P, P, P, P, P, 1 << 20, 4, 128, 256, None]
+        a[i] += 8
+        assert f(*a) == 1
+
+
 def test_linear_fp8_block_bytes():
     n = C.c_size_t(7)
     f = B.lib().po_linear_fp8_block_bytes
