@@ -933,7 +933,8 @@ __global__ void __launch_bounds__(256) attn_fwd64_kernel(const bf16_t* q, const 
     if constexpr (SPLIT == 3) {
         if (piece == sp.n - 1) {
             // one source of keys: n_keys of them, of which a lane's rows see `see` and some row of the wavefront see_max
-            auto keys = [&](const bf16_t* kb, const bf16_t* vb, int64_t ld, int n_keys, int see0, int see1, int see_max) {
+            // (mixed: there are rows of other requests, which see none of them)
+            auto keys = [&](const bf16_t* kb, const bf16_t* vb, int64_t ld, int n_keys, int see0, int see1, int see_max, bool mixed) {
                 bf16x8 kf[KS], vf[2][HT];
                 auto load_k = [&](int key0) {
                     const bf16_t* const kr = kb + (int64_t)min(key0 + pk, n_keys - 1) * (Hkv * HD) + lhi * 8;
@@ -991,6 +992,30 @@ __global__ void __launch_bounds__(256) attn_fwd64_kernel(const bf16_t* q, const 
                         }
                         lrow[qt] += sum;
                     }
+                    // A value of infinity or NaN times their probabilities of 0 would spoil the other requests' rows: it counts as 0,
+                    // and the rows that see these keys become NaN by their sum.  (Exponent all ones: the sum's bits 15 and 31.)
+                    if (mixed) {
+                        uint32_t odd = 0;
+#pragma unroll
+                        for (int j2 = 0; j2 < 2; ++j2)
+#pragma unroll
+                            for (int ht = 0; ht < HT; ++ht) {
+                                uint4 w = __builtin_bit_cast(uint4, vf[j2][ht]);
+                                auto finite = [&](uint32_t& x) {
+                                    const uint32_t o = (((x & 0x7f807f80u) + 0x00800080u) >> 15) & 0x00010001u;
+                                    odd |= o;
+                                    x &= ~(o * 0xffffu);
+                                };
+                                finite(w.x); finite(w.y); finite(w.z); finite(w.w);
+                                vf[j2][ht] = __builtin_bit_cast(bf16x8, w);
+                            }
+                        if (__any(odd)) {
+                            uint32_t nan_bits = 0x7fc00000u;
+                            asm volatile("" : "+v"(nan_bits));                   // (built without honouring NaNs)
+                            if (see0 > key0) lrow[0] = __uint_as_float(nan_bits);
+                            if (see1 > key0) lrow[1] = __uint_as_float(nan_bits);
+                        }
+                    }
 #pragma unroll
                     for (int j2 = 0; j2 < 2; ++j2)
 #pragma unroll
@@ -1001,7 +1026,7 @@ __global__ void __launch_bounds__(256) attn_fwd64_kernel(const bf16_t* q, const 
             };
             if (sp.n2 > 0)
                 keys(sp.k2 + ((int64_t)sp.tiles2 * 64 * Hkv + kvh) * HD, sp.vt2 + ((int64_t)kvh * HD + l31) * sp.ldv2 + sp.tiles2 * 64, sp.ldv2,
-                     sp.n2, sp.n2, sp.n2, sp.n2);
+                     sp.n2, sp.n2, sp.n2, sp.n2, false);
             if (sp.own && qw < n_virtual) {
                 const int r0 = __builtin_amdgcn_readfirstlane(vreq[0]), r1 = __builtin_amdgcn_readlane(vreq[1], 31);
                 const int last = min(qw + 63, n_virtual - 1) / group;                  // the wavefront's last row
@@ -1010,7 +1035,7 @@ __global__ void __launch_bounds__(256) attn_fwd64_kernel(const bf16_t* q, const 
                     const int first_row = sp.tab.row0[r];
                     const int hidden = sq.kv_len - sq.q_len + 1 - first_row;           // row c of the table sees c + hidden keys
                     keys(k_own + ((int64_t)sq.kv_row * Hkv + kvh) * HD, vt_own + ((int64_t)kvh * HD + l31) * ldv_own + sq.kv_row, ldv_own, sq.kv_len,
-                         vreq[0] == r ? vrow[0] + hidden : 0, vreq[1] == r ? vrow[1] + hidden : 0, min(last, first_row + sq.q_len - 1) + hidden);
+                         vreq[0] == r ? vrow[0] + hidden : 0, vreq[1] == r ? vrow[1] + hidden : 0, min(last, first_row + sq.q_len - 1) + hidden, r0 != r1);
                 }
             }
             PO_MFMA_END();

@@ -54,6 +54,34 @@ def test_float32_with_128_rows_a_workgroup(name):
         compare(b, out, mark)
 
 
+@pytest.mark.parametrize("name", FORMS)
+def test_a_request_with_nan_keys_and_values_spoils_no_other(name):
+    form, pieces, (hq, hkv, hd), spec, n2, given = FORMS[name]
+    b = Batch(len(name), "bf16", hq, hkv, hd, requests_of(spec), n2)
+    q, k, v, k2, v2 = b.device()
+    size = B.po_attention_shared_bytes(B.PO_BF16, b.req, n2, hq, hkv, hd) if given is None else given
+    run = lambda: B.po_op_attention_shared(q, k, v, b.req, k2, v2, n2, q_prescaled=b.pre, scratch=torch.empty(size, dtype=torch.uint8, device="cuda"))
+    want = run()
+    with_keys = [r for r in b.req.tolist() if r[1] > 0 and r[3] > 0]
+    for q0, nq, k0, nk in (with_keys[0], with_keys[len(with_keys) // 2], with_keys[-1]):
+        keep = k[k0:k0 + nk].clone(), v[:, k0:k0 + nk].clone()
+        k[k0:k0 + nk], v[:, k0:k0 + nk] = float("nan"), float("inf")
+        got = run()
+        k[k0:k0 + nk], v[:, k0:k0 + nk] = keep
+        assert torch.equal(got[:q0], want[:q0]) and torch.equal(got[q0 + nq:], want[q0 + nq:])
+        # queries of NaN too: a tile may then take the exponents' references of all its rows anew, so twice the tolerance of one result,
+        # 2^-8 of the largest value for the probabilities' and the result's rounding each
+        keep = q[q0:q0 + nq].clone()
+        q[q0:q0 + nq] = float("nan")
+        got = run()
+        q[q0:q0 + nq] = keep
+        got[q0:q0 + nq] = want[q0:q0 + nq]
+        top = max(float(x.nan_to_num(0.0).abs().max()) for x in (b.v.float(), b.v2.float()))
+        assert float((got.float() - want.float()).abs().max()) <= 4 * 2.0 ** -8 * top
+        if len(with_keys) == 1:
+            break
+
+
 def test_scores_that_grow_along_the_keys():
     """the reference of the exponentials is left behind again and again, and by more than a float32 exponent covers"""
     for name in FORMS:
