@@ -804,8 +804,8 @@ def po_op_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None
     float32 log-probs [rows]).  scratch: uint8 of at least po_sample_bytes; allocated if None"""
     import torch
     rows, V = logits.shape
-    ld = logits.stride(0)
-    if rows and V and logits.stride(1) != 1:
+    ld = logits.stride(0) if rows > 1 else V                  # (one row's pitch may be any number)
+    if rows and V > 1 and logits.stride(1) != 1:
         raise ValueError("logits: a row's values must lie side by side")
     f32 = torch.float32
     stream = _operands(("logits", logits[:1], f32), ("u", u, f32), ("temperature", temperature, f32), ("top_k", top_k, torch.int32),

@@ -605,7 +605,7 @@ Plan plan(const SharedTable& t, int Hq, int Hkv, int hd, int n2, size_t scratch_
         const int64_t wgs = groups * np;
         if (wgs + own_wgs > MOST) break;
         take({SPLIT, np, per, own_per, rt, np + own_slots},
-             3.0 + std::max({wgs > 256 && wgs <= 512 ? 2.0 * pre : pre, own_most, (wgs * pre + own_wgs * own_us) / 256.0, read_us}) + 3.0 + (np + own_slots) * slot_us);
+             4.0 + std::max({wgs > 256 && wgs <= 512 ? 2.0 * pre : pre, own_most, (wgs * pre + own_wgs * own_us) / 256.0, read_us}) + 3.0 + (np + own_slots) * slot_us);
         if (np == 0) break;
     }
     return best;

@@ -21,8 +21,8 @@
 //   4  parts, for those rows: every tile's kept weight; the last workgroup of a row to finish draws.
 // What bounds it: many rows, the float64 arithmetic of the weights (8 cycles an operation and wavefront: 256 rows of 128256 without
 // filters 67 us, of which reading takes 21; 190 to 200 with top_p, whose rows are weighed three times); few rows, four launches
-// and the steps within them, each a wait for memory or a barrier: one row with top_k and top_p 35 us, with top_p alone 53.
-// 64 rows of mixed settings 104.  A row a workgroup (no parts) took 60, 176 and 178 us where these take 35, 104 and 67.
+// and the steps within them, each a wait for memory or a barrier: one row with top_k and top_p 31 us, with top_p alone 52.
+// 64 rows of mixed settings 101.  A row a workgroup (no parts) took 60, 176 and 178 us where these take 32, 101 and 67.
 #include "po_internal.h"
 
 #include <float.h>
@@ -644,8 +644,12 @@ __global__ void __launch_bounds__(NT) sample_parts_kernel(const Call c) {
     // the largest logit of a thread, and the SUB it is in; the lowest that may be drawn
     float m = -INFINITY, low = INFINITY;
     int where = 0;
+    float kept[16];                                          // the logits of a part that its wavefronts read at once
+    const bool once = c1 - c0 <= NWAVE * SUB;
     if (s.how == COUNT) clear_bins(sh);
     for_each_sub(r, c0, c1, [&](int i0, const float (&v)[16]) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) kept[j] = v[j];
         float mi = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 16; ++j) mi = fmaxf(mi, v[j]);
@@ -663,8 +667,10 @@ __global__ void __launch_bounds__(NT) sample_parts_kernel(const Call c) {
     });
     unsigned long long best = 0;
     if (m > -INFINITY) {
+        if (!once) read_sub(r, where, kept);
         int i = where + lane;                                    // (one of the 16 of this thread in that SUB)
-        for (int j = 0; j < 15 && r.z[min(i, c.V - 1)] != m; ++j) i += 64;
+#pragma unroll
+        for (int j = 15; j >= 0; --j) i = kept[j] == m ? where + lane + j * 64 : i;
         best = (unsigned long long)key_of(m) << 32 | (uint32_t)~i;
     }
     best = block_max(sh, best);
@@ -699,10 +705,16 @@ __global__ void __launch_bounds__(NT) sample_parts_kernel(const Call c) {
     if (n <= PART_CAP && best) {
         if (t == 0) sh.n_list = 0;
         __syncthreads();
-        for_each(r, c0, c1, [&](float l, int i) {
+        const auto put = [&](float l, int i) {
             const uint32_t key = key_of(l);
             if (key && key >= lowest) c.h.list[at * PART_CAP + atomicAdd(&sh.n_list, 1)] = (unsigned long long)key << 32 | (uint32_t)~i;
-        });
+        };
+        if (!once) {
+            for_each(r, c0, c1, put);
+        } else if (c0 + wave * SUB < c1) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) put(kept[j], c0 + wave * SUB + j * 64 + lane);
+        }
     }
     if (t == 0) c.h.listed[at] = best == 0 ? 0 : n <= PART_CAP ? n : PART_CAP + 1;
 }
@@ -819,12 +831,15 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(const Call c) {
         __syncthreads();
         int total = 0;
         for (int i = 0; i < c.parts; ++i) total += sh.part_end[i];
+        const auto entry = [&](int e) {
+            int i = 0;
+            while (e >= sh.part_end[i]) e -= sh.part_end[i++];
+            return c.h.list[((int64_t)row * c.parts + i) * PART_CAP + e];
+        };
+        const unsigned long long mine = whole && t < total ? entry(t) : 0;           // (a part that holds too many has none)
         const auto listed = [&](auto f) {
-            for (int e = t; e < total; e += NT) {
-                int i = 0, x = e;
-                while (x >= sh.part_end[i]) x -= sh.part_end[i++];
-                f(c.h.list[((int64_t)row * c.parts + i) * PART_CAP + x]);
-            }
+            if (t < total) f(mine);
+            for (int e = t + NT; e < total; e += NT) f(entry(e));
         };
         if (whole) {
             // what can be among the first k of them, by equal steps of keys between the lowest and the highest

@@ -83,3 +83,15 @@ def test_what_an_earlier_call_left_in_the_scratch_does_not_show():
                 want.append((tok, lp))
             else:
                 assert torch.equal(tok, want[i][0]) and torch.equal(lp, want[i][1])
+
+
+def test_one_row_or_one_column_of_any_pitch():
+    rng = np.random.default_rng(16)
+    z = torch.from_numpy((rng.standard_normal(5000) * 2).astype(np.float32)).cuda()
+    u = torch.tensor([0.37], device="cuda")
+    want = B.po_op_sample(z[None], u)
+    for pitch in (1, 7, 4999):
+        got = B.po_op_sample(z.as_strided((1, 5000), (pitch, 1)), u)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    tok, lp = B.po_op_sample(z.as_strided((3, 1), (7, 5)), u.repeat(3))
+    assert tok.tolist() == [0, 0, 0] and lp.tolist() == [0.0, 0.0, 0.0]
