@@ -222,7 +222,9 @@ __device__ int find_bin(Shared& sh, G goal_of, int base_n, double base_w, int fi
     return b;
 }
 
+// (behind a barrier: wavefronts still on their way from find_bin read the bin that it found)
 __device__ void clear_bins(Shared& sh) {
+    __syncthreads();
     for (int b = threadIdx.x; b < BINS; b += NT) { sh.count[b] = 0; sh.weight[b] = 0; }
     __syncthreads();
 }
