@@ -1073,7 +1073,7 @@ void launch_sample(const float* logits, int64_t ld, int rows, int V, const float
     // at most MAX_TILES tiles of whole SUBs; histogram weights of as many digits as V of them may add up
     c.ts = tile_of(V);
     c.fix = 62;
-    while (c.fix > 0 && ((int64_t)V << c.fix) > ((int64_t)1 << 62)) --c.fix;
+    while (V > (int64_t)1 << (62 - c.fix)) --c.fix;
     c.fix = std::min(c.fix, 44);
     c.parts = parts_of(rows, V, c.ts, &c.part_len);
     lay_out(&c.h, (unsigned char*)scratch, rows, c.parts, top_k || top_p);

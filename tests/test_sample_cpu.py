@@ -52,3 +52,10 @@ def test_parts_whose_lists_together_are_longer_than_one(lib, order):
     z = (rng.standard_normal((2, 70000)) * 0.5).astype(np.float32)
     z[:, ::9] = 3.0
     check(lib, z, rng.random(2, dtype=np.float32), None, [900, 900], [1.0, 0.5], None, order)
+
+
+@pytest.mark.parametrize("p,k", [(0.37, None), (0.71, 1600000)])
+def test_millions_of_equal_logits(lib, p, k):
+    """their weights all fall into one bin of whole numbers"""
+    z = np.full((1, (1 << 21) + 77), 0.5, dtype=np.float32)
+    check(lib, z, [0.83], None, k and [k], [p])
