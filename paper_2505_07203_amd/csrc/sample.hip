@@ -56,6 +56,7 @@ struct Shared {
     unsigned long long list[CAP];           // key << 32 | ~index: descending order is the order of the tokens
     double tile[MAX_TILES];
     float tile_top[MAX_TILES];
+    short ref[2048];                        // reference exponents of a digit's bins
     int n_list;
     int part_end[16];
     // answers of a search, written by the one thread that finds them
@@ -231,7 +232,7 @@ __device__ void clear_bins(Shared& sh) {
 
 __device__ __forceinline__ void add_to_bin(Shared& sh, int b, double w, int digits) {
     atomicAdd(&sh.count[b], 1);                               // whole numbers: the order of the additions does not show
-    const unsigned long long f = (unsigned long long)ldexp(w, digits);
+    const unsigned long long f = (unsigned long long)(ldexp(w, digits) + 0.5);      // (to the nearest: sums of many keep no bias)
     if (f) atomicAdd(&sh.weight[b], f);
 }
 
@@ -321,44 +322,103 @@ __device__ void find_in_list(Shared& sh, const Row& r, const Goal& goal, int n, 
     __syncthreads();
 }
 
-// The same over the whole row with nothing known, for bins that hold more than CAP tokens: the key digit by digit (11, 11, 10
-// bits), then the right one of the tokens with that key by a count of tiles.
-__device__ void find_in_row(Shared& sh, const Row& r, const Goal& goal, int fix) {
-    uint32_t prefix = 0;
+// Float64 sums, in one order, of the weights of the tokens above a key and of all, and the number of tokens with that key.
+struct Sums {
+    double above, all;
+    int equal;
+};
+__device__ Sums sums_at(Shared& sh, const Row& r, uint32_t key) {
+    double above = 0.0, all = 0.0;
+    int equal = 0;
+    for_each<false>(r, 0, r.V, [&](float l, int) {
+        const uint32_t x = key_of(l);
+        const double w = x ? r.weight(l, sh.table) : 0.0;
+        all += w;
+        above += x > key ? w : 0.0;
+        equal += x == key;
+    });
+    Sums s;
+    block_scan(sh, 0, all);
+    s.all = sh.scan_w[NT - 1];
+    block_scan(sh, equal, above);
+    s.above = sh.scan_w[NT - 1];
+    s.equal = sh.scan_n[NT - 1];
+    return s;
+}
+
+// The same over the whole row with nothing known, for bins that hold more tokens than a list: the key digit by digit (11, 11, 10
+// bits), then the right one of the tokens with that key by a count of tiles.  p_of_all > 0: the goal is that share of all weights,
+// and goal.sum near it.  sum_too: whether sh.cut_sum is wanted.
+// Where the goal is a sum, bins count weights in whole numbers with their highest key for reference.  Keys with the same leading bits
+// can be many powers of 2 apart, and what rounding takes from millions of weights can be worth a few others; so the key that this
+// leads to is held against float64 sums, and where it is not the one (seen for two million logits) the keys 16, 256, .. on and then
+// the middle of what is left are, at most 40 more.  One look at the sums is a pass without atomics: 35 of the 390 us of 128256 logits of
+// the bf16 grid under top_p.
+__device__ void find_in_row(Shared& sh, const Row& r, Goal goal, double p_of_all, bool sum_too, int fix) {
+    const bool by_count = goal.k > 0;
+    const uint32_t top = key_of(r.top);
+    uint32_t key = 0;
     int base_n = 0;
     double base_w = 0.0;
     for (int shift = 21; shift >= 0; shift = shift == 21 ? 10 : shift == 10 ? 0 : -1) {
-        const int bits = shift == 0 ? 10 : 11;
+        const int bits = shift == 0 ? 10 : 11, last = (1 << bits) - 1;
         const uint32_t upper = shift == 21 ? 0u : 0xffffffffu << (shift + bits);
-        // no token of this group weighs more than its highest key
-        const uint32_t high = shift == 21 ? key_of(r.top) : min(prefix | ~upper, key_of(r.top));
-        const double wh = r.weight(value_of(high), sh.table);
-        const int ref = wh > 0.0 ? ilogb(wh) + 1 : -1000;
         clear_bins(sh);
+        if (!by_count) {
+            for (int b = threadIdx.x; b <= last; b += NT) {
+                const double high = r.weight(value_of(min(key | (uint32_t)(last - b) << shift | ((1u << shift) - 1), top)), sh.table);
+                sh.ref[b] = (short)(high > 0.0 ? ilogb(high) + 1 : -1000);
+            }
+            __syncthreads();
+        }
         for_each<false>(r, 0, r.V, [&](float l, int) {
-            const uint32_t key = key_of(l);
-            if (key && (key & upper) == prefix)
-                add_to_bin(sh, (1 << bits) - 1 - (int)((key >> shift) & ((1u << bits) - 1)), r.weight(l, sh.table), fix - ref);
+            const uint32_t x = key_of(l);
+            if (!x || (x & upper) != key) return;
+            const int b = last - (int)((x >> shift) & (uint32_t)last);
+            if (by_count) atomicAdd(&sh.count[b], 1);
+            else add_to_bin(sh, b, r.weight(l, sh.table), fix - sh.ref[b]);
         });
         __syncthreads();
-        const int b = find_bin<true>(sh, [&](double) { return goal; }, base_n, base_w, fix, [&](int) { return ref; });
-        prefix |= (uint32_t)((1 << bits) - 1 - b) << shift;
+        const auto same = [&](double) { return goal; };
+        const int b = by_count ? find_bin<false>(sh, same, base_n, 0.0, 0, [](int) { return 0; })
+                               : find_bin<true>(sh, same, base_n, base_w, fix, [&](int i) { return (int)sh.ref[i & 2047]; });
+        key |= (uint32_t)(last - b) << shift;
         base_n = sh.above_n;
         base_w = sh.above_w;
         __syncthreads();
     }
     // tokens of this key: all of one weight; how many of them
-    const int ties = sh.count[1023 - (int)(prefix & 1023u)];
-    const double w = r.weight(value_of(prefix), sh.table);
-    int want = goal.k > 0 ? goal.k - base_n : ties;
-    if (goal.k <= 0 && w > 0.0) want = (int)fmin(fmax(ceil((goal.sum - base_w) / w), 1.0), (double)ties);
+    int ties = sh.count[1023 - (int)(key & 1023u)], want = goal.k - base_n;
+    double w = 0.0;
+    if (!by_count || sum_too) {
+        uint32_t low = 1, high = top, step = 16;                 // keys between which it is, and how far to go from the last one
+        bool reached = true;
+        for (;;) {
+            const Sums s = sums_at(sh, r, key);
+            ties = s.equal;
+            base_w = s.above;
+            w = r.weight(value_of(key), sh.table);
+            if (by_count || !reached) break;
+            if (p_of_all > 0.0) goal = Goal::share(p_of_all, s.all);
+            const bool enough = base_w + ties * w >= goal.sum;
+            if (base_w < goal.sum && enough) break;
+            if (base_w < goal.sum) high = key - 1;
+            else low = key + 1;
+            // (sums of these and of those above them, rounded each for itself: the goal between the two, reached by the last of them)
+            reached = low <= high;
+            const uint32_t middle = reached ? low + (high - low) / 2 : low;
+            key = middle < key ? key - min(key - middle, step) : key + min(middle - key, step);
+            step = min(step, 1u << 24) * 16;
+        }
+        if (!by_count) want = reached ? (int)fmin(ceil((goal.sum - base_w) / w), (double)ties) : ties;
+    }
     want = max(1, min(want, ties));
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     __syncthreads();
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int a = wave; a < NT; a += NWAVE) {
         int n = 0;
         if (a < r.tiles)
-            for (int i = a * r.ts + lane; i < min(r.V, (a + 1) * r.ts); i += 64) n += key_of(r.z[i]) == prefix;
+            for (int i = a * r.ts + lane; i < min(r.V, (a + 1) * r.ts); i += 64) n += key_of(r.z[i]) == key;
         for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off);
         if (lane == 0) sh.count[a] = n;
     }
@@ -368,11 +428,11 @@ __device__ void find_in_row(Shared& sh, const Row& r, const Goal& goal, int fix)
     if (wave == 0) {
         int seen = t ? sh.scan_n[t - 1] : 0;
         for (int i = t * r.ts; i < min(r.V, (t + 1) * r.ts) && seen < want; i += 64) {
-            const bool tie = i + lane < min(r.V, (t + 1) * r.ts) && key_of(r.z[i + lane]) == prefix;
+            const bool tie = i + lane < min(r.V, (t + 1) * r.ts) && key_of(r.z[i + lane]) == key;
             const unsigned long long b = __ballot(tie);
             const int upto = seen + __popcll(b & (0xffffffffffffffffull >> (63 - lane)));
             if (tie && upto == want) {
-                sh.cut = (unsigned long long)prefix << 32 | (uint32_t)~(i + lane);
+                sh.cut = (unsigned long long)key << 32 | (uint32_t)~(i + lane);
                 sh.cut_sum = base_w + want * w;
             }
             seen += __popcll(b);
@@ -825,6 +885,10 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(const Call c) {
         leave(0);
         return;
     }
+    // what the whole row has to be searched for, where lists are too short; the last kept token so far
+    Goal goal{0, 0.0};
+    double p_of_all = 0.0;
+    unsigned long long cut = 0;
     if (s.how == COUNT) {
         // the parts' lists, one behind the other: entry e of all
         int n_part = (lane & 15) < c.parts ? c.h.listed[(int64_t)row * c.parts + (lane & 15)] : 0;
@@ -867,110 +931,111 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(const Call c) {
                 return;
             }
         }
-        // (thousands of keys with the same leading bits) the k-th and, in its place, the last one that top_p leaves, from the row
-        find_in_row(sh, r, Goal{s.k, 0.0}, c.fix);
-        unsigned long long cut = sh.cut;
-        const double sum = sh.cut_sum;
-        __syncthreads();
-        if (s.by_p) {
-            find_in_row(sh, r, Goal::share(s.p, sum), c.fix);
-            cut = sh.cut > cut ? sh.cut : cut;
-        }
-        leave(cut);
-        return;
-    }
-    // ---- WEIGH: the parts' bins added up
-    const Steps st(c, row, r, s.T);
-    const auto ref = [&](int b) { return st.ref(b); };
-    {
-        static_assert(PER == 4, "a thread's bins are one and two 16-byte loads");
-        int4 n = {0, 0, 0, 0};
-        unsigned long long w[4] = {0, 0, 0, 0};
+        // (thousands of keys with the same leading bits)
+        goal.k = s.k;
+    } else {
+        // ---- WEIGH: the parts' bins added up
+        const Steps st(c, row, r, s.T);
+        const auto ref = [&](int b) { return st.ref(b); };
+        {
+            static_assert(PER == 4, "a thread's bins are one and two 16-byte loads");
+            int4 n = {0, 0, 0, 0};
+            unsigned long long w[4] = {0, 0, 0, 0};
 #pragma unroll 4
-        for (int i = 0; i < c.parts; ++i) {
-            const int64_t at = ((int64_t)row * c.parts + i) * BINS + t * 4;
-            const int4 x = *(const int4*)(c.h.count + at);
-            const ulonglong2 a = *(const ulonglong2*)(c.h.weight + at), b = *(const ulonglong2*)(c.h.weight + at + 2);
-            n.x += x.x; n.y += x.y; n.z += x.z; n.w += x.w;
-            w[0] += a.x; w[1] += a.y; w[2] += b.x; w[3] += b.y;
-        }
-        *(int4*)(sh.count + t * 4) = n;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sh.weight[t * 4 + j] = w[j];
-    }
-    __syncthreads();
-    if (s.by_k) {
-        // (more than K_MAX tokens) one workgroup; -> whether the bins still are there
-        const auto search = [&](const Goal& goal) {
-            const int b = find_bin<true>(sh, [&](double) { return goal; }, 0, 0.0, c.fix, ref), n = sh.count[b], base_n = sh.above_n;
-            const double base_w = sh.above_w;
-            if (n > CAP) {
-                find_in_row(sh, r, goal, c.fix);
-                return false;
+            for (int i = 0; i < c.parts; ++i) {
+                const int64_t at = ((int64_t)row * c.parts + i) * BINS + t * 4;
+                const int4 x = *(const int4*)(c.h.count + at);
+                const ulonglong2 a = *(const ulonglong2*)(c.h.weight + at), b = *(const ulonglong2*)(c.h.weight + at + 2);
+                n.x += x.x; n.y += x.y; n.z += x.z; n.w += x.w;
+                w[0] += a.x; w[1] += a.y; w[2] += b.x; w[3] += b.y;
             }
-            if (t == 0) sh.n_list = 0;
-            __syncthreads();
-            for_each<false>(r, 0, c.V, [&](float l, int i) {
-                if (l > -INFINITY && st.bin(l) == b) sh.list[atomicAdd(&sh.n_list, 1)] = (unsigned long long)key_of(l) << 32 | (uint32_t)~i;
-            });
-            __syncthreads();
-            sort_list(sh, n);
-            find_in_list(sh, r, goal, n, base_n, base_w);
-            return true;
-        };
-        const bool still = search(Goal{s.k, 0.0});
-        unsigned long long cut = sh.cut;
-        const double sum = sh.cut_sum;
-        __syncthreads();
-        if (s.by_p) {
-            if (!still) fill_bins<false>(sh, r, st, 0, c.V, c.fix);
-            search(Goal::share(s.p, sum));
-            cut = sh.cut > cut ? sh.cut : cut;
+            *(int4*)(sh.count + t * 4) = n;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sh.weight[t * 4 + j] = w[j];
         }
-        leave(cut);
-        return;
+        __syncthreads();
+        if (s.by_k) {
+            // (more than K_MAX tokens) one workgroup
+            const auto in_list = [&](const Goal& g) {
+                const int b = find_bin<true>(sh, [&](double) { return g; }, 0, 0.0, c.fix, ref), n = sh.count[b], base_n = sh.above_n;
+                const double base_w = sh.above_w;
+                if (n > CAP) return false;
+                if (t == 0) sh.n_list = 0;
+                __syncthreads();
+                for_each<false>(r, 0, c.V, [&](float l, int i) {
+                    if (l > -INFINITY && st.bin(l) == b) sh.list[atomicAdd(&sh.n_list, 1)] = (unsigned long long)key_of(l) << 32 | (uint32_t)~i;
+                });
+                __syncthreads();
+                sort_list(sh, n);
+                find_in_list(sh, r, g, n, base_n, base_w);
+                return true;
+            };
+            goal.k = s.k;
+            if (in_list(goal)) {
+                cut = sh.cut;
+                if (!s.by_p) {
+                    leave(cut);
+                    return;
+                }
+                goal = Goal::share(s.p, sh.cut_sum);
+                __syncthreads();
+                if (in_list(goal)) {
+                    leave(sh.cut > cut ? sh.cut : cut);
+                    return;
+                }
+            }
+        } else {
+            // top_p alone: every part's workgroup finds the bin in which it ends and lists its part's tokens of that bin, or, if they are
+            // few, of all up to it; the last one takes them together
+            const int b = find_bin<true>(sh, [&](double all) { return Goal::share(s.p, all); }, 0, 0.0, c.fix, ref);
+            const int n_bin = sh.count[b], above_n = sh.above_n;
+            const double above_w = sh.above_w, sum = sh.total_w;
+            goal = Goal::share(s.p, sum);
+            __syncthreads();
+            if (n_bin <= PART_CAP) {
+                const bool all = above_n + n_bin <= NT;
+                const int64_t at = (int64_t)row * c.parts + part;
+                const int c0 = part * c.part_len;
+                if (t == 0) sh.n_list = 0;
+                __syncthreads();
+                for_each(r, c0, min(c.V, c0 + c.part_len), [&](float l, int i) {
+                    if (!(l > -INFINITY)) return;
+                    const int x = st.bin(l);
+                    if (x == b || (all && x < b)) hand(c.h.list + at * PART_CAP + atomicAdd(&sh.n_list, 1), (unsigned long long)key_of(l) << 32 | (uint32_t)~i);
+                });
+                __syncthreads();
+                if (t == 0) hand(c.h.listed + at, sh.n_list);
+                if (!last_to_finish(sh, c.h.finished + row * 2, c.parts)) return;
+                int n = 0;
+                for (int i = 0; i < c.parts; ++i) {
+                    const int64_t from = (int64_t)row * c.parts + i;
+                    const int ni = handed(c.h.listed + from);
+                    for (int e = t; e < ni; e += NT) sh.list[n + e] = handed(c.h.list + from * PART_CAP + e);
+                    n += ni;
+                }
+                __syncthreads();
+                if (all) {
+                    finish_list(sh, r, n, false, 0, true, s.p, sum, s.floor_w, s.u, answer);
+                    return;
+                }
+                sort_list(sh, n);
+                find_in_list(sh, r, goal, n, above_n, above_w);
+                leave(sh.cut);
+                return;
+            }
+            if (part != 0) return;
+            p_of_all = s.p;
+        }
     }
-    // top_p alone: every part's workgroup finds the bin in which it ends and lists its part's tokens of that bin, or, if they are
-    // few, of all up to it; the last one takes them together
-    const int b = find_bin<true>(sh, [&](double all) { return Goal::share(s.p, all); }, 0, 0.0, c.fix, ref);
-    const int n_bin = sh.count[b], above_n = sh.above_n;
-    const double above_w = sh.above_w, sum = sh.total_w;
-    const Goal goal = Goal::share(s.p, sum);
-    __syncthreads();
-    if (n_bin > PART_CAP) {
-        if (part != 0) return;
-        find_in_row(sh, r, goal, c.fix);
-        leave(sh.cut);
-        return;
+    // the whole row: the k-th and, in its place, the last one that top_p leaves
+    for (;;) {
+        find_in_row(sh, r, goal, p_of_all, s.by_p, c.fix);
+        cut = sh.cut > cut ? sh.cut : cut;
+        if (goal.k <= 0 || !s.by_p) break;
+        goal = Goal::share(s.p, sh.cut_sum);
+        __syncthreads();
     }
-    const bool all = above_n + n_bin <= NT;
-    const int64_t at = (int64_t)row * c.parts + part;
-    const int c0 = part * c.part_len;
-    if (t == 0) sh.n_list = 0;
-    __syncthreads();
-    for_each(r, c0, min(c.V, c0 + c.part_len), [&](float l, int i) {
-        if (!(l > -INFINITY)) return;
-        const int x = st.bin(l);
-        if (x == b || (all && x < b)) hand(c.h.list + at * PART_CAP + atomicAdd(&sh.n_list, 1), (unsigned long long)key_of(l) << 32 | (uint32_t)~i);
-    });
-    __syncthreads();
-    if (t == 0) hand(c.h.listed + at, sh.n_list);
-    if (!last_to_finish(sh, c.h.finished + row * 2, c.parts)) return;
-    int n = 0;
-    for (int i = 0; i < c.parts; ++i) {
-        const int64_t from = (int64_t)row * c.parts + i;
-        const int ni = handed(c.h.listed + from);
-        for (int e = t; e < ni; e += NT) sh.list[n + e] = handed(c.h.list + from * PART_CAP + e);
-        n += ni;
-    }
-    __syncthreads();
-    if (all) {
-        finish_list(sh, r, n, false, 0, true, s.p, sum, s.floor_w, s.u, answer);
-        return;
-    }
-    sort_list(sh, n);
-    find_in_list(sh, r, goal, n, above_n, above_w);
-    leave(sh.cut);
+    leave(cut);
 }
 
 // ---- launch 4

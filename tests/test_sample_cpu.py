@@ -59,3 +59,66 @@ def test_millions_of_equal_logits(lib, p, k):
     """their weights all fall into one bin of whole numbers"""
     z = np.full((1, (1 << 21) + 77), 0.5, dtype=np.float32)
     check(lib, z, [0.83], None, k and [k], [p])
+
+
+def far_above_the_bulk(rng, V, top=14.0):
+    """one token that holds much of the weight, the rest spread over millions, 10^-7 of the whole or less each"""
+    z = rng.standard_normal((1, V)).astype(np.float32)
+    z[0, V // 3] = top
+    return z
+
+
+@pytest.mark.parametrize("seed", [1, 2])
+def test_weights_far_below_the_largest_count_in_full(lib, seed):
+    z = far_above_the_bulk(np.random.default_rng(seed), 1 << 22)
+    for u in (0.31, 0.62, 0.93):
+        check(lib, z, [u], None, None, [0.9])
+
+
+def test_weights_far_below_the_largest_with_top_k(lib):
+    rng = np.random.default_rng(3)
+    z = far_above_the_bulk(rng, 1 << 21)
+    z[0, 1::2] = np.round(z[0, 1::2] * 2) / 2
+    for u in (0.29, 0.71):
+        check(lib, z, [u], None, [1500000], [0.8])
+
+
+@pytest.mark.parametrize("T", [1.0, 0.05, 0.01, 0.001])
+@pytest.mark.parametrize("k", [0, 900, 45000])
+def test_plateaus_far_below_the_largest(lib, T, k):
+    """60000 tokens of three values, 21 to 22 powers of e below one: keys with the same leading bits, and weights hundreds of powers apart at
+    the low temperatures.  top_p ends in the middle of what top_k leaves; u near 1, since the one token has all but 10^-5 of the weight"""
+    z = np.resize(np.array([69.0 + 3 * T, 69.0 + 2.5 * T, 69.0 + 2 * T], dtype=np.float32), (1, 60000))
+    z[0, 7] = 69.0 + 24 * T
+    w = np.sort(np.exp((z[0].astype(np.float64) - z[0].max()) / np.float64(np.float32(T))))[::-1][:k or None]
+    c = np.cumsum(w)
+
+    def away_from_the_sums(x, sums):
+        """the next lower number that no running sum is near to: the weights are 7e-10 of the whole and less"""
+        x = np.float32(x)
+        while np.abs(sums - np.float64(x) * sums[-1]).min() < 5e-11 * sums[-1]:
+            x = np.nextafter(x, np.float32(0))
+        return x
+    p = away_from_the_sums(c[len(c) // 2] / c[-1], c)
+    assert p < 1 and c[0] < np.float64(p) * c[-1]
+    n = 1 + int(np.searchsorted(c, np.float64(p) * c[-1]))
+    w = np.exp((z[0].astype(np.float64) - z[0].max()) / np.float64(np.float32(T)))
+    kept = np.cumsum(w[np.sort(np.argsort(-z[0], kind="stable")[:n])])
+    for u in (0.2, 1 - 2.0 ** -18, 1 - 2.0 ** -24):
+        check(lib, z, [away_from_the_sums(u, kept)], [T], [k] if k else None, [p])
+
+
+def test_bulk_that_shares_a_bin_with_a_far_larger_token(lib):
+    """two million equal weights, 10 powers of e below the largest and in one bin of leading bits with it, each half a digit off there; the last
+    kept token is among 3000 neighbouring numbers in the next bin, at the end of the row"""
+    T, V, n = np.float32(0.18), 1 << 21, 3000
+    top = np.float32(13.9)
+    near = np.float32(12.1) + np.arange(4000, dtype=np.float32) * np.float32(2.0 ** -20)
+    digits = np.exp((near.astype(np.float64) - np.float64(top)) / np.float64(T)) * 2.0 ** 40
+    z = np.full((1, V), near[np.argmin(np.abs(digits - np.floor(digits) - 0.5))], dtype=np.float32)
+    z[0, 5], z[0, 9] = top, -20.0
+    z[0, -n:] = np.float32(11.2) - np.arange(n, dtype=np.float32) * np.float32(2.0 ** -20)
+    w = np.exp((z[0].astype(np.float64) - np.float64(top)) / np.float64(T))
+    c = np.cumsum(np.sort(w)[::-1])
+    for share in (c[-n // 2], c[-n // 3]):
+        check(lib, z, [1 - 2.0 ** -24], [T], None, [share / c[-1]])
