@@ -33,7 +33,7 @@
 namespace po {
 namespace {
 
-constexpr int NT = 1024;            // threads of a workgroup: one row
+constexpr int NT = 1024;            // threads of a workgroup: one part of a row
 constexpr int NWAVE = NT / 64;
 constexpr int BINS = 4096;
 constexpr int PER = BINS / NT;      // bins of a thread
@@ -55,7 +55,6 @@ struct Shared {
     alignas(16) int count[BINS];
     unsigned long long list[CAP];           // key << 32 | ~index: descending order is the order of the tokens
     double tile[MAX_TILES];
-    float tile_top[MAX_TILES];
     short ref[2048];                        // reference exponents of a digit's bins
     int n_list;
     int part_end[16];
