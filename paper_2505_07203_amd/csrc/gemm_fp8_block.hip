@@ -494,15 +494,17 @@ Plan plan(int epi, int64_t M, int N, int K, size_t scratch_bytes) {
 
 bool gemm_fp8_block_supported(int N, int K) { return K > 0 && K % 128 == 0 && N > 0 && N % 64 == 0; }
 
+int64_t quant_blocks_workgroups(int64_t rows, int K, int block_rows) {
+    const int64_t kb = K / 128;
+    return block_rows == 1 ? (rows * kb * 16 + 255) / 256 : (rows + 127) / 128 * kb;
+}
+
 void launch_quant_blocks(const bf16_t* x, unsigned char* q, float* scales, int64_t rows, int K, int block_rows, hipStream_t s) {
     if (rows <= 0) return;
     const int kb = K / 128;
-    if (block_rows == 1)
-        hipLaunchKernelGGL(quant_groups_kernel, dim3((unsigned)((rows * kb * 16 + 255) / 256)), dim3(256), 0, s, (const uint4*)x, (uint2*)q,
-                           scales, rows, kb);
-    else
-        hipLaunchKernelGGL(quant_blocks_kernel, dim3((unsigned)((rows + 127) / 128 * kb)), dim3(256), 0, s, (const uint4*)x, (uint2*)q,
-                           scales, rows, kb);
+    const dim3 grid((unsigned)quant_blocks_workgroups(rows, K, block_rows)), block(256);
+    if (block_rows == 1) hipLaunchKernelGGL(quant_groups_kernel, grid, block, 0, s, (const uint4*)x, (uint2*)q, scales, rows, kb);
+    else hipLaunchKernelGGL(quant_blocks_kernel, grid, block, 0, s, (const uint4*)x, (uint2*)q, scales, rows, kb);
 }
 
 size_t gemm_fp8_block_scratch(int64_t M, int N, int K) {

@@ -1691,7 +1691,7 @@ po_status po_op_quantize_blocks(const void* x, void* codes, float* scales, int64
     if (!x || !codes || !scales || x == codes || rows <= 0 || K <= 0 || (block_rows != 1 && block_rows != 128)) return PO_ERR_INVALID_ARG;
     if (misaligned16(x) || misaligned16(codes)) return PO_ERR_INVALID_ARG;
     if (K % 128) return PO_ERR_BAD_CONFIG;
-    if (rows > (int64_t)1 << 24 || rows * K > (int64_t)1 << 40) return PO_ERR_TOO_LONG;
+    if (rows > (int64_t)1 << 24 || quant_blocks_workgroups(rows, K, block_rows) > MAX_WORKGROUPS_256) return PO_ERR_TOO_LONG;
     launch_quant_blocks((const bf16_t*)x, (unsigned char*)codes, scales, rows, K, block_rows, (hipStream_t)stream);
     PO_HIP(hipGetLastError());
     return PO_OK;

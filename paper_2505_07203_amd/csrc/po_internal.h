@@ -34,6 +34,9 @@ static inline int current_device() {
     return device;
 }
 
+// HIP takes fewer than 2^32 threads in a launch's first dimension: so many workgroups of 256
+constexpr int64_t MAX_WORKGROUPS_256 = ((int64_t)1 << 24) - 1;
+
 static inline int64_t round_up64(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 // ---- launchers: "basic" kernels, any dtype (dtype: 0 = fp32, 1 = bf16) ----------------
@@ -212,6 +215,7 @@ bool attention_mfma_supported(int Hq, int Hkv, int hd);
 // ---- FP8 linear layers with a scale per block of 128 ------------------------------------------------
 // bf16 [rows, K] -> codes and scales: block_rows 1: blocks of a row x 128, scales [K / 128][rows]; block_rows 128: blocks of
 // 128 x 128, scales [ceil(rows / 128)][K / 128] (K % 128 == 0)
+int64_t quant_blocks_workgroups(int64_t rows, int K, int block_rows);      // of 256 threads
 void launch_quant_blocks(const bf16_t* x, unsigned char* q, float* scales, int64_t rows, int K, int block_rows, hipStream_t s);
 // C = sum over blocks of sa * sw * (Qa Qw^T) with the epilogues EPI_STORE, EPI_RESIDUAL, EPI_SILU_MUL (weight rows interleaved
 // gate / up in blocks of 32, scales of the gate rows then of the up rows); contiguous operands.  part (may be null): scratch for
