@@ -430,6 +430,11 @@ __global__ void __launch_bounds__(256) block_reduce_kernel(const float* __restri
     *(uint4*)(C + row * n_out + col) = make_uint4(lo.x, lo.y, hi.x, hi.y);
 }
 
+// of a split: its tiles, filled up to the same number on each XCD
+int64_t tile_workgroups(int64_t M, int N, int mr) {
+    return round_up64((M + 64 * mr - 1) / (64 * mr) * (((int64_t)N + 127) / 128), 8);
+}
+
 template <int EPI, int MR, int D>
 void launch_tile(BlockParams bp, int splits, hipStream_t s) {
     constexpr int SMEM = D * ((64 * MR + 128) * BKB + 1024);
@@ -437,9 +442,9 @@ void launch_tile(BlockParams bp, int splits, hipStream_t s) {
     static OncePerDevice lds;
     lds.run(current_device(), [] { allow_dynamic_lds((const void*)(gemm_fp8_block_kernel<EPI, MR, D>), SMEM); });
     bp.g.mt = (bp.g.M + 64 * MR - 1) / (64 * MR);
-    bp.g.nt = (bp.g.N + 127) / 128;
-    const int per_xcd = (bp.g.mt * bp.g.nt + 7) / 8;
-    hipLaunchKernelGGL((gemm_fp8_block_kernel<EPI, MR, D>), dim3((unsigned)(per_xcd * 8), (unsigned)splits), dim3(256), SMEM, s, bp);
+    bp.g.nt = (int)(((int64_t)bp.g.N + 127) / 128);
+    const dim3 grid((unsigned)tile_workgroups(bp.g.M, bp.g.N, MR), (unsigned)splits);
+    hipLaunchKernelGGL((gemm_fp8_block_kernel<EPI, MR, D>), grid, dim3(256), SMEM, s, bp);
 }
 
 template <int EPI>
@@ -462,6 +467,7 @@ void launch_strips(const BlockParams& bp, hipStream_t s) {
 // weights take from memory; and the second kernel of a split launch.  Fitted to 28 shapes (1 .. 3000 rows; 4096 x 14336,
 // 4096 x 4096, 28672 x 4096, 7168 x 5120), every height and 1 .. 16 splits: the pick is 1.4 % off the fastest on average, 7 % at most.
 // Strips (mr 0) where those are expected to take less: a compute unit takes in 23 KB of its strips a microsecond, less with more rows.
+// What has more workgroups than a launch takes does not come into it.
 struct Plan {
     int mr, per;
 };
@@ -471,7 +477,8 @@ Plan plan(int epi, int64_t M, int N, int K, size_t scratch_bytes) {
     Plan best{1, slices};
     double t_best = 1e30;
     for (int mr = 1; mr <= 4; ++mr) {
-        const int64_t tiles = ((M + 64 * mr - 1) / (64 * mr)) * ((N + 127) / 128);
+        const int64_t tiles = ((M + 64 * mr - 1) / (64 * mr)) * (((int64_t)N + 127) / 128);
+        if (tile_workgroups(M, N, mr) > MAX_WORKGROUPS_256) continue;
         for (int splits = 1; splits <= 16 && 2 * splits <= std::max(slices, 2); ++splits) {
             const int per = (slices + splits - 1) / splits, n = (slices + per - 1) / per;
             const double bytes = (double)n * (double)M * N * 4.0;
@@ -485,7 +492,7 @@ Plan plan(int epi, int64_t M, int N, int K, size_t scratch_bytes) {
     if (M <= 16) {
         const int rows = epi == EPI_SILU_MUL ? 32 : 16, strips = N / rows;
         const double turns = strips <= 768 ? (strips + 255) / 256 : strips / 256.0;        // (then several share a compute unit)
-        if (3.9 + turns * rows * (double)K * (1.0 + 0.023 * M) / 23.0e3 < t_best) best = {0, slices};
+        if (strips <= MAX_WORKGROUPS_256 && 3.9 + turns * rows * (double)K * (1.0 + 0.023 * M) / 23.0e3 < t_best) best = {0, slices};
     }
     return best;
 }
@@ -493,6 +500,7 @@ Plan plan(int epi, int64_t M, int N, int K, size_t scratch_bytes) {
 }  // namespace
 
 bool gemm_fp8_block_supported(int N, int K) { return K > 0 && K % 128 == 0 && N > 0 && N % 64 == 0; }
+bool gemm_fp8_block_fits(int64_t M, int N) { return tile_workgroups(M, N, 4) <= MAX_WORKGROUPS_256; }
 
 int64_t quant_blocks_workgroups(int64_t rows, int K, int block_rows) {
     const int64_t kb = K / 128;

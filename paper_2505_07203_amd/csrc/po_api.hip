@@ -1701,7 +1701,7 @@ po_status po_op_quantize_blocks(const void* x, void* codes, float* scales, int64
 static po_status fp8_block_shape(int64_t M, int32_t N, int32_t K) {
     if (M <= 0 || N <= 0 || K <= 0) return PO_ERR_INVALID_ARG;
     if (!gemm_fp8_block_supported(N, K)) return PO_ERR_BAD_CONFIG;
-    if (M > (int64_t)1 << 24 || K >= 1 << 23 || M * N > (int64_t)1 << 40) return PO_ERR_TOO_LONG;
+    if (M > (int64_t)1 << 24 || K >= 1 << 23 || !gemm_fp8_block_fits(M, N)) return PO_ERR_TOO_LONG;
     return PO_OK;
 }
 

@@ -221,6 +221,7 @@ void launch_quant_blocks(const bf16_t* x, unsigned char* q, float* scales, int64
 // gate / up in blocks of 32, scales of the gate rows then of the up rows); contiguous operands.  part (may be null): scratch for
 // launches of few tiles, which split the reduction with it; gemm_fp8_block_scratch: what that takes at most.
 bool gemm_fp8_block_supported(int N, int K);
+bool gemm_fp8_block_fits(int64_t M, int N);        // in a launch, in tiles of 256 rows
 size_t gemm_fp8_block_scratch(int64_t M, int N, int K);
 void launch_gemm_fp8_block(int epi, const unsigned char* A, const float* sa, const unsigned char* W, const float* sw, bf16_t* C,
                            const bf16_t* R, int64_t M, int N, int K, float* part, size_t part_bytes, hipStream_t s);
