@@ -559,15 +559,17 @@ Plan plan(const SharedTable& t, int Hq, int Hkv, int hd, int n2, size_t scratch_
         return std::max(us * narrow, keys_read * key_bytes / 4.2e6);
     };
     double t_best = 5.0 + tokens_us((double)tiles32 * Hkv, n2 + own_max, n2 + seen, (double)n2 + own_sum);
+    // (pieces that one launch can join: hd / 4 threads a row and head)
+    const bool joined = ((int64_t)rows * Hq * (hd / 4) + 255) / 256 <= MAX_WORKGROUPS_256;
     const auto take = [&](const Plan& p, double us) {
-        if (us < t_best && p.slots * row_bytes <= (double)scratch_bytes) { best = p; t_best = us; }
+        if (us < t_best && (p.slots == 0 || joined) && p.slots * row_bytes <= (double)scratch_bytes) { best = p; t_best = us; }
     };
     // 128 rows a workgroup: 64 keys 1.3 us alone, 0.85 a workgroup with two on a compute unit, 6 more for its beginning and end
     const double wg128 = (double)tiles128 * Hkv, c1 = hd == 128 ? 1.3 : 0.9, c2 = hd == 128 ? 0.85 : 0.65;
     take({ROWS, 0, 0, 0, 1, 0}, 5.0 + std::max((wg128 <= 256 ? c1 : 2.0 * c2) * (std::ceil((n2 + own_max) / 64.0) + 2.0),
                                               std::max(wg128 / 256.0 * c2 * ((n2 + seen) / 64.0 + 6.0), ((double)n2 + own_sum) * key_bytes / 3.6e6)));
     if (n2 == 0 && own_max == 0) return best;
-    constexpr int64_t MOST = 1 << 24;                         // workgroups of a form with pieces: far beyond where pieces help
+    constexpr int64_t MOST = MAX_WORKGROUPS_256;              // workgroups of a launch of pieces
     // own keys by pieces, and the join
     const int own_per = (int)std::min<int64_t>(2048, std::max<int64_t>(512, (own_sum * Hkv / 256 + 255) / 256 * 256));
     const int own_slots = ceil_div(own_max, own_per);
@@ -582,7 +584,7 @@ Plan plan(const SharedTable& t, int Hq, int Hkv, int hd, int n2, size_t scratch_
         const double finish_rows = std::ceil((double)vr / (double)tiles32 / 4.0);        // (128 threads: four rows at once)
         for (int np = 1; np <= std::min(tiles2, 64); ++np) {
             const int per = ceil_div(tiles2, np);
-            if (ceil_div(tiles2, per) != np || (uint64_t)per * 64 * (uint64_t)Hkv * 256 >= (1ull << 32)) continue;
+            if (ceil_div(tiles2, per) != np || (uint64_t)per * 64 * (uint64_t)Hkv * 256 >= (1ull << 32) || wgs * np > MOST) continue;
             const double us = 6.0 + ceil_div(wgs * np, 256) * (per + 5) * 1.35;
             take({TILES, np, 0, 0, 1, np > 1 ? np : 0}, us + ceil_div(wgs, 256) * in_tile + (np > 1 ? 4.0 + np * slot_us : 0.0));
             if (!own_wgs || own_wgs > MOST) continue;

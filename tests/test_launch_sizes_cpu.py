@@ -28,3 +28,16 @@ def test_linear_fp8_block(M, N):
 def test_linear_fp8_block_below(M, N):
     assert ((M + 255) // 256) * ((N + 127) // 128) < (1 << 24) - 8
     assert B.po_linear_fp8_block_bytes(M, N, 128) == 0
+
+
+@pytest.mark.parametrize("n,q_len,kv_len,n2,heads", [(2, 2151765, 1, 3191445, (32, 8, 128)), (64, 530799, 663537, 11307814, (4, 1, 128)),
+                                                     (8, 187627, 1, 16361822, (64, 64, 128)), (20, 17039, 458, 16067298, (320, 64, 128)),
+                                                     (64, 4349, 0, 655911, (512, 64, 128))])
+def test_attention_shared(n, q_len, kv_len, n2, heads):
+    """the prefix in pieces: the tiles' launch times the pieces, and the launch that joins them with hd / 4 threads a row and head"""
+    Hq, Hkv, hd = heads
+    form, pieces = B.po_attention_shared_form([(i * q_len, q_len, 0, kv_len) for i in range(n)], n2, Hq, Hkv, hd)
+    if form.startswith("TILES"):
+        assert (n * q_len * (Hq // Hkv) + 255) // 256 * Hkv * pieces * 256 < 1 << 32
+    if form in ("SPLIT", "TILES_SPLIT") or (form == "TILES" and pieces > 1):
+        assert n * q_len * Hq * (hd // 4) < 1 << 32
