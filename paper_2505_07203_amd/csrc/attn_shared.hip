@@ -595,6 +595,8 @@ Plan plan(const SharedTable& t, int Hq, int Hkv, int hd, int n2, size_t scratch_
         }
     }
     // the prefix like the own keys, with 32 or 64 rows of any requests: 256 keys of a workgroup 1.9 or 5 us, 3 or 10 for its beginning and end
+    // (the 4.0 of it, at near ties: with 3.0, 43 single tokens of 40 heads with 370 keys alone took 29 us by pieces instead of 17, and 39 x 8
+    // rows with 652 keys 41 instead of 27; 79 x 1 with 92 keys behind 1082 lose most by it, 44 instead of 35)
     const int rt = vr <= 32 ? 1 : 2;
     const int64_t groups = (vr + 32 * rt - 1) / (32 * rt) * Hkv;
     const double own_us = own_wgs ? (3.0 + 1.9 * std::ceil(std::min<double>(own_per, seen) / 256)) * narrow : 0.0;

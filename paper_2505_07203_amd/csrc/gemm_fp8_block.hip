@@ -73,6 +73,7 @@ __global__ void __launch_bounds__(256) quant_groups_kernel(const uint4* __restri
 }
 
 // Blocks of 128 x 128, a workgroup each (the last row of blocks may be shorter): scales[block of rows][block of K].
+// Bound by memory: 4096 x 14336 29 us (6.1 TB/s read and written), 28672 x 4096 64 (5.5), 4096 x 4096 10.4, too few bytes for a full rate.
 __global__ void __launch_bounds__(256) quant_blocks_kernel(const uint4* __restrict__ x, uint2* __restrict__ q,
                                                            float* __restrict__ scales, int64_t rows, int kb) {
     __shared__ float part[4];

@@ -20,10 +20,11 @@
 //   3  rows: the head of the order that holds everything kept, gathered and sorted in LDS, and the draw; or, where that is longer
 //      than a list, the last kept token.
 //   4  parts, for those rows: every tile's kept weight; the last workgroup of a row to finish draws.
-// What bounds it: many rows, the float64 arithmetic of the weights (8 cycles an operation and wavefront: 256 rows of 128256 without
-// filters 67 us, of which reading takes 21; 190 to 200 with top_p, whose rows are weighed three times); few rows, four launches
-// and the steps within them, each a wait for memory or a barrier: one row with top_k and top_p 31 us, with top_p alone 52.
-// 64 rows of mixed settings 101.  A row a workgroup (no parts) took 60, 176 and 178 us where these take 32, 101 and 67.
+// What bounds it: many rows, the float64 arithmetic of the weights (8 cycles an operation and wavefront: 256 rows of 152064 without
+// filters 64 us, of which reading takes 25; 112 with min_p, 217 with top_p, whose rows are weighed three times; 48 greedy); few rows,
+// four launches and the steps within them, each a wait for memory or a barrier: one row of 128256 with top_k and top_p 32 us, with
+// top_p alone 56, with min_p 25, greedy 9.  64 rows of mixed settings 99.  A row a workgroup (no parts) took 60, 176 and 178 us where
+// these take 32, 99 and 64.
 #include "po_internal.h"
 
 #include <float.h>
