@@ -99,13 +99,14 @@ struct Row {
     }
 };
 
-// the SUB logits from i0 on, lane l the ones at i0 + l, + 64, ..; -inf past the end
+// the SUB logits from i0 on, lane l the ones at i0 + l, + 64, ..; -inf past the end.  (The sum quiets a signalling NaN, which the larger of
+// it and a number would otherwise be; of a quiet one and a number it is the number.)
 __device__ __forceinline__ void read_sub(const Row& r, int i0, float (&v)[16]) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
         const int i = i0 + j * 64 + lane;
-        const float x = r.z[min(i, r.V - 1)];
+        const float x = r.z[min(i, r.V - 1)] + 0.0f;
         v[j] = i < r.V ? x : -INFINITY;
     }
 }

@@ -46,3 +46,21 @@ def test_vocabularies_of_the_bf16_grid():
     z = torch.from_numpy((rng.standard_normal((8, 128256)) + 10).astype(np.float32)).to(torch.bfloat16).float().numpy()
     z[:, 77] = 26.0
     check(z, rng.random(8, dtype=np.float32), None, [0, 0, 0, 0, 20000, 90000, 900, 0], [0.999, 0.9995, 0.9999, 0.99995, 0.99, 0.9995, 0.9, 0.99999])
+
+
+def test_signalling_nans():
+    """as memory that nobody wrote may hold them; and rows of random bits"""
+    rng = np.random.default_rng(9)
+    z = (rng.standard_normal((6, 20000)) * 2).astype(np.float32)
+    z[:, 100], z[:, 17100] = 12.0, 11.5
+    bits = z.view(np.uint32)
+    bits[:, 164], bits[:, 17164], bits[:, 17228] = 0x7fa00000, 0xffa00000, 0x7f800001
+    bits[3, 200:9000] = 0x7fbfffff
+    with np.errstate(all="ignore"):
+        check(z, rng.random(6, dtype=np.float32), [1.0, 1.0, 0.0, 0.7, 1.0, 1.0], [0, 50, 0, 0, 0, 3000], [1.0, 0.9, 1.0, 0.9, 1.0, 0.8],
+              [0.0, 0.0, 0.0, 0.0, 0.1, 0.0])
+        check(z, rng.random(6, dtype=np.float32))
+        for V in (1, 70, 4000, 40000, 70000):
+            for k in (None, [1, 20, 1000, 1025, 3000, 0, 5, 60] * 4):
+                check(rng.integers(0, 2 ** 32, (32, V), dtype=np.uint32).view(np.float32), rng.random(32, dtype=np.float32), [0.5, 1.0, 100.0, 1e30] * 8, k,
+                      k and [0.9, 0.5] * 16)

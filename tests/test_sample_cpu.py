@@ -122,3 +122,17 @@ def test_bulk_that_shares_a_bin_with_a_far_larger_token(lib):
     c = np.cumsum(np.sort(w)[::-1])
     for share in (c[-n // 2], c[-n // 3]):
         check(lib, z, [1 - 2.0 ** -24], [T], None, [share / c[-1]])
+
+
+def test_signalling_nans(lib):
+    """as memory that nobody wrote may hold them, each behind a larger logit that the same thread reads: of the two the number counts"""
+    rng = np.random.default_rng(9)
+    z = (rng.standard_normal((6, 20000)) * 2).astype(np.float32)
+    z[:, 100], z[:, 17100] = 12.0, 11.5
+    bits = z.view(np.uint32)
+    bits[:, 164], bits[:, 17164], bits[:, 17228] = 0x7fa00000, 0xffa00000, 0x7f800001
+    bits[3, 200:9000] = 0x7fbfffff
+    with np.errstate(invalid="ignore"):
+        check(lib, z, rng.random(6, dtype=np.float32), [1.0, 1.0, 0.0, 0.7, 1.0, 1.0], [0, 50, 0, 0, 0, 3000], [1.0, 0.9, 1.0, 0.9, 1.0, 0.8],
+              [0.0, 0.0, 0.0, 0.0, 0.1, 0.0])
+        check(lib, z, rng.random(6, dtype=np.float32))
