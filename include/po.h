@@ -614,7 +614,7 @@ po_status po_op_lm_head(int32_t dtype, const void* dev_x, const void* dev_w, flo
  * beginning of that order of top_k tokens; of those the shortest beginning whose sum of w is at least top_p times the sum of the
  * top_k; of those the tokens with w >= min_p; the first token always.  The token drawn is the first kept one, by INDEX, at which
  * the running sum of kept w exceeds u times their whole sum; logprobs[row] (dev_logprobs may be NULL) = log(w / sum of kept w).
- * Sums and comparisons are float64.
+ * Sums and comparisons are float64, or whole numbers of 38 binary digits or more a weight where the order of additions is free.
  * The four settings are arrays [rows] on the device, each may be NULL (off; temperature 1).  temperature <= 0 or NaN: the first of
  * the order, log-prob 0; top_k <= 0 or >= V, top_p >= 1 or NaN, min_p <= 0 or NaN: off.  u outside [0, 1) is moved to the nearest
  * value inside, NaN to 0.  Logits of -infinity and NaN are never drawn; with +infinity among them only those are.  A row

@@ -7,10 +7,11 @@
 // which the running sum of kept w exceeds u times their whole sum.
 //
 // Whole numbers come out, so sums and comparisons are float64 throughout: an error of 1e-7 in a running sum over 10^5 tokens
-// would move a draw to its neighbour once in a hundred.  The exponential is the only costly part (a float64 operation takes a
-// compute unit a cycle per wavefront): 2^y by a table of 256 values of 2^(j / 256) in LDS and a polynomial of degree 4, about 16
-// operations.  Its relative error at exp(-x) is below 4e-16 + x 2^-52 (against 64-bit mantissas, 2 10^7 random x up to 70): the
-// exponent's own rounding is most of it.
+// would move a draw to its neighbour once in a hundred.  (Bins, which many threads add to in any order, count whole numbers of 44
+// binary digits a weight, 38 with 2^24 logits.)  The exponential is the only costly part (a float64 operation takes a compute unit
+// a cycle per wavefront): 2^y by a table of 256 values of 2^(j / 256) in LDS and a polynomial of degree 4, about 16 operations.  Its
+// relative error at exp(-x) is below 4e-16 + x 2^-52 (against 64-bit mantissas, 2 10^7 random x up to 70): the exponent's own
+// rounding is most of it.
 //
 // A row is cut into parts, a workgroup each, so that few rows use many compute units, and goes through up to four launches:
 //   1  parts: nothing but a temperature: every tile's weight (SUB logits), its own largest logit for reference.  top_k up to
