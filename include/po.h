@@ -437,8 +437,9 @@ po_status po_op_attention_split_prefix(const void* dev_q, const void* dev_k, con
  * [kv_rows, Hkv, hd] (ldv, ldv2 unused).  dev_k2 [n2, Hkv, hd], dev_v2: the prefix, [Hkv*hd][ldv2] (ldv2 >= n2 a multiple of 8) or rows
  * as v; any n2, 0 = none (then they may be NULL).  What lies beyond a request's or the prefix's last key is not used, whatever it
  * holds.  head_dim 64 or 128; pointers 16-byte aligned.  Scores and values must be finite, and the exponents of 2 that scores stand
- * for (scores times log2(e) / sqrt(head_dim) with q_prescaled 0) below 2^30 in magnitude, where float32 no longer tells 64 from 0; where a
- * request's own are not, its rows may hold anything, the other requests' are as if they were.  q_prescaled as in po_op_attention. */
+ * for (scores times log2(e) / sqrt(head_dim) with q_prescaled 0) below 2^30 in magnitude, where float32 no longer tells 64 from 0, and
+ * values below 2^64 (their sums are float32, and divided last); where a request's own are not, its rows may hold anything, the other
+ * requests' are as if they were.  q_prescaled as in po_op_attention. */
 typedef struct { int64_t q_row, q_len, kv_row, kv_len; } po_request_rows;
 /* (dev_scratch may be NULL: then no call runs in parts.  po_attention_shared_bytes: the scratch that these requests can use; 0: none.
  * Host only.) */

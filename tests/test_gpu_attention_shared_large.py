@@ -8,6 +8,8 @@ import torch
 
 from paper_2505_07203_amd import binding as B
 from tests.shared_forms import FORMS, requests_of
+from tests.test_gpu_attention_shared import Batch
+from tests.test_gpu_attention_shared_forms import compare
 
 pytestmark = pytest.mark.gpu
 
@@ -38,3 +40,26 @@ def test_scores_up_to_2_to_29(name, pre):
     for q0, nq, k0, nk in req.tolist():
         if nq and n2 + nk > 0 and n2:
             assert bool((o[q0:q0 + nq].float().abs().amax((1, 2)) > 0).all())
+
+
+@pytest.mark.parametrize("above", [0.0, 14.5, -14.5])
+@pytest.mark.parametrize("name", FORMS)
+def test_values_up_to_2_to_63(name, above):
+    """the same, with own keys' scores 29 powers of 2 above the prefix's or below them: definition and tolerances of
+    tests/test_gpu_attention_shared.py, which go with the values"""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    form, pieces, (hq, hkv, hd), spec, n2, given = FORMS[name]
+    if n2 * sum(s[0] * s[1] for s in spec) > 2e6:
+        pytest.skip("a long reference")
+    b = Batch(len(name), "bf16", hq, hkv, hd, requests_of(spec), n2)
+    b.q[..., 0] = 2.0
+    b.k[..., 0] = torch.where(b.k[..., 0].isnan(), b.k[..., 0], torch.full_like(b.k[..., 0], above))
+    b.k2[:n2, :, 0] = 0.0
+    b.v, b.v2 = b.v * 2.0 ** 60, b.v2 * 2.0 ** 60                            # (of a few times 1 each)
+    q, k, v, k2, v2 = b.device()
+    out = torch.full_like(q, 777.0)
+    mark = out.clone()
+    size = B.po_attention_shared_bytes(B.PO_BF16, b.req, n2, hq, hkv, hd) if given is None else given
+    B.po_op_attention_shared(q, k, v, b.req, k2, v2, n2, out=out, q_prescaled=b.pre, scratch=torch.empty(size, dtype=torch.uint8, device="cuda"))
+    compare(b, out, mark)
