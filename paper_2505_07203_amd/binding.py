@@ -43,6 +43,8 @@ EXPORTS = [
     "po_sched_create", "po_sched_destroy", "po_sched_set_jct_model", "po_sched_fit_jct_model", "po_sched_push",
     "po_sched_size", "po_sched_pick", "po_sched_remove", "po_op_rope_static", "po_op_mfma_peak", "po_op_stream_copy",
     "po_op_quantize_blocks", "po_linear_fp8_block_bytes", "po_op_linear_fp8_block", "po_op_sample", "po_op_attention_shared", "po_attention_shared_bytes", "po_attention_shared_form", "po_sample_bytes",
+    "po_op_add_rmsnorm_quantize", "po_op_adapters", "po_adapters_bytes", "po_op_token_logprobs", "po_token_logprobs_bytes",
+    "po_op_lm_head_logprobs", "po_lm_head_logprobs_bytes",
 ]
 
 
@@ -151,6 +153,13 @@ def lib() -> C.CDLL:
     L.po_op_attention_shared.argtypes = [i32, vp, i64, vp, vp, i64, i64, vp, vp, i32, vp, vp, i64, i64, i32, i32, i32, i32, vp, sz, vp]
     L.po_attention_shared_form.argtypes = [vp, i32, i64, i32, i32, i32, sz, C.POINTER(i32), C.POINTER(i32)]
     L.po_attention_shared_bytes.argtypes = [i32, vp, i32, i64, i32, i32, i32, C.POINTER(sz)]
+    L.po_op_add_rmsnorm_quantize.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, f32, vp]
+    L.po_adapters_bytes.argtypes = [i32, vp, i32, i32, i64, i32, i32, vp, i32, C.POINTER(sz)]
+    L.po_op_adapters.argtypes = [i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, i64, i32, i32, vp, i32, vp, sz, vp]
+    L.po_token_logprobs_bytes.argtypes = [i64, i32, i32, C.POINTER(sz)]
+    L.po_op_token_logprobs.argtypes = [i32, vp, i64, i64, i32, vp, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+    L.po_lm_head_logprobs_bytes.argtypes = [i32, i64, i32, i32, C.POINTER(sz)]
+    L.po_op_lm_head_logprobs.argtypes = [i32, vp, vp, vp, vp, vp, i64, i32, i32, vp, sz, vp]
     f64 = C.c_double
     L.po_sched_create.argtypes = [f64, C.POINTER(vp)]
     L.po_sched_destroy.argtypes = [vp]
@@ -614,6 +623,77 @@ def po_op_linear_fp8_block(a_codes, a_scales, w_codes, w_scales, residual=None, 
     return c
 
 
+def po_op_add_rmsnorm_quantize(x, delta, g, eps: float, block: int = 0, normed: bool = False, codes: bool = True, h=None):
+    """bf16 x [rows, d], delta like x or None, gains g [d] -> (h = x + delta, uint8 codes [rows, d], float32 scales [rows] (block 0) or
+    [d/128, rows] (block 128), normalised bf16 rows).  h: where the sum goes, x or delta among others; without delta it is x itself.
+    normed: the bf16 rows are wanted (else None); codes: the codes are (else None, None)"""
+    import torch
+    rows, d = x.shape
+    bf16 = torch.bfloat16
+    if h is None:
+        h = x if delta is None else torch.empty_like(x)
+    stream = _operands(("x", x, bf16), ("delta", delta, bf16), ("g", g, bf16), ("h", h, bf16))
+    _shape("g", g, d)
+    _shape("h", h, rows, d)
+    if delta is not None:
+        _shape("delta", delta, rows, d)
+    y = torch.empty((rows, d), dtype=bf16, device=x.device) if normed else None
+    c = s = None
+    if codes:
+        c = torch.empty((rows, d), dtype=torch.uint8, device=x.device)
+        s = torch.empty((d // 128, rows) if block else rows, dtype=torch.float32, device=x.device)
+    check(lib().po_op_add_rmsnorm_quantize(x.data_ptr(), None if delta is None else delta.data_ptr(), g.data_ptr(),
+                                           None if h is x and delta is None else h.data_ptr(), y.data_ptr() if normed else None,
+                                           c.data_ptr() if codes else None, s.data_ptr() if codes else None, rows, d, block, eps, stream))
+    return h, c, s, y
+
+
+def _adapter_rows(segments):
+    r = np.ascontiguousarray(segments, dtype=np.int64)
+    if r.ndim != 2 or r.shape[1] != 3:
+        raise ValueError(f"segments: shape (n, 3) expected, got {r.shape}")
+    return r
+
+
+def po_adapters_bytes(dtype: int, ranks, width: int, rows: int, N: int, K: int, segments) -> int:
+    """bytes of scratch that po_op_adapters needs for these requests (host only); dtype: PO_F32 or PO_BF16"""
+    seg, rk = _adapter_rows(segments), np.ascontiguousarray(ranks, dtype=np.int32)
+    n = C.c_size_t(0)
+    check(lib().po_adapters_bytes(dtype, rk.ctypes.data, len(rk), width, rows, N, K, seg.ctypes.data, len(seg), C.byref(n)))
+    return n.value
+
+
+def po_op_adapters(x, a, b, ranks, scales, segments, residual=None, out=None, scratch=None):
+    """x [rows, K] times the adapters of its requests, onto residual [rows, N] (None: zeros) -> out (residual itself: in place; None: a new
+    tensor).  Pool a [slots, width, K], b [slots, N, width]; ranks, scales [slots] and segments, int64 [n, 3] of (row, n_rows, slot or
+    -1), on the host.  scratch: uint8 of at least po_adapters_bytes; allocated if None"""
+    import torch
+    rows, K = x.shape
+    slots, width = a.shape[:2]
+    N = b.shape[1]
+    dt = x.dtype
+    c = torch.empty((rows, N), dtype=dt, device=x.device) if out is None else out
+    stream = _operands(("x", x, dt), ("a", a, dt), ("b", b, dt), ("residual", residual, dt), ("out", c, dt), ("scratch", scratch, torch.uint8))
+    _shape("a", a, slots, width, K)
+    _shape("b", b, slots, N, width)
+    _shape("out", c, rows, N)
+    if residual is not None:
+        _shape("residual", residual, rows, N)
+    seg = _adapter_rows(segments)
+    rk, sc = np.ascontiguousarray(ranks, dtype=np.int32), np.ascontiguousarray(scales, dtype=np.float32)
+    if rk.shape != (slots,) or sc.shape != (slots,):
+        raise ValueError(f"ranks, scales: shape ({slots},) expected, got {rk.shape}, {sc.shape}")
+    code, hr, hs = _dt(x), rk.ctypes.data, seg.ctypes.data
+    if scratch is None:
+        need = C.c_size_t(0)
+        check(lib().po_adapters_bytes(code, hr, slots, width, rows, N, K, hs, len(seg), C.byref(need)))
+        scratch = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+    check(lib().po_op_adapters(code, x.data_ptr(), a.data_ptr(), b.data_ptr(), hr, sc.ctypes.data, slots, width,
+                               None if residual is None else residual.data_ptr(), c.data_ptr(), rows, N, K, hs, len(seg), scratch.data_ptr(),
+                               scratch.numel(), stream))
+    return c
+
+
 def attention_q_scale(head_dim: int) -> float:
     """log2(e) / sqrt(head_dim) as the float32 the library uses: the factor between the rotated queries and what
     po_op_attention expects with q_prescaled"""
@@ -822,6 +902,69 @@ def po_op_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None
     check(lib().po_op_sample(logits.data_ptr(), ld, rows, V, *settings, tokens.data_ptr(), logprobs.data_ptr(), scratch.data_ptr(),
                              scratch.numel(), stream))
     return tokens, logprobs
+
+
+def po_token_logprobs_bytes(rows: int, V: int, top: int = 0) -> int:
+    """bytes of scratch that po_op_token_logprobs needs (host only)"""
+    n = C.c_size_t(0)
+    check(lib().po_token_logprobs_bytes(rows, V, top, C.byref(n)))
+    return n.value
+
+
+def po_op_token_logprobs(logits, tokens=None, top: int = 0, scratch=None):
+    """float32 or bfloat16 logits [rows, V] (rows may have a pitch), int32 tokens [rows, n] or None -> (their log-probs [rows, n], entropy
+    [rows], int32 ids of the `top` most likely tokens [rows, top], their log-probs [rows, top]).  scratch: uint8 of at least
+    po_token_logprobs_bytes; allocated if None"""
+    import torch
+    rows, V = logits.shape
+    ld = logits.stride(0) if rows > 1 else V                  # (one row's pitch may be any number)
+    if rows and V > 1 and logits.stride(1) != 1:
+        raise ValueError("logits: a row's values must lie side by side")
+    if ld < V:
+        raise ValueError("logits: rows overlap")
+    stream = _operands(("logits", logits[:1], logits.dtype), ("tokens", tokens, torch.int32), ("scratch", scratch, torch.uint8))
+    n = 0
+    if tokens is not None:
+        n = tokens.shape[-1]
+        _shape("tokens", tokens, rows, n)
+    dev, f32 = logits.device, torch.float32
+    lp = torch.empty((rows, n), dtype=f32, device=dev)
+    ent = torch.empty(rows, dtype=f32, device=dev)
+    ids = torch.empty((rows, max(top, 0)), dtype=torch.int32, device=dev)
+    tlp = torch.empty((rows, max(top, 0)), dtype=f32, device=dev)
+    if scratch is None:
+        scratch = torch.empty(po_token_logprobs_bytes(rows, V, top), dtype=torch.uint8, device=dev)
+    check(lib().po_op_token_logprobs(_dt(logits), logits.data_ptr(), ld, rows, V, tokens.data_ptr() if n else None, n, top,
+                                     lp.data_ptr() if n else None, ent.data_ptr(), ids.data_ptr() if top else None, tlp.data_ptr() if top else None,
+                                     scratch.data_ptr(), scratch.numel(), stream))
+    return lp, ent, ids, tlp
+
+
+def po_lm_head_logprobs_bytes(dtype: int, rows: int, V: int, d: int) -> int:
+    """bytes of scratch that po_op_lm_head_logprobs needs (host only); dtype: PO_F32 or PO_BF16"""
+    n = C.c_size_t(0)
+    check(lib().po_lm_head_logprobs_bytes(dtype, rows, V, d, C.byref(n)))
+    return n.value
+
+
+def po_op_lm_head_logprobs(x, w, tokens=None, scratch=None):
+    """hidden rows x [rows, d] behind the LM head w [V, d], int32 tokens [rows] or None -> (their log-probs [rows] or None, entropy [rows]).
+    scratch: uint8 of at least po_lm_head_logprobs_bytes; allocated if None"""
+    import torch
+    rows, d = x.shape
+    V = w.shape[0]
+    stream = _operands(("x", x, x.dtype), ("w", w, x.dtype), ("tokens", tokens, torch.int32), ("scratch", scratch, torch.uint8))
+    _shape("w", w, V, d)
+    if tokens is not None:
+        _shape("tokens", tokens, rows)
+    code = _dt(x)
+    lp = None if tokens is None else torch.empty(rows, dtype=torch.float32, device=x.device)
+    ent = torch.empty(rows, dtype=torch.float32, device=x.device)
+    if scratch is None:
+        scratch = torch.empty(po_lm_head_logprobs_bytes(code, rows, V, d), dtype=torch.uint8, device=x.device)
+    check(lib().po_op_lm_head_logprobs(code, x.data_ptr(), w.data_ptr(), None if tokens is None else tokens.data_ptr(),
+                                       None if lp is None else lp.data_ptr(), ent.data_ptr(), rows, V, d, scratch.data_ptr(), scratch.numel(), stream))
+    return lp, ent
 
 
 def po_op_rope_table(n: int, head_dim: int, theta: float):

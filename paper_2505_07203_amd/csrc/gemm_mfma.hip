@@ -777,6 +777,15 @@ void launch_gemm_mfma(int epi, const bf16_t* A, int64_t lda, const bf16_t* W, in
     }
 }
 
+void launch_gemm_mfma_f32(const bf16_t* A, int64_t lda, const bf16_t* W, int64_t ldw, float* C, int64_t ldc, int64_t M, int N, int K,
+                          hipStream_t s) {
+    if (M <= 0 || N <= 0) return;
+    GemmParams p = base_params(A, lda, W, ldw, M, N, K);
+    p.dst = (bf16_t*)C;
+    p.ld = ldc;
+    launch_form<EPI_PARTIAL>(pick_form(TILES, p, 1), p, s, 1);
+}
+
 namespace gemm {
 
 int64_t form_tiles(const TileForm& t, int64_t M, int N) { return ((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn); }

@@ -1,0 +1,363 @@
+// Log-probabilities of given tokens, the entropy and the most likely tokens of rows of logits (gfx950).
+//
+//   m = max_i l_i,  S = sum_i exp(l_i - m),  T = sum_i (l_i - m) exp(l_i - m)
+//   log p(t) = (l_t - m) - log S,   entropy = log S - T / S
+//
+// A row is read once, in pieces by a wavefront each: (m, S, T) of a piece, and the largest logit of each of its chunks of 512.
+// A second kernel, a workgroup per row, joins the pieces and finds the first tokens of the order (logit descending, index
+// ascending).  They lie in the chunks whose largest logits come first in that order, as many chunks as tokens: an element of any
+// other chunk has the largest elements of all of those before it.  The same holds for the runs of 8 within those chunks, so
+// at most 8 elements a token are ordered in the end, whatever the row holds, and no more than `top` chunks are read again.
+// NaN counts as -infinity; -infinity has no weight; with +infinity among the logits only those have, the same each.
+#include "po_internal.h"
+
+#include <algorithm>
+
+namespace po {
+namespace {
+
+constexpr int CHUNK = 512;                       // logits; 8 a lane
+constexpr int PER_WAVE = 4;                      // chunks of a piece
+constexpr int PIECE = CHUNK * PER_WAVE;
+constexpr int MAX_TOP = 64;
+
+struct Stats { float m, s, t, pad; };            // of a piece
+
+// the logits of a lane: 8 from i on, -infinity beyond V
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const T* row, int i, int V, float (&v)[8]) {
+    if (VEC && i + 8 <= V) {
+        if (sizeof(T) == 4) {
+            const float4 a = *(const float4*)(row + i), b = *(const float4*)(row + i + 4);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
+            const uint4 a = *(const uint4*)(row + i);
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                v[2 * c] = __uint_as_float(w[c] << 16);
+                v[2 * c + 1] = __uint_as_float(w[c] & 0xffff0000u);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int c = 0; c < 8; ++c) v[c] = i + c < V ? to_f32(row[i + c]) : -INFINITY;
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+    for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
+    return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+    return v;
+}
+
+// adds a logit of a row with maximum m (finite) to S and T.  Below -200 a term is 0 in float32, and -infinity and NaN (which
+// fmaxf turns into the other operand) go there.
+__device__ __forceinline__ void add_term(float l, float m, float& s, float& t) {
+    const float d = fmaxf(l - m, -200.0f), e = __expf(d);
+    s += e;
+    t = fmaf(d, e, t);
+}
+
+// (m, S, T) of the wavefront's values, whatever is among them; every lane gets all three
+template <int N>
+__device__ __forceinline__ Stats wave_stats(const float (&v)[N]) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = fmaxf(m, v[i]);
+    m = wave_max(m);
+    Stats r = {m, 0.f, 0.f, 0.f};
+    if (m == INFINITY) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) r.s += v[i] == INFINITY ? 1.f : 0.f;
+    } else if (m > -INFINITY) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) add_term(v[i], m, r.s, r.t);
+    }
+    r.s = wave_sum(r.s);
+    r.t = wave_sum(r.t);
+    return r;
+}
+
+// Pieces of rows: a wavefront each.  at (may be null): the logit of token tokens[row], where the piece holds it.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) logprob_pieces_kernel(const T* __restrict__ logits, int64_t ld, int V, int pieces, int64_t total,
+                                                             Stats* __restrict__ stats, int64_t stats_ld, float* __restrict__ chunk_max, int chunks,
+                                                             const int32_t* __restrict__ tokens, int first_token, float* __restrict__ at) {
+    const int lane = threadIdx.x & 63;
+    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (w >= total) return;
+    const int64_t r = w / pieces;
+    const int p = (int)(w - r * pieces), i0 = p * PIECE;
+    const T* row = logits + r * ld;
+    float v[8 * PER_WAVE];
+#pragma unroll
+    for (int c = 0; c < PER_WAVE; ++c) {
+        float x[8];
+        load8<T, VEC>(row, i0 + c * CHUNK + lane * 8, V, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[c * 8 + e] = x[e];
+    }
+    if (chunk_max) {
+#pragma unroll
+        for (int c = 0; c < PER_WAVE; ++c) {
+            float m = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = fmaxf(m, v[c * 8 + e]);
+            m = wave_max(m);
+            if (lane == 0 && p * PER_WAVE + c < chunks) chunk_max[r * chunks + p * PER_WAVE + c] = m;
+        }
+    }
+    const Stats st = wave_stats(v);
+    if (lane == 0) {
+        stats[r * stats_ld + p] = st;
+        if (at) {
+            const int64_t t = (int64_t)tokens[r] - first_token;
+            if (t >= i0 && t < i0 + PIECE && t < V) at[r] = to_f32(row[t]);
+        }
+    }
+}
+
+// what joins pieces: their m, S, T relative to a common maximum
+struct Sums { double s, t; };
+__device__ __forceinline__ void join(const Stats& x, float m, Sums& r) {
+    if (x.m == m) {                              // (also where both are infinite)
+        r.s += x.s;
+        r.t += x.t;
+    } else if (x.m > -INFINITY && m < INFINITY) {
+        const double d = (double)x.m - (double)m, e = (double)__expf((float)d);
+        r.s += x.s * e;
+        r.t += ((double)x.t + d * x.s) * e;
+    }
+}
+__device__ __forceinline__ float entropy_of(const Sums& r, float m) { return m > -INFINITY ? (float)fmax(0.0, log(r.s) - r.t / r.s) : 0.f; }
+__device__ __forceinline__ float logprob_of(float l, float m, double log_s) {
+    if (!(l > -INFINITY)) return -INFINITY;      // (NaN too)
+    if (m == INFINITY) return l == INFINITY ? (float)-log_s : -INFINITY;
+    return (float)((double)l - (double)m - log_s);
+}
+
+// Orders logits: the larger key first.  0: a logit without weight.
+__device__ __forceinline__ unsigned long long order_key(float l, uint32_t index) {
+    if (!(l > -INFINITY)) return 0;
+    const uint32_t b = __float_as_uint(l + 0.0f), u = b & 0x80000000u ? ~b : b | 0x80000000u;       // (-0 is 0)
+    return ((unsigned long long)u << 32) | (uint32_t)~index;
+}
+__device__ __forceinline__ float key_logit(unsigned long long k) {
+    const uint32_t u = (uint32_t)(k >> 32);
+    return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+
+constexpr int RUNS = MAX_TOP * (CHUNK / 8);      // of the chunks that are read again
+
+// Leaves in out[0 .. min(n, top)) the largest of keys[0 .. n), in order.  All different, but for zeros, which are left out.  (The
+// callers' barriers stand around it.)
+__device__ __forceinline__ void largest(const unsigned long long* keys, int n, int top, unsigned long long* out) {
+    for (int i = threadIdx.x; i < n; i += 256) {
+        const unsigned long long k = keys[i];
+        if (k == 0) continue;
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += keys[j] > k;
+        if (rank < top) out[rank] = k;
+    }
+}
+
+// A row's answer, by a workgroup.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__ logits, int64_t ld, int V, int pieces, int chunks,
+                                                           const Stats* __restrict__ stats, const float* __restrict__ chunk_max,
+                                                           const int32_t* __restrict__ tokens, int n_tokens, float* __restrict__ logprobs,
+                                                           float* __restrict__ entropy, int top, int32_t* __restrict__ top_tokens,
+                                                           float* __restrict__ top_logprobs) {
+    __shared__ double red_s[4], red_t[4];
+    __shared__ float red_m[4];
+    __shared__ unsigned long long keys[RUNS], best[MAX_TOP];
+    __shared__ int count;
+    const int64_t r = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const T* row = logits + r * ld;
+    const Stats* st = stats + r * pieces;
+    float m = -INFINITY;
+    for (int i = tid; i < pieces; i += 256) m = fmaxf(m, st[i].m);
+    m = wave_max(m);
+    if (lane == 0) red_m[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
+    Sums sum = {0.0, 0.0};
+    for (int i = tid; i < pieces; i += 256) join(st[i], m, sum);
+    for (int off = 32; off > 0; off >>= 1) {
+        sum.s += __shfl_xor(sum.s, off);
+        sum.t += __shfl_xor(sum.t, off);
+    }
+    if (lane == 0) { red_s[wave] = sum.s; red_t[wave] = sum.t; }
+    __syncthreads();
+    sum = {red_s[0] + red_s[1] + red_s[2] + red_s[3], red_t[0] + red_t[1] + red_t[2] + red_t[3]};
+    const double log_s = log(sum.s);
+    if (tid == 0 && entropy) entropy[r] = entropy_of(sum, m);
+    for (int i = tid; i < n_tokens; i += 256) {
+        const int32_t t = tokens[r * n_tokens + i];
+        logprobs[r * n_tokens + i] = t >= 0 && t < V ? logprob_of(to_f32(row[t]), m, log_s) : -INFINITY;
+    }
+    if (top == 0) return;
+
+    // the chunks that hold them, as keys of (largest logit, chunk)
+    const float lowest = m == INFINITY ? INFINITY : -INFINITY;         // of a logit with weight
+    if (tid < MAX_TOP) best[tid] = 0;
+    const float* cm = chunk_max + r * chunks;
+    // (chunks that a list does not hold at once: in turns, the best so far among them)
+    for (int c0 = 0; c0 < chunks || c0 == 0; c0 += RUNS - MAX_TOP) {
+        const int n = min(chunks - c0, RUNS - MAX_TOP);
+        __syncthreads();
+        for (int i = tid; i < n; i += 256) keys[i] = cm[c0 + i] >= lowest ? order_key(cm[c0 + i], c0 + i) : 0;
+        if (tid < MAX_TOP) keys[n + tid] = best[tid];
+        __syncthreads();
+        if (tid < MAX_TOP) best[tid] = 0;
+        __syncthreads();
+        largest(keys, n + MAX_TOP, top, best);
+    }
+    __syncthreads();
+    int n_chunks = 0;
+    while (n_chunks < top && best[n_chunks]) ++n_chunks;
+    // (as many elements as tokens are wanted are as large as this)
+    const float floor_logit = n_chunks == top ? key_logit(best[top - 1]) : lowest;
+    // the runs of 8 in them that reach as far
+    if (tid == 0) count = 0;
+    __syncthreads();
+    for (int i = tid; i < n_chunks * (CHUNK / 8); i += 256) {
+        const int at = (int)(uint32_t)~best[i / (CHUNK / 8)] * CHUNK + (i % (CHUNK / 8)) * 8;
+        float v[8];
+        load8<T, VEC>(row, at, V, v);
+        unsigned long long k = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const unsigned long long ke = v[e] >= floor_logit ? order_key(v[e], at + e) : 0;
+            k = ke > k ? ke : k;
+        }
+        if (k) keys[atomicAdd(&count, 1)] = k;   // (their order in the list changes nothing: the keys are ranked)
+    }
+    __syncthreads();
+    const int runs = count;
+    if (tid < MAX_TOP) best[tid] = 0;
+    __syncthreads();
+    largest(keys, runs, top, best);
+    __syncthreads();
+    // their elements
+    if (tid == 0) count = 0;
+    __syncthreads();
+    for (int i = tid; i < top * 8; i += 256) {
+        if (!best[i >> 3]) continue;
+        const int at = (int)((uint32_t)~best[i >> 3] & ~7u) + (i & 7);
+        const float l = at < V ? to_f32(row[at]) : -INFINITY;
+        const unsigned long long k = l >= floor_logit ? order_key(l, at) : 0;
+        if (k) keys[atomicAdd(&count, 1)] = k;
+    }
+    __syncthreads();
+    const int n = count;
+    if (tid < MAX_TOP) best[tid] = 0;
+    __syncthreads();
+    largest(keys, n, top, best);
+    __syncthreads();
+    for (int i = tid; i < top; i += 256) {
+        const unsigned long long k = best[i];
+        top_tokens[r * top + i] = k ? (int32_t)(uint32_t)~k : -1;
+        top_logprobs[r * top + i] = k ? logprob_of(key_logit(k), m, log_s) : -INFINITY;
+    }
+}
+
+inline int pieces_of(int V) { return (V + PIECE - 1) / PIECE; }
+inline int chunks_of(int V) { return (V + CHUNK - 1) / CHUNK; }
+
+template <typename T, bool VEC>
+void run(const T* logits, int64_t ld, int64_t rows, int V, const int32_t* tokens, int n_tokens, int top, float* logprobs, float* entropy,
+         int32_t* top_tokens, float* top_logprobs, void* scratch, hipStream_t s) {
+    const int pieces = pieces_of(V), chunks = chunks_of(V);
+    Stats* stats = (Stats*)scratch;
+    float* cm = top ? (float*)(stats + rows * pieces) : nullptr;
+    const int64_t total = rows * pieces;
+    hipLaunchKernelGGL((logprob_pieces_kernel<T, VEC>), dim3((unsigned)((total + 3) / 4)), dim3(256), 0, s, logits, ld, V, pieces, total, stats,
+                       (int64_t)pieces, cm, chunks, (const int32_t*)nullptr, 0, (float*)nullptr);
+    hipLaunchKernelGGL((logprob_rows_kernel<T, VEC>), dim3((unsigned)rows), dim3(256), 0, s, logits, ld, V, pieces, chunks, stats, cm, tokens,
+                       n_tokens, logprobs, entropy, top, top_tokens, top_logprobs);
+}
+
+}  // namespace
+
+bool token_logprobs_fits(int64_t rows, int V) { return (rows * pieces_of(V) + 3) / 4 <= MAX_WORKGROUPS_256; }
+
+size_t token_logprobs_scratch(int64_t rows, int V, int top) {
+    return (size_t)rows * ((size_t)pieces_of(V) * sizeof(Stats) + (top ? (size_t)chunks_of(V) * 4 : 0));
+}
+
+void launch_token_logprobs(int dtype, const void* logits, int64_t ld, int64_t rows, int V, const int32_t* tokens, int n_tokens, int top,
+                           float* logprobs, float* entropy, int32_t* top_tokens, float* top_logprobs, void* scratch, hipStream_t s) {
+    const int esz = dtype == 0 ? 4 : 2;
+    const bool vec = (uintptr_t)logits % 16 == 0 && (rows == 1 || ld * esz % 16 == 0);
+#define PO_RUN(T, VEC) run<T, VEC>((const T*)logits, ld, rows, V, tokens, n_tokens, top, logprobs, entropy, top_tokens, top_logprobs, scratch, s)
+    if (dtype == 0) { if (vec) PO_RUN(float, true); else PO_RUN(float, false); }
+    else { if (vec) PO_RUN(bf16_t, true); else PO_RUN(bf16_t, false); }
+#undef PO_RUN
+}
+
+// ------------------------------------------------------------------ through the LM head
+// Logits of hidden rows, formed in panels of columns in scratch, each reduced to its pieces' (m, S, T) before the next.
+namespace {
+
+// columns of a panel: what stays in the memory-side cache (256 MiB of logits), at least a piece
+inline int64_t panel_width(int64_t rows, int V) {
+    return std::min(std::max<int64_t>(1, std::min<int64_t>(16, ((int64_t)1 << 26) / rows / PIECE)) * PIECE, round_up64(V, PIECE));
+}
+
+// a row's answer from its pieces: a wavefront each
+__global__ void __launch_bounds__(256) head_rows_kernel(const Stats* __restrict__ stats, int pieces, const float* __restrict__ at,
+                                                        const int32_t* __restrict__ tokens, int V, int64_t rows, float* __restrict__ logprobs,
+                                                        float* __restrict__ entropy) {
+    const int lane = threadIdx.x & 63;
+    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (r >= rows) return;
+    const Stats* st = stats + r * pieces;
+    float m = -INFINITY;
+    for (int i = lane; i < pieces; i += 64) m = fmaxf(m, st[i].m);
+    m = wave_max(m);
+    Sums sum = {0.0, 0.0};
+    for (int i = lane; i < pieces; i += 64) join(st[i], m, sum);
+    for (int off = 32; off > 0; off >>= 1) {
+        sum.s += __shfl_xor(sum.s, off);
+        sum.t += __shfl_xor(sum.t, off);
+    }
+    if (lane) return;
+    if (entropy) entropy[r] = entropy_of(sum, m);
+    if (logprobs) {
+        const int32_t t = tokens[r];
+        logprobs[r] = t >= 0 && t < V ? logprob_of(at[r], m, log(sum.s)) : -INFINITY;
+    }
+}
+
+}  // namespace
+
+size_t head_logprobs_scratch(int dtype, int64_t rows, int V, int d) {
+    return (size_t)rows * ((size_t)panel_width(rows, V) * 4 + (size_t)pieces_of(V) * sizeof(Stats) + 4);
+}
+
+void launch_head_logprobs(int dtype, const void* x, const void* w, int64_t rows, int V, int d, const int32_t* tokens, float* logprobs,
+                          float* entropy, void* scratch, hipStream_t s) {
+    const int64_t width = panel_width(rows, V);
+    const int pieces = pieces_of(V);
+    float* panel = (float*)scratch;
+    Stats* stats = (Stats*)(panel + rows * width);
+    float* at = (float*)(stats + rows * pieces);
+    for (int v0 = 0; v0 < V; v0 += (int)width) {
+        const int n = (int)std::min<int64_t>(width, V - v0), p = pieces_of(n);
+        if (dtype == 0) launch_gemm_basic(0, x, d, (const float*)w + (int64_t)v0 * d, d, panel, width, nullptr, nullptr, 0, rows, n, d, s);
+        else launch_gemm_mfma_f32((const bf16_t*)x, d, (const bf16_t*)w + (int64_t)v0 * d, d, panel, width, rows, n, d, s);
+        const int64_t total = rows * p;
+        hipLaunchKernelGGL((logprob_pieces_kernel<float, true>), dim3((unsigned)((total + 3) / 4)), dim3(256), 0, s, panel, width, n, p, total,
+                           stats + v0 / PIECE, (int64_t)pieces, (float*)nullptr, 0, tokens, v0, tokens ? at : nullptr);
+    }
+    hipLaunchKernelGGL(head_rows_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, stats, pieces, at, tokens, V, rows, logprobs, entropy);
+}
+
+}  // namespace po

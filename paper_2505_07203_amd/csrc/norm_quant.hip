@@ -1,0 +1,136 @@
+// The residual's addition, RMS norm and 8-bit codes in one pass (gfx950).
+//
+//   h = bf16(x + delta),  y = h * rsqrt(mean(h^2) + eps) * g,  codes = e4m3(y * (448 / amax)), scale = amax / 448
+//
+// amax = max |y| over a row or over each block of 128 of it.  y is a float32 number throughout: it is rounded once, to the code (and once to bf16
+// where the rows are wanted too), not to bf16 first and then to the code.
+#include "po_internal.h"
+
+#include <math.h>
+
+namespace po {
+namespace {
+
+constexpr float E4M3_MAX = 448.0f;
+constexpr float AMAX_MIN = 448.0f * 0x1p-126f;    // below it both quotients would not be normal numbers
+
+struct NormQuant {
+    const uint4 *x, *delta, *g;
+    uint4 *h, *y;
+    uint2* codes;
+    float* scales;
+    int64_t rows;
+    int vecs;                     // of 8 values in a row
+    float eps, inv_d;
+};
+
+__device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        f[2 * c] = __uint_as_float(w[c] << 16);
+        f[2 * c + 1] = __uint_as_float(w[c] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) w[c] = (uint32_t)f2bf(f[2 * c]) | ((uint32_t)f2bf(f[2 * c + 1]) << 16);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint2 encode8(const float (&f)[8], float inv) {
+    int lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[0] * inv, f[1] * inv, 0, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[2] * inv, f[3] * inv, lo, true);
+    int hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[4] * inv, f[5] * inv, 0, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[6] * inv, f[7] * inv, hi, true);
+    return make_uint2((uint32_t)lo, (uint32_t)hi);
+}
+
+// A workgroup per row, whose values stay in registers: QV vectors of 8 a thread.  BLOCK: a scale per 128 values, which 16 lanes hold.
+template <int QV, bool BLOCK>
+__global__ void __launch_bounds__(256) norm_quant_kernel(const NormQuant p) {
+    __shared__ float part[4], partm[4];
+    const int64_t row = blockIdx.x, at = row * p.vecs;
+    float f[QV][8];
+    float ss = 0.f;
+#pragma unroll
+    for (int j = 0; j < QV; ++j) {
+        const int i = threadIdx.x + j * 256;
+        if (i < p.vecs) {
+            unpack8(p.x[at + i], f[j]);
+            if (p.delta) {
+                float a[8];
+                unpack8(p.delta[at + i], a);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) a[e] += f[j][e];
+                const uint4 h = pack8(a);
+                unpack8(h, f[j]);
+                if (p.h) p.h[at + i] = h;
+            } else if (p.h) {
+                p.h[at + i] = pack8(f[j]);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ss = fmaf(f[j][e], f[j][e], ss);
+        }
+    }
+    for (int off = 32; off > 0; off >>= 1) ss += __shfl_xor(ss, off);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = ss;
+    __syncthreads();
+    const float r = 1.0f / sqrtf((part[0] + part[1] + part[2] + part[3]) * p.inv_d + p.eps);
+    float m = 0.f;
+#pragma unroll
+    for (int j = 0; j < QV; ++j) {
+        const int i = threadIdx.x + j * 256;
+        if (i < p.vecs) {
+            float g[8];
+            unpack8(p.g[i], g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                f[j][e] = f[j][e] * r * g[e];
+                m = fmaxf(m, fabsf(f[j][e]));
+            }
+            if (p.y) p.y[at + i] = pack8(f[j]);
+            if (BLOCK && p.codes) {              // (vecs is a multiple of 16: the 16 lanes of a block are here together)
+                for (int off = 8; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+                const float amax = m > 0.f ? fmaxf(m, AMAX_MIN) : E4M3_MAX;
+                p.codes[at + i] = encode8(f[j], __fdiv_rn(E4M3_MAX, amax));
+                if ((threadIdx.x & 15) == 0) p.scales[(int64_t)(i >> 4) * p.rows + row] = __fdiv_rn(amax, E4M3_MAX);
+                m = 0.f;
+            }
+        }
+    }
+    if (BLOCK || !p.codes) return;
+    for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+    if ((threadIdx.x & 63) == 0) partm[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(partm[0], partm[1]), fmaxf(partm[2], partm[3]));
+    const float amax = m > 0.f ? fmaxf(m, AMAX_MIN) : E4M3_MAX;
+    const float inv = __fdiv_rn(E4M3_MAX, amax);
+    if (threadIdx.x == 0) p.scales[row] = __fdiv_rn(amax, E4M3_MAX);
+#pragma unroll
+    for (int j = 0; j < QV; ++j) {
+        const int i = threadIdx.x + j * 256;
+        if (i < p.vecs) p.codes[at + i] = encode8(f[j], inv);
+    }
+}
+
+template <bool BLOCK>
+void run(const NormQuant& p, hipStream_t s) {
+    const dim3 grid((unsigned)p.rows), wg(256);
+    if (p.vecs <= 256) hipLaunchKernelGGL((norm_quant_kernel<1, BLOCK>), grid, wg, 0, s, p);
+    else if (p.vecs <= 512) hipLaunchKernelGGL((norm_quant_kernel<2, BLOCK>), grid, wg, 0, s, p);
+    else if (p.vecs <= 1024) hipLaunchKernelGGL((norm_quant_kernel<4, BLOCK>), grid, wg, 0, s, p);
+    else hipLaunchKernelGGL((norm_quant_kernel<8, BLOCK>), grid, wg, 0, s, p);
+}
+
+}  // namespace
+
+void launch_add_rmsnorm_quantize(const bf16_t* x, const bf16_t* delta, const bf16_t* g, bf16_t* h, bf16_t* y, unsigned char* codes, float* scales,
+                                 int64_t rows, int d, bool blocks, float eps, hipStream_t s) {
+    const NormQuant p = {(const uint4*)x, (const uint4*)delta, (const uint4*)g, (uint4*)h, (uint4*)y, (uint2*)codes, scales, rows, d / 8, eps,
+                         1.0f / (float)d};
+    if (blocks) run<true>(p, s);
+    else run<false>(p, s);
+}
+
+}  // namespace po

@@ -2,6 +2,7 @@
 // (layer loop, token-chunk loop, one HIP stream, no device<->host synchronisation inside
 // a request except the final one).
 #include "../../include/po.h"
+#include "adapters.h"
 #include "attn_shared.h"
 #include "po_internal.h"
 
@@ -1788,6 +1789,112 @@ po_status po_op_sample(const float* logits, int64_t ld, int64_t rows, int32_t V,
     if (st != PO_OK) return st;
     if (scratch_bytes < sample_scratch(rows, V, top_k != nullptr, top_p != nullptr)) return PO_ERR_WORKSPACE_TOO_SMALL;
     launch_sample(logits, ld, (int)rows, V, u, temperature, top_k, top_p, min_p, tokens, logprobs, scratch, (hipStream_t)stream);
+    PO_HIP(hipGetLastError());
+    return PO_OK;
+}
+
+po_status po_op_add_rmsnorm_quantize(const void* x, const void* delta, const void* g, void* h, void* y, void* codes, float* scales, int64_t rows,
+                                     int32_t d, int32_t block, float eps, void* stream) {
+    if (!x || !g || (!y && !codes) || (codes != nullptr) != (scales != nullptr) || rows <= 0 || d <= 0) return PO_ERR_INVALID_ARG;
+    if ((block != 0 && block != 128) || (h && h == y) || !(eps >= 0.f)) return PO_ERR_INVALID_ARG;
+    if (codes && (codes == x || codes == delta || codes == h || codes == y)) return PO_ERR_INVALID_ARG;
+    if (misaligned16(x) || misaligned16(delta) || misaligned16(g) || misaligned16(h) || misaligned16(y) || misaligned16(codes)) return PO_ERR_INVALID_ARG;
+    if (d % 8 || (block && d % block) || d > 16384) return PO_ERR_BAD_CONFIG;
+    if (rows > MAX_WORKGROUPS_256) return PO_ERR_TOO_LONG;
+    launch_add_rmsnorm_quantize((const bf16_t*)x, (const bf16_t*)delta, (const bf16_t*)g, (bf16_t*)h, (bf16_t*)y, (unsigned char*)codes, scales,
+                                rows, d, block != 0, eps, (hipStream_t)stream);
+    PO_HIP(hipGetLastError());
+    return PO_OK;
+}
+
+// slots, rows ascending and apart within `rows`, sizes that the kernels' numbers hold
+static po_status adapter_shape(int32_t dtype, const int32_t* ranks, int32_t n_slots, int32_t width, int64_t rows, int32_t N, int32_t K,
+                               const po_adapter_rows* seg, int32_t n_seg) {
+    if (bad_dtype(dtype) || !ranks || n_slots <= 0 || width <= 0 || rows <= 0 || N <= 0 || K <= 0 || n_seg < 0 || (n_seg && !seg)) return PO_ERR_INVALID_ARG;
+    if (width % 8 || width > 128 || N % 8 || K % 8) return PO_ERR_BAD_CONFIG;
+    if (rows > (int64_t)1 << 23 || N > 1 << 22 || K > 1 << 22) return PO_ERR_TOO_LONG;
+    for (int32_t i = 0; i < n_slots; ++i)
+        if (ranks[i] < 0 || ranks[i] > width) return PO_ERR_INVALID_ARG;
+    int64_t row = 0;
+    for (int32_t i = 0; i < n_seg; ++i) {
+        if (seg[i].row < row || seg[i].n_rows < 0 || seg[i].row > rows || seg[i].n_rows > rows - seg[i].row) return PO_ERR_INVALID_ARG;
+        if (seg[i].adapter < -1 || seg[i].adapter >= n_slots) return PO_ERR_INVALID_ARG;
+        row = seg[i].row + seg[i].n_rows;
+    }
+    return PO_OK;
+}
+
+po_status po_adapters_bytes(int32_t dtype, const int32_t* ranks, int32_t n_slots, int32_t width, int64_t rows, int32_t N, int32_t K,
+                            const po_adapter_rows* segments, int32_t n_segments, size_t* scratch_bytes) {
+    if (!scratch_bytes) return PO_ERR_INVALID_ARG;
+    const po_status st = adapter_shape(dtype, ranks, n_slots, width, rows, N, K, segments, n_segments);
+    if (st == PO_OK) *scratch_bytes = adapters_scratch(rows, width);
+    return st;
+}
+
+po_status po_op_adapters(int32_t dtype, const void* x, const void* a, const void* b, const int32_t* ranks, const float* scales, int32_t n_slots,
+                         int32_t width, const void* residual, void* c, int64_t rows, int32_t N, int32_t K, const po_adapter_rows* segments,
+                         int32_t n_segments, void* scratch, size_t scratch_bytes, void* stream) {
+    if (!x || !a || !b || !scales || !c || x == c || x == residual) return PO_ERR_INVALID_ARG;
+    const po_status st = adapter_shape(dtype, ranks, n_slots, width, rows, N, K, segments, n_segments);
+    if (st != PO_OK) return st;
+    if (misaligned16(x) || misaligned16(a) || misaligned16(b) || misaligned16(residual) || misaligned16(c) || ((uintptr_t)scratch & 255)) return PO_ERR_INVALID_ARG;
+    const size_t need = adapters_scratch(rows, width);
+    if (need && !scratch) return PO_ERR_INVALID_ARG;
+    if (scratch_bytes < need) return PO_ERR_WORKSPACE_TOO_SMALL;
+    launch_adapters(dtype, x, a, b, ranks, scales, width, residual, c, rows, N, K, segments, n_segments, (float*)scratch, (hipStream_t)stream);
+    PO_HIP(hipGetLastError());
+    return PO_OK;
+}
+
+static po_status logprob_shape(int64_t rows, int32_t V, int32_t top) {
+    if (rows <= 0 || V <= 0 || top < 0 || top > 64) return PO_ERR_INVALID_ARG;
+    return rows > 1 << 20 || V > 1 << 24 || !token_logprobs_fits(rows, V) ? PO_ERR_TOO_LONG : PO_OK;
+}
+
+po_status po_token_logprobs_bytes(int64_t rows, int32_t V, int32_t top, size_t* scratch_bytes) {
+    if (!scratch_bytes) return PO_ERR_INVALID_ARG;
+    const po_status st = logprob_shape(rows, V, top);
+    if (st == PO_OK) *scratch_bytes = token_logprobs_scratch(rows, V, top);
+    return st;
+}
+
+po_status po_op_token_logprobs(int32_t dtype, const void* logits, int64_t ld, int64_t rows, int32_t V, const int32_t* tokens, int32_t n_tokens,
+                               int32_t top, float* logprobs, float* entropy, int32_t* top_tokens, float* top_logprobs, void* scratch,
+                               size_t scratch_bytes, void* stream) {
+    if (bad_dtype(dtype) || !logits || !scratch || ((uintptr_t)scratch & 255) || ld < V || n_tokens < 0) return PO_ERR_INVALID_ARG;
+    if ((n_tokens && (!tokens || !logprobs)) || (top && (!top_tokens || !top_logprobs)) || (!n_tokens && !top && !entropy)) return PO_ERR_INVALID_ARG;
+    if ((uintptr_t)logits & (dtype == PO_F32 ? 3 : 1)) return PO_ERR_INVALID_ARG;
+    const po_status st = logprob_shape(rows, V, top);
+    if (st != PO_OK) return st;
+    if (scratch_bytes < token_logprobs_scratch(rows, V, top)) return PO_ERR_WORKSPACE_TOO_SMALL;
+    launch_token_logprobs(dtype, logits, ld, rows, V, tokens, n_tokens, top, logprobs, entropy, top_tokens, top_logprobs, scratch, (hipStream_t)stream);
+    PO_HIP(hipGetLastError());
+    return PO_OK;
+}
+
+static po_status head_shape(int32_t dtype, int64_t rows, int32_t V, int32_t d) {
+    if (bad_dtype(dtype) || rows <= 0 || V <= 0 || d <= 0) return PO_ERR_INVALID_ARG;
+    if (d % (dtype == PO_F32 ? 4 : 64)) return PO_ERR_BAD_CONFIG;
+    // (tiles of both operands are addressed with 32-bit offsets)
+    return rows > 1 << 20 || V > 1 << 24 || d > 1 << 16 || !token_logprobs_fits(rows, V) ? PO_ERR_TOO_LONG : PO_OK;
+}
+
+po_status po_lm_head_logprobs_bytes(int32_t dtype, int64_t rows, int32_t V, int32_t d, size_t* scratch_bytes) {
+    if (!scratch_bytes) return PO_ERR_INVALID_ARG;
+    const po_status st = head_shape(dtype, rows, V, d);
+    if (st == PO_OK) *scratch_bytes = head_logprobs_scratch(dtype, rows, V, d);
+    return st;
+}
+
+po_status po_op_lm_head_logprobs(int32_t dtype, const void* x, const void* w, const int32_t* tokens, float* logprobs, float* entropy, int64_t rows,
+                                 int32_t V, int32_t d, void* scratch, size_t scratch_bytes, void* stream) {
+    if (!x || !w || !scratch || ((uintptr_t)scratch & 255) || misaligned16(x) || misaligned16(w)) return PO_ERR_INVALID_ARG;
+    if ((tokens != nullptr) != (logprobs != nullptr) || (!tokens && !entropy)) return PO_ERR_INVALID_ARG;
+    const po_status st = head_shape(dtype, rows, V, d);
+    if (st != PO_OK) return st;
+    if (scratch_bytes < head_logprobs_scratch(dtype, rows, V, d)) return PO_ERR_WORKSPACE_TOO_SMALL;
+    launch_head_logprobs(dtype, x, w, rows, V, d, tokens, logprobs, entropy, scratch, (hipStream_t)stream);
     PO_HIP(hipGetLastError());
     return PO_OK;
 }

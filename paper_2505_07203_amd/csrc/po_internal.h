@@ -232,6 +232,25 @@ void launch_sample(const float* logits, int64_t ld, int rows, int V, const float
 // bytes of scratch (256-byte aligned) that it needs, by which settings are given
 size_t sample_scratch(int64_t rows, int V, bool top_k, bool top_p);
 
+// ---- operators around the shared products ------------------------------------------------------------
+// h = bf16(x + delta), y = rmsnorm(h; g), codes and scales of y per row or (blocks) per 128 values of it, scales [d / 128][rows]; delta, h,
+// y and codes may each be null (d % 8 == 0, blocks: d % 128 == 0; d <= 16384)
+void launch_add_rmsnorm_quantize(const bf16_t* x, const bf16_t* delta, const bf16_t* g, bf16_t* h, bf16_t* y, unsigned char* codes, float* scales,
+                                 int64_t rows, int d, bool blocks, float eps, hipStream_t s);
+
+// log-probs of given tokens, entropy (may be null) and the `top` most likely tokens of each row of logits (row pitch ld)
+bool token_logprobs_fits(int64_t rows, int V);                     // in a launch
+size_t token_logprobs_scratch(int64_t rows, int V, int top);
+void launch_token_logprobs(int dtype, const void* logits, int64_t ld, int64_t rows, int V, const int32_t* tokens, int n_tokens, int top,
+                           float* logprobs, float* entropy, int32_t* top_tokens, float* top_logprobs, void* scratch, hipStream_t s);
+// the same of one token a row (or none: tokens and logprobs null) and the entropy, of the logits x w^T, which are not kept
+size_t head_logprobs_scratch(int dtype, int64_t rows, int V, int d);
+void launch_head_logprobs(int dtype, const void* x, const void* w, int64_t rows, int V, int d, const int32_t* tokens, float* logprobs,
+                          float* entropy, void* scratch, hipStream_t s);
+// C (float32, row pitch ldc) = A W^T of bf16 operands, K % 64 == 0; ldc a multiple of 64, and columns up to the next multiple of 64 are written
+void launch_gemm_mfma_f32(const bf16_t* A, int64_t lda, const bf16_t* W, int64_t ldw, float* C, int64_t ldc, int64_t M, int N, int K,
+                          hipStream_t s);
+
 // ---- micro-peaks (measurement only)
 double launch_mfma_peak(int kind, int waves_per_simd, int iters, const void* operands, size_t operand_bytes, float* sink,
                         hipStream_t s);
