@@ -38,79 +38,119 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
     for (int c = 0; c < 4; ++c) w[c] = (uint32_t)f2bf(f[2 * c]) | ((uint32_t)f2bf(f[2 * c + 1]) << 16);
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ uint2 encode8(const float (&f)[8], float inv) {
-    int lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[0] * inv, f[1] * inv, 0, false);
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[2] * inv, f[3] * inv, lo, true);
-    int hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[4] * inv, f[5] * inv, 0, false);
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[6] * inv, f[7] * inv, hi, true);
+// What a code is a multiple of.  The row's 1 / rms cancels in y * (448 / amax): with p = h * g (exact, a product of two bf16 numbers) and
+// pm = max |p| the code is that of p * 448 / pm, which inv + inv_lo (448 / pm to 2^-46) gives with one rounding, so that codes are those of exact
+// arithmetic but for values within 2^-24 of a border.  Where p or 448 / pm leaves the range of normal numbers, or amax is raised, y itself is taken.
+struct Code {
+    float inv, inv_lo, scale;
+    bool of_p;
+};
+__device__ __forceinline__ Code code_of(float pm, float r) {
+    const float ym = pm * r;
+    Code c;
+    c.of_p = pm >= 0x1p-100f && pm < 0x1p120f && ym >= AMAX_MIN && ym < 0x1p120f;
+    if (c.of_p) {
+        c.inv = __fdiv_rn(E4M3_MAX, pm);
+        c.inv_lo = __fdiv_rn(fmaf(-c.inv, pm, E4M3_MAX), pm);
+        c.scale = __fdiv_rn(ym, E4M3_MAX);
+    }
+    return c;
+}
+__device__ __forceinline__ Code code_of_y(float ym) {
+    const float amax = ym > 0.f ? fmaxf(ym, AMAX_MIN) : E4M3_MAX;
+    return {__fdiv_rn(E4M3_MAX, amax), 0.f, __fdiv_rn(amax, E4M3_MAX), false};
+}
+__device__ __forceinline__ uint2 encode8(const float (&h)[8], const float (&g)[8], float r, const Code& c) {
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float p = h[e] * g[e];
+        f[e] = c.of_p ? fmaf(p, c.inv, p * c.inv_lo) : h[e] * r * g[e] * c.inv;
+    }
+    int lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], lo, true);
+    int hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[4], f[5], 0, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[6], f[7], hi, true);
     return make_uint2((uint32_t)lo, (uint32_t)hi);
 }
 
 // A workgroup per row, whose values stay in registers: QV vectors of 8 a thread.  BLOCK: a scale per 128 values, which 16 lanes hold.
 template <int QV, bool BLOCK>
 __global__ void __launch_bounds__(256) norm_quant_kernel(const NormQuant p) {
-    __shared__ float part[4], partm[4];
+    __shared__ float part[4], partm[4], party[4];
     const int64_t row = blockIdx.x, at = row * p.vecs;
-    float f[QV][8];
+    float h[QV][8];
+    uint4 gv[QV];
     float ss = 0.f;
 #pragma unroll
     for (int j = 0; j < QV; ++j) {
         const int i = threadIdx.x + j * 256;
         if (i < p.vecs) {
-            unpack8(p.x[at + i], f[j]);
+            gv[j] = p.g[i];
+            unpack8(p.x[at + i], h[j]);
             if (p.delta) {
                 float a[8];
                 unpack8(p.delta[at + i], a);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) a[e] += f[j][e];
-                const uint4 h = pack8(a);
-                unpack8(h, f[j]);
-                if (p.h) p.h[at + i] = h;
+                for (int e = 0; e < 8; ++e) a[e] += h[j][e];
+                const uint4 v = pack8(a);
+                unpack8(v, h[j]);
+                if (p.h) p.h[at + i] = v;
             } else if (p.h) {
-                p.h[at + i] = pack8(f[j]);
+                p.h[at + i] = pack8(h[j]);
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ss = fmaf(f[j][e], f[j][e], ss);
+            for (int e = 0; e < 8; ++e) ss = fmaf(h[j][e], h[j][e], ss);
         }
     }
     for (int off = 32; off > 0; off >>= 1) ss += __shfl_xor(ss, off);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = ss;
     __syncthreads();
     const float r = 1.0f / sqrtf((part[0] + part[1] + part[2] + part[3]) * p.inv_d + p.eps);
-    float m = 0.f;
+    float pm = 0.f, ym = 0.f;                    // (ym: for the rare case alone, but a pass over registers)
 #pragma unroll
     for (int j = 0; j < QV; ++j) {
         const int i = threadIdx.x + j * 256;
         if (i < p.vecs) {
-            float g[8];
-            unpack8(p.g[i], g);
+            float g[8], y[8];
+            unpack8(gv[j], g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                f[j][e] = f[j][e] * r * g[e];
-                m = fmaxf(m, fabsf(f[j][e]));
+                y[e] = h[j][e] * r * g[e];
+                pm = fmaxf(pm, fabsf(h[j][e] * g[e]));
+                ym = fmaxf(ym, fabsf(y[e]));
             }
-            if (p.y) p.y[at + i] = pack8(f[j]);
+            if (p.y) p.y[at + i] = pack8(y);
             if (BLOCK && p.codes) {              // (vecs is a multiple of 16: the 16 lanes of a block are here together)
-                for (int off = 8; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
-                const float amax = m > 0.f ? fmaxf(m, AMAX_MIN) : E4M3_MAX;
-                p.codes[at + i] = encode8(f[j], __fdiv_rn(E4M3_MAX, amax));
-                if ((threadIdx.x & 15) == 0) p.scales[(int64_t)(i >> 4) * p.rows + row] = __fdiv_rn(amax, E4M3_MAX);
-                m = 0.f;
+                for (int off = 8; off > 0; off >>= 1) pm = fmaxf(pm, __shfl_xor(pm, off));
+                Code c = code_of(pm, r);
+                if (!c.of_p) {
+                    for (int off = 8; off > 0; off >>= 1) ym = fmaxf(ym, __shfl_xor(ym, off));
+                    c = code_of_y(ym);
+                }
+                p.codes[at + i] = encode8(h[j], g, r, c);
+                if ((threadIdx.x & 15) == 0) p.scales[(int64_t)(i >> 4) * p.rows + row] = c.scale;
+                pm = ym = 0.f;
             }
         }
     }
     if (BLOCK || !p.codes) return;
-    for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
-    if ((threadIdx.x & 63) == 0) partm[threadIdx.x >> 6] = m;
+    for (int off = 32; off > 0; off >>= 1) {
+        pm = fmaxf(pm, __shfl_xor(pm, off));
+        ym = fmaxf(ym, __shfl_xor(ym, off));
+    }
+    if ((threadIdx.x & 63) == 0) { partm[threadIdx.x >> 6] = pm; party[threadIdx.x >> 6] = ym; }
     __syncthreads();
-    m = fmaxf(fmaxf(partm[0], partm[1]), fmaxf(partm[2], partm[3]));
-    const float amax = m > 0.f ? fmaxf(m, AMAX_MIN) : E4M3_MAX;
-    const float inv = __fdiv_rn(E4M3_MAX, amax);
-    if (threadIdx.x == 0) p.scales[row] = __fdiv_rn(amax, E4M3_MAX);
+    Code c = code_of(fmaxf(fmaxf(partm[0], partm[1]), fmaxf(partm[2], partm[3])), r);
+    if (!c.of_p) c = code_of_y(fmaxf(fmaxf(party[0], party[1]), fmaxf(party[2], party[3])));
+    if (threadIdx.x == 0) p.scales[row] = c.scale;
 #pragma unroll
     for (int j = 0; j < QV; ++j) {
         const int i = threadIdx.x + j * 256;
-        if (i < p.vecs) p.codes[at + i] = encode8(f[j], inv);
+        if (i >= p.vecs) continue;
+        float g[8];
+        unpack8(gv[j], g);
+        p.codes[at + i] = encode8(h[j], g, r, c);
     }
 }
 

@@ -1,8 +1,8 @@
 """Low-rank adapters of many requests against float64 arithmetic on the same operands.
 
-Tolerances.  T = x A^T is a float32 sum whose terms pass at most K / 32 + 64 roundings (the matrix instruction's chain, its own adds, sums of
-pieces; 2^-23 each, cuts among them), or K / 64 + 64 where 64 lanes add; the second product likewise over at most 128 terms with the scale, and with
-bfloat16 T is kept to 2^-16 of itself.  The result's rounding is 2^-8 of the value (bfloat16) or 2^-24."""
+Tolerances.  T = x A^T is a float32 sum whose terms pass at most K / 32 + 64 roundings in bfloat16 (the matrix instruction's chain over steps of 32, its own
+adds, sums of pieces; 2^-23 each, cuts among them) and K / 16 + 64 in float32 (four products an instruction, a quarter of K a wavefront); the
+second product likewise over at most 128 terms with the scale, and with bfloat16 T is kept to 2^-16 of itself.  The result's rounding is 2^-8 of the value (bfloat16) or 2^-24."""
 import numpy as np
 import pytest
 import torch
@@ -40,7 +40,7 @@ def reference(x, a, b, ranks, scales, segments, res):
         r = ranks[s]
         xd, ad, bd = x[row:row + n].double(), a[s, :r].double(), b[s, :, :r].double()
         t, ta = xd @ ad.t(), xd.abs() @ ad.abs().t()
-        et = (K / 32 + 64) * 2.0 ** -23 * ta + 2.0 ** -16 * t.abs()
+        et = (K / (32 if x.dtype == torch.bfloat16 else 16) + 64) * 2.0 ** -23 * ta + (2.0 ** -16 * t.abs() if x.dtype == torch.bfloat16 else 0)
         sc = float(np.float32(scales[s]))
         want[row:row + n] += sc * (t @ bd.t())
         err[row:row + n] += abs(sc) * (et @ bd.abs().t() + (r + 16) * 2.0 ** -23 * ((t.abs() + et) @ bd.abs().t()))
