@@ -114,26 +114,48 @@ __global__ void __launch_bounds__(256) adapter_down_kernel(const AdapterParams p
     for (int m = 0; m < MR; ++m)
 #pragma unroll
         for (int j = 0; j < NR; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    constexpr int U = MR + NR <= 4 ? 4 : 2;      // steps whose loads are under way together
-    int s = s0;
-    for (; s + U <= s1 && (s + U) * 32 <= p.K; s += U) {
+    // U steps are multiplied while the next U are on their way
+    constexpr int U = MR + NR <= 2 ? 4 : MR + NR <= 8 ? 2 : 1;
+    struct Stage {
         Frag<T> x[U][MR], a[U][NR];
+    };
+    auto fetch = [&](Stage& g, int at) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (int m = 0; m < MR; ++m)
 #pragma unroll
-            for (int m = 0; m < MR; ++m) load(x[u][m], xp[m] + (s + u) * 32);
+            for (int u = 0; u < U; ++u) load(g.x[u][m], xp[m] + (at + u) * 32);
 #pragma unroll
-            for (int j = 0; j < NR; ++j)
-                if (j < nr) load(a[u][j], ap[j] + (s + u) * 32);
-        }
+        for (int j = 0; j < NR; ++j)
+            if (j < nr) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) load(g.a[u][j], ap[j] + (at + u) * 32);
+            }
+    };
+    auto multiply = [&](const Stage& g) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int j = 0; j < NR; ++j)
                 if (j < nr) {
 #pragma unroll
-                    for (int m = 0; m < MR; ++m) acc[m][j] = mma(a[u][j], x[u][m], acc[m][j]);
+                    for (int m = 0; m < MR; ++m) acc[m][j] = mma(g.a[u][j], g.x[u][m], acc[m][j]);
                 }
+    };
+    int s = s0;
+    const int whole = min(s1, p.K >> 5);         // (steps without a border of K)
+    if (s + U <= whole) {
+        Stage g0, g1;
+        fetch(g0, s);
+        for (; s + 3 * U <= whole; s += 2 * U) {
+            fetch(g1, s + U);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(g0);
+            fetch(g0, s + 2 * U);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(g1);
+        }
+        multiply(g0);
+        s += U;
     }
     for (; s < s1; ++s) {
         const bool in = s * 32 + l4 * 8 < p.K;   // (K is a multiple of 8)
@@ -213,8 +235,9 @@ __device__ __forceinline__ void store_out(float* p, const float (&v)[8]) {
     *(float4*)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
 }
 
-// C of a tile of 16 MR rows and p.cols columns, a quarter of them a wavefront, 32 at a time.  Of those, product h takes the columns 8 g + 4 h + e
-// (g, e < 4) as its rows 4 g + e, so that a lane ends up with the eight consecutive ones from 8 (lane >> 4) on, of row lane & 15.
+// C of a tile of 16 MR rows and p.cols columns, a quarter of them a wavefront, 64 at a time (lines of 128 bytes in bf16).  Product h of those takes the
+// columns 32 (h / 2) + 8 g + 4 (h & 1) + e (g, e < 4) as its rows 4 g + e, so that a lane ends up with eight consecutive ones, from 8 (lane >> 4) on of
+// either half, of row lane & 15.
 template <typename T, int MR, int KS>
 __global__ void __launch_bounds__(256) adapter_up_kernel(const AdapterParams p, const Table tab) {
     constexpr int NP = Parts<T>::N;
@@ -258,22 +281,26 @@ __global__ void __launch_bounds__(256) adapter_up_kernel(const AdapterParams p, 
             for (int i = 0; i < NP; ++i)
                 if (k < ks) t[m][k][i] = tf[m][k][i][lane];
     const T* b = (const T*)p.b + (int64_t)sg.slot * p.N * p.width;
-    const int n1 = min((int)(blockIdx.y + 1) * p.cols, p.N), share = p.cols >> 2;
-    for (int c0 = blockIdx.y * p.cols + wave * share; c0 < min((int)blockIdx.y * p.cols + (wave + 1) * share, n1); c0 += 32) {
-        const int col = c0 + l4 * 8;
-        float out[MR][8];
+    const int share = p.cols >> 2, first = blockIdx.y * p.cols + wave * share, n1 = min(first + share, p.N);
+    for (int c0 = first; c0 < n1; c0 += 64) {
+        float out[MR][2][8];
 #pragma unroll
-        for (int m = 0; m < MR; ++m) {
+        for (int m = 0; m < MR; ++m)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) out[m][e] = 0.f;
-            if (p.res && r0 + m * 16 + l15 < end && col < p.N) load_out(out[m], (const T*)p.res + (int64_t)(r0 + m * 16 + l15) * p.N + col);
-        }
-        f32x4 acc[MR][2];
+            for (int q = 0; q < 2; ++q) {
+                const int col = c0 + q * 32 + l4 * 8;
 #pragma unroll
-        for (int m = 0; m < MR; ++m) acc[m][0] = acc[m][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int e = 0; e < 8; ++e) out[m][q][e] = 0.f;
+                if (p.res && r0 + m * 16 + l15 < end && col < n1) load_out(out[m][q], (const T*)p.res + (int64_t)(r0 + m * 16 + l15) * p.N + col);
+            }
+        f32x4 acc[MR][4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const T* bp = b + (int64_t)min(c0 + (l15 >> 2) * 8 + h * 4 + (l15 & 3), p.N - 1) * p.width + l4 * 8;
+        for (int m = 0; m < MR; ++m)
+#pragma unroll
+            for (int h = 0; h < 4; ++h) acc[m][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const T* bp = b + (int64_t)min(c0 + (h >> 1) * 32 + (l15 >> 2) * 8 + (h & 1) * 4 + (l15 & 3), p.N - 1) * p.width + l4 * 8;
 #pragma unroll
             for (int k = 0; k < KS; ++k)
                 if (k < ks) {
@@ -291,14 +318,17 @@ __global__ void __launch_bounds__(256) adapter_up_kernel(const AdapterParams p, 
                 }
         }
 #pragma unroll
-        for (int m = 0; m < MR; ++m) {
+        for (int m = 0; m < MR; ++m)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                out[m][e] += acc[m][0][e];
-                out[m][4 + e] += acc[m][1][e];
+            for (int q = 0; q < 2; ++q) {
+                const int col = c0 + q * 32 + l4 * 8;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    out[m][q][e] += acc[m][2 * q][e];
+                    out[m][q][4 + e] += acc[m][2 * q + 1][e];
+                }
+                if (r0 + m * 16 + l15 < end && col < n1) store_out((T*)p.c + (int64_t)(r0 + m * 16 + l15) * p.N + col, out[m][q]);
             }
-            if (r0 + m * 16 + l15 < end && col < p.N) store_out((T*)p.c + (int64_t)(r0 + m * 16 + l15) * p.N + col, out[m]);
-        }
     }
 }
 
@@ -328,7 +358,7 @@ void plan(Launch& l, int N, int K) {
     l.pieces = std::max(1, std::min({8, 1024 / t.tiles, steps / 16}));
     l.per = ((steps + l.pieces * 4 - 1) / (l.pieces * 4) + 1) / 2 * 2;         // (whole lines of 128 bytes)
     l.cols = 1024;
-    while (l.cols > 128 && (int64_t)t.tiles * ((N + l.cols - 1) / l.cols) < 1024) l.cols /= 2;
+    while (l.cols > 256 && (int64_t)t.tiles * ((N + l.cols - 1) / l.cols) < 1024) l.cols /= 2;
     l.floats = l.rank ? (size_t)l.pieces * t.tiles * 16 * l.mr * 16 * l.nr : 0;
 }
 

@@ -23,69 +23,91 @@ constexpr int MAX_TOP = 64;
 
 struct Stats { float m, s, t, pad; };            // of a piece
 
-// the logits of a lane: 8 from i on, -infinity beyond V
+// the logits of a lane: 8 from i on; they exist, and lie on 16 bytes
+__device__ __forceinline__ void load8_whole(const float* p, float (&v)[8]) {
+    const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void load8_whole(const bf16_t* p, float (&v)[8]) {
+    const uint4 a = *(const uint4*)p;
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        v[2 * c] = __uint_as_float(w[c] << 16);
+        v[2 * c + 1] = __uint_as_float(w[c] & 0xffff0000u);
+    }
+}
+// -infinity beyond V
 template <typename T, bool VEC>
 __device__ __forceinline__ void load8(const T* row, int i, int V, float (&v)[8]) {
     if (VEC && i + 8 <= V) {
-        if (sizeof(T) == 4) {
-            const float4 a = *(const float4*)(row + i), b = *(const float4*)(row + i + 4);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        } else {
-            const uint4 a = *(const uint4*)(row + i);
-            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                v[2 * c] = __uint_as_float(w[c] << 16);
-                v[2 * c + 1] = __uint_as_float(w[c] & 0xffff0000u);
-            }
-        }
+        load8_whole(row + i, v);
         return;
     }
 #pragma unroll
     for (int c = 0; c < 8; ++c) v[c] = i + c < V ? to_f32(row[i + c]) : -INFINITY;
 }
 
+// Over a wavefront, all lanes get it: rotations within rows of 16 lanes on the vector ALU, then the four rows (the same by way of LDS,
+// six exchanges for each of seven reductions a piece, took 11 us of LDS in 256 rows of 152064).
+template <int CTRL>
+__device__ __forceinline__ float rotated(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true)); }
+__device__ __forceinline__ float of_row(float v, int row) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), row * 16)); }
 __device__ __forceinline__ float wave_max(float v) {
-    for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
-    return v;
+    v = fmaxf(v, rotated<0x128>(v));
+    v = fmaxf(v, rotated<0x124>(v));
+    v = fmaxf(v, rotated<0x122>(v));
+    v = fmaxf(v, rotated<0x121>(v));
+    return fmaxf(fmaxf(of_row(v, 0), of_row(v, 1)), fmaxf(of_row(v, 2), of_row(v, 3)));
 }
 __device__ __forceinline__ float wave_sum(float v) {
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
-    return v;
+    v += rotated<0x128>(v);
+    v += rotated<0x124>(v);
+    v += rotated<0x122>(v);
+    v += rotated<0x121>(v);
+    return (of_row(v, 0) + of_row(v, 1)) + (of_row(v, 2) + of_row(v, 3));
 }
 
-// adds a logit of a row with maximum m (finite) to S and T.  Below -200 a term is 0 in float32, and -infinity and NaN (which
-// fmaxf turns into the other operand) go there.
-__device__ __forceinline__ void add_term(float l, float m, float& s, float& t) {
-    const float d = fmaxf(l - m, -200.0f), e = __expf(d);
-    s += e;
-    t = fmaf(d, e, t);
-}
-
-// (m, S, T) of the wavefront's values, whatever is among them; every lane gets all three
-template <int N>
-__device__ __forceinline__ Stats wave_stats(const float (&v)[N]) {
-    float m = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < N; ++i) m = fmaxf(m, v[i]);
-    m = wave_max(m);
+// S and T of the wavefront's values with maximum m, in powers of 2 (T log2(e)).  -infinity and NaN make T NaN; then once more with
+// every distance held to where a term is 0 in float32 (fmaxf turns NaN into its other operand).
+__device__ __forceinline__ Stats wave_stats(const float (&x)[PER_WAVE][8], float m) {
+    constexpr int N = PER_WAVE * 8;
+    const float(&v)[N] = *(const float(*)[N])&x;
+    constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f;
     Stats r = {m, 0.f, 0.f, 0.f};
     if (m == INFINITY) {
 #pragma unroll
         for (int i = 0; i < N; ++i) r.s += v[i] == INFINITY ? 1.f : 0.f;
+        r.s = wave_sum(r.s);
     } else if (m > -INFINITY) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) add_term(v[i], m, r.s, r.t);
+        for (int i = 0; i < N; ++i) {
+            const float d = (v[i] - m) * LOG2E, e = __builtin_amdgcn_exp2f(d);
+            r.s += e;
+            r.t = fmaf(d, e, r.t);
+        }
+        r.t = wave_sum(r.t);
+        if (!(r.t > -INFINITY)) {
+            r.s = r.t = 0.f;
+            asm volatile("" : "+v"(m));          // (else the compiler keeps the first pass's 32 distances for this one)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float d = fmaxf((v[i] - m) * LOG2E, -250.0f), e = __builtin_amdgcn_exp2f(d);
+                r.s += e;
+                r.t = fmaf(d, e, r.t);
+            }
+            r.t = wave_sum(r.t);
+        }
+        r.s = wave_sum(r.s);
+        r.t *= LN2;
     }
-    r.s = wave_sum(r.s);
-    r.t = wave_sum(r.t);
     return r;
 }
 
 // Pieces of rows: a wavefront each.  at (may be null): the logit of token tokens[row], where the piece holds it.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) logprob_pieces_kernel(const T* __restrict__ logits, int64_t ld, int V, int pieces, int64_t total,
+__global__ void __launch_bounds__(256, 6) logprob_pieces_kernel(const T* __restrict__ logits, int64_t ld, int V, int pieces, int64_t total,
                                                              Stats* __restrict__ stats, int64_t stats_ld, float* __restrict__ chunk_max, int chunks,
                                                              const int32_t* __restrict__ tokens, int first_token, float* __restrict__ at) {
     const int lane = threadIdx.x & 63;
@@ -94,25 +116,42 @@ __global__ void __launch_bounds__(256) logprob_pieces_kernel(const T* __restrict
     const int64_t r = w / pieces;
     const int p = (int)(w - r * pieces), i0 = p * PIECE;
     const T* row = logits + r * ld;
-    float v[8 * PER_WAVE];
+    float v[PER_WAVE][8];
+    if (VEC && i0 + PIECE <= V) {
+#pragma unroll
+        for (int c = 0; c < PER_WAVE; ++c) load8_whole(row + i0 + c * CHUNK + lane * 8, v[c]);
+    } else {
+#pragma unroll 1
+        for (int c = 0; c < PER_WAVE; ++c) {
+            float x[8];
+            load8<T, VEC>(row, i0 + c * CHUNK + lane * 8, V, x);
+#pragma unroll
+            for (int u = 0; u < PER_WAVE; ++u)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[u][e] = u == c ? x[e] : v[u][e];
+        }
+    }
+    float cm[PER_WAVE];
 #pragma unroll
     for (int c = 0; c < PER_WAVE; ++c) {
-        float x[8];
-        load8<T, VEC>(row, i0 + c * CHUNK + lane * 8, V, x);
+        cm[c] = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[c * 8 + e] = x[e];
+        for (int e = 0; e < 8; ++e) cm[c] = fmaxf(cm[c], v[c][e]);
     }
+    float m = -INFINITY;
     if (chunk_max) {
 #pragma unroll
         for (int c = 0; c < PER_WAVE; ++c) {
-            float m = -INFINITY;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) m = fmaxf(m, v[c * 8 + e]);
-            m = wave_max(m);
-            if (lane == 0 && p * PER_WAVE + c < chunks) chunk_max[r * chunks + p * PER_WAVE + c] = m;
+            cm[c] = wave_max(cm[c]);
+            m = fmaxf(m, cm[c]);
+            if (lane == 0 && p * PER_WAVE + c < chunks) chunk_max[r * chunks + p * PER_WAVE + c] = cm[c];
         }
+    } else {
+#pragma unroll
+        for (int c = 0; c < PER_WAVE; ++c) m = fmaxf(m, cm[c]);
+        m = wave_max(m);
     }
-    const Stats st = wave_stats(v);
+    const Stats st = wave_stats(v, m);
     if (lane == 0) {
         stats[r * stats_ld + p] = st;
         if (at) {
@@ -153,20 +192,29 @@ __device__ __forceinline__ float key_logit(unsigned long long k) {
 }
 
 constexpr int RUNS = MAX_TOP * (CHUNK / 8);      // of the chunks that are read again
+constexpr int LIST = 512;                        // elements that are ordered at once; 8 of each of MAX_TOP runs
 
-// Leaves in out[0 .. min(n, top)) the largest of keys[0 .. n), in order.  All different, but for zeros, which are left out.  (The
-// callers' barriers stand around it.)
-__device__ __forceinline__ void largest(const unsigned long long* keys, int n, int top, unsigned long long* out) {
+// Leaves in out[0 .. min(n, top)) the largest of keys[0 .. n), in order; keys[n .. n + 8) are overwritten.  All different, but for
+// zeros, which are left out.  (The callers' barriers stand around it.)
+__device__ __forceinline__ void largest(unsigned long long* keys, int n, int top, unsigned long long* out) {
+    if (threadIdx.x < 8) keys[n + threadIdx.x] = 0;
+    __syncthreads();
     for (int i = threadIdx.x; i < n; i += 256) {
         const unsigned long long k = keys[i];
         if (k == 0) continue;
         int rank = 0;
-        for (int j = 0; j < n; ++j) rank += keys[j] > k;
+        for (int j = 0; j < n; j += 8) {
+            unsigned long long o[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) o[c] = keys[j + c];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) rank += o[c] > k;
+        }
         if (rank < top) out[rank] = k;
     }
 }
 
-// A row's answer, by a workgroup.
+// A row's answer, by a workgroup.  What bounds it is the way of its loads, one after another: pieces and chunks; the chunks that hold the answer.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__ logits, int64_t ld, int V, int pieces, int chunks,
                                                            const Stats* __restrict__ stats, const float* __restrict__ chunk_max,
@@ -175,96 +223,138 @@ __global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__
                                                            float* __restrict__ top_logprobs) {
     __shared__ double red_s[4], red_t[4];
     __shared__ float red_m[4];
-    __shared__ unsigned long long keys[RUNS], best[MAX_TOP];
+    extern __shared__ unsigned long long keys[];     // RUNS + 8, only where top > 0
+    __shared__ unsigned long long best[MAX_TOP];
     __shared__ int count;
     const int64_t r = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const T* row = logits + r * ld;
     const Stats* st = stats + r * pieces;
-    float m = -INFINITY;
-    for (int i = tid; i < pieces; i += 256) m = fmaxf(m, st[i].m);
+    const float* cm = chunk_max + r * chunks;
+    // (first turn of each list and the first token: asked for together)
+    const Stats none = {-INFINITY, 0.f, 0.f, 0.f};
+    const Stats first = tid < pieces ? st[tid] : none;
+    float cm0[2] = {-INFINITY, -INFINITY};
+    if (top) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (tid + i * 256 < chunks) cm0[i] = cm[tid + i * 256];
+    }
+    float given = -INFINITY;
+    if (tid < n_tokens) {
+        const int32_t t = tokens[r * n_tokens + tid];
+        if (t >= 0 && t < V) given = to_f32(row[t]);
+    }
+    float m = first.m;
+    for (int i = tid + 256; i < pieces; i += 256) m = fmaxf(m, st[i].m);
     m = wave_max(m);
     if (lane == 0) red_m[wave] = m;
+    if (tid < MAX_TOP) best[tid] = 0;
+    if (tid == 0) count = 0;
     __syncthreads();
     m = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
     Sums sum = {0.0, 0.0};
-    for (int i = tid; i < pieces; i += 256) join(st[i], m, sum);
+    join(first, m, sum);
+    for (int i = tid + 256; i < pieces; i += 256) join(st[i], m, sum);
     for (int off = 32; off > 0; off >>= 1) {
         sum.s += __shfl_xor(sum.s, off);
         sum.t += __shfl_xor(sum.t, off);
     }
     if (lane == 0) { red_s[wave] = sum.s; red_t[wave] = sum.t; }
+    const float lowest = m == INFINITY ? INFINITY : -INFINITY;         // of a logit with weight
+    // the chunks that hold the first tokens, as keys of (largest logit, chunk).  (More than a list holds: in turns, the best so far among them.)
+    if (top) {
+        for (int c0 = 0; c0 < chunks; c0 += RUNS - MAX_TOP) {
+            const int n = min(chunks - c0, RUNS - MAX_TOP), more = c0 ? MAX_TOP : 0;
+            if (c0) __syncthreads();
+            for (int i = tid; i < n; i += 256) {
+                const float c = c0 || i >= 512 ? cm[c0 + i] : i < 256 ? cm0[0] : cm0[1];
+                keys[i] = c >= lowest ? order_key(c, c0 + i) : 0;
+            }
+            if (tid < more) keys[n + tid] = best[tid];
+            __syncthreads();
+            if (tid < more) best[tid] = 0;
+            largest(keys, n + more, top, best);
+        }
+    }
     __syncthreads();
     sum = {red_s[0] + red_s[1] + red_s[2] + red_s[3], red_t[0] + red_t[1] + red_t[2] + red_t[3]};
     const double log_s = log(sum.s);
-    if (tid == 0 && entropy) entropy[r] = entropy_of(sum, m);
-    for (int i = tid; i < n_tokens; i += 256) {
+    if (tid < n_tokens) logprobs[r * n_tokens + tid] = logprob_of(given, m, log_s);
+    for (int i = tid + 256; i < n_tokens; i += 256) {
         const int32_t t = tokens[r * n_tokens + i];
         logprobs[r * n_tokens + i] = t >= 0 && t < V ? logprob_of(to_f32(row[t]), m, log_s) : -INFINITY;
     }
+    if (tid == 0 && entropy) entropy[r] = m > -INFINITY ? (float)fmax(0.0, log_s - sum.t / sum.s) : 0.f;
     if (top == 0) return;
 
-    // the chunks that hold them, as keys of (largest logit, chunk)
-    const float lowest = m == INFINITY ? INFINITY : -INFINITY;         // of a logit with weight
-    if (tid < MAX_TOP) best[tid] = 0;
-    const float* cm = chunk_max + r * chunks;
-    // (chunks that a list does not hold at once: in turns, the best so far among them)
-    for (int c0 = 0; c0 < chunks || c0 == 0; c0 += RUNS - MAX_TOP) {
-        const int n = min(chunks - c0, RUNS - MAX_TOP);
-        __syncthreads();
-        for (int i = tid; i < n; i += 256) keys[i] = cm[c0 + i] >= lowest ? order_key(cm[c0 + i], c0 + i) : 0;
-        if (tid < MAX_TOP) keys[n + tid] = best[tid];
-        __syncthreads();
-        if (tid < MAX_TOP) best[tid] = 0;
-        __syncthreads();
-        largest(keys, n + MAX_TOP, top, best);
-    }
-    __syncthreads();
     int n_chunks = 0;
     while (n_chunks < top && best[n_chunks]) ++n_chunks;
     // (as many elements as tokens are wanted are as large as this)
     const float floor_logit = n_chunks == top ? key_logit(best[top - 1]) : lowest;
-    // the runs of 8 in them that reach as far
-    if (tid == 0) count = 0;
-    __syncthreads();
-    for (int i = tid; i < n_chunks * (CHUNK / 8); i += 256) {
-        const int at = (int)(uint32_t)~best[i / (CHUNK / 8)] * CHUNK + (i % (CHUNK / 8)) * 8;
-        float v[8];
-        load8<T, VEC>(row, at, V, v);
-        unsigned long long k = 0;
+    // their elements that reach as far: mostly a few more than are wanted
+    const int runs_in = n_chunks * (CHUNK / 8);
+    for (int i0 = tid; i0 < runs_in; i0 += 1024) {
+        float v[4][8];
+        int at[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const unsigned long long ke = v[e] >= floor_logit ? order_key(v[e], at + e) : 0;
-            k = ke > k ? ke : k;
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + u * 256;
+            at[u] = i < runs_in ? (int)(uint32_t)~best[i / (CHUNK / 8)] * CHUNK + (i % (CHUNK / 8)) * 8 : V;
+            load8<T, VEC>(row, at[u], V, v[u]);
         }
-        if (k) keys[atomicAdd(&count, 1)] = k;   // (their order in the list changes nothing: the keys are ranked)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (v[u][e] >= floor_logit && v[u][e] > -INFINITY) {
+                    const int slot = atomicAdd(&count, 1);         // (their order in the list changes nothing: the keys are ranked)
+                    if (slot < LIST) keys[slot] = order_key(v[u][e], at[u] + e);
+                }
     }
     __syncthreads();
-    const int runs = count;
-    if (tid < MAX_TOP) best[tid] = 0;
-    __syncthreads();
-    largest(keys, runs, top, best);
-    __syncthreads();
-    // their elements
-    if (tid == 0) count = 0;
-    __syncthreads();
-    for (int i = tid; i < top * 8; i += 256) {
-        if (!best[i >> 3]) continue;
-        const int at = (int)((uint32_t)~best[i >> 3] & ~7u) + (i & 7);
-        const float l = at < V ? to_f32(row[at]) : -INFINITY;
-        const unsigned long long k = l >= floor_logit ? order_key(l, at) : 0;
-        if (k) keys[atomicAdd(&count, 1)] = k;
+    int n = count;
+    if (n > LIST) {
+        // many as large as that: first the runs of 8 that hold the answer, by their first and largest element
+        __syncthreads();
+        if (tid == 0) count = 0;
+        __syncthreads();
+        for (int i = tid; i < runs_in; i += 256) {
+            const int at = (int)(uint32_t)~best[i / (CHUNK / 8)] * CHUNK + (i % (CHUNK / 8)) * 8;
+            float v[8];
+            load8<T, VEC>(row, at, V, v);
+            unsigned long long k = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const unsigned long long ke = v[e] >= floor_logit ? order_key(v[e], at + e) : 0;
+                k = ke > k ? ke : k;
+            }
+            if (k) keys[atomicAdd(&count, 1)] = k;
+        }
+        __syncthreads();
+        const int runs = count;
+        if (tid < MAX_TOP) best[tid] = 0;
+        largest(keys, runs, top, best);
+        __syncthreads();
+        if (tid == 0) count = 0;
+        __syncthreads();
+        for (int i = tid; i < top * 8; i += 256) {
+            if (!best[i >> 3]) continue;
+            const int at = (int)((uint32_t)~best[i >> 3] & ~7u) + (i & 7);
+            const float l = at < V ? to_f32(row[at]) : -INFINITY;
+            const unsigned long long k = l >= floor_logit ? order_key(l, at) : 0;
+            if (k) keys[atomicAdd(&count, 1)] = k;
+        }
+        __syncthreads();
+        n = count;
     }
-    __syncthreads();
-    const int n = count;
     if (tid < MAX_TOP) best[tid] = 0;
-    __syncthreads();
     largest(keys, n, top, best);
     __syncthreads();
-    for (int i = tid; i < top; i += 256) {
-        const unsigned long long k = best[i];
-        top_tokens[r * top + i] = k ? (int32_t)(uint32_t)~k : -1;
-        top_logprobs[r * top + i] = k ? logprob_of(key_logit(k), m, log_s) : -INFINITY;
+    if (tid < top) {
+        const unsigned long long k = best[tid];
+        top_tokens[r * top + tid] = k ? (int32_t)(uint32_t)~k : -1;
+        top_logprobs[r * top + tid] = k ? logprob_of(key_logit(k), m, log_s) : -INFINITY;
     }
 }
 
@@ -280,7 +370,7 @@ void run(const T* logits, int64_t ld, int64_t rows, int V, const int32_t* tokens
     const int64_t total = rows * pieces;
     hipLaunchKernelGGL((logprob_pieces_kernel<T, VEC>), dim3((unsigned)((total + 3) / 4)), dim3(256), 0, s, logits, ld, V, pieces, total, stats,
                        (int64_t)pieces, cm, chunks, (const int32_t*)nullptr, 0, (float*)nullptr);
-    hipLaunchKernelGGL((logprob_rows_kernel<T, VEC>), dim3((unsigned)rows), dim3(256), 0, s, logits, ld, V, pieces, chunks, stats, cm, tokens,
+    hipLaunchKernelGGL((logprob_rows_kernel<T, VEC>), dim3((unsigned)rows), dim3(256), top ? (RUNS + 8) * 8 : 0, s, logits, ld, V, pieces, chunks, stats, cm, tokens,
                        n_tokens, logprobs, entropy, top, top_tokens, top_logprobs);
 }
 

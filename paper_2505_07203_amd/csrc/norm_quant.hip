@@ -159,6 +159,7 @@ void run(const NormQuant& p, hipStream_t s) {
     const dim3 grid((unsigned)p.rows), wg(256);
     if (p.vecs <= 256) hipLaunchKernelGGL((norm_quant_kernel<1, BLOCK>), grid, wg, 0, s, p);
     else if (p.vecs <= 512) hipLaunchKernelGGL((norm_quant_kernel<2, BLOCK>), grid, wg, 0, s, p);
+    else if (p.vecs <= 768) hipLaunchKernelGGL((norm_quant_kernel<3, BLOCK>), grid, wg, 0, s, p);
     else if (p.vecs <= 1024) hipLaunchKernelGGL((norm_quant_kernel<4, BLOCK>), grid, wg, 0, s, p);
     else hipLaunchKernelGGL((norm_quant_kernel<8, BLOCK>), grid, wg, 0, s, p);
 }
