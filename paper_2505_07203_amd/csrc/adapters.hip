@@ -7,6 +7,7 @@
 // of the slots that it uses.  Both launches are bound by memory, operands go from there to registers in the matrix instruction's own
 // order, 16 bytes a lane and load.
 #include "adapters.h"
+#include "slice_window.h"
 
 #include <string.h>
 
@@ -67,6 +68,14 @@ __device__ __forceinline__ void load(Frag<float>& f, const float* p) {
     f.lo = *(const f32x4*)p;
     f.hi = *(const f32x4*)(p + 4);
 }
+// from a row in LDS, whose 16-byte segments are XOR-swizzled with the row
+__device__ __forceinline__ void load(Frag<bf16_t>& f, const unsigned char* row, int at, int swizzle) {
+    f.v = *(const bf16x8*)(row + ((at ^ swizzle) << 4));
+}
+__device__ __forceinline__ void load(Frag<float>& f, const unsigned char* row, int at, int swizzle) {
+    f.lo = *(const f32x4*)(row + (((2 * at) ^ swizzle) << 4));
+    f.hi = *(const f32x4*)(row + (((2 * at + 1) ^ swizzle) << 4));
+}
 __device__ __forceinline__ void zero(Frag<bf16_t>& f) { f.v = __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0)); }
 __device__ __forceinline__ void zero(Frag<float>& f) { f.lo = f.hi = f32x4{0.f, 0.f, 0.f, 0.f}; }
 __device__ __forceinline__ f32x4 mma(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x4 c) {
@@ -95,26 +104,61 @@ __device__ __forceinline__ void keep(Frag<float>& f, int n) {
     }
 }
 
-// T of a run of rows of one request over one piece of K, 16 rows at a time.  A wavefront takes C steps of 32 of the piece, 512 bytes of a row, and
-// holds that part of A in registers for all its rows: A is read once a run, x in visits of 512 bytes, two groups of rows ahead.  The
-// wavefronts' sums meet in LDS.  A lane of a product of 16 ranks and 16 rows holds row lane & 15 and ranks 4 (lane >> 4) .. + 3.
+// T of a run of rows of one request over one piece of K, 16 rows at a time.  A wavefront takes C steps of 32 of the piece, 512 bytes of a row
+// (256 with ranks beyond 64), and holds that part of A in registers for all its rows: A is read once a run.  x goes straight into a ring of D
+// groups of rows in LDS, a load covering whole lines of two rows (four); 16-byte segments are XOR-swizzled with the row on the global side, so
+// that a fragment's 16 rows meet 16 different banks.  Fragments loaded from memory to registers touch 64 bytes of a line each and
+// came to half the rate: two prompts of 8000 rows of K 14336, rank 64, 161 us.  The wavefronts' sums meet in LDS.  A lane of a product of 16
+// ranks and 16 rows holds row lane & 15 and ranks 4 (lane >> 4) .. + 3.
 constexpr int DOWN_WAVES = 8;
-template <typename T, int NR> struct DownSteps { static constexpr int C = (NR == 8 ? 4 : 8) * 2 / (int)sizeof(T); };
+template <typename T, int NR> struct Down {
+    static constexpr int ROWB = NR == 8 ? 256 : 512;             // bytes of a row that a wavefront takes
+    static constexpr int C = ROWB / 32 / (int)sizeof(T);         // steps
+    static constexpr int GROUP = 16 * ROWB, NL = GROUP / 1024;   // bytes of a group, and its loads
+    static constexpr int D = NR == 8 ? 3 : 2;
+    static constexpr int WAVE = D * GROUP + NR * 1024;           // LDS of a wavefront: the ring, and its sums
+    static_assert(DOWN_WAVES * WAVE <= 160 * 1024, "LDS of a compute unit");
+};
 
 template <typename T, int NR>
 __global__ void __launch_bounds__(64 * DOWN_WAVES, 2) adapter_down_kernel(const AdapterParams p, const Table tab) {
-    constexpr int C = DownSteps<T, NR>::C;
-    extern __shared__ f32x4 red[];               // [2][waves][NR][64]
+    typedef Down<T, NR> L;
+    constexpr int C = L::C, D = L::D, ROWB = L::ROWB, SEGS = ROWB / 16, RPL = 1024 / ROWB;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int si = segment_of(tab.down0, tab.n, blockIdx.x);
     const Segment& sg = tab.seg[si];
     const int rank = sg.rank();
     if (rank == 0) return;
-    const int g0 = ((int)blockIdx.x - tab.down0[si]) * p.groups, g1 = min(g0 + p.groups, (sg.n + 15) >> 4), last = sg.row + sg.n - 1;
+    const int g0 = ((int)blockIdx.x - tab.down0[si]) * p.groups, g1 = min(g0 + p.groups, (sg.n + 15) >> 4);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int l15 = lane & 15, l4 = lane >> 4;
     const int nr = (rank + 15) >> 4;
     const int k0 = ((int)blockIdx.y * waves + wave) * (C * 32);
-    const bool whole = k0 + C * 32 <= p.K;
+    const int ks = min(p.K - k0, C * 32);        // elements of K of this wavefront (none: 0 or less)
+    unsigned char* const ring = smem + wave * L::WAVE;
+    f32x4* const red = (f32x4*)(ring + D * L::GROUP);
+
+    // loads of a group: rows behind the request's last one read as zero, what lies behind K in a row is dropped with the fragments
+    const uint32_t pitch = (uint32_t)p.K * (uint32_t)sizeof(T);
+    uint32_t vo[8];                              // (NL entries used)
+#pragma unroll
+    for (int i = 0; i < L::NL; ++i) {
+        const int row = i * RPL + lane / SEGS;
+        vo[i] = (uint32_t)row * pitch + (uint32_t)(((lane & (SEGS - 1)) ^ row) << 4);
+    }
+    const unsigned char* const xbase = (const unsigned char*)p.x + ((int64_t)sg.row * p.K + k0) * (int64_t)sizeof(T);
+#define PO_FETCH(g_, pos_)                                                                                             \
+    {                                                                                                                  \
+        const int at_ = (g_), rows_ = at_ < g1 ? min(16, sg.n - at_ * 16) : 0;                                         \
+        const uint32_t bytes_ = rows_ > 0 && ks > 0 ? (uint32_t)(rows_ - 1) * pitch + (uint32_t)ks * (uint32_t)sizeof(T) : 0u; \
+        const __amdgpu_buffer_rsrc_t rs_ = __builtin_amdgcn_make_buffer_rsrc(                                          \
+            (void*)(xbase + (int64_t)(bytes_ ? at_ : g0) * 16 * pitch), 0, (int)bytes_, 0x00020000);                   \
+        _Pragma("unroll") for (int i = 0; i < L::NL; ++i)                                                              \
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(                                                                  \
+                rs_, (__attribute__((address_space(3))) void*)(ring + (pos_) * L::GROUP + i * 1024), 16, vo[i], 0, 0, 0); \
+    }
+#pragma unroll
+    for (int d = 0; d < D; ++d) PO_FETCH(g0 + d, d)
     Frag<T> a[NR][C];                            // (ranks behind the slot's last one: that one again)
 #pragma unroll
     for (int j = 0; j < NR; ++j)
@@ -122,25 +166,28 @@ __global__ void __launch_bounds__(64 * DOWN_WAVES, 2) adapter_down_kernel(const 
             const T* ap = (const T*)p.a + ((int64_t)sg.slot() * p.width + min(j * 16 + l15, rank - 1)) * p.K + k0 + l4 * 8;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                if (whole || k0 + c * 32 + l4 * 8 < p.K) load(a[j][c], ap + c * 32);       // (K is a multiple of 8)
+                if (c * 32 + l4 * 8 < ks) load(a[j][c], ap + c * 32);          // (K is a multiple of 8)
                 else zero(a[j][c]);
             }
         }
-    auto fetch = [&](Frag<T> (&x)[C], int g) {   // (rows behind the request's last one: that one again)
-        const T* xp = (const T*)p.x + (int64_t)min(sg.row + g * 16 + l15, last) * p.K + k0 + l4 * 8;
-        if (whole) {
-#pragma unroll
-            for (int c = 0; c < C; ++c) load(x[c], xp + c * 32);
-        } else {
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                if (k0 + c * 32 + l4 * 8 < p.K) load(x[c], xp + c * 32);
-                else zero(x[c]);
-            }
-        }
-    };
+    // (A is here before the loop: from then on the counter of loads counts the ring's alone, and at the end of a turn a store)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     float* const t = p.t + (int64_t)blockIdx.y * p.plane + (int64_t)sg.group0 * 16 * p.rp;
-    auto turn = [&](Frag<T> (&x)[C], int g) {
+    int pos = 0;
+    for (int g = g0; g < g1; ++g) {
+        PO_WAIT_LOADS((D - 1) * L::NL);            // the group has landed (loads return in order)
+        Frag<T> x[C];
+        const unsigned char* const u = ring + pos * L::GROUP + l15 * ROWB;
+#pragma unroll
+        for (int c = 0; c < C; ++c) load(x[c], u, c * 4 + l4, l15);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                     // (every fragment is in registers: the place is free)
+        PO_FETCH(g + D, pos)
+        pos = pos + 1 == D ? 0 : pos + 1;
+        if (ks < C * 32) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (c * 32 + l4 * 8 >= ks) zero(x[c]);
+        }
         f32x4 acc[NR];
 #pragma unroll
         for (int j = 0; j < NR; ++j)
@@ -149,25 +196,20 @@ __global__ void __launch_bounds__(64 * DOWN_WAVES, 2) adapter_down_kernel(const 
 #pragma unroll
                 for (int c = 0; c < C; ++c) acc[j] = mma(a[j][c], x[c], acc[j]);
             }
-        if (g + 2 < g1) fetch(x, g + 2);
-        f32x4* const mine = red + (g & 1) * waves * (NR * 64);     // (two places in turn: one barrier a group)
+        asm volatile("s_barrier" ::: "memory");                                // (the sums of the group before have been read)
 #pragma unroll
         for (int j = 0; j < NR; ++j)
-            if (j < nr) mine[(wave * NR + j) * 64 + lane] = acc[j];
+            if (j < nr) red[j * 64 + lane] = acc[j];
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");         // (not for the loads that are under way)
         for (int j = wave; j < nr; j += waves) {
-            f32x4 v = mine[j * 64 + lane];
-            for (int w = 1; w < waves; ++w) v += mine[(w * NR + j) * 64 + lane];
+            f32x4 v = *(const f32x4*)(smem + D * L::GROUP + (j * 64 + lane) * 16);
+            for (int w = 1; w < waves; ++w) v += *(const f32x4*)(smem + w * L::WAVE + D * L::GROUP + (j * 64 + lane) * 16);
             *(f32x4*)(t + (int64_t)(g * 16 + l15) * p.rp + j * 16 + 4 * l4) = v;
         }
-    };
-    Frag<T> x0[C], x1[C];
-    fetch(x0, g0);
-    if (g0 + 1 < g1) fetch(x1, g0 + 1);
-    for (int g = g0; g < g1; g += 2) {
-        turn(x0, g);
-        if (g + 1 < g1) turn(x1, g + 1);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
+#undef PO_FETCH
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (nothing is on its way into LDS when the workgroup ends)
 }
 
 // the fragments of T in the second product: bf16 in two parts (the rounding of T and that of what it left, 2^-16 of T together),
@@ -191,40 +233,35 @@ __device__ __forceinline__ void split(const float (&v)[8], Frag<float> (&f)[1]) 
     f[0].hi = f32x4{v[4], v[5], v[6], v[7]};
 }
 
-// eight values as they lie in memory
-template <typename T> struct Raw;
-template <> struct Raw<bf16_t> { uint4 w; };
-template <> struct Raw<float> { float4 a, b; };
-__device__ __forceinline__ void unpack(const Raw<bf16_t>& r, float (&v)[8]) {
-    const uint32_t u[4] = {r.w.x, r.w.y, r.w.z, r.w.w};
+// 16 bytes of a row of C or R
+__device__ __forceinline__ void unpack(const uint4& w, float (&v)[8]) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
         v[2 * c] = __uint_as_float(u[c] << 16);
         v[2 * c + 1] = __uint_as_float(u[c] & 0xffff0000u);
     }
 }
-__device__ __forceinline__ void unpack(const Raw<float>& r, float (&v)[8]) {
-    v[0] = r.a.x; v[1] = r.a.y; v[2] = r.a.z; v[3] = r.a.w;
-    v[4] = r.b.x; v[5] = r.b.y; v[6] = r.b.z; v[7] = r.b.w;
+__device__ __forceinline__ void unpack(const uint4& w, float (&v)[4]) {
+    v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
 }
-__device__ __forceinline__ void store_out(bf16_t* p, const float (&v)[8]) {
+__device__ __forceinline__ uint4 pack(const float (&v)[8]) {
     uint32_t w[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c) w[c] = (uint32_t)f2bf(v[2 * c]) | ((uint32_t)f2bf(v[2 * c + 1]) << 16);
-    *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void store_out(float* p, const float (&v)[8]) {
-    *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
-    *(float4*)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+__device__ __forceinline__ uint4 pack(const float (&v)[4]) {
+    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
 }
 
-// C of a tile of 16 MR rows and p.cols columns, a quarter of them a wavefront, 64 at a time (lines of 128 bytes in bf16).  Product h of those takes the
-// columns 32 (h / 2) + 8 g + 4 (h & 1) + e (g, e < 4) as its rows 4 g + e, so that a lane ends up with eight consecutive ones, from 8 (lane >> 4) on of
-// either half, of row lane & 15.
+// C of a tile of 16 MR rows and p.cols columns, 64 at a time, the four wavefronts side by side.  Products h of 16 columns leave a lane with four of them
+// of row lane & 15; they pass through LDS (16-byte groups XOR-swizzled with the row), so that R is read and C written in whole lines.
 template <typename T, int MR, int KS>
 __global__ void __launch_bounds__(256) adapter_up_kernel(const AdapterParams p, const Table tab) {
     constexpr int NP = Parts<T>::N;
     __shared__ Frag<T> tf[MR][KS][NP][64];
+    __shared__ __attribute__((aligned(16))) unsigned char stage[4][4096];
     const int si = segment_of(tab.up0, tab.n, blockIdx.x);
     const Segment& sg = tab.seg[si];
     const int tile = (int)blockIdx.x - tab.up0[si];
@@ -266,35 +303,25 @@ __global__ void __launch_bounds__(256) adapter_up_kernel(const AdapterParams p, 
         for (int i = 0; i < NP; ++i) tf[m][k][i][lane] = part[i];
     }
     __syncthreads();
-    Frag<T> t[MR][KS][NP];
-#pragma unroll
-    for (int m = 0; m < MR; ++m)
-#pragma unroll
-        for (int k = 0; k < KS; ++k)
-#pragma unroll
-            for (int i = 0; i < NP; ++i)
-                if (k < ks) t[m][k][i] = tf[m][k][i][lane];
     const T* b = (const T*)p.b + (int64_t)sg.slot() * p.N * p.width;
-    const int share = p.cols >> 2, first = blockIdx.y * p.cols + wave * share, n1 = min(first + share, p.N);
-    for (int c0 = first; c0 < n1; c0 += 64) {
-        Raw<T> out[MR][2];
+    constexpr int V = 16 / (int)sizeof(T), LPR = 64 / V, RPP = 64 / LPR, PASSES = 16 / RPP;      // of 16 bytes; lanes of a row; rows of a pass
+    unsigned char* const stg = stage[wave];
+    const int n1 = min((int)(blockIdx.y + 1) * p.cols, p.N);
+    for (int c0 = blockIdx.y * p.cols + wave * 64; c0 < n1; c0 += 256) {
+        const int col = c0 + (lane & (LPR - 1)) * V;
+        uint4 out[MR][PASSES];
 #pragma unroll
         for (int m = 0; m < MR; ++m)
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int row = r0 + m * 16 + l15, col = c0 + q * 32 + l4 * 8;
-                if (p.res && row < end && col < n1) out[m][q] = *(const Raw<T>*)((const T*)p.res + (int64_t)row * p.N + col);
-                else out[m][q] = Raw<T>{};
+            for (int i = 0; i < PASSES; ++i) {
+                const int row = r0 + m * 16 + i * RPP + lane / LPR;
+                out[m][i] = make_uint4(0, 0, 0, 0);
+                if (p.res && row < end && col < n1) out[m][i] = *(const uint4*)((const T*)p.res + (int64_t)row * p.N + col);
             }
-        f32x4 acc[MR][4];
-#pragma unroll
-        for (int m = 0; m < MR; ++m)
-#pragma unroll
-            for (int h = 0; h < 4; ++h) acc[m][h] = f32x4{0.f, 0.f, 0.f, 0.f};
         Frag<T> w[4][KS];
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
-            const T* bp = b + (int64_t)min(c0 + (h >> 1) * 32 + (l15 >> 2) * 8 + (h & 1) * 4 + (l15 & 3), p.N - 1) * p.width + l4 * 8;
+            const T* bp = b + (int64_t)min(c0 + h * 16 + l15, p.N - 1) * p.width + l4 * 8;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 const int left = rank - k * 32 - l4 * 8;
@@ -309,29 +336,38 @@ __global__ void __launch_bounds__(256) adapter_up_kernel(const AdapterParams p, 
                 for (int k = 0; k < KS; ++k) keep(w[h][k], rank - k * 32 - l4 * 8);
         }
 #pragma unroll
-        for (int h = 0; h < 4; ++h)
+        for (int m = 0; m < MR; ++m) {
+            f32x4 acc[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) acc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < KS; ++k)
                 if (k < ks) {
 #pragma unroll
-                    for (int m = 0; m < MR; ++m)
+                    for (int h = 0; h < 4; ++h)
 #pragma unroll
-                        for (int i = NP - 1; i >= 0; --i) acc[m][h] = mma(w[h][k], t[m][k][i], acc[m][h]);
+                        for (int i = NP - 1; i >= 0; --i) acc[h] = mma(w[h][k], tf[m][k][i][lane], acc[h]);
                 }
 #pragma unroll
-        for (int m = 0; m < MR; ++m)
+            for (int h = 0; h < 4; ++h) *(f32x4*)(stg + l15 * 256 + (((h * 4 + l4) ^ l15) << 4)) = acc[h];
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int row = r0 + m * 16 + l15, col = c0 + q * 32 + l4 * 8;
-                float v[8];
-                unpack(out[m][q], v);
+            for (int i = 0; i < PASSES; ++i) {
+                const int rl = i * RPP + lane / LPR, row = r0 + m * 16 + rl;
+                float v[V];
+                unpack(out[m][i], v);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[e] += acc[m][2 * q][e];
-                    v[4 + e] += acc[m][2 * q + 1][e];
+                for (int q = 0; q < V / 4; ++q) {
+                    const f32x4 d = *(const f32x4*)(stg + rl * 256 + ((((lane & (LPR - 1)) * (V / 4) + q) ^ rl) << 4));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[q * 4 + e] += d[e];
                 }
-                if (row < end && col < n1) store_out((T*)p.c + (int64_t)row * p.N + col, v);
+                if (row < end && col < n1) *(uint4*)((T*)p.c + (int64_t)row * p.N + col) = pack(v);
             }
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_wave_barrier();
+        }
     }
 }
 
@@ -341,8 +377,10 @@ struct Launch {
     int total;                 // groups of 16 rows
 };
 
-inline int down_steps(int nr, int esz) { return (nr == 8 ? 4 : 8) * 2 / esz; }
-inline int k_slices(int nr, int esz, int K) { return (K + 32 * down_steps(nr, esz) - 1) / (32 * down_steps(nr, esz)); }
+inline int k_slices(int nr, int esz, int K) {                    // of a wavefront each
+    const int k = (nr == 8 ? 256 : 512) / esz;
+    return (K + k - 1) / k;
+}
 inline int k_pieces(int nr, int esz, int K) { return (k_slices(nr, esz, K) + DOWN_WAVES - 1) / DOWN_WAVES; }
 
 // tiles and columns of a launch
@@ -358,7 +396,19 @@ void plan(Launch& l, int esz, int N, int K) {
     }
     l.nr = l.rank <= 16 ? 1 : l.rank <= 32 ? 2 : l.rank <= 64 ? 4 : 8;
     l.mr = longest <= 16 ? 1 : l.nr == 8 ? 2 : 4;
-    l.groups = std::max(1, std::min(16, l.total * k_pieces(l.nr, esz, K) / 512));
+    // rows of a workgroup of the first launch, one a compute unit: rounds of them, each with the time of its groups and of about two more
+    // for A and the ends
+    const int pieces = k_pieces(l.nr, esz, K);
+    int64_t best = INT64_MAX;
+    for (int g = 1; g <= 64; ++g) {
+        int64_t wgs = 0;
+        for (int i = 0; i < t.n; ++i) wgs += t.seg[i].rank() ? ((t.seg[i].n + 15) / 16 + g - 1) / g : 0;
+        const int64_t time = (wgs * pieces + 255) / 256 * (std::min(g, (longest + 15) / 16) + 2);
+        if (time < best) {
+            best = time;
+            l.groups = g;
+        }
+    }
     t.down0[0] = t.up0[0] = 0;
     for (int i = 0; i < t.n; ++i) {
         const int g = (t.seg[i].n + 15) / 16;
@@ -407,12 +457,11 @@ void for_launches(const int32_t* ranks, const float* scales, bool in_place, int 
 template <typename T, int MR, int NR>
 void run_t(const AdapterParams& p, const Launch& l, hipStream_t s) {
     if (l.rank) {
-        constexpr int LDS = 2 * DOWN_WAVES * NR * 64 * 16;
+        constexpr int WAVE = Down<T, NR>::WAVE;
         static OncePerDevice once;
-        if (LDS > 64 * 1024) once.run(current_device(), [] { allow_dynamic_lds((const void*)(adapter_down_kernel<T, NR>), LDS); });
+        once.run(current_device(), [] { allow_dynamic_lds((const void*)(adapter_down_kernel<T, NR>), DOWN_WAVES * WAVE); });
         const int waves = std::min(DOWN_WAVES, k_slices(NR, sizeof(T), p.K));
-        hipLaunchKernelGGL((adapter_down_kernel<T, NR>), dim3((unsigned)l.tab.down0[l.tab.n], (unsigned)p.pieces), dim3(64 * waves),
-                           2 * waves * NR * 64 * 16, s, p, l.tab);
+        hipLaunchKernelGGL((adapter_down_kernel<T, NR>), dim3((unsigned)l.tab.down0[l.tab.n], (unsigned)p.pieces), dim3(64 * waves), waves * WAVE, s, p, l.tab);
     }
     hipLaunchKernelGGL((adapter_up_kernel<T, MR, (NR + 1) / 2>), dim3((unsigned)l.tab.up0[l.tab.n], (unsigned)((p.N + p.cols - 1) / p.cols)), dim3(256), 0, s, p, l.tab);
 }

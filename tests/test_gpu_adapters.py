@@ -84,6 +84,11 @@ SHAPES = [
     (700, 320, 14336, [16, 32], 32, [(0, 333, 1), (333, 367, 0)]),
     (2100, 640, 512, [64, 128, 8], 128, [(0, 1000, 2), (1000, 1, 0), (1001, 1099, 1)]),
     (33, 64, 64, [16], 16, []),
+    # runs of many groups of 16 rows a workgroup, their last one ragged, K not whole slices
+    (20011, 64, 520, [16, 64], 64, [(0, 9000, 0), (9001, 11003, 1)]),
+    (17003, 136, 1160, [128, 30], 128, [(0, 30, 1), (30, 16973, 0)]),
+    (9990, 64, 4104, [8], 8, [(3, 9987, 0)]),
+    (16400, 72, 2560, [32], 32, [(0, 16400, 0)]),
 ]
 
 
