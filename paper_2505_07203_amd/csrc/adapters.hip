@@ -76,6 +76,10 @@ __device__ __forceinline__ void load(Frag<float>& f, const unsigned char* row, i
     f.lo = *(const f32x4*)(row + (((2 * at) ^ swizzle) << 4));
     f.hi = *(const f32x4*)(row + (((2 * at + 1) ^ swizzle) << 4));
 }
+// 16 bytes of a fragment
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+__device__ __forceinline__ void set(Frag<bf16_t>& f, int, const u32x4& v) { f.v = __builtin_bit_cast(bf16x8, v); }
+__device__ __forceinline__ void set(Frag<float>& f, int q, const u32x4& v) { (q ? f.hi : f.lo) = __builtin_bit_cast(f32x4, v); }
 __device__ __forceinline__ void zero(Frag<bf16_t>& f) { f.v = __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0)); }
 __device__ __forceinline__ void zero(Frag<float>& f) { f.lo = f.hi = f32x4{0.f, 0.f, 0.f, 0.f}; }
 __device__ __forceinline__ f32x4 mma(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x4 c) {
@@ -255,21 +259,28 @@ __device__ __forceinline__ uint4 pack(const float (&v)[4]) {
     return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
 }
 
-// C of a tile of 16 MR rows and p.cols columns, 64 at a time, the four wavefronts side by side.  Products h of 16 columns leave a lane with four of them
+// C of a tile of 16 MR rows and p.cols columns, 64 at a time, the wavefronts side by side.  Products h of 16 columns leave a lane with four of them
 // of row lane & 15; they pass through LDS (16-byte groups XOR-swizzled with the row), so that R is read and C written in whole lines.
+// A tile's B and T are read by its workgroups alone, so these are large: what a compute unit can have under way towards it is the limit here, and
+// reads that the caches answer take their places in it like those of R (64 x 1024 by four wavefronts, three workgroups a compute unit: 89 us of
+// 16000 x 4096, 12 of them for the planes of T, 10 for B).
+constexpr int up_waves(int esz, int ks) { return esz == 4 || ks == 4 ? 8 : 16; }         // (16: 128 registers a lane)
+
 template <typename T, int MR, int KS>
-__global__ void __launch_bounds__(256) adapter_up_kernel(const AdapterParams p, const Table tab) {
-    constexpr int NP = Parts<T>::N;
+__global__ void __launch_bounds__(64 * up_waves(sizeof(T), KS)) adapter_up_kernel(const AdapterParams p, const Table tab) {
+    constexpr int NP = Parts<T>::N, E = (int)sizeof(T), UP_WAVES = up_waves(E, KS);
     __shared__ Frag<T> tf[MR][KS][NP][64];
-    __shared__ __attribute__((aligned(16))) unsigned char stage[4][4096];
-    const int si = segment_of(tab.up0, tab.n, blockIdx.x);
+    __shared__ __attribute__((aligned(16))) unsigned char stage[UP_WAVES][4096];
+    // (a tile's workgroups side by side: those that run together cover whole rows)
+    const int chunks = (p.N + p.cols - 1) / p.cols, at = (int)(blockIdx.x / (unsigned)chunks), chunk = (int)blockIdx.x - at * chunks;
+    const int si = segment_of(tab.up0, tab.n, at);
     const Segment& sg = tab.seg[si];
-    const int tile = (int)blockIdx.x - tab.up0[si];
-    const int rank = sg.rank(), r0 = sg.row + tile * (16 * MR), end = sg.row + sg.n;
+    const int tile = at - tab.up0[si];
+    const int rank = sg.rank(), r0 = sg.row + tile * (16 * MR), rows = min(16 * MR, sg.row + sg.n - r0);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l15 = lane & 15, l4 = lane >> 4;
     const int ks = (rank + 31) >> 5;
-    for (int f = wave; f < MR * ks; f += 4) {    // (a wavefront at a time: group f / ks, step f % ks)
+    for (int f = wave; f < MR * ks; f += UP_WAVES) {     // (a wavefront at a time: group f / ks, step f % ks)
         const int m = f / ks, k = f - m * ks, j0 = k * 32 + l4 * 8;
         const int group = min(tile * MR + m, (sg.n - 1) >> 4);       // (groups behind the last one: that one again)
         const float* t = p.t + ((int64_t)(sg.group0 + group) * 16 + l15) * p.rp + j0;
@@ -303,32 +314,38 @@ __global__ void __launch_bounds__(256) adapter_up_kernel(const AdapterParams p, 
         for (int i = 0; i < NP; ++i) tf[m][k][i][lane] = part[i];
     }
     __syncthreads();
-    const T* b = (const T*)p.b + (int64_t)sg.slot() * p.N * p.width;
-    constexpr int V = 16 / (int)sizeof(T), LPR = 64 / V, RPP = 64 / LPR, PASSES = 16 / RPP;      // of 16 bytes; lanes of a row; rows of a pass
+    // R and C by the tile's rows, B by its slot: what lies behind their ends reads as zero and is not written, and so does what a lane's offset is
+    // moved out of bounds for
+    constexpr int V = 16 / E, LPR = 64 / V, RPP = 64 / LPR, PASSES = 16 / RPP;           // of 16 bytes; lanes of a row; rows of a pass
+    constexpr uint32_t NONE = 0x80000000u;
     unsigned char* const stg = stage[wave];
-    const int n1 = min((int)(blockIdx.y + 1) * p.cols, p.N);
-    for (int c0 = blockIdx.y * p.cols + wave * 64; c0 < n1; c0 += 256) {
-        const int col = c0 + (lane & (LPR - 1)) * V;
-        uint4 out[MR][PASSES];
+    const uint32_t pitch = (uint32_t)p.N * E, bytes = (uint32_t)rows * pitch;
+    const int64_t tile_at = (int64_t)r0 * p.N * E;
+    const __amdgpu_buffer_rsrc_t rr = __builtin_amdgcn_make_buffer_rsrc((void*)((const unsigned char*)(p.res ? p.res : p.c) + tile_at), 0, p.res ? (int)bytes : 0, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void*)((unsigned char*)p.c + tile_at), 0, (int)bytes, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)((const unsigned char*)p.b + (int64_t)sg.slot() * p.N * p.width * E), 0, (int)((uint32_t)p.N * (uint32_t)p.width * E), 0x00020000);
+    uint32_t vb[4];                              // (KS entries used)
+#pragma unroll
+    for (int k = 0; k < KS; ++k) vb[k] = rank - k * 32 - l4 * 8 > 0 ? (uint32_t)(l15 * p.width + k * 32 + l4 * 8) * E : NONE;
+    const uint32_t vr = (uint32_t)(lane / LPR) * pitch + (uint32_t)(lane & (LPR - 1)) * 16u;
+    const int n1 = min((chunk + 1) * p.cols, p.N);
+    for (int c0 = chunk * p.cols + wave * 64; c0 < n1; c0 += UP_WAVES * 64) {
+        Frag<T> w[4][KS];
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int q = 0; q < E / 2; ++q)
+                    set(w[h][k], q, __builtin_amdgcn_raw_buffer_load_b128(rb, vb[k], (uint32_t)(c0 + h * 16) * (uint32_t)p.width * E + q * 16, 0));
+        const uint32_t vo = c0 + (lane & (LPR - 1)) * V < p.N ? vr : NONE;
+        u32x4 out[MR][PASSES];                   // (behind B: loads return in order, and B comes from a cache)
 #pragma unroll
         for (int m = 0; m < MR; ++m)
 #pragma unroll
-            for (int i = 0; i < PASSES; ++i) {
-                const int row = r0 + m * 16 + i * RPP + lane / LPR;
-                out[m][i] = make_uint4(0, 0, 0, 0);
-                if (p.res && row < end && col < n1) out[m][i] = *(const uint4*)((const T*)p.res + (int64_t)row * p.N + col);
-            }
-        Frag<T> w[4][KS];
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            const T* bp = b + (int64_t)min(c0 + h * 16 + l15, p.N - 1) * p.width + l4 * 8;
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                const int left = rank - k * 32 - l4 * 8;
-                if (left > 0) load(w[h][k], bp + k * 32);            // (width is a multiple of 8)
-                else zero(w[h][k]);
-            }
-        }
+            for (int i = 0; i < PASSES; ++i)
+                out[m][i] = __builtin_amdgcn_raw_buffer_load_b128(rr, vo, (uint32_t)c0 * E + (uint32_t)(m * 16 + i * RPP) * pitch, 0);
         if (rank & 7) {
 #pragma unroll
             for (int h = 0; h < 4; ++h)
@@ -344,9 +361,11 @@ __global__ void __launch_bounds__(256) adapter_up_kernel(const AdapterParams p, 
             for (int k = 0; k < KS; ++k)
                 if (k < ks) {
 #pragma unroll
-                    for (int h = 0; h < 4; ++h)
+                    for (int i = NP - 1; i >= 0; --i) {
+                        const Frag<T> t = tf[m][k][i][lane];
 #pragma unroll
-                        for (int i = NP - 1; i >= 0; --i) acc[h] = mma(w[h][k], tf[m][k][i][lane], acc[h]);
+                        for (int h = 0; h < 4; ++h) acc[h] = mma(w[h][k], t, acc[h]);
+                    }
                 }
 #pragma unroll
             for (int h = 0; h < 4; ++h) *(f32x4*)(stg + l15 * 256 + (((h * 4 + l4) ^ l15) << 4)) = acc[h];
@@ -354,16 +373,18 @@ __global__ void __launch_bounds__(256) adapter_up_kernel(const AdapterParams p, 
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) {
-                const int rl = i * RPP + lane / LPR, row = r0 + m * 16 + rl;
+                const int rl = i * RPP + lane / LPR;
                 float v[V];
-                unpack(out[m][i], v);
+                unpack(__builtin_bit_cast(uint4, out[m][i]), v);
 #pragma unroll
                 for (int q = 0; q < V / 4; ++q) {
                     const f32x4 d = *(const f32x4*)(stg + rl * 256 + ((((lane & (LPR - 1)) * (V / 4) + q) ^ rl) << 4));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[q * 4 + e] += d[e];
                 }
-                if (row < end && col < n1) *(uint4*)((T*)p.c + (int64_t)row * p.N + col) = pack(v);
+                // (no scalar offset: with one the compiler takes a store's registers as free at once, and the next instruction overwrote
+                // the first of them before the last lanes were read)
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, pack(v)), rc, vo + ((uint32_t)c0 * E + (uint32_t)(m * 16 + i * RPP) * pitch), 0, 0);
             }
             asm volatile("" ::: "memory");
             __builtin_amdgcn_wave_barrier();
@@ -415,8 +436,8 @@ void plan(Launch& l, int esz, int N, int K) {
         t.down0[i + 1] = t.down0[i] + (g + l.groups - 1) / l.groups;
         t.up0[i + 1] = t.up0[i] + (g + l.mr - 1) / l.mr;
     }
-    l.cols = 1024;
-    while (l.cols > 256 && (int64_t)t.up0[t.n] * ((N + l.cols - 1) / l.cols) < 1024) l.cols /= 2;
+    l.cols = 4096;
+    while (l.cols > 64 * up_waves(esz, l.nr / 2) && (int64_t)t.up0[t.n] * ((N + l.cols - 1) / l.cols) < 200) l.cols /= 2;
 }
 size_t floats_of(const Launch& l, int esz, int K) { return l.rank ? (size_t)k_pieces(l.nr, esz, K) * l.total * 16 * (16 * l.nr) : 0; }
 
@@ -463,7 +484,8 @@ void run_t(const AdapterParams& p, const Launch& l, hipStream_t s) {
         const int waves = std::min(DOWN_WAVES, k_slices(NR, sizeof(T), p.K));
         hipLaunchKernelGGL((adapter_down_kernel<T, NR>), dim3((unsigned)l.tab.down0[l.tab.n], (unsigned)p.pieces), dim3(64 * waves), waves * WAVE, s, p, l.tab);
     }
-    hipLaunchKernelGGL((adapter_up_kernel<T, MR, (NR + 1) / 2>), dim3((unsigned)l.tab.up0[l.tab.n], (unsigned)((p.N + p.cols - 1) / p.cols)), dim3(256), 0, s, p, l.tab);
+    hipLaunchKernelGGL((adapter_up_kernel<T, MR, (NR + 1) / 2>), dim3((unsigned)l.tab.up0[l.tab.n] * (unsigned)((p.N + p.cols - 1) / p.cols)), dim3(64 * up_waves(sizeof(T), (NR + 1) / 2)), 0, s,
+                       p, l.tab);
 }
 
 template <typename T>

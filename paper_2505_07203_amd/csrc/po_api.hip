@@ -1812,7 +1812,7 @@ static po_status adapter_shape(int32_t dtype, const int32_t* ranks, int32_t n_sl
                                const po_adapter_rows* seg, int32_t n_seg) {
     if (bad_dtype(dtype) || !ranks || n_slots <= 0 || width <= 0 || rows <= 0 || N <= 0 || K <= 0 || n_seg < 0 || (n_seg && !seg)) return PO_ERR_INVALID_ARG;
     if (width % 8 || width > 128 || N % 8 || K % 8) return PO_ERR_BAD_CONFIG;
-    if (rows > (int64_t)1 << 23 || N > 1 << 22 || K > 1 << 17 || n_slots >= 1 << 23) return PO_ERR_TOO_LONG;
+    if (rows > (int64_t)1 << 23 || N > 1 << 20 || K > 1 << 17 || n_slots >= 1 << 23) return PO_ERR_TOO_LONG;
     for (int32_t i = 0; i < n_slots; ++i)
         if (ranks[i] < 0 || ranks[i] > width) return PO_ERR_INVALID_ARG;
     int64_t row = 0;

@@ -42,7 +42,7 @@ def test_adapters_refusals():
     refused(B.lib().po_op_adapters, ok, [
         (0, 2, 1), (0, -1, 1), (1, None, 1), (2, None, 1), (3, None, 1), (4, None, 1), (5, None, 1), (6, 0, 1), (7, 0, 1), (7, 12, 2), (7, 136, 2), (7, 8, 1), (9, None, 1), (9, P, 1), (8, P, 1),
         (10, 0, 1), (10, 9, 1), (11, 0, 1), (11, 60, 2), (12, -8, 1), (12, 100, 2), (13, None, 1), (14, -1, 1), (15, None, 1), (15, 6 * P + 64, 1), (16, 0, 6), (6, 2, 1),
-        (10, (1 << 23) + 1, 4), (11, (1 << 22) + 8, 4), (12, (1 << 17) + 8, 4), (4, ints(8, 17, 0), 1), (4, ints(-1, 16, 0), 1),
+        (10, (1 << 23) + 1, 4), (11, (1 << 20) + 8, 4), (12, (1 << 17) + 8, 4), (4, ints(8, 17, 0), 1), (4, ints(-1, 16, 0), 1),
         (13, segs((0, 4, 0), (3, 3, -1), (9, 1, 2)), 1), (13, segs((0, 4, 0), (4, -1, -1), (9, 1, 2)), 1), (13, segs((0, 4, 3), (4, 3, -1), (9, 1, 2)), 1),
         (13, segs((0, 4, -2), (4, 3, -1), (9, 1, 2)), 1), (13, segs((-1, 4, 0), (4, 3, -1), (9, 1, 2)), 1), (13, segs((0, 4, 0), (4, 3, -1), (9, 2, 2)), 1),
         (13, segs((0, 4, 0), (4, 3, -1), (1 << 62, 1 << 62, 2)), 1)] + [(i, ok[i] + 8, 1) for i in (1, 2, 3, 8, 9)])
