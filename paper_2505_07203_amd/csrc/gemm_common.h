@@ -4,6 +4,7 @@
 #include "slice_window.h"
 
 #include <type_traits>
+#include <utility>
 
 namespace po {
 
@@ -37,6 +38,8 @@ struct GemmParams {
     const float* sw;
     float q_scale;       // EPI_QKV_ROPE: factor on the rotated Q values before they are rounded (1, or the softmax
                          // scale in log2 units when the attention kernel expects Q scaled; K and V are never scaled)
+    const int32_t* tok;  // EPI_LOGPROB: a token of each row, or null, and where its logit goes
+    float* at;
     bool w_cached;       // (launchers) the weights are expected in the memory-side cache
 };
 
@@ -541,6 +544,96 @@ __device__ __forceinline__ void tile_epilogue16(const GemmParams& p, const f32x4
             __builtin_amdgcn_sched_barrier(0);
         }
     }
+}
+
+// f(0), .., f(N - 1) as constants (a loop of this size is no longer unrolled, and its accumulators would move to memory)
+template <typename F, int... I>
+__device__ __forceinline__ void for_each_constant(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+
+// (m, S, T) of a wavefront's patch of 16 MU rows x 64 logits, for launch_gemm_logprob; acc as in tile_epilogue16.  Into LDS: out[row of the
+// tile] for each of the three, planes of `plane` floats.  The four lanes of a row exchange by way of LDS; the exponentials, 128 a
+// lane with MU 8, are what this costs (3 us of a tile's 90 at K 4096).
+template <int MU>
+__device__ __forceinline__ void tile_logprob(const GemmParams& p, const f32x4 (&acc)[MU][4], float* out, int plane, int tile_row, int row_base, int col_base, int lane) {
+    constexpr float LOG2E = 1.44269504f;
+    const int l15 = lane & 15, l4 = lane >> 4;
+    const int left = p.N - col_base - 4 * l4;              // logits of tile t exist where 16 t + e < left
+    const bool none = col_base >= p.N, ragged = col_base + 64 > p.N;
+    for_each_constant([&](auto uc) {
+        constexpr int u = decltype(uc)::value;
+        float m = -INFINITY, s = 0.f, t = 0.f;
+        if (!none) {
+            float v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = acc[u][i >> 2][i & 3];
+            if (ragged) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if ((i >> 2) * 16 + (i & 3) >= left) v[i] = -INFINITY;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) m = fmaxf(m, v[i]);
+            m = fmaxf(m, __shfl_xor(m, 16));
+            m = fmaxf(m, __shfl_xor(m, 32));
+            if (ragged) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {             // (a logit that is not there: where its term is 0 in float32)
+                    const float d = fmaxf((v[i] - m) * LOG2E, -250.0f), e = __builtin_amdgcn_exp2f(d);
+                    s += e;
+                    t = fmaf(d, e, t);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float d = (v[i] - m) * LOG2E, e = __builtin_amdgcn_exp2f(d);
+                    s += e;
+                    t = fmaf(d, e, t);
+                }
+            }
+            s += __shfl_xor(s, 16);
+            t += __shfl_xor(t, 16);
+            s += __shfl_xor(s, 32);
+            t += __shfl_xor(t, 32);
+            if (p.tok) {
+                const int row = row_base + u * 16 + l15;
+                const int64_t d = row < p.M ? (int64_t)p.tok[row] - col_base : -1;
+                if (d >= 0 && d < 64 && d < p.N - col_base && ((d >> 2) & 3) == l4) {
+                    float x = v[0];
+#pragma unroll
+                    for (int i = 1; i < 16; ++i) x = d == (i >> 2) * 16 + 4 * l4 + (i & 3) ? v[i] : x;
+                    p.at[row] = x;
+                }
+            }
+        }
+        if (l4 == 0) {
+            float* o = out + tile_row + u * 16 + l15;
+            o[0] = m;
+            o[plane] = s;
+            o[2 * plane] = t;
+        }
+    }, std::make_integer_sequence<int, MU>{});
+}
+// joins the patches of a row (WN of them, in LDS, BM_ rows and three planes each) and writes its block's numbers
+template <int WN, int BM_>
+__device__ __forceinline__ void tile_logprob_join(const GemmParams& p, const float* in, int tn, int m0, int tid) {
+    constexpr float LOG2E = 1.44269504f;
+    if (tid >= BM_ || m0 + tid >= p.M) return;
+    float m = -INFINITY, s = 0.f, t = 0.f;
+#pragma unroll
+    for (int w = 0; w < WN; ++w) m = fmaxf(m, in[w * 3 * BM_ + tid]);
+#pragma unroll
+    for (int w = 0; w < WN; ++w) {
+        const float* o = in + w * 3 * BM_ + tid;
+        if (o[0] > -INFINITY) {
+            const float d = (o[0] - m) * LOG2E, e = __builtin_amdgcn_exp2f(d);
+            s = fmaf(o[BM_], e, s);
+            t = fmaf(fmaf(d, o[BM_], o[2 * BM_]), e, t);
+        }
+    }
+    float* q = (float*)p.dst + (int64_t)tn * p.M + m0 + tid;
+    q[0] = m;
+    q[p.ldr] = s;
+    q[2 * p.ldr] = t;
 }
 
 // ---- block tiles and K splits, shared by the bf16 and the FP8 GEMM (defined with the bf16 kernels)

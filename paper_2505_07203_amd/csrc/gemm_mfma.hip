@@ -188,7 +188,12 @@ __global__ void __launch_bounds__(NT_BF16) gemm_bf16_mfma_kernel(const GemmParam
 #undef PO_DMA
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
-    if (EPI == EPI_PARTIAL) {
+    if (EPI == EPI_LOGPROB) {
+        float* const sums = (float*)smem;                  // [4][3][BM_]
+        tile_logprob<MU>(p, acc, sums + wn * 3 * BM_, BM_, wm * (MU * 16), m0 + wm * (MU * 16), n0 + wn * 64, lane);
+        __syncthreads();
+        tile_logprob_join<4, BM_>(p, sums, tn, m0, tid);
+    } else if (EPI == EPI_PARTIAL) {
         GemmParams q = p;
         q.dst = (bf16_t*)((float*)p.dst + (int64_t)blockIdx.y * p.ldr);
         tile_epilogue16<EPI, MU>(q, acc, smem + wave * 4096, m0 + wm * (MU * 16), n0 + wn * 64, lane);
@@ -367,7 +372,12 @@ __global__ void __launch_bounds__(256, 2) gemm_bf16_small_kernel(const GemmParam
 #undef PO_DMA_W
 #undef PO_SLICE_RSRC
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (EPI == EPI_PARTIAL) {
+    if (EPI == EPI_LOGPROB) {
+        float* const sums = (float*)smem;                  // [2][3][BM_]
+        tile_logprob<MU>(p, acc, sums + wn * 3 * BM_, BM_, wm * (MU * 16), m0 + wm * (MU * 16), n0 + wn * 64, lane);
+        __syncthreads();
+        tile_logprob_join<2, BM_>(p, sums, tn, m0, tid);
+    } else if (EPI == EPI_PARTIAL) {
         GemmParams q = p;
         q.dst = (bf16_t*)((float*)p.dst + (int64_t)blockIdx.y * p.ldr);
         tile_epilogue16<EPI, MU>(q, acc, smem + wave * 4096, m0 + wm * (MU * 16), n0 + wn * 64, lane);
@@ -709,8 +719,8 @@ void launch_strips(const GemmParams& p, hipStream_t s) {
 
 template <int EPI>
 void launch_form(int form, const GemmParams& p, hipStream_t s, int splits = 1) {
-    if (EPI != EPI_PARTIAL && form == STRIPS) {
-        constexpr int E = EPI == EPI_PARTIAL ? EPI_STORE : EPI;
+    if (EPI != EPI_PARTIAL && EPI != EPI_LOGPROB && form == STRIPS) {
+        constexpr int E = EPI == EPI_PARTIAL || EPI == EPI_LOGPROB ? EPI_STORE : EPI;
         if (p.M <= 2) launch_strips<E, 1>(p, s);
         else launch_strips<E, 8>(p, s);
         return;
@@ -777,13 +787,20 @@ void launch_gemm_mfma(int epi, const bf16_t* A, int64_t lda, const bf16_t* W, in
     }
 }
 
-void launch_gemm_mfma_f32(const bf16_t* A, int64_t lda, const bf16_t* W, int64_t ldw, float* C, int64_t ldc, int64_t M, int N, int K,
-                          hipStream_t s) {
+int gemm_logprob_blocks(int64_t M, int N, int K) {
+    const int bn = FORMS[pick_form(TILES, base_params(nullptr, K, nullptr, K, M, N, K), 1)].bn;
+    return (N + bn - 1) / bn;
+}
+
+void launch_gemm_logprob(const bf16_t* A, int64_t lda, const bf16_t* W, int64_t ldw, float* stats, const int32_t* tok, float* at, int64_t M, int N,
+                         int K, hipStream_t s) {
     if (M <= 0 || N <= 0) return;
     GemmParams p = base_params(A, lda, W, ldw, M, N, K);
-    p.dst = (bf16_t*)C;
-    p.ld = ldc;
-    launch_form<EPI_PARTIAL>(pick_form(TILES, p, 1), p, s, 1);
+    p.dst = (bf16_t*)stats;
+    p.ldr = gemm_logprob_blocks(M, N, K) * M;
+    p.tok = tok;
+    p.at = at;
+    launch_form<EPI_LOGPROB>(pick_form(TILES, p, 1), p, s);
 }
 
 namespace gemm {

@@ -173,7 +173,6 @@ __device__ __forceinline__ void join(const Stats& x, float m, Sums& r) {
         r.t += ((double)x.t + d * x.s) * e;
     }
 }
-__device__ __forceinline__ float entropy_of(const Sums& r, float m) { return m > -INFINITY ? (float)fmax(0.0, log(r.s) - r.t / r.s) : 0.f; }
 __device__ __forceinline__ float logprob_of(float l, float m, double log_s) {
     if (!(l > -INFINITY)) return -INFINITY;      // (NaN too)
     if (m == INFINITY) return l == INFINITY ? (float)-log_s : -INFINITY;
@@ -393,12 +392,22 @@ void launch_token_logprobs(int dtype, const void* logits, int64_t ld, int64_t ro
 }
 
 // ------------------------------------------------------------------ through the LM head
-// Logits of hidden rows, formed in panels of columns in scratch, each reduced to its pieces' (m, S, T) before the next.
+// bf16: the product leaves (m, S, T) of blocks of 256 or 128 columns (launch_gemm_logprob).  float32: logits in panels of columns in scratch,
+// each reduced to its pieces' (m, S, T) before the next.
 namespace {
 
 // columns of a panel: what stays in the memory-side cache (256 MiB of logits), at least a piece
 inline int64_t panel_width(int64_t rows, int V) {
     return std::min(std::max<int64_t>(1, std::min<int64_t>(16, ((int64_t)1 << 26) / rows / PIECE)) * PIECE, round_up64(V, PIECE));
+}
+
+__device__ __forceinline__ void head_answer(const Sums& sum, float m, float at, const int32_t* tokens, int V, int64_t r, float* logprobs, float* entropy) {
+    const double log_s = log(sum.s);
+    if (entropy) entropy[r] = m > -INFINITY ? (float)fmax(0.0, log_s - sum.t / sum.s) : 0.f;
+    if (logprobs) {
+        const int32_t t = tokens[r];
+        logprobs[r] = t >= 0 && t < V ? logprob_of(at, m, log_s) : -INFINITY;
+    }
 }
 
 // a row's answer from its pieces: a wavefront each
@@ -418,22 +427,68 @@ __global__ void __launch_bounds__(256) head_rows_kernel(const Stats* __restrict_
         sum.s += __shfl_xor(sum.s, off);
         sum.t += __shfl_xor(sum.t, off);
     }
-    if (lane) return;
-    if (entropy) entropy[r] = entropy_of(sum, m);
-    if (logprobs) {
-        const int32_t t = tokens[r];
-        logprobs[r] = t >= 0 && t < V ? logprob_of(at[r], m, log(sum.s)) : -INFINITY;
+    if (lane == 0) head_answer(sum, m, logprobs ? at[r] : 0.f, tokens, V, r, logprobs, entropy);
+}
+
+// ... from its blocks' planes [blocks][rows]: R rows (a power of two) side by side in a workgroup, 256 / R threads a row
+__global__ void __launch_bounds__(256) head_blocks_kernel(const float* __restrict__ stats, int64_t plane, int blocks, int R, const float* __restrict__ at,
+                                                          const int32_t* __restrict__ tokens, int V, int64_t rows, float* __restrict__ logprobs,
+                                                          float* __restrict__ entropy) {
+    constexpr float LN2 = 0.693147181f;
+    __shared__ float ms[256];
+    __shared__ double ss[256], ts[256];
+    const int tid = threadIdx.x, parts = 256 / R, part = tid / R;
+    const int64_t r = (int64_t)blockIdx.x * R + tid % R;
+    float m = -INFINITY;
+    if (r < rows)
+        for (int i = part; i < blocks; i += parts) m = fmaxf(m, stats[i * rows + r]);
+    ms[tid] = m;
+    __syncthreads();
+    for (int n = 128; n >= R; n >>= 1) {
+        if (tid < n) ms[tid] = fmaxf(ms[tid], ms[tid + n]);
+        __syncthreads();
     }
+    m = ms[tid % R];
+    Sums sum = {0.0, 0.0};
+    if (r < rows)
+        for (int i = part; i < blocks; i += parts) {
+            const float* q = stats + i * rows + r;
+            join(Stats{q[0], q[plane], q[2 * plane] * LN2, 0.f}, m, sum);
+        }
+    ss[tid] = sum.s;
+    ts[tid] = sum.t;
+    __syncthreads();
+    for (int n = 128; n >= R; n >>= 1) {
+        if (tid < n) {
+            ss[tid] += ss[tid + n];
+            ts[tid] += ts[tid + n];
+        }
+        __syncthreads();
+    }
+    if (tid < R && r < rows) head_answer(Sums{ss[tid], ts[tid]}, m, logprobs ? at[r] : 0.f, tokens, V, r, logprobs, entropy);
 }
 
 }  // namespace
 
 size_t head_logprobs_scratch(int dtype, int64_t rows, int V, int d) {
+    if (dtype != 0) return (size_t)rows * ((size_t)gemm_logprob_blocks(rows, V, d) * 12 + 4);
     return (size_t)rows * ((size_t)panel_width(rows, V) * 4 + (size_t)pieces_of(V) * sizeof(Stats) + 4);
 }
 
 void launch_head_logprobs(int dtype, const void* x, const void* w, int64_t rows, int V, int d, const int32_t* tokens, float* logprobs,
                           float* entropy, void* scratch, hipStream_t s) {
+    if (dtype != 0) {
+        const int blocks = gemm_logprob_blocks(rows, V, d);
+        const int64_t plane = (int64_t)blocks * rows;
+        float* stats = (float*)scratch;
+        float* at = stats + 3 * plane;
+        launch_gemm_logprob((const bf16_t*)x, d, (const bf16_t*)w, d, stats, tokens, at, rows, V, d, s);
+        int R = 1;
+        while (R < 16 && R < rows) R *= 2;
+        hipLaunchKernelGGL(head_blocks_kernel, dim3((unsigned)((rows + R - 1) / R)), dim3(256), 0, s, stats, plane, blocks, R, at, tokens, V, rows, logprobs,
+                           entropy);
+        return;
+    }
     const int64_t width = panel_width(rows, V);
     const int pieces = pieces_of(V);
     float* panel = (float*)scratch;
@@ -441,8 +496,7 @@ void launch_head_logprobs(int dtype, const void* x, const void* w, int64_t rows,
     float* at = (float*)(stats + rows * pieces);
     for (int v0 = 0; v0 < V; v0 += (int)width) {
         const int n = (int)std::min<int64_t>(width, V - v0), p = pieces_of(n);
-        if (dtype == 0) launch_gemm_basic(0, x, d, (const float*)w + (int64_t)v0 * d, d, panel, width, nullptr, nullptr, 0, rows, n, d, s);
-        else launch_gemm_mfma_f32((const bf16_t*)x, d, (const bf16_t*)w + (int64_t)v0 * d, d, panel, width, rows, n, d, s);
+        launch_gemm_basic(0, x, d, (const float*)w + (int64_t)v0 * d, d, panel, width, nullptr, nullptr, 0, rows, n, d, s);
         const int64_t total = rows * p;
         hipLaunchKernelGGL((logprob_pieces_kernel<float, true>), dim3((unsigned)((total + 3) / 4)), dim3(256), 0, s, panel, width, n, p, total,
                            stats + v0 / PIECE, (int64_t)pieces, (float*)nullptr, 0, tokens, v0, tokens ? at : nullptr);

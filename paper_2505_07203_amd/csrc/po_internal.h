@@ -69,7 +69,7 @@ void launch_pack_gate_up(int dtype, const void* wg, const void* wu, void* wgu, i
                          hipStream_t s);
 
 // ---- launchers: bf16 MFMA kernels ------------------------------------------------------
-enum { EPI_STORE = 0, EPI_RESIDUAL = 1, EPI_SILU_MUL = 2, EPI_QKV_ROPE = 3, EPI_PARTIAL = 4 };
+enum { EPI_STORE = 0, EPI_RESIDUAL = 1, EPI_SILU_MUL = 2, EPI_QKV_ROPE = 3, EPI_PARTIAL = 4, EPI_LOGPROB = 5 };
 // C[M,N] = A[M,K] W[N,K]^T with bf16 MFMA, fp32 accumulation.
 //   EPI_STORE    : C = acc (+ bias[N], bf16)
 //   EPI_RESIDUAL : C = acc + R  (added in fp32; R may alias C)
@@ -247,9 +247,12 @@ void launch_token_logprobs(int dtype, const void* logits, int64_t ld, int64_t ro
 size_t head_logprobs_scratch(int dtype, int64_t rows, int V, int d);
 void launch_head_logprobs(int dtype, const void* x, const void* w, int64_t rows, int V, int d, const int32_t* tokens, float* logprobs,
                           float* entropy, void* scratch, hipStream_t s);
-// C (float32, row pitch ldc) = A W^T of bf16 operands, K % 64 == 0; ldc a multiple of 64, and columns up to the next multiple of 64 are written
-void launch_gemm_mfma_f32(const bf16_t* A, int64_t lda, const bf16_t* W, int64_t ldw, float* C, int64_t ldc, int64_t M, int N, int K,
-                          hipStream_t s);
+// Logits A W^T of bf16 operands (K % 64 == 0, any N), of which a block of columns leaves (m, S, T) for each row: the largest logit, and over the
+// block sum exp(l - m) and sum (l - m) exp(l - m) log2(e): three planes of float32 [blocks][M] at `stats`.  Where tok is not null, at[row] = the
+// logit of token tok[row] (nothing where there is no such column).  gemm_logprob_blocks: their number.
+int gemm_logprob_blocks(int64_t M, int N, int K);
+void launch_gemm_logprob(const bf16_t* A, int64_t lda, const bf16_t* W, int64_t ldw, float* stats, const int32_t* tok, float* at, int64_t M, int N,
+                         int K, hipStream_t s);
 
 // ---- micro-peaks (measurement only)
 double launch_mfma_peak(int kind, int waves_per_simd, int iters, const void* operands, size_t operand_bytes, float* sink,
