@@ -404,6 +404,8 @@ inline int k_slices(int nr, int esz, int K) {                    // of a wavefro
 }
 inline int k_pieces(int nr, int esz, int K) { return (k_slices(nr, esz, K) + DOWN_WAVES - 1) / DOWN_WAVES; }
 
+inline int nr_of(int rank) { return rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8; }
+
 // tiles and columns of a launch
 void plan(Launch& l, int esz, int N, int K) {
     Table& t = l.tab;
@@ -413,22 +415,23 @@ void plan(Launch& l, int esz, int N, int K) {
         l.rank = std::max(l.rank, t.seg[i].rank());
         longest = std::max(longest, t.seg[i].n);
         t.seg[i].group0 = l.total;
-        l.total += (t.seg[i].n + 15) / 16;
+        if (t.seg[i].rank()) l.total += (t.seg[i].n + 15) / 16;
     }
-    l.nr = l.rank <= 16 ? 1 : l.rank <= 32 ? 2 : l.rank <= 64 ? 4 : 8;
+    l.nr = nr_of(l.rank);
     l.mr = longest <= 16 ? 1 : l.nr == 8 ? 2 : 4;
     // rows of a workgroup of the first launch, one a compute unit: rounds of them, each with the time of its groups and of about two more
     // for A and the ends
-    const int pieces = k_pieces(l.nr, esz, K);
+    const int pieces = k_pieces(l.nr, esz, K), most = (longest + 15) / 16;
     int64_t best = INT64_MAX;
-    for (int g = 1; g <= 64; ++g) {
+    for (int g : {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 56, 64}) {
         int64_t wgs = 0;
         for (int i = 0; i < t.n; ++i) wgs += t.seg[i].rank() ? ((t.seg[i].n + 15) / 16 + g - 1) / g : 0;
-        const int64_t time = (wgs * pieces + 255) / 256 * (std::min(g, (longest + 15) / 16) + 2);
+        const int64_t time = (wgs * pieces + 255) / 256 * (std::min(g, most) + 2);
         if (time < best) {
             best = time;
             l.groups = g;
         }
+        if (g >= most) break;
     }
     t.down0[0] = t.up0[0] = 0;
     for (int i = 0; i < t.n; ++i) {
@@ -439,8 +442,6 @@ void plan(Launch& l, int esz, int N, int K) {
     l.cols = 4096;
     while (l.cols > 64 * up_waves(esz, l.nr / 2) && (int64_t)t.up0[t.n] * ((N + l.cols - 1) / l.cols) < 200) l.cols /= 2;
 }
-size_t floats_of(const Launch& l, int esz, int K) { return l.rank ? (size_t)k_pieces(l.nr, esz, K) * l.total * 16 * (16 * l.nr) : 0; }
-
 // calls f(Launch&) for every launch's table of requests, tiles counted
 template <typename F>
 void for_launches(const int32_t* ranks, const float* scales, bool in_place, int esz, int64_t rows, int N, int K, const po_adapter_rows* seg, int n_seg, F f) {
@@ -509,13 +510,17 @@ void run(AdapterParams p, const Launch& l, hipStream_t s) {
 
 }  // namespace
 
-size_t adapters_scratch(int dtype, const int32_t* ranks, int64_t rows, int N, int K, const po_adapter_rows* seg, int n_seg) {
-    size_t most = 0;
-    const int esz = dtype == 0 ? 4 : 2;
-    // (in place or not changes the tables of launches: the larger of both)
-    for (const bool in_place : {false, true})
-        for_launches(ranks, nullptr, in_place, esz, rows, N, K, seg, n_seg, [&](const Launch& l) { most = std::max(most, floats_of(l, esz, K)); });
-    return most * sizeof(float);
+// (of all requests in one launch: each of several takes less)
+size_t adapters_scratch(int dtype, const int32_t* ranks, int K, const po_adapter_rows* seg, int n_seg) {
+    int rank = 0;
+    int64_t groups = 0;
+    for (int i = 0; i < n_seg; ++i) {
+        const int r = seg[i].adapter < 0 ? 0 : ranks[seg[i].adapter];
+        if (r) groups += (seg[i].n_rows + 15) / 16;
+        rank = std::max(rank, r);
+    }
+    const int nr = nr_of(rank);
+    return rank ? (size_t)k_pieces(nr, dtype == 0 ? 4 : 2, K) * (size_t)groups * 16 * (16 * nr) * sizeof(float) : 0;
 }
 
 void launch_adapters(int dtype, const void* x, const void* a, const void* b, const int32_t* ranks, const float* scales, int width, const void* res,

@@ -173,6 +173,12 @@ __device__ __forceinline__ void join(const Stats& x, float m, Sums& r) {
         r.t += ((double)x.t + d * x.s) * e;
     }
 }
+// the sums relative to another maximum, at least as large
+__device__ __forceinline__ Sums moved(const Sums& r, float from, float to) {
+    if (from == to || !(from > -INFINITY)) return r;
+    const double d = (double)from - (double)to, e = (double)__expf((float)d);
+    return {r.s * e, (r.t + d * r.s) * e};
+}
 __device__ __forceinline__ float logprob_of(float l, float m, double log_s) {
     if (!(l > -INFINITY)) return -INFINITY;      // (NaN too)
     if (m == INFINITY) return l == INFINITY ? (float)-log_s : -INFINITY;
@@ -435,37 +441,47 @@ __global__ void __launch_bounds__(256) head_blocks_kernel(const float* __restric
                                                           const int32_t* __restrict__ tokens, int V, int64_t rows, float* __restrict__ logprobs,
                                                           float* __restrict__ entropy) {
     constexpr float LN2 = 0.693147181f;
-    __shared__ float ms[256];
-    __shared__ double ss[256], ts[256];
-    const int tid = threadIdx.x, parts = 256 / R, part = tid / R;
-    const int64_t r = (int64_t)blockIdx.x * R + tid % R;
+    __shared__ float ms[4][16];
+    __shared__ double ss[4][16], ts[4][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, parts = 256 / R, at_r = tid % R;
+    const int64_t r = (int64_t)blockIdx.x * R + at_r, rr = r < rows ? r : rows - 1;
+    // a thread's blocks, four loads under way together
     float m = -INFINITY;
-    if (r < rows)
-        for (int i = part; i < blocks; i += parts) m = fmaxf(m, stats[i * rows + r]);
-    ms[tid] = m;
-    __syncthreads();
-    for (int n = 128; n >= R; n >>= 1) {
-        if (tid < n) ms[tid] = fmaxf(ms[tid], ms[tid + n]);
-        __syncthreads();
-    }
-    m = ms[tid % R];
     Sums sum = {0.0, 0.0};
-    if (r < rows)
-        for (int i = part; i < blocks; i += parts) {
-            const float* q = stats + i * rows + r;
-            join(Stats{q[0], q[plane], q[2 * plane] * LN2, 0.f}, m, sum);
+    for (int i0 = tid / R; i0 < blocks; i0 += 4 * parts) {
+        Stats q[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + u * parts;
+            q[u] = Stats{-INFINITY, 0.f, 0.f, 0.f};
+            if (i < blocks) {
+                const float* g = stats + i * rows + rr;
+                q[u] = Stats{g[0], g[plane], g[2 * plane], 0.f};
+            }
         }
-    ss[tid] = sum.s;
-    ts[tid] = sum.t;
-    __syncthreads();
-    for (int n = 128; n >= R; n >>= 1) {
-        if (tid < n) {
-            ss[tid] += ss[tid + n];
-            ts[tid] += ts[tid + n];
-        }
-        __syncthreads();
+        const float more = fmaxf(fmaxf(fmaxf(q[0].m, q[1].m), fmaxf(q[2].m, q[3].m)), m);
+        sum = moved(sum, m, more);
+        m = more;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) join(Stats{q[u].m, q[u].s, q[u].t * LN2, 0.f}, m, sum);
     }
-    if (tid < R && r < rows) head_answer(Sums{ss[tid], ts[tid]}, m, logprobs ? at[r] : 0.f, tokens, V, r, logprobs, entropy);
+    // over the lanes of a row, then over the wavefronts
+    float top = m;
+    for (int off = 32; off >= R; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+    if (lane < R) ms[wave][lane] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(ms[0][at_r], ms[1][at_r]), fmaxf(ms[2][at_r], ms[3][at_r]));
+    sum = moved(sum, m, top);
+    for (int off = 32; off >= R; off >>= 1) {
+        sum.s += __shfl_xor(sum.s, off);
+        sum.t += __shfl_xor(sum.t, off);
+    }
+    if (lane < R) { ss[wave][lane] = sum.s; ts[wave][lane] = sum.t; }
+    __syncthreads();
+    if (tid < R && r < rows) {
+        sum = {ss[0][tid] + ss[1][tid] + ss[2][tid] + ss[3][tid], ts[0][tid] + ts[1][tid] + ts[2][tid] + ts[3][tid]};
+        head_answer(sum, top, logprobs ? at[r] : 0.f, tokens, V, r, logprobs, entropy);
+    }
 }
 
 }  // namespace
@@ -483,8 +499,8 @@ void launch_head_logprobs(int dtype, const void* x, const void* w, int64_t rows,
         float* stats = (float*)scratch;
         float* at = stats + 3 * plane;
         launch_gemm_logprob((const bf16_t*)x, d, (const bf16_t*)w, d, stats, tokens, at, rows, V, d, s);
-        int R = 1;
-        while (R < 16 && R < rows) R *= 2;
+        int R = 1;                               // (as many workgroups as fill the card, before whole lines of a plane)
+        while (R < 16 && rows >= 800 * R) R *= 2;
         hipLaunchKernelGGL(head_blocks_kernel, dim3((unsigned)((rows + R - 1) / R)), dim3(256), 0, s, stats, plane, blocks, R, at, tokens, V, rows, logprobs,
                            entropy);
         return;

@@ -1828,7 +1828,7 @@ po_status po_adapters_bytes(int32_t dtype, const int32_t* ranks, int32_t n_slots
                             const po_adapter_rows* segments, int32_t n_segments, size_t* scratch_bytes) {
     if (!scratch_bytes) return PO_ERR_INVALID_ARG;
     const po_status st = adapter_shape(dtype, ranks, n_slots, width, rows, N, K, segments, n_segments);
-    if (st == PO_OK) *scratch_bytes = adapters_scratch(dtype, ranks, rows, N, K, segments, n_segments);
+    if (st == PO_OK) *scratch_bytes = adapters_scratch(dtype, ranks, K, segments, n_segments);
     return st;
 }
 
@@ -1839,7 +1839,7 @@ po_status po_op_adapters(int32_t dtype, const void* x, const void* a, const void
     const po_status st = adapter_shape(dtype, ranks, n_slots, width, rows, N, K, segments, n_segments);
     if (st != PO_OK) return st;
     if (misaligned16(x) || misaligned16(a) || misaligned16(b) || misaligned16(residual) || misaligned16(c) || ((uintptr_t)scratch & 255)) return PO_ERR_INVALID_ARG;
-    const size_t need = adapters_scratch(dtype, ranks, rows, N, K, segments, n_segments);
+    const size_t need = adapters_scratch(dtype, ranks, K, segments, n_segments);
     if (need && !scratch) return PO_ERR_INVALID_ARG;
     if (scratch_bytes < need) return PO_ERR_WORKSPACE_TOO_SMALL;
     launch_adapters(dtype, x, a, b, ranks, scales, width, residual, c, rows, N, K, segments, n_segments, (float*)scratch, (hipStream_t)stream);
