@@ -33,7 +33,7 @@ struct Segment {
 struct Table {
     int n;
     Segment seg[MAX_SEGMENTS];
-    int down0[MAX_SEGMENTS + 1], up0[MAX_SEGMENTS + 1];        // first row tile of each request in either launch, and their number
+    int down0[MAX_SEGMENTS + 1], up0[MAX_SEGMENTS + 1];        // first run of rows of each request in the first launch and in the last one, and their number
 };
 static_assert(sizeof(Table) <= 3840, "with the parameters within 4096 bytes of kernel arguments");
 struct AdapterParams {
@@ -44,8 +44,9 @@ struct AdapterParams {
     int N, K, width;
     int rp;                    // ranks of a row of t: 16 NR of the launch
     int pieces;                // of K
-    int groups;                // of 16 rows that a workgroup of the first launch takes
-    int cols;                  // of a workgroup of the second launch
+    int groups, up_groups;     // of 16 rows that a workgroup of the first launch and of the last one takes
+    void* frags;               // T as fragments, of ks steps each
+    int ks;
 };
 
 // the request a tile belongs to: one load a lane instead of a chain of them
@@ -259,101 +260,209 @@ __device__ __forceinline__ uint4 pack(const float (&v)[4]) {
     return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
 }
 
-// C of a tile of 16 MR rows and p.cols columns, 64 at a time, the wavefronts side by side.  Products h of 16 columns leave a lane with four of them
-// of row lane & 15; they pass through LDS (16-byte groups XOR-swizzled with the row), so that R is read and C written in whole lines.
-// A tile's B and T are read by its workgroups alone, so these are large: what a compute unit can have under way towards it is the limit here, and
-// reads that the caches answer take their places in it like those of R (64 x 1024 by four wavefronts, three workgroups a compute unit: 89 us of
-// 16000 x 4096, 12 of them for the planes of T, 10 for B).
-constexpr int up_waves(int esz, int ks) { return esz == 4 || ks == 4 ? 8 : 16; }         // (16: 128 registers a lane)
+// What both kernels of the second launch do with 16 rows x 64 columns: the products of 16 columns each leave a lane with four of them of row lane & 15;
+// they pass through 4 KiB of LDS of the wavefront's own (16-byte groups XOR-swizzled with the row), so that R is read and C written in whole lines.
+// R and C go by the rows' own bounds: what lies behind their ends reads as zero and is not written, and so does what a lane's offset is
+// moved out of bounds for.
+template <typename T> struct Out {
+    static constexpr int E = (int)sizeof(T), V = 16 / E, LPR = 64 / V, RPP = 64 / LPR, PASSES = 16 / RPP;      // of 16 bytes; lanes of a row; rows of a pass
+};
+constexpr uint32_t NONE = 0x80000000u;
 
-template <typename T, int MR, int KS>
-__global__ void __launch_bounds__(64 * up_waves(sizeof(T), KS)) adapter_up_kernel(const AdapterParams p, const Table tab) {
-    constexpr int NP = Parts<T>::N, E = (int)sizeof(T), UP_WAVES = up_waves(E, KS);
-    __shared__ Frag<T> tf[MR][KS][NP][64];
-    __shared__ __attribute__((aligned(16))) unsigned char stage[UP_WAVES][4096];
-    // (a tile's workgroups side by side: those that run together cover whole rows)
-    const int chunks = (p.N + p.cols - 1) / p.cols, at = (int)(blockIdx.x / (unsigned)chunks), chunk = (int)blockIdx.x - at * chunks;
-    const int si = segment_of(tab.up0, tab.n, at);
-    const Segment& sg = tab.seg[si];
-    const int tile = at - tab.up0[si];
-    const int rank = sg.rank(), r0 = sg.row + tile * (16 * MR), rows = min(16 * MR, sg.row + sg.n - r0);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+template <typename T>
+__device__ __forceinline__ void add_out(const f32x4 (&acc)[4], const u32x4 (&r)[Out<T>::PASSES], unsigned char* stg, __amdgpu_buffer_rsrc_t rc, uint32_t vo,
+                                        uint32_t pitch, int lane) {
+    typedef Out<T> O;
     const int l15 = lane & 15, l4 = lane >> 4;
-    const int ks = (rank + 31) >> 5;
-    for (int f = wave; f < MR * ks; f += UP_WAVES) {     // (a wavefront at a time: group f / ks, step f % ks)
-        const int m = f / ks, k = f - m * ks, j0 = k * 32 + l4 * 8;
-        const int group = min(tile * MR + m, (sg.n - 1) >> 4);       // (groups behind the last one: that one again)
-        const float* t = p.t + ((int64_t)(sg.group0 + group) * 16 + l15) * p.rp + j0;
-        float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 0.f;
-        if (j0 < rank)
-            for (int i0 = 0; i0 < p.pieces; i0 += 8) {               // (eight pieces' loads under way together)
-                f32x4 a[8], b[8];
+    for (int h = 0; h < 4; ++h) *(f32x4*)(stg + l15 * 256 + (((h * 4 + l4) ^ l15) << 4)) = acc[h];
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i0 + i < p.pieces) {
-                        a[i] = *(const f32x4*)(t + (i0 + i) * p.plane);
-                        b[i] = *(const f32x4*)(t + (i0 + i) * p.plane + 4);
-                    }
+    for (int i = 0; i < O::PASSES; ++i) {
+        const int rl = i * O::RPP + lane / O::LPR;
+        float v[O::V];
+        unpack(__builtin_bit_cast(uint4, r[i]), v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i0 + i < p.pieces) {
+        for (int q = 0; q < O::V / 4; ++q) {
+            const f32x4 d = *(const f32x4*)(stg + rl * 256 + ((((lane & (O::LPR - 1)) * (O::V / 4) + q) ^ rl) << 4));
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            v[e] += a[i][e];
-                            v[4 + e] += b[i][e];
-                        }
-                    }
-            }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = j0 + e < rank ? v[e] * sg.scale : 0.f;
-        Frag<T> part[NP];
-        split(v, part);
-#pragma unroll
-        for (int i = 0; i < NP; ++i) tf[m][k][i][lane] = part[i];
+            for (int e = 0; e < 4; ++e) v[q * 4 + e] += d[e];
+        }
+        // (no scalar offset: with one the compiler takes a store's registers as free at once, and the next instruction overwrote
+        // the first of them before the last lanes were read)
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, pack(v)), rc, vo + (uint32_t)(i * O::RPP) * pitch, 0, 0);
     }
-    __syncthreads();
-    // R and C by the tile's rows, B by its slot: what lies behind their ends reads as zero and is not written, and so does what a lane's offset is
-    // moved out of bounds for
-    constexpr int V = 16 / E, LPR = 64 / V, RPP = 64 / LPR, PASSES = 16 / RPP;           // of 16 bytes; lanes of a row; rows of a pass
-    constexpr uint32_t NONE = 0x80000000u;
-    unsigned char* const stg = stage[wave];
-    const uint32_t pitch = (uint32_t)p.N * E, bytes = (uint32_t)rows * pitch;
-    const int64_t tile_at = (int64_t)r0 * p.N * E;
-    const __amdgpu_buffer_rsrc_t rr = __builtin_amdgcn_make_buffer_rsrc((void*)((const unsigned char*)(p.res ? p.res : p.c) + tile_at), 0, p.res ? (int)bytes : 0, 0x00020000);
-    const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void*)((unsigned char*)p.c + tile_at), 0, (int)bytes, 0x00020000);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// the sum of the planes of T at a lane's eight ranks, times the scale; 0 behind the rank
+__device__ __forceinline__ void sum_planes(const AdapterParams& p, const float* t, int j0, int rank, float scale, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+    if (j0 < rank)
+        for (int i0 = 0; i0 < p.pieces; i0 += 8) {         // (eight pieces' loads under way together)
+            f32x4 a[8], b[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i0 + i < p.pieces) {
+                    a[i] = *(const f32x4*)(t + (i0 + i) * p.plane);
+                    b[i] = *(const f32x4*)(t + (i0 + i) * p.plane + 4);
+                }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i0 + i < p.pieces) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[e] += a[i][e];
+                        v[4 + e] += b[i][e];
+                    }
+                }
+        }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = j0 + e < rank ? v[e] * scale : 0.f;
+}
+
+// C of up to 16 rows of a request and 64 columns a wavefront, for batches of requests of up to 16 rows: every wavefront adds the planes of T itself.
+// Its loads are all under way together: this is what a single token waits for.
+template <typename T, int KS>
+__global__ void __launch_bounds__(256) adapter_up_few_kernel(const AdapterParams p, const Table tab) {
+    typedef Out<T> O;
+    constexpr int NP = Parts<T>::N, E = O::E;
+    __shared__ __attribute__((aligned(16))) unsigned char stage[4][4096];
+    const int chunks = (p.N + 255) / 256, si = (int)(blockIdx.x / (unsigned)chunks);       // (a tile is a request)
+    const Segment& sg = tab.seg[si];
+    const int rank = sg.rank(), lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l15 = lane & 15, l4 = lane >> 4;
+    const int c0 = ((int)blockIdx.x - si * chunks) * 256 + wave * 64;
+    if (c0 >= p.N) return;
+    const uint32_t pitch = (uint32_t)p.N * E, bytes = (uint32_t)sg.n * pitch;
+    const int64_t at = (int64_t)sg.row * p.N * E;
+    const __amdgpu_buffer_rsrc_t rr = __builtin_amdgcn_make_buffer_rsrc((void*)((const unsigned char*)(p.res ? p.res : p.c) + at), 0, p.res ? (int)bytes : 0, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void*)((unsigned char*)p.c + at), 0, (int)bytes, 0x00020000);
     const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(
         (void*)((const unsigned char*)p.b + (int64_t)sg.slot() * p.N * p.width * E), 0, (int)((uint32_t)p.N * (uint32_t)p.width * E), 0x00020000);
-    uint32_t vb[4];                              // (KS entries used)
+    Frag<T> w[4][KS];
 #pragma unroll
-    for (int k = 0; k < KS; ++k) vb[k] = rank - k * 32 - l4 * 8 > 0 ? (uint32_t)(l15 * p.width + k * 32 + l4 * 8) * E : NONE;
-    const uint32_t vr = (uint32_t)(lane / LPR) * pitch + (uint32_t)(lane & (LPR - 1)) * 16u;
-    const int n1 = min((chunk + 1) * p.cols, p.N);
-    for (int c0 = chunk * p.cols + wave * 64; c0 < n1; c0 += UP_WAVES * 64) {
-        Frag<T> w[4][KS];
+    for (int k = 0; k < KS; ++k) {
+        const uint32_t vb = rank - k * 32 - l4 * 8 > 0 ? (uint32_t)(l15 * p.width + k * 32 + l4 * 8) * E : NONE;
 #pragma unroll
         for (int h = 0; h < 4; ++h)
 #pragma unroll
-            for (int k = 0; k < KS; ++k)
+            for (int q = 0; q < E / 2; ++q)
+                set(w[h][k], q, __builtin_amdgcn_raw_buffer_load_b128(rb, vb, (uint32_t)(c0 + h * 16) * (uint32_t)p.width * E + q * 16, 0));
+    }
+    const uint32_t vo = c0 + (lane & (O::LPR - 1)) * O::V < p.N ? (uint32_t)(lane / O::LPR) * pitch + (uint32_t)(lane & (O::LPR - 1)) * 16u + (uint32_t)c0 * E : NONE;
+    u32x4 r[O::PASSES];
 #pragma unroll
-                for (int q = 0; q < E / 2; ++q)
-                    set(w[h][k], q, __builtin_amdgcn_raw_buffer_load_b128(rb, vb[k], (uint32_t)(c0 + h * 16) * (uint32_t)p.width * E + q * 16, 0));
-        const uint32_t vo = c0 + (lane & (LPR - 1)) * V < p.N ? vr : NONE;
-        u32x4 out[MR][PASSES];                   // (behind B: loads return in order, and B comes from a cache)
+    for (int i = 0; i < O::PASSES; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rr, vo, (uint32_t)(i * O::RPP) * pitch, 0);
+    f32x4 acc[4];
 #pragma unroll
-        for (int m = 0; m < MR; ++m)
+    for (int h = 0; h < 4; ++h) acc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < PASSES; ++i)
-                out[m][i] = __builtin_amdgcn_raw_buffer_load_b128(rr, vo, (uint32_t)c0 * E + (uint32_t)(m * 16 + i * RPP) * pitch, 0);
-        if (rank & 7) {
+    for (int k = 0; k < KS; ++k)
+        if (k * 32 < rank) {
+            const int j0 = k * 32 + l4 * 8;
+            float v[8];
+            sum_planes(p, p.t + ((int64_t)sg.group0 * 16 + l15) * p.rp + j0, j0, rank, sg.scale, v);
+            Frag<T> t[NP];
+            split(v, t);
 #pragma unroll
-            for (int h = 0; h < 4; ++h)
+            for (int h = 0; h < 4; ++h) {
+                if (rank & 7) keep(w[h][k], rank - j0);
 #pragma unroll
-                for (int k = 0; k < KS; ++k) keep(w[h][k], rank - k * 32 - l4 * 8);
+                for (int i = NP - 1; i >= 0; --i) acc[h] = mma(w[h][k], t[i], acc[h]);
+            }
         }
+    add_out<T>(acc, r, stage[wave], rc, vo, pitch, lane);
+}
+
+// Longer requests: first T as the second product's fragments, in the order of its lanes: [group][step][part][lane] (in scratch behind the planes) ...
+template <typename T>
+__global__ void __launch_bounds__(256) adapter_join_kernel(const AdapterParams p, const Table tab) {
+    constexpr int NP = Parts<T>::N;
+    const int si = segment_of(tab.up0, tab.n, blockIdx.x);
+    const Segment& sg = tab.seg[si];
+    const int rank = sg.rank(), ks = (rank + 31) >> 5, lane = threadIdx.x & 63, l15 = lane & 15, l4 = lane >> 4;
+    const int g0 = ((int)blockIdx.x - tab.up0[si]) * p.up_groups, g1 = min(g0 + p.up_groups, (sg.n + 15) >> 4);
+    for (int f = threadIdx.x >> 6; f < (g1 - g0) * ks; f += 4) {
+        const int g = g0 + f / ks, k = f % ks, j0 = k * 32 + l4 * 8;
+        float v[8];
+        sum_planes(p, p.t + ((int64_t)(sg.group0 + g) * 16 + l15) * p.rp + j0, j0, rank, sg.scale, v);
+        Frag<T> part[NP];
+        split(v, part);
+        Frag<T>* o = (Frag<T>*)p.frags + (((int64_t)(sg.group0 + g) * p.ks + k) * NP) * 64 + lane;
 #pragma unroll
-        for (int m = 0; m < MR; ++m) {
+        for (int i = 0; i < NP; ++i) o[i * 64] = part[i];
+    }
+}
+
+// ... then C of a run of rows of one request and 4 x 16 H columns, a quarter a wavefront, which holds its part of B in registers for all of
+// them: B is read once a run.  16 rows at a time, the next ones' R and T on their way; wavefronts wait for nobody.
+template <typename T, int KS> struct UpCols {
+    static constexpr int H = 32 / (int)sizeof(T) / (KS == 1 ? 1 : KS / 2);              // 128 registers of B (64 with one step)
+};
+template <typename T, int KS>
+__global__ void __launch_bounds__(256, 2) adapter_up_kernel(const AdapterParams p, const Table tab) {
+    typedef Out<T> O;
+    constexpr int NP = Parts<T>::N, E = O::E, H = UpCols<T, KS>::H, SUB = H / 4;          // SUB: 64 columns each
+    __shared__ __attribute__((aligned(16))) unsigned char stage[4][4096];
+    // (a run's workgroups side by side: those that run together cover whole rows)
+    const int chunks = (p.N + 64 * H - 1) / (64 * H), at = (int)(blockIdx.x / (unsigned)chunks);
+    const int si = segment_of(tab.up0, tab.n, at);
+    const Segment& sg = tab.seg[si];
+    const int rank = sg.rank(), ks = (rank + 31) >> 5;
+    const int g0 = (at - tab.up0[si]) * p.up_groups, g1 = min(g0 + p.up_groups, (sg.n + 15) >> 4);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l15 = lane & 15, l4 = lane >> 4;
+    const int c0 = ((int)blockIdx.x - at * chunks) * (64 * H) + wave * (16 * H);
+    if (c0 >= p.N) return;
+    const uint32_t pitch = (uint32_t)p.N * E;
+    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)((const unsigned char*)p.b + (int64_t)sg.slot() * p.N * p.width * E), 0, (int)((uint32_t)p.N * (uint32_t)p.width * E), 0x00020000);
+    Frag<T> w[H][KS];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+        const uint32_t vb = rank - k * 32 - l4 * 8 > 0 ? (uint32_t)(l15 * p.width + k * 32 + l4 * 8) * E : NONE;
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int q = 0; q < E / 2; ++q)
+                set(w[h][k], q, __builtin_amdgcn_raw_buffer_load_b128(rb, vb, (uint32_t)(c0 + h * 16) * (uint32_t)p.width * E + q * 16, 0));
+    }
+    if (rank & 7) {
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int k = 0; k < KS; ++k) keep(w[h][k], rank - k * 32 - l4 * 8);
+    }
+    const uint32_t vr = (uint32_t)(lane / O::LPR) * pitch + (uint32_t)(lane & (O::LPR - 1)) * 16u + (uint32_t)c0 * E;
+    uint32_t vo[SUB];
+#pragma unroll
+    for (int b = 0; b < SUB; ++b) vo[b] = c0 + b * 64 + (lane & (O::LPR - 1)) * O::V < p.N ? vr + b * 64 * E : NONE;
+    const Frag<T>* const frags = (const Frag<T>*)p.frags + (int64_t)sg.group0 * p.ks * NP * 64 + lane;
+    u32x4 r[SUB][O::PASSES];
+    auto fetch_t = [&](Frag<T> (&t)[KS][NP], int g) {
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+            if (k < ks) {
+#pragma unroll
+                for (int i = 0; i < NP; ++i) t[k][i] = frags[(((int64_t)g * p.ks + k) * NP + i) * 64];
+            }
+    };
+    auto fetch_r = [&](int b, int g) {
+        const __amdgpu_buffer_rsrc_t rr = __builtin_amdgcn_make_buffer_rsrc((void*)((const unsigned char*)(p.res ? p.res : p.c) + (int64_t)(sg.row + g * 16) * pitch), 0,
+                                                                            p.res ? (int)((uint32_t)min(16, sg.n - g * 16) * pitch) : 0, 0x00020000);
+#pragma unroll
+        for (int i = 0; i < O::PASSES; ++i) r[b][i] = __builtin_amdgcn_raw_buffer_load_b128(rr, vo[b], (uint32_t)(i * O::RPP) * pitch, 0);
+    };
+    // (the next rows' R go where this one's are no longer needed: B, two of these and of T do not fit the registers)
+    auto turn = [&](const Frag<T> (&t)[KS][NP], Frag<T> (&next)[KS][NP], int g) {
+        const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void*)((unsigned char*)p.c + (int64_t)(sg.row + g * 16) * pitch), 0,
+                                                                            (int)((uint32_t)min(16, sg.n - g * 16) * pitch), 0x00020000);
+        const bool more = g + 1 < g1;
+        if (more) fetch_t(next, g + 1);
+#pragma unroll
+        for (int b = 0; b < SUB; ++b) {
             f32x4 acc[4];
 #pragma unroll
             for (int h = 0; h < 4; ++h) acc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -361,40 +470,28 @@ __global__ void __launch_bounds__(64 * up_waves(sizeof(T), KS)) adapter_up_kerne
             for (int k = 0; k < KS; ++k)
                 if (k < ks) {
 #pragma unroll
-                    for (int i = NP - 1; i >= 0; --i) {
-                        const Frag<T> t = tf[m][k][i][lane];
+                    for (int i = NP - 1; i >= 0; --i)
 #pragma unroll
-                        for (int h = 0; h < 4; ++h) acc[h] = mma(w[h][k], t, acc[h]);
-                    }
+                        for (int h = 0; h < 4; ++h) acc[h] = mma(w[b * 4 + h][k], t[k][i], acc[h]);
                 }
-#pragma unroll
-            for (int h = 0; h < 4; ++h) *(f32x4*)(stg + l15 * 256 + (((h * 4 + l4) ^ l15) << 4)) = acc[h];
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int i = 0; i < PASSES; ++i) {
-                const int rl = i * RPP + lane / LPR;
-                float v[V];
-                unpack(__builtin_bit_cast(uint4, out[m][i]), v);
-#pragma unroll
-                for (int q = 0; q < V / 4; ++q) {
-                    const f32x4 d = *(const f32x4*)(stg + rl * 256 + ((((lane & (LPR - 1)) * (V / 4) + q) ^ rl) << 4));
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[q * 4 + e] += d[e];
-                }
-                // (no scalar offset: with one the compiler takes a store's registers as free at once, and the next instruction overwrote
-                // the first of them before the last lanes were read)
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, pack(v)), rc, vo + ((uint32_t)c0 * E + (uint32_t)(m * 16 + i * RPP) * pitch), 0, 0);
-            }
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_wave_barrier();
+            add_out<T>(acc, r[b], stage[wave], rc, vo[b], pitch, lane);
+            if (more) fetch_r(b, g + 1);
         }
+    };
+    Frag<T> t0[KS][NP], t1[KS][NP];
+    fetch_t(t0, g0);
+#pragma unroll
+    for (int b = 0; b < SUB; ++b) fetch_r(b, g0);
+    for (int g = g0; g < g1; g += 2) {
+        turn(t0, t1, g);
+        if (g + 1 < g1) turn(t1, t0, g + 1);
     }
 }
 
 struct Launch {
     Table tab;
-    int rank, mr, nr, groups, cols;
+    int rank, nr, groups, up_groups;
+    bool few;                  // requests of up to 16 rows
     int total;                 // groups of 16 rows
 };
 
@@ -406,7 +503,10 @@ inline int k_pieces(int nr, int esz, int K) { return (k_slices(nr, esz, K) + DOW
 
 inline int nr_of(int rank) { return rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8; }
 
-// tiles and columns of a launch
+constexpr int ks_of(int nr) { return (nr + 1) / 2; }
+inline int up_h(int nr, int esz) { return 32 / esz / (nr <= 2 ? 1 : ks_of(nr) / 2); }
+
+// runs of rows of a launch
 void plan(Launch& l, int esz, int N, int K) {
     Table& t = l.tab;
     int longest = 0;
@@ -418,30 +518,37 @@ void plan(Launch& l, int esz, int N, int K) {
         if (t.seg[i].rank()) l.total += (t.seg[i].n + 15) / 16;
     }
     l.nr = nr_of(l.rank);
-    l.mr = longest <= 16 ? 1 : l.nr == 8 ? 2 : 4;
-    // rows of a workgroup of the first launch, one a compute unit: rounds of them, each with the time of its groups and of about two more
-    // for A and the ends
-    const int pieces = k_pieces(l.nr, esz, K), most = (longest + 15) / 16;
-    int64_t best = INT64_MAX;
-    for (int g : {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 56, 64}) {
-        int64_t wgs = 0;
-        for (int i = 0; i < t.n; ++i) wgs += t.seg[i].rank() ? ((t.seg[i].n + 15) / 16 + g - 1) / g : 0;
-        const int64_t time = (wgs * pieces + 255) / 256 * (std::min(g, most) + 2);
-        if (time < best) {
-            best = time;
-            l.groups = g;
+    l.few = longest <= 16;
+    // Rows of a workgroup: rounds of workgroups, one a compute unit in the first launch and two in the last, each with the time of its groups
+    // and of two more for A, or one for B.  On eight batches, every number of groups from 1 to 64 timed for either launch, the whole
+    // call is within 8 % of the fastest (two prompts of 8000 rows, K 14336, rank 64: 32 groups 200 us, 28 246, 8 219, 1 409).
+    const int pieces = k_pieces(l.nr, esz, K), most = (longest + 15) / 16, chunks = (N + 64 * up_h(l.nr, esz) - 1) / (64 * up_h(l.nr, esz));
+    auto run = [&](bool down, int wide, int slots, int more) {
+        int64_t best = INT64_MAX;
+        int pick = 1;
+        for (int g : {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 56, 64}) {
+            int64_t wgs = 0;
+            for (int i = 0; i < t.n; ++i)
+                if (!down || t.seg[i].rank()) wgs += ((t.seg[i].n + 15) / 16 + g - 1) / g;
+            const int64_t time = (wgs * wide + slots - 1) / slots * (std::min(g, most) + more);
+            if (time < best) {
+                best = time;
+                pick = g;
+            }
+            if (g >= most) break;
         }
-        if (g >= most) break;
-    }
+        return pick;
+    };
+    l.groups = l.few ? 1 : run(true, pieces, 256, 2);
+    l.up_groups = l.few ? 1 : run(false, chunks, 512, 1);
     t.down0[0] = t.up0[0] = 0;
     for (int i = 0; i < t.n; ++i) {
         const int g = (t.seg[i].n + 15) / 16;
         t.down0[i + 1] = t.down0[i] + (g + l.groups - 1) / l.groups;
-        t.up0[i + 1] = t.up0[i] + (g + l.mr - 1) / l.mr;
+        t.up0[i + 1] = t.up0[i] + (g + l.up_groups - 1) / l.up_groups;
     }
-    l.cols = 4096;
-    while (l.cols > 64 * up_waves(esz, l.nr / 2) && (int64_t)t.up0[t.n] * ((N + l.cols - 1) / l.cols) < 200) l.cols /= 2;
 }
+
 // calls f(Launch&) for every launch's table of requests, tiles counted
 template <typename F>
 void for_launches(const int32_t* ranks, const float* scales, bool in_place, int esz, int64_t rows, int N, int K, const po_adapter_rows* seg, int n_seg, F f) {
@@ -476,8 +583,9 @@ void for_launches(const int32_t* ranks, const float* scales, bool in_place, int 
     flush();
 }
 
-template <typename T, int MR, int NR>
+template <typename T, int NR>
 void run_t(const AdapterParams& p, const Launch& l, hipStream_t s) {
+    constexpr int KS = ks_of(NR), H = UpCols<T, KS>::H;
     if (l.rank) {
         constexpr int WAVE = Down<T, NR>::WAVE;
         static OncePerDevice once;
@@ -485,8 +593,13 @@ void run_t(const AdapterParams& p, const Launch& l, hipStream_t s) {
         const int waves = std::min(DOWN_WAVES, k_slices(NR, sizeof(T), p.K));
         hipLaunchKernelGGL((adapter_down_kernel<T, NR>), dim3((unsigned)l.tab.down0[l.tab.n], (unsigned)p.pieces), dim3(64 * waves), waves * WAVE, s, p, l.tab);
     }
-    hipLaunchKernelGGL((adapter_up_kernel<T, MR, (NR + 1) / 2>), dim3((unsigned)l.tab.up0[l.tab.n] * (unsigned)((p.N + p.cols - 1) / p.cols)), dim3(64 * up_waves(sizeof(T), (NR + 1) / 2)), 0, s,
-                       p, l.tab);
+    if (l.few) {
+        hipLaunchKernelGGL((adapter_up_few_kernel<T, KS>), dim3((unsigned)l.tab.n * (unsigned)((p.N + 255) / 256)), dim3(256), 0, s, p, l.tab);
+        return;
+    }
+    const unsigned runs = (unsigned)l.tab.up0[l.tab.n];
+    if (l.rank) hipLaunchKernelGGL((adapter_join_kernel<T>), dim3(runs), dim3(256), 0, s, p, l.tab);
+    hipLaunchKernelGGL((adapter_up_kernel<T, KS>), dim3(runs * (unsigned)((p.N + 64 * H - 1) / (64 * H))), dim3(256), 0, s, p, l.tab);
 }
 
 template <typename T>
@@ -495,16 +608,14 @@ void run(AdapterParams p, const Launch& l, hipStream_t s) {
     p.pieces = k_pieces(l.nr, sizeof(T), p.K);
     p.plane = (int64_t)l.total * 16 * p.rp;
     p.groups = l.groups;
-    p.cols = l.cols;
-    switch (l.nr * 8 + l.mr) {
-        case 8 + 1: run_t<T, 1, 1>(p, l, s); break;
-        case 16 + 1: run_t<T, 1, 2>(p, l, s); break;
-        case 32 + 1: run_t<T, 1, 4>(p, l, s); break;
-        case 64 + 1: run_t<T, 1, 8>(p, l, s); break;
-        case 8 + 4: run_t<T, 4, 1>(p, l, s); break;
-        case 16 + 4: run_t<T, 4, 2>(p, l, s); break;
-        case 32 + 4: run_t<T, 4, 4>(p, l, s); break;
-        default: run_t<T, 2, 8>(p, l, s); break;
+    p.up_groups = l.up_groups;
+    p.ks = ks_of(l.nr);
+    p.frags = p.t + p.pieces * p.plane;
+    switch (l.nr) {
+        case 1: run_t<T, 1>(p, l, s); break;
+        case 2: run_t<T, 2>(p, l, s); break;
+        case 4: run_t<T, 4>(p, l, s); break;
+        default: run_t<T, 8>(p, l, s); break;
     }
 }
 
@@ -520,7 +631,8 @@ size_t adapters_scratch(int dtype, const int32_t* ranks, int K, const po_adapter
         rank = std::max(rank, r);
     }
     const int nr = nr_of(rank);
-    return rank ? (size_t)k_pieces(nr, dtype == 0 ? 4 : 2, K) * (size_t)groups * 16 * (16 * nr) * sizeof(float) : 0;
+    // planes of T, and T as fragments (32 ranks a step: of float32, or of two bf16 numbers)
+    return rank ? (size_t)groups * 16 * sizeof(float) * ((size_t)k_pieces(nr, dtype == 0 ? 4 : 2, K) * (16 * nr) + 32 * ks_of(nr)) : 0;
 }
 
 void launch_adapters(int dtype, const void* x, const void* a, const void* b, const int32_t* ranks, const float* scales, int width, const void* res,
