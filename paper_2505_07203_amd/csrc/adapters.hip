@@ -385,16 +385,16 @@ __global__ void __launch_bounds__(256) adapter_join_kernel(const AdapterParams p
     const Segment& sg = tab.seg[si];
     const int rank = sg.rank(), ks = (rank + 31) >> 5, lane = threadIdx.x & 63, l15 = lane & 15, l4 = lane >> 4;
     const int g0 = ((int)blockIdx.x - tab.up0[si]) * p.up_groups, g1 = min(g0 + p.up_groups, (sg.n + 15) >> 4);
-    for (int f = threadIdx.x >> 6; f < (g1 - g0) * ks; f += 4) {
-        const int g = g0 + f / ks, k = f % ks, j0 = k * 32 + l4 * 8;
-        float v[8];
-        sum_planes(p, p.t + ((int64_t)(sg.group0 + g) * 16 + l15) * p.rp + j0, j0, rank, sg.scale, v);
-        Frag<T> part[NP];
-        split(v, part);
-        Frag<T>* o = (Frag<T>*)p.frags + (((int64_t)(sg.group0 + g) * p.ks + k) * NP) * 64 + lane;
+    const int f = (int)blockIdx.y * 4 + (threadIdx.x >> 6);        // (a wavefront per group and step)
+    if (f >= (g1 - g0) * ks) return;
+    const int g = g0 + f / ks, k = f % ks, j0 = k * 32 + l4 * 8;
+    float v[8];
+    sum_planes(p, p.t + ((int64_t)(sg.group0 + g) * 16 + l15) * p.rp + j0, j0, rank, sg.scale, v);
+    Frag<T> part[NP];
+    split(v, part);
+    Frag<T>* o = (Frag<T>*)p.frags + (((int64_t)(sg.group0 + g) * p.ks + k) * NP) * 64 + lane;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) o[i * 64] = part[i];
-    }
+    for (int i = 0; i < NP; ++i) o[i * 64] = part[i];
 }
 
 // ... then C of a run of rows of one request and 4 x 16 H columns, a quarter a wavefront, which holds its part of B in registers for all of
@@ -598,7 +598,7 @@ void run_t(const AdapterParams& p, const Launch& l, hipStream_t s) {
         return;
     }
     const unsigned runs = (unsigned)l.tab.up0[l.tab.n];
-    if (l.rank) hipLaunchKernelGGL((adapter_join_kernel<T>), dim3(runs), dim3(256), 0, s, p, l.tab);
+    if (l.rank) hipLaunchKernelGGL((adapter_join_kernel<T>), dim3(runs, (unsigned)((l.up_groups * KS + 3) / 4)), dim3(256), 0, s, p, l.tab);
     hipLaunchKernelGGL((adapter_up_kernel<T, KS>), dim3(runs * (unsigned)((p.N + 64 * H - 1) / (64 * H))), dim3(256), 0, s, p, l.tab);
 }
 

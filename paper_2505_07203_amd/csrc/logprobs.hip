@@ -199,23 +199,36 @@ __device__ __forceinline__ float key_logit(unsigned long long k) {
 constexpr int RUNS = MAX_TOP * (CHUNK / 8);      // of the chunks that are read again
 constexpr int LIST = 512;                        // elements that are ordered at once; 8 of each of MAX_TOP runs
 
-// Leaves in out[0 .. min(n, top)) the largest of keys[0 .. n), in order; keys[n .. n + 8) are overwritten.  All different, but for
-// zeros, which are left out.  (The callers' barriers stand around it.)
-__device__ __forceinline__ void largest(unsigned long long* keys, int n, int top, unsigned long long* out) {
-    if (threadIdx.x < 8) keys[n + threadIdx.x] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += 256) {
-        const unsigned long long k = keys[i];
-        if (k == 0) continue;
-        int rank = 0;
-        for (int j = 0; j < n; j += 8) {
+// Leaves in out[0 .. min(n, top)) the largest of keys[0 .. n), in order; keys[n .. n + 32) are overwritten.  All different, but for
+// zeros, which are left out.  256 keys at a time are ranked, a thread holding four of them: each wavefront compares all of them with every
+// fourth eight of the list (read as a broadcast, which a thread per key would read four times as often), and ranks[256] adds up.  (The
+// callers' barriers stand around it.)
+__device__ __forceinline__ void largest(unsigned long long* keys, int n, int top, unsigned long long* out, int* ranks) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (tid < 32) keys[n + tid] = 0;
+    for (int i0 = 0; i0 < n; i0 += 256) {
+        ranks[tid] = 0;
+        __syncthreads();
+        unsigned long long k[4];
+        int rank[4] = {0, 0, 0, 0};
+        const int mine = min(n - i0, 256);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) k[u] = u * 64 + lane < mine ? keys[i0 + u * 64 + lane] : ~0ull;
+        for (int j = wave * 8; j < n; j += 32) {
             unsigned long long o[8];
 #pragma unroll
             for (int c = 0; c < 8; ++c) o[c] = keys[j + c];
 #pragma unroll
-            for (int c = 0; c < 8; ++c) rank += o[c] > k;
+            for (int c = 0; c < 8; ++c)
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (u * 64 < mine) rank[u] += o[c] > k[u];
         }
-        if (rank < top) out[rank] = k;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (u * 64 + lane < mine) atomicAdd(&ranks[u * 64 + lane], rank[u]);
+        __syncthreads();
+        if (tid < mine && keys[i0 + tid] && ranks[tid] < top) out[ranks[tid]] = keys[i0 + tid];
     }
 }
 
@@ -228,9 +241,9 @@ __global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__
                                                            float* __restrict__ top_logprobs) {
     __shared__ double red_s[4], red_t[4];
     __shared__ float red_m[4];
-    extern __shared__ unsigned long long keys[];     // RUNS + 8, only where top > 0
+    extern __shared__ unsigned long long keys[];     // RUNS + 32, only where top > 0
     __shared__ unsigned long long best[MAX_TOP];
-    __shared__ int count;
+    __shared__ int count, ranks[256];
     const int64_t r = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const T* row = logits + r * ld;
@@ -279,7 +292,7 @@ __global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__
             if (tid < more) keys[n + tid] = best[tid];
             __syncthreads();
             if (tid < more) best[tid] = 0;
-            largest(keys, n + more, top, best);
+            largest(keys, n + more, top, best, ranks);
         }
     }
     __syncthreads();
@@ -293,8 +306,7 @@ __global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__
     if (tid == 0 && entropy) entropy[r] = m > -INFINITY ? (float)fmax(0.0, log_s - sum.t / sum.s) : 0.f;
     if (top == 0) return;
 
-    int n_chunks = 0;
-    while (n_chunks < top && best[n_chunks]) ++n_chunks;
+    const int n_chunks = __popcll(__ballot(lane < top && best[lane] != 0));
     // (as many elements as tokens are wanted are as large as this)
     const float floor_logit = n_chunks == top ? key_logit(best[top - 1]) : lowest;
     // their elements that reach as far: mostly a few more than are wanted
@@ -309,13 +321,20 @@ __global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__
             load8<T, VEC>(row, at[u], V, v[u]);
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < 4; ++u) {
+            int n = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (v[u][e] >= floor_logit && v[u][e] > -INFINITY) {
-                    const int slot = atomicAdd(&count, 1);         // (their order in the list changes nothing: the keys are ranked)
-                    if (slot < LIST) keys[slot] = order_key(v[u][e], at[u] + e);
-                }
+            for (int e = 0; e < 8; ++e) n += v[u][e] >= floor_logit && v[u][e] > -INFINITY;
+            if (n) {
+                int slot = atomicAdd(&count, n);                   // (their order in the list changes nothing: the keys are ranked)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (v[u][e] >= floor_logit && v[u][e] > -INFINITY) {
+                        if (slot < LIST) keys[slot] = order_key(v[u][e], at[u] + e);
+                        ++slot;
+                    }
+            }
+        }
     }
     __syncthreads();
     int n = count;
@@ -339,7 +358,7 @@ __global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__
         __syncthreads();
         const int runs = count;
         if (tid < MAX_TOP) best[tid] = 0;
-        largest(keys, runs, top, best);
+        largest(keys, runs, top, best, ranks);
         __syncthreads();
         if (tid == 0) count = 0;
         __syncthreads();
@@ -354,7 +373,7 @@ __global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__
         n = count;
     }
     if (tid < MAX_TOP) best[tid] = 0;
-    largest(keys, n, top, best);
+    largest(keys, n, top, best, ranks);
     __syncthreads();
     if (tid < top) {
         const unsigned long long k = best[tid];
@@ -375,7 +394,7 @@ void run(const T* logits, int64_t ld, int64_t rows, int V, const int32_t* tokens
     const int64_t total = rows * pieces;
     hipLaunchKernelGGL((logprob_pieces_kernel<T, VEC>), dim3((unsigned)((total + 3) / 4)), dim3(256), 0, s, logits, ld, V, pieces, total, stats,
                        (int64_t)pieces, cm, chunks, (const int32_t*)nullptr, 0, (float*)nullptr);
-    hipLaunchKernelGGL((logprob_rows_kernel<T, VEC>), dim3((unsigned)rows), dim3(256), top ? (RUNS + 8) * 8 : 0, s, logits, ld, V, pieces, chunks, stats, cm, tokens,
+    hipLaunchKernelGGL((logprob_rows_kernel<T, VEC>), dim3((unsigned)rows), dim3(256), top ? (RUNS + 32) * 8 : 0, s, logits, ld, V, pieces, chunks, stats, cm, tokens,
                        n_tokens, logprobs, entropy, top, top_tokens, top_logprobs);
 }
 
