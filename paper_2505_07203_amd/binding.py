@@ -637,15 +637,20 @@ def po_op_add_rmsnorm_quantize(x, delta, g, eps: float, block: int = 0, normed: 
     _shape("h", h, rows, d)
     if delta is not None:
         _shape("delta", delta, rows, d)
-    y = torch.empty((rows, d), dtype=bf16, device=x.device) if normed else None
+    y = torch.empty_like(x) if normed else None
     c = s = None
     if codes:
-        c = torch.empty((rows, d), dtype=torch.uint8, device=x.device)
+        c = torch.empty_like(x, dtype=torch.uint8)
         s = torch.empty((d // 128, rows) if block else rows, dtype=torch.float32, device=x.device)
     check(lib().po_op_add_rmsnorm_quantize(x.data_ptr(), None if delta is None else delta.data_ptr(), g.data_ptr(),
                                            None if h is x and delta is None else h.data_ptr(), y.data_ptr() if normed else None,
                                            c.data_ptr() if codes else None, s.data_ptr() if codes else None, rows, d, block, eps, stream))
     return h, c, s, y
+
+
+def _address(a):
+    """of a host array's first element (a.ctypes.data takes three times as long, and a call with four arrays is a small one)"""
+    return C.addressof(C.c_char.from_buffer(a)) if a.size and a.flags.writeable else a.ctypes.data
 
 
 def _adapter_rows(segments):
@@ -672,7 +677,7 @@ def po_op_adapters(x, a, b, ranks, scales, segments, residual=None, out=None, sc
     slots, width = a.shape[:2]
     N = b.shape[1]
     dt = x.dtype
-    c = torch.empty((rows, N), dtype=dt, device=x.device) if out is None else out
+    c = out if out is not None else torch.empty((rows, N), dtype=dt, device=x.device) if residual is None else torch.empty_like(residual)
     stream = _operands(("x", x, dt), ("a", a, dt), ("b", b, dt), ("residual", residual, dt), ("out", c, dt), ("scratch", scratch, torch.uint8))
     _shape("a", a, slots, width, K)
     _shape("b", b, slots, N, width)
@@ -683,12 +688,12 @@ def po_op_adapters(x, a, b, ranks, scales, segments, residual=None, out=None, sc
     rk, sc = np.ascontiguousarray(ranks, dtype=np.int32), np.ascontiguousarray(scales, dtype=np.float32)
     if rk.shape != (slots,) or sc.shape != (slots,):
         raise ValueError(f"ranks, scales: shape ({slots},) expected, got {rk.shape}, {sc.shape}")
-    code, hr, hs = _dt(x), rk.ctypes.data, seg.ctypes.data
+    code, hr, hs = _dt(x), _address(rk), _address(seg)
     if scratch is None:
         need = C.c_size_t(0)
         check(lib().po_adapters_bytes(code, hr, slots, width, rows, N, K, hs, len(seg), C.byref(need)))
         scratch = torch.empty(need.value, dtype=torch.uint8, device=x.device)
-    check(lib().po_op_adapters(code, x.data_ptr(), a.data_ptr(), b.data_ptr(), hr, sc.ctypes.data, slots, width,
+    check(lib().po_op_adapters(code, x.data_ptr(), a.data_ptr(), b.data_ptr(), hr, _address(sc), slots, width,
                                None if residual is None else residual.data_ptr(), c.data_ptr(), rows, N, K, hs, len(seg), scratch.data_ptr(),
                                scratch.numel(), stream))
     return c
@@ -922,16 +927,20 @@ def po_op_token_logprobs(logits, tokens=None, top: int = 0, scratch=None):
         raise ValueError("logits: a row's values must lie side by side")
     if ld < V:
         raise ValueError("logits: rows overlap")
-    stream = _operands(("logits", logits[:1], logits.dtype), ("tokens", tokens, torch.int32), ("scratch", scratch, torch.uint8))
+    stream = _operands(("tokens", tokens, torch.int32), ("scratch", scratch, torch.uint8))
+    if logits.get_device() != torch.cuda.current_device():
+        raise ValueError(f"logits: on {logits.device}, not on the current GPU")
     n = 0
+    dev, f32 = logits.device, torch.float32
     if tokens is not None:
         n = tokens.shape[-1]
         _shape("tokens", tokens, rows, n)
-    dev, f32 = logits.device, torch.float32
-    lp = torch.empty((rows, n), dtype=f32, device=dev)
+        lp = torch.empty_like(tokens, dtype=f32)
+    else:
+        lp = torch.empty((rows, 0), dtype=f32, device=dev)
     ent = torch.empty(rows, dtype=f32, device=dev)
     ids = torch.empty((rows, max(top, 0)), dtype=torch.int32, device=dev)
-    tlp = torch.empty((rows, max(top, 0)), dtype=f32, device=dev)
+    tlp = torch.empty_like(ids, dtype=f32)
     if scratch is None:
         scratch = torch.empty(po_token_logprobs_bytes(rows, V, top), dtype=torch.uint8, device=dev)
     check(lib().po_op_token_logprobs(_dt(logits), logits.data_ptr(), ld, rows, V, tokens.data_ptr() if n else None, n, top,

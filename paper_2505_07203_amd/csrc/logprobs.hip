@@ -422,9 +422,7 @@ void launch_token_logprobs(int dtype, const void* logits, int64_t ld, int64_t ro
 namespace {
 
 // columns of a panel: what stays in the memory-side cache (256 MiB of logits), at least a piece
-inline int64_t panel_width(int64_t rows, int V) {
-    return std::min(std::max<int64_t>(1, std::min<int64_t>(16, ((int64_t)1 << 26) / rows / PIECE)) * PIECE, round_up64(V, PIECE));
-}
+inline int64_t panel_width(int64_t rows, int V) { return std::min(std::max<int64_t>(1, ((int64_t)1 << 26) / rows / PIECE) * PIECE, round_up64(V, PIECE)); }
 
 __device__ __forceinline__ void head_answer(const Sums& sum, float m, float at, const int32_t* tokens, int V, int64_t r, float* logprobs, float* entropy) {
     const double log_s = log(sum.s);
