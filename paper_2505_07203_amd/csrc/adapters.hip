@@ -262,8 +262,8 @@ __device__ __forceinline__ uint4 pack(const float (&v)[4]) {
 
 // What both kernels of the second launch do with 16 rows x 64 columns: the products of 16 columns each leave a lane with four of them of row lane & 15;
 // they pass through 4 KiB of LDS of the wavefront's own (16-byte groups XOR-swizzled with the row), so that R is read and C written in whole lines.
-// R and C go by the rows' own bounds: what lies behind their ends reads as zero and is not written, and so does what a lane's offset is
-// moved out of bounds for.
+// R and C go by the rows' own bounds, B by its slot's: what lies behind their ends reads as zero and is not written, and so does what a lane's offset
+// is moved out of bounds for.  Whole offsets are the lane's (a scalar offset may not count in the check of bounds).
 template <typename T> struct Out {
     static constexpr int E = (int)sizeof(T), V = 16 / E, LPR = 64 / V, RPP = 64 / LPR, PASSES = 16 / RPP;      // of 16 bytes; lanes of a row; rows of a pass
 };
@@ -350,12 +350,12 @@ __global__ void __launch_bounds__(256) adapter_up_few_kernel(const AdapterParams
         for (int h = 0; h < 4; ++h)
 #pragma unroll
             for (int q = 0; q < E / 2; ++q)
-                set(w[h][k], q, __builtin_amdgcn_raw_buffer_load_b128(rb, vb, (uint32_t)(c0 + h * 16) * (uint32_t)p.width * E + q * 16, 0));
+                set(w[h][k], q, __builtin_amdgcn_raw_buffer_load_b128(rb, vb + (uint32_t)(c0 + h * 16) * (uint32_t)p.width * E + q * 16, 0, 0));
     }
     const uint32_t vo = c0 + (lane & (O::LPR - 1)) * O::V < p.N ? (uint32_t)(lane / O::LPR) * pitch + (uint32_t)(lane & (O::LPR - 1)) * 16u + (uint32_t)c0 * E : NONE;
     u32x4 r[O::PASSES];
 #pragma unroll
-    for (int i = 0; i < O::PASSES; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rr, vo, (uint32_t)(i * O::RPP) * pitch, 0);
+    for (int i = 0; i < O::PASSES; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rr, vo + (uint32_t)(i * O::RPP) * pitch, 0, 0);
     f32x4 acc[4];
 #pragma unroll
     for (int h = 0; h < 4; ++h) acc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -427,7 +427,7 @@ __global__ void __launch_bounds__(256, 2) adapter_up_kernel(const AdapterParams 
         for (int h = 0; h < H; ++h)
 #pragma unroll
             for (int q = 0; q < E / 2; ++q)
-                set(w[h][k], q, __builtin_amdgcn_raw_buffer_load_b128(rb, vb, (uint32_t)(c0 + h * 16) * (uint32_t)p.width * E + q * 16, 0));
+                set(w[h][k], q, __builtin_amdgcn_raw_buffer_load_b128(rb, vb + (uint32_t)(c0 + h * 16) * (uint32_t)p.width * E + q * 16, 0, 0));
     }
     if (rank & 7) {
 #pragma unroll
@@ -453,7 +453,7 @@ __global__ void __launch_bounds__(256, 2) adapter_up_kernel(const AdapterParams 
         const __amdgpu_buffer_rsrc_t rr = __builtin_amdgcn_make_buffer_rsrc((void*)((const unsigned char*)(p.res ? p.res : p.c) + (int64_t)(sg.row + g * 16) * pitch), 0,
                                                                             p.res ? (int)((uint32_t)min(16, sg.n - g * 16) * pitch) : 0, 0x00020000);
 #pragma unroll
-        for (int i = 0; i < O::PASSES; ++i) r[b][i] = __builtin_amdgcn_raw_buffer_load_b128(rr, vo[b], (uint32_t)(i * O::RPP) * pitch, 0);
+        for (int i = 0; i < O::PASSES; ++i) r[b][i] = __builtin_amdgcn_raw_buffer_load_b128(rr, vo[b] + (uint32_t)(i * O::RPP) * pitch, 0, 0);
     };
     // (the next rows' R go where this one's are no longer needed: B, two of these and of T do not fit the registers)
     auto turn = [&](const Frag<T> (&t)[KS][NP], Frag<T> (&next)[KS][NP], int g) {

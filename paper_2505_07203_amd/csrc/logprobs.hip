@@ -105,32 +105,27 @@ __device__ __forceinline__ Stats wave_stats(const float (&x)[PER_WAVE][8], float
     return r;
 }
 
-// Pieces of rows: a wavefront each.  at (may be null): the logit of token tokens[row], where the piece holds it.
+// the logits of a wavefront's piece p
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256, 6) logprob_pieces_kernel(const T* __restrict__ logits, int64_t ld, int V, int pieces, int64_t total,
-                                                             Stats* __restrict__ stats, int64_t stats_ld, float* __restrict__ chunk_max, int chunks,
-                                                             const int32_t* __restrict__ tokens, int first_token, float* __restrict__ at) {
-    const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (w >= total) return;
-    const int64_t r = w / pieces;
-    const int p = (int)(w - r * pieces), i0 = p * PIECE;
-    const T* row = logits + r * ld;
-    float v[PER_WAVE][8];
+__device__ __forceinline__ void load_piece(const T* row, int p, int V, float (&v)[PER_WAVE][8]) {
+    const int lane = threadIdx.x & 63, i0 = p * PIECE;
     if (VEC && i0 + PIECE <= V) {
 #pragma unroll
         for (int c = 0; c < PER_WAVE; ++c) load8_whole(row + i0 + c * CHUNK + lane * 8, v[c]);
-    } else {
-#pragma unroll 1
-        for (int c = 0; c < PER_WAVE; ++c) {
-            float x[8];
-            load8<T, VEC>(row, i0 + c * CHUNK + lane * 8, V, x);
-#pragma unroll
-            for (int u = 0; u < PER_WAVE; ++u)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[u][e] = u == c ? x[e] : v[u][e];
-        }
+        return;
     }
+#pragma unroll 1
+    for (int c = 0; c < PER_WAVE; ++c) {
+        float x[8];
+        load8<T, VEC>(row, i0 + c * CHUNK + lane * 8, V, x);
+#pragma unroll
+        for (int u = 0; u < PER_WAVE; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[u][e] = u == c ? x[e] : v[u][e];
+    }
+}
+// ... its sums, and the largest logits of its chunks where they are asked for (chunk_max: of the row)
+__device__ __forceinline__ Stats piece_stats(const float (&v)[PER_WAVE][8], int p, float* chunk_max, int chunks) {
     float cm[PER_WAVE];
 #pragma unroll
     for (int c = 0; c < PER_WAVE; ++c) {
@@ -144,15 +139,30 @@ __global__ void __launch_bounds__(256, 6) logprob_pieces_kernel(const T* __restr
         for (int c = 0; c < PER_WAVE; ++c) {
             cm[c] = wave_max(cm[c]);
             m = fmaxf(m, cm[c]);
-            if (lane == 0 && p * PER_WAVE + c < chunks) chunk_max[r * chunks + p * PER_WAVE + c] = cm[c];
+            if ((threadIdx.x & 63) == 0 && p * PER_WAVE + c < chunks) chunk_max[p * PER_WAVE + c] = cm[c];
         }
     } else {
 #pragma unroll
         for (int c = 0; c < PER_WAVE; ++c) m = fmaxf(m, cm[c]);
         m = wave_max(m);
     }
-    const Stats st = wave_stats(v, m);
-    if (lane == 0) {
+    return wave_stats(v, m);
+}
+
+// Pieces of rows: a wavefront each.  at (may be null): the logit of token tokens[row], where the piece holds it.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256, 6) logprob_pieces_kernel(const T* __restrict__ logits, int64_t ld, int V, int pieces, int64_t total,
+                                                                Stats* __restrict__ stats, int64_t stats_ld, float* __restrict__ chunk_max, int chunks,
+                                                                const int32_t* __restrict__ tokens, int first_token, float* __restrict__ at) {
+    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (w >= total) return;
+    const int64_t r = w / pieces;
+    const int p = (int)(w - r * pieces), i0 = p * PIECE;
+    const T* row = logits + r * ld;
+    float v[PER_WAVE][8];
+    load_piece<T, VEC>(row, p, V, v);
+    const Stats st = piece_stats(v, p, chunk_max ? chunk_max + r * chunks : nullptr, chunks);
+    if ((threadIdx.x & 63) == 0) {
         stats[r * stats_ld + p] = st;
         if (at) {
             const int64_t t = (int64_t)tokens[r] - first_token;
@@ -202,19 +212,19 @@ constexpr int LIST = 512;                        // elements that are ordered at
 // Leaves in out[0 .. min(n, top)) the largest of keys[0 .. n), in order; keys[n .. n + 32) are overwritten.  All different, but for
 // zeros, which are left out.  256 keys at a time are ranked, a thread holding four of them: each wavefront compares all of them with every
 // fourth eight of the list (read as a broadcast, which a thread per key would read four times as often), and ranks[256] adds up.  (The
-// callers' barriers stand around it.)
+// callers' barriers stand around it; threads from 256 on only wait.)
 __device__ __forceinline__ void largest(unsigned long long* keys, int n, int top, unsigned long long* out, int* ranks) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (tid < 32) keys[n + tid] = 0;
     for (int i0 = 0; i0 < n; i0 += 256) {
-        ranks[tid] = 0;
+        if (tid < 256) ranks[tid] = 0;
         __syncthreads();
         unsigned long long k[4];
         int rank[4] = {0, 0, 0, 0};
         const int mine = min(n - i0, 256);
 #pragma unroll
         for (int u = 0; u < 4; ++u) k[u] = u * 64 + lane < mine ? keys[i0 + u * 64 + lane] : ~0ull;
-        for (int j = wave * 8; j < n; j += 32) {
+        for (int j = wave < 4 ? wave * 8 : n; j < n; j += 32) {
             unsigned long long o[8];
 #pragma unroll
             for (int c = 0; c < 8; ++c) o[c] = keys[j + c];
@@ -226,29 +236,39 @@ __device__ __forceinline__ void largest(unsigned long long* keys, int n, int top
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-            if (u * 64 + lane < mine) atomicAdd(&ranks[u * 64 + lane], rank[u]);
+            if (wave < 4 && u * 64 + lane < mine) atomicAdd(&ranks[u * 64 + lane], rank[u]);
         __syncthreads();
         if (tid < mine && keys[i0 + tid] && ranks[tid] < top) out[ranks[tid]] = keys[i0 + tid];
     }
 }
 
-// A row's answer, by a workgroup.  What bounds it is the way of its loads, one after another: pieces and chunks; the chunks that hold the answer.
+// What a workgroup that answers for a row needs of LDS, beside the list of keys
+struct RowShared {
+    double red_s[4], red_t[4];
+    unsigned long long best[MAX_TOP];
+    float red_m[4];
+    int count, ranks[256];
+};
+struct RowAnswer {
+    const int32_t* tokens;
+    int n_tokens;
+    float *logprobs, *entropy;
+    int top;
+    int32_t* top_tokens;
+    float* top_logprobs;
+};
+
+// A row's answer, by a workgroup of which 256 threads work, from its pieces' sums and its chunks' largest logits.  What bounds it is the way of its
+// loads, one after another: pieces and chunks; the chunks that hold the answer.  keys: RUNS + 32, only where top > 0.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__ logits, int64_t ld, int V, int pieces, int chunks,
-                                                           const Stats* __restrict__ stats, const float* __restrict__ chunk_max,
-                                                           const int32_t* __restrict__ tokens, int n_tokens, float* __restrict__ logprobs,
-                                                           float* __restrict__ entropy, int top, int32_t* __restrict__ top_tokens,
-                                                           float* __restrict__ top_logprobs) {
-    __shared__ double red_s[4], red_t[4];
-    __shared__ float red_m[4];
-    extern __shared__ unsigned long long keys[];     // RUNS + 32, only where top > 0
-    __shared__ unsigned long long best[MAX_TOP];
-    __shared__ int count, ranks[256];
-    const int64_t r = blockIdx.x;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const T* row = logits + r * ld;
-    const Stats* st = stats + r * pieces;
-    const float* cm = chunk_max + r * chunks;
+__device__ __forceinline__ void answer_row(const T* row, int64_t r, int V, int pieces, int chunks, const Stats* st, const float* cm, const RowAnswer& a,
+                                           unsigned long long* keys, RowShared& sh) {
+    double(&red_s)[4] = sh.red_s, (&red_t)[4] = sh.red_t;
+    float(&red_m)[4] = sh.red_m;
+    unsigned long long(&best)[MAX_TOP] = sh.best;
+    int &count = sh.count, (&ranks)[256] = sh.ranks;
+    const int n_tokens = a.n_tokens, top = a.top, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int tid = threadIdx.x < 256 ? (int)threadIdx.x : 1 << 30;    // (the others only wait)
     // (first turn of each list and the first token: asked for together)
     const Stats none = {-INFINITY, 0.f, 0.f, 0.f};
     const Stats first = tid < pieces ? st[tid] : none;
@@ -256,17 +276,17 @@ __global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__
     if (top) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            if (tid + i * 256 < chunks) cm0[i] = cm[tid + i * 256];
+            if (tid < 256 && tid + i * 256 < chunks) cm0[i] = cm[tid + i * 256];
     }
     float given = -INFINITY;
     if (tid < n_tokens) {
-        const int32_t t = tokens[r * n_tokens + tid];
+        const int32_t t = a.tokens[r * n_tokens + tid];
         if (t >= 0 && t < V) given = to_f32(row[t]);
     }
     float m = first.m;
     for (int i = tid + 256; i < pieces; i += 256) m = fmaxf(m, st[i].m);
     m = wave_max(m);
-    if (lane == 0) red_m[wave] = m;
+    if (lane == 0 && wave < 4) red_m[wave] = m;
     if (tid < MAX_TOP) best[tid] = 0;
     if (tid == 0) count = 0;
     __syncthreads();
@@ -278,7 +298,7 @@ __global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__
         sum.s += __shfl_xor(sum.s, off);
         sum.t += __shfl_xor(sum.t, off);
     }
-    if (lane == 0) { red_s[wave] = sum.s; red_t[wave] = sum.t; }
+    if (lane == 0 && wave < 4) { red_s[wave] = sum.s; red_t[wave] = sum.t; }
     const float lowest = m == INFINITY ? INFINITY : -INFINITY;         // of a logit with weight
     // the chunks that hold the first tokens, as keys of (largest logit, chunk).  (More than a list holds: in turns, the best so far among them.)
     if (top) {
@@ -298,12 +318,12 @@ __global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__
     __syncthreads();
     sum = {red_s[0] + red_s[1] + red_s[2] + red_s[3], red_t[0] + red_t[1] + red_t[2] + red_t[3]};
     const double log_s = log(sum.s);
-    if (tid < n_tokens) logprobs[r * n_tokens + tid] = logprob_of(given, m, log_s);
+    if (tid < n_tokens) a.logprobs[r * n_tokens + tid] = logprob_of(given, m, log_s);
     for (int i = tid + 256; i < n_tokens; i += 256) {
-        const int32_t t = tokens[r * n_tokens + i];
-        logprobs[r * n_tokens + i] = t >= 0 && t < V ? logprob_of(to_f32(row[t]), m, log_s) : -INFINITY;
+        const int32_t t = a.tokens[r * n_tokens + i];
+        a.logprobs[r * n_tokens + i] = t >= 0 && t < V ? logprob_of(to_f32(row[t]), m, log_s) : -INFINITY;
     }
-    if (tid == 0 && entropy) entropy[r] = m > -INFINITY ? (float)fmax(0.0, log_s - sum.t / sum.s) : 0.f;
+    if (tid == 0 && a.entropy) a.entropy[r] = m > -INFINITY ? (float)fmax(0.0, log_s - sum.t / sum.s) : 0.f;
     if (top == 0) return;
 
     const int n_chunks = __popcll(__ballot(lane < top && best[lane] != 0));
@@ -377,25 +397,66 @@ __global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__
     __syncthreads();
     if (tid < top) {
         const unsigned long long k = best[tid];
-        top_tokens[r * top + tid] = k ? (int32_t)(uint32_t)~k : -1;
-        top_logprobs[r * top + tid] = k ? logprob_of(key_logit(k), m, log_s) : -INFINITY;
+        a.top_tokens[r * top + tid] = k ? (int32_t)(uint32_t)~k : -1;
+        a.top_logprobs[r * top + tid] = k ? logprob_of(key_logit(k), m, log_s) : -INFINITY;
     }
+}
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__ logits, int64_t ld, int V, int pieces, int chunks,
+                                                           const Stats* __restrict__ stats, const float* __restrict__ chunk_max, const RowAnswer a) {
+    extern __shared__ unsigned long long keys[];
+    __shared__ RowShared sh;
+    const int64_t r = blockIdx.x;
+    answer_row<T, VEC>(logits + r * ld, r, V, pieces, chunks, stats + r * pieces, chunk_max + r * chunks, a, keys, sh);
+}
+
+// Many long rows: pieces and answer of a row by one workgroup, sums and largest logits in LDS, one launch, so that the next row's logits are read
+// while one is answered.  The same arithmetic in the same order as by the two kernels.  Float32 rows of 128256, five alternatives, us
+// against the two kernels: 256 rows 31 / 31, 1024 103 / 106, 2048 186 / 207; 1024 rows of 2048 logits 33 / 26 (half of the wavefronts only wait
+// during the answer).
+constexpr int WHOLE_WAVES = 8, WHOLE_CHUNKS = 1024;            // (rows of up to 2^19 logits)
+inline bool whole_rows(int64_t rows, int pieces, int chunks) { return rows >= 768 && pieces >= 32 && chunks <= WHOLE_CHUNKS; }
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(64 * WHOLE_WAVES, 4) logprob_whole_kernel(const T* __restrict__ logits, int64_t ld, int V, int pieces, int chunks, const RowAnswer a) {
+    extern __shared__ unsigned long long keys[];
+    __shared__ RowShared sh;
+    __shared__ Stats st[WHOLE_CHUNKS / PER_WAVE];
+    __shared__ float cm[WHOLE_CHUNKS];
+    const int64_t r = blockIdx.x;
+    const T* row = logits + r * ld;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    float v[PER_WAVE][8], next[PER_WAVE][8];
+    if (wave < pieces) load_piece<T, VEC>(row, wave, V, v);
+    for (int p = wave; p < pieces; p += 2 * WHOLE_WAVES) {     // (the next piece on its way)
+        if (p + WHOLE_WAVES < pieces) load_piece<T, VEC>(row, p + WHOLE_WAVES, V, next);
+        const Stats x = piece_stats(v, p, a.top ? cm : nullptr, chunks);
+        if ((threadIdx.x & 63) == 0) st[p] = x;
+        if (p + WHOLE_WAVES >= pieces) break;
+        if (p + 2 * WHOLE_WAVES < pieces) load_piece<T, VEC>(row, p + 2 * WHOLE_WAVES, V, v);
+        const Stats y = piece_stats(next, p + WHOLE_WAVES, a.top ? cm : nullptr, chunks);
+        if ((threadIdx.x & 63) == 0) st[p + WHOLE_WAVES] = y;
+    }
+    __syncthreads();
+    answer_row<T, VEC>(row, r, V, pieces, chunks, st, cm, a, keys, sh);
 }
 
 inline int pieces_of(int V) { return (V + PIECE - 1) / PIECE; }
 inline int chunks_of(int V) { return (V + CHUNK - 1) / CHUNK; }
 
 template <typename T, bool VEC>
-void run(const T* logits, int64_t ld, int64_t rows, int V, const int32_t* tokens, int n_tokens, int top, float* logprobs, float* entropy,
-         int32_t* top_tokens, float* top_logprobs, void* scratch, hipStream_t s) {
-    const int pieces = pieces_of(V), chunks = chunks_of(V);
+void run(const T* logits, int64_t ld, int64_t rows, int V, const RowAnswer& a, void* scratch, hipStream_t s) {
+    const int pieces = pieces_of(V), chunks = chunks_of(V), lds = a.top ? (RUNS + 32) * 8 : 0;
+    if (whole_rows(rows, pieces, chunks)) {
+        hipLaunchKernelGGL((logprob_whole_kernel<T, VEC>), dim3((unsigned)rows), dim3(64 * WHOLE_WAVES), lds, s, logits, ld, V, pieces, chunks, a);
+        return;
+    }
     Stats* stats = (Stats*)scratch;
-    float* cm = top ? (float*)(stats + rows * pieces) : nullptr;
+    float* cm = a.top ? (float*)(stats + rows * pieces) : nullptr;
     const int64_t total = rows * pieces;
     hipLaunchKernelGGL((logprob_pieces_kernel<T, VEC>), dim3((unsigned)((total + 3) / 4)), dim3(256), 0, s, logits, ld, V, pieces, total, stats,
                        (int64_t)pieces, cm, chunks, (const int32_t*)nullptr, 0, (float*)nullptr);
-    hipLaunchKernelGGL((logprob_rows_kernel<T, VEC>), dim3((unsigned)rows), dim3(256), top ? (RUNS + 32) * 8 : 0, s, logits, ld, V, pieces, chunks, stats, cm, tokens,
-                       n_tokens, logprobs, entropy, top, top_tokens, top_logprobs);
+    hipLaunchKernelGGL((logprob_rows_kernel<T, VEC>), dim3((unsigned)rows), dim3(256), lds, s, logits, ld, V, pieces, chunks, stats, cm, a);
 }
 
 }  // namespace
@@ -410,7 +471,8 @@ void launch_token_logprobs(int dtype, const void* logits, int64_t ld, int64_t ro
                            float* logprobs, float* entropy, int32_t* top_tokens, float* top_logprobs, void* scratch, hipStream_t s) {
     const int esz = dtype == 0 ? 4 : 2;
     const bool vec = (uintptr_t)logits % 16 == 0 && (rows == 1 || ld * esz % 16 == 0);
-#define PO_RUN(T, VEC) run<T, VEC>((const T*)logits, ld, rows, V, tokens, n_tokens, top, logprobs, entropy, top_tokens, top_logprobs, scratch, s)
+    const RowAnswer a = {tokens, n_tokens, logprobs, entropy, top, top_tokens, top_logprobs};
+#define PO_RUN(T, VEC) run<T, VEC>((const T*)logits, ld, rows, V, a, scratch, s)
     if (dtype == 0) { if (vec) PO_RUN(float, true); else PO_RUN(float, false); }
     else { if (vec) PO_RUN(bf16_t, true); else PO_RUN(bf16_t, false); }
 #undef PO_RUN

@@ -160,6 +160,33 @@ def test_strides():
         check(base[::2, :3000], tk[::2].contiguous(), 3)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_many_long_rows(dtype):
+    """rows that a workgroup each reads and answers: the bits of the same rows by themselves, which are held to the definition"""
+    V = 66_001
+    z, tk = logits(12, V, 12, dtype)
+    z[1] = -float("inf")
+    z[2, 100:] = -float("inf")
+    z[3] = 2.5
+    z[4, [7, 60_000]] = float("inf")
+    z[5, ::3] = float("nan")
+    z[6] = (torch.arange(V, device="cuda") // 700).to(dtype)
+    tk[7] = torch.tensor([-1, V, 0], dtype=torch.int32)
+    for top in (0, 1, 20, 64):
+        want = check(z, tk, top)
+        for rows in (768, 1000):
+            pick = torch.arange(rows, device="cuda") * 7 % 12
+            got = B.po_op_token_logprobs(z[pick], tk[pick], top=top)
+            assert all(torch.equal(a, b[pick]) for a, b in zip(got, want))
+    odd = torch.cat((z, z[:, :3]), 1)[:, 1:V + 1]                     # a pitch that is no multiple of 16 bytes
+    pick = torch.arange(800, device="cuda") % 12
+    base = torch.empty(800, V + 4, dtype=dtype, device="cuda")
+    base[:, 1:V + 1] = odd[pick]
+    want = B.po_op_token_logprobs(odd.contiguous(), tk, top=9)
+    got = B.po_op_token_logprobs(base[:, 1:V + 1], tk[pick], top=9)
+    assert all(torch.equal(a, b[pick]) for a, b in zip(got, want))
+
+
 def test_scratch_and_neighbours():
     """what scratch held changes nothing, nor does a neighbour; nothing is written past the outputs"""
     z, tk = logits(9, 5001, 10)
