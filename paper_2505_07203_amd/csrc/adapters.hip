@@ -112,9 +112,12 @@ __device__ __forceinline__ void keep(Frag<float>& f, int n) {
 // T of a run of rows of one request over one piece of K, 16 rows at a time.  A wavefront takes C steps of 32 of the piece, 512 bytes of a row
 // (256 with ranks beyond 64), and holds that part of A in registers for all its rows: A is read once a run.  x goes straight into a ring of D
 // groups of rows in LDS, a load covering whole lines of two rows (four); 16-byte segments are XOR-swizzled with the row on the global side, so
-// that a fragment's 16 rows meet 16 different banks.  Fragments loaded from memory to registers touch 64 bytes of a line each and
-// came to half the rate: two prompts of 8000 rows of K 14336, rank 64, 161 us.  The wavefronts' sums meet in LDS.  A lane of a product of 16
-// ranks and 16 rows holds row lane & 15 and ranks 4 (lane >> 4) .. + 3.
+// that a fragment's 16 rows meet 16 different banks.  The wavefronts' sums meet in LDS.  A lane of a product of 16 ranks and 16 rows holds row
+// lane & 15 and ranks 4 (lane >> 4) .. + 3.
+// What bounds it: x from memory.  16584 rows of K 14336, rank 64, 120 us (4.0 TB/s), of which the loads alone, with nothing done between them, take
+// 104 to 114; the fragments straight from memory to registers, 64 bytes of a line each, 161 where this took 149 (runs of rows of another
+// length).  7394 rows of K 4096 in 41 requests 26: one round of workgroups, each of which waits for A first.  64 single tokens 7.4.
+// (LDS is read as vectors of bf16 or float: as uint4 the compiler, which cannot tell them from what the loads write, waits for all loads.)
 constexpr int DOWN_WAVES = 8;
 template <typename T, int NR> struct Down {
     static constexpr int ROWB = NR == 8 ? 256 : 512;             // bytes of a row that a wavefront takes
@@ -325,7 +328,7 @@ __device__ __forceinline__ void sum_planes(const AdapterParams& p, const float* 
 }
 
 // C of up to 16 rows of a request and 64 columns a wavefront, for batches of requests of up to 16 rows: every wavefront adds the planes of T itself.
-// Its loads are all under way together: this is what a single token waits for.
+// Its loads are all under way together: this is what a single token waits for (64 of them, N 4096, rank 16: 5 us).
 template <typename T, int KS>
 __global__ void __launch_bounds__(256) adapter_up_few_kernel(const AdapterParams p, const Table tab) {
     typedef Out<T> O;
@@ -377,7 +380,8 @@ __global__ void __launch_bounds__(256) adapter_up_few_kernel(const AdapterParams
     add_out<T>(acc, r, stage[wave], rc, vo, pitch, lane);
 }
 
-// Longer requests: first T as the second product's fragments, in the order of its lanes: [group][step][part][lane] (in scratch behind the planes) ...
+// Longer requests: first T as the second product's fragments, in the order of its lanes: [group][step][part][lane] (in scratch behind the planes;
+// 16584 rows, rank 64, seven planes: 9 us) ...
 template <typename T>
 __global__ void __launch_bounds__(256) adapter_join_kernel(const AdapterParams p, const Table tab) {
     constexpr int NP = Parts<T>::N;
@@ -398,7 +402,9 @@ __global__ void __launch_bounds__(256) adapter_join_kernel(const AdapterParams p
 }
 
 // ... then C of a run of rows of one request and 4 x 16 H columns, a quarter a wavefront, which holds its part of B in registers for all of
-// them: B is read once a run.  16 rows at a time, the next ones' R and T on their way; wavefronts wait for nobody.
+// them: B is read once a run.  16 rows at a time, the next ones' R and T on their way; wavefronts wait for nobody.  What bounds it: R and C,
+// 16584 x 4096 with rank 64 59 us (4.6 TB/s; a copy of as many bytes 46).  Tiles of 64 rows x 1024 columns that read B and the planes of T
+// anew took 89: what a compute unit can have under way towards it is the limit there, and reads that caches answer take their places in it.
 template <typename T, int KS> struct UpCols {
     static constexpr int H = 32 / (int)sizeof(T) / (KS == 1 ? 1 : KS / 2);              // 128 registers of B (64 with one step)
 };

@@ -8,6 +8,9 @@
 // ascending).  They lie in the chunks whose largest logits come first in that order, as many chunks as tokens: an element of any
 // other chunk has the largest elements of all of those before it.  The same holds for the runs of 8 within those chunks, so
 // at most 8 elements a token are ordered in the end, whatever the row holds, and no more than `top` chunks are read again.
+// What bounds it: many rows, reading them (1024 float32 rows of 128256: pieces 93 us, 5.7 TB/s; 256 of 152064 in bf16 18.5, 4.2: five
+// operations and an exponential a logit), then the answers, 11 to 18 us a launch whatever the rows, a chain of loads, exchanges and rankings;
+// one row, that chain (4.9 + 11.4 us).
 // NaN counts as -infinity; -infinity has no weight; with +infinity among the logits only those have, the same each.
 #include "po_internal.h"
 
@@ -515,7 +518,8 @@ __global__ void __launch_bounds__(256) head_rows_kernel(const Stats* __restrict_
     if (lane == 0) head_answer(sum, m, logprobs ? at[r] : 0.f, tokens, V, r, logprobs, entropy);
 }
 
-// ... from its blocks' planes [blocks][rows]: R rows (a power of two) side by side in a workgroup, 256 / R threads a row
+// ... from its blocks' planes [blocks][rows]: R rows (a power of two) side by side in a workgroup, 256 / R threads a row (one row of 1002 blocks 5 us,
+// 150 of 1188 10, 4001 of 501 20)
 __global__ void __launch_bounds__(256) head_blocks_kernel(const float* __restrict__ stats, int64_t plane, int blocks, int R, const float* __restrict__ at,
                                                           const int32_t* __restrict__ tokens, int V, int64_t rows, float* __restrict__ logprobs,
                                                           float* __restrict__ entropy) {
