@@ -633,7 +633,7 @@ po_status po_op_sample(const float* dev_logits, int64_t ld, int64_t rows, int32_
  *   h = bf16(x + delta),  y = h * rsqrt(mean(h^2) + eps) * g,  codes = e4m3(y * (448 / amax)) round to nearest even,  scale = amax / 448
  * with amax = max|y| over the row (block 0: scales [rows], as po_op_linear_fp8 reads them) or over each block of 128 of it (block 128:
  * scales [d / 128][rows], as po_op_linear_fp8_block reads them), raised to 448 * 2^-126 where it is below that and not zero; amax == 0:
- * codes 0, scale 1.  y is float32 until its one rounding, to the code (po_op_rmsnorm_quantize rounds it to bf16 first), and to bf16 in dev_y.
+ * codes 0, scale 1 (so a row of zeros, with eps 0 too).  y is float32 until its one rounding, to the code (po_op_rmsnorm_quantize rounds it to bf16 first), and to bf16 in dev_y.
  * Each may be NULL: dev_delta (h = x), dev_h, dev_y, dev_codes (with dev_scales); of dev_y and dev_codes one is given.  dev_h may be dev_x or
  * dev_delta, and so may dev_y (but not both the same); dev_codes overlaps nothing.  d % 8 == 0 (block 128: d % 128 == 0), d <= 16384;
  * pointers 16-byte aligned.  Finite inputs, the sum of a row's h^2 below 2^127; a row that has others may hold anything, the
@@ -649,8 +649,9 @@ po_status po_op_add_rmsnorm_quantize(const void* dev_x, const void* dev_delta, c
  * rest holds (rank 0: an empty slot).  ranks, scales [n_slots] and segments are HOST arrays, read before the call returns (a captured
  * call keeps them).  segments: rows ascending and apart, n_rows may be 0, adapter -1 = none.  The product with A is a float32 number
  * (PO_BF16: the sum of two bf16 numbers, 2^-16 off at most); C is rounded once.
- * N and K multiples of 8; width a multiple of 8, at most 128; pointers 16-byte aligned.  x overlaps neither C nor the residual.  Finite inputs; a
- * row that has others may hold anything, the other rows are as if it had none.
+ * N (up to 2^20) and K (up to 2^17) multiples of 8; width a multiple of 8, at most 128; up to 2^23 rows, fewer slots; pointers 16-byte aligned.  x
+ * overlaps neither C nor the residual, and those are the same or apart.  Finite inputs; a row that has others may hold anything, the other rows
+ * are as if it had none.
  * dev_scratch (256-byte aligned): po_adapters_bytes of what the call is given (host only); nothing in it is expected or
  * left, calls that may run at the same time need one each.  The same call gives the same bits every time. */
 typedef struct { int64_t row, n_rows, adapter; } po_adapter_rows;
@@ -666,7 +667,8 @@ po_status po_op_adapters(int32_t dtype, const void* dev_x, const void* dev_a, co
  * n_tokens and top may be 0 (their arrays then NULL).  NaN counts as -infinity; tokens of -infinity have no weight (log-prob -infinity) and are no
  * alternatives: where a row has fewer than `top` others, the rest are token -1, log-prob -infinity.  With +infinity among the logits only those
  * have weight, the same each.  A row without any weight: entropy 0, every log-prob -infinity.  Exponentials and sums of a piece of
- * 2048 logits are float32, sums of pieces and logarithms float64.  Every call gives the same bits.
+ * 2048 logits are float32, sums of pieces and logarithms float64.  Up to 2^20 rows, V up to 2^24, any rows * V up to 2^36 (PO_ERR_TOO_LONG).  Every
+ * call gives the same bits.
  * dev_scratch (256-byte aligned): po_token_logprobs_bytes (host only); nothing in it is expected or left, calls that may run at
  * the same time need one each. */
 po_status po_token_logprobs_bytes(int64_t rows, int32_t V, int32_t top, size_t* scratch_bytes);
@@ -676,7 +678,7 @@ po_status po_op_token_logprobs(int32_t dtype, const void* dev_logits, int64_t ld
 /* The log-probability of one token and the entropy for each of many hidden rows x [rows, d] behind the LM head W [V, d], whose logits
  * never exist as a whole: a prompt scored token by token (x after the final norm, row i with token i + 1).  tokens [rows] and logprobs
  * [rows] may both be NULL, entropy [rows] may be NULL (not all three); an id outside [0, V): -infinity.  dtype PO_F32 (d % 4 == 0) or
- * PO_BF16 (d % 64 == 0), any V; logits are float32 sums, not rounded.  Pointers 16-byte aligned.  Finite inputs; a row that has others may hold
+ * PO_BF16 (d % 64 == 0), d up to 2^16, rows and V as above; logits are float32 sums, not rounded.  Pointers 16-byte aligned.  Finite inputs; a row that has others may hold
  * anything, the other rows are as if it had none.  dev_scratch (256-byte aligned): po_lm_head_logprobs_bytes (host only), as above.
  * How a row's sums are rounded depends on rows, V and d alone; every call gives the same bits. */
 po_status po_lm_head_logprobs_bytes(int32_t dtype, int64_t rows, int32_t V, int32_t d, size_t* scratch_bytes);

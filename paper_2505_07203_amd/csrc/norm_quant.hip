@@ -110,7 +110,8 @@ __global__ void __launch_bounds__(256) norm_quant_kernel(const NormQuant p) {
     for (int off = 32; off > 0; off >>= 1) ss += __shfl_xor(ss, off);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = ss;
     __syncthreads();
-    const float r = 1.0f / sqrtf((part[0] + part[1] + part[2] + part[3]) * p.inv_d + p.eps);
+    const float mean = (part[0] + part[1] + part[2] + part[3]) * p.inv_d + p.eps;
+    const float r = mean > 0.f ? 1.0f / sqrtf(mean) : 0.f;               // (a row of zeros with eps 0: zeros)
     float pm = 0.f, ym = 0.f;                    // (ym: for the rare case alone, but a pass over registers)
 #pragma unroll
     for (int j = 0; j < QV; ++j) {

@@ -145,3 +145,15 @@ def test_refusals():
             B.po_op_add_rmsnorm_quantize(a["x"], a["delta"], a["gain"], 1e-5)
     with pytest.raises(B.PoError):
         B.po_op_add_rmsnorm_quantize(x[:, :200].contiguous(), None, gain[:200].contiguous(), 1e-5, block=128)
+
+
+@pytest.mark.parametrize("block", [0, 128])
+def test_zeros_without_eps(block):
+    """a row of zeros stays one, and says nothing about its neighbours"""
+    x = torch.zeros(3, 256, device="cuda").bfloat16()
+    x[1] = torch.linspace(-3, 5, 256, device="cuda").bfloat16()
+    gain = torch.full((256,), 1.5, device="cuda").bfloat16()
+    h, c, s, y = B.po_op_add_rmsnorm_quantize(x, None, gain, 0.0, block, normed=True)
+    check(x[1:2], None, gain, block, 0.0, h[1:2], c[1:2], (s[:, 1:2] if block else s[1:2]), y[1:2])
+    z = torch.tensor([0, 2], device="cuda")
+    assert not c[z].any() and not y[z].any() and bool(((s[:, z] if block else s[z]) == 1).all())
