@@ -2,10 +2,10 @@
 //
 //   C[r] = R[r] + scale_a T[r] B_a^T,  T[r] = x[r] A_a^T,    A_a [rank, K], B_a [N, rank]: the adapter a of the request that row r belongs to
 //
-// Adapters lie in slots of a pool, A [slots][width][K] and B [slots][N][width].  Two launches: T, in pieces of K, each a plane of float32 sums in
-// scratch; then C, whose workgroups add the planes first.  A request's rows multiply with its slot alone, so a batch costs the bytes of its rows and
-// of the slots that it uses.  Both launches are bound by memory, operands go from there to registers in the matrix instruction's own
-// order, 16 bytes a lane and load.
+// Adapters lie in slots of a pool, A [slots][width][K] and B [slots][N][width].  First T, in pieces of K, each a plane of float32 sums in scratch.
+// Then C: of requests of up to 16 rows by wavefronts that add the planes themselves; of longer ones from T joined to the matrix instruction's
+// fragments by a launch of its own.  A request's rows multiply with its slot alone, so a batch costs the bytes of its rows and of the
+// slots that it uses, and memory bounds it.
 #include "adapters.h"
 #include "slice_window.h"
 
@@ -328,7 +328,8 @@ __device__ __forceinline__ void sum_planes(const AdapterParams& p, const float* 
 }
 
 // C of up to 16 rows of a request and 64 columns a wavefront, for batches of requests of up to 16 rows: every wavefront adds the planes of T itself.
-// Its loads are all under way together: this is what a single token waits for (64 of them, N 4096, rank 16: 5 us).
+// Its loads are all under way together: this is what a single token waits for (64 of them, N 4096, rank 16: 5.1 us; by the two kernels below
+// 3.2 + 6.2).
 template <typename T, int KS>
 __global__ void __launch_bounds__(256) adapter_up_few_kernel(const AdapterParams p, const Table tab) {
     typedef Out<T> O;

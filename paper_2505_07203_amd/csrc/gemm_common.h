@@ -575,20 +575,11 @@ __device__ __forceinline__ void tile_logprob(const GemmParams& p, const f32x4 (&
             for (int i = 0; i < 16; ++i) m = fmaxf(m, v[i]);
             m = fmaxf(m, __shfl_xor(m, 16));
             m = fmaxf(m, __shfl_xor(m, 32));
-            if (ragged) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {             // (a logit that is not there: where its term is 0 in float32)
-                    const float d = fmaxf((v[i] - m) * LOG2E, -250.0f), e = __builtin_amdgcn_exp2f(d);
-                    s += e;
-                    t = fmaf(d, e, t);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float d = (v[i] - m) * LOG2E, e = __builtin_amdgcn_exp2f(d);
-                    s += e;
-                    t = fmaf(d, e, t);
-                }
+            for (int i = 0; i < 16; ++i) {                 // (no distance beyond where its term is 0 in float32: an infinite one would make T NaN)
+                const float d = fmaxf((v[i] - m) * LOG2E, -250.0f), e = __builtin_amdgcn_exp2f(d);
+                s += e;
+                t = fmaf(d, e, t);
             }
             s += __shfl_xor(s, 16);
             t += __shfl_xor(t, 16);
@@ -625,7 +616,7 @@ __device__ __forceinline__ void tile_logprob_join(const GemmParams& p, const flo
     for (int w = 0; w < WN; ++w) {
         const float* o = in + w * 3 * BM_ + tid;
         if (o[0] > -INFINITY) {
-            const float d = (o[0] - m) * LOG2E, e = __builtin_amdgcn_exp2f(d);
+            const float d = fmaxf((o[0] - m) * LOG2E, -250.0f), e = __builtin_amdgcn_exp2f(d);
             s = fmaf(o[BM_], e, s);
             t = fmaf(fmaf(d, o[BM_], o[2 * BM_]), e, t);
         }

@@ -141,3 +141,22 @@ def test_refusals():
             B.po_op_lm_head_logprobs(*a)
     with pytest.raises(B.PoError):
         B.po_op_lm_head_logprobs(x[:, :96].contiguous(), w[:, :96].contiguous(), t)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,V", [(1, 300), (5, 5000), (300, 256)])
+def test_logits_further_apart_than_float32(dtype, rows, V):
+    """logits of -2^127 and 2^127, whose distance is no float32 number: the weight is that of the larger ones, the same each, which is
+    exact but for the logarithm (2^-21 of it)"""
+    x = torch.zeros(rows, 64, device="cuda", dtype=dtype)
+    x[:, 5] = 2.0 ** 63
+    w = torch.zeros(V, 64, device="cuda", dtype=dtype)
+    w[:, 5] = -2.0 ** 64
+    high = torch.arange(3, V, 7, device="cuda")
+    w[high, 5] = 2.0 ** 64
+    t = torch.full((rows,), 3, dtype=torch.int32, device="cuda")
+    lp, ent = B.po_op_lm_head_logprobs(x, w, t)
+    want = torch.full((rows,), len(high), dtype=torch.float64, device="cuda").log()
+    assert bool(((lp.double() + want).abs() <= 2.0 ** -21 * want).all()) and bool(((ent.double() - want).abs() <= 2.0 ** -21 * want).all())
+    lp, _ = B.po_op_lm_head_logprobs(x, w, t + 1)
+    assert bool((lp < -3e38).all())
