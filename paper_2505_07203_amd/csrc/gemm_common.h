@@ -550,33 +550,33 @@ __device__ __forceinline__ void tile_epilogue16(const GemmParams& p, const f32x4
 template <typename F, int... I>
 __device__ __forceinline__ void for_each_constant(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
 
-// (m, S, T) of a wavefront's patch of 16 MU rows x 64 logits, for launch_gemm_logprob; acc as in tile_epilogue16.  Into LDS: out[row of the
+// (m, S, T) of a wavefront's patch of 16 MU rows x 16 CT logits, for launch_gemm_logprob; acc as in tile_epilogue16.  Into LDS: out[row of the
 // tile] for each of the three, planes of `plane` floats.  The four lanes of a row exchange by way of LDS.  Costs no more than
 // storing the tile: 4001 rows, N 128256, K 4096 2957 us, stored in bf16 2950 to 3080.
-template <int MU>
-__device__ __forceinline__ void tile_logprob(const GemmParams& p, const f32x4 (&acc)[MU][4], float* out, int plane, int tile_row, int row_base, int col_base, int lane) {
+template <int MU, int CT>
+__device__ __forceinline__ void tile_logprob(const GemmParams& p, const f32x4 (&acc)[MU][CT], float* out, int plane, int tile_row, int row_base, int col_base, int lane) {
     constexpr float LOG2E = 1.44269504f;
     const int l15 = lane & 15, l4 = lane >> 4;
     const int left = p.N - col_base - 4 * l4;              // logits of tile t exist where 16 t + e < left
-    const bool none = col_base >= p.N, ragged = col_base + 64 > p.N;
+    const bool none = col_base >= p.N, ragged = col_base + 16 * CT > p.N;
     for_each_constant([&](auto uc) {
         constexpr int u = decltype(uc)::value;
         float m = -INFINITY, s = 0.f, t = 0.f;
         if (!none) {
-            float v[16];
+            float v[4 * CT];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = acc[u][i >> 2][i & 3];
+            for (int i = 0; i < 4 * CT; ++i) v[i] = acc[u][i >> 2][i & 3];
             if (ragged) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
+                for (int i = 0; i < 4 * CT; ++i)
                     if ((i >> 2) * 16 + (i & 3) >= left) v[i] = -INFINITY;
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) m = fmaxf(m, v[i]);
+            for (int i = 0; i < 4 * CT; ++i) m = fmaxf(m, v[i]);
             m = fmaxf(m, __shfl_xor(m, 16));
             m = fmaxf(m, __shfl_xor(m, 32));
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {                 // (no distance beyond where its term is 0 in float32: an infinite one would make T NaN)
+            for (int i = 0; i < 4 * CT; ++i) {             // (no distance beyond where its term is 0 in float32: an infinite one would make T NaN)
                 const float d = fmaxf((v[i] - m) * LOG2E, -250.0f), e = __builtin_amdgcn_exp2f(d);
                 s += e;
                 t = fmaf(d, e, t);
@@ -588,10 +588,10 @@ __device__ __forceinline__ void tile_logprob(const GemmParams& p, const f32x4 (&
             if (p.tok) {
                 const int row = row_base + u * 16 + l15;
                 const int64_t d = row < p.M ? (int64_t)p.tok[row] - col_base : -1;
-                if (d >= 0 && d < 64 && d < p.N - col_base && ((d >> 2) & 3) == l4) {
+                if (d >= 0 && d < 16 * CT && d < p.N - col_base && ((d >> 2) & 3) == l4) {
                     float x = v[0];
 #pragma unroll
-                    for (int i = 1; i < 16; ++i) x = d == (i >> 2) * 16 + 4 * l4 + (i & 3) ? v[i] : x;
+                    for (int i = 1; i < 4 * CT; ++i) x = d == (i >> 2) * 16 + 4 * l4 + (i & 3) ? v[i] : x;
                     p.at[row] = x;
                 }
             }

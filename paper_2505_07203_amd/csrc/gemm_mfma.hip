@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(NT_BF16) gemm_bf16_mfma_kernel(const GemmParam
 
     if (EPI == EPI_LOGPROB) {
         float* const sums = (float*)smem;                  // [4][3][BM_]
-        tile_logprob<MU>(p, acc, sums + wn * 3 * BM_, BM_, wm * (MU * 16), m0 + wm * (MU * 16), n0 + wn * 64, lane);
+        tile_logprob(p, acc, sums + wn * 3 * BM_, BM_, wm * (MU * 16), m0 + wm * (MU * 16), n0 + wn * 64, lane);
         __syncthreads();
         tile_logprob_join<4, BM_>(p, sums, tn, m0, tid);
     } else if (EPI == EPI_PARTIAL) {
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(256, 2) gemm_bf16_small_kernel(const GemmParam
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if (EPI == EPI_LOGPROB) {
         float* const sums = (float*)smem;                  // [2][3][BM_]
-        tile_logprob<MU>(p, acc, sums + wn * 3 * BM_, BM_, wm * (MU * 16), m0 + wm * (MU * 16), n0 + wn * 64, lane);
+        tile_logprob(p, acc, sums + wn * 3 * BM_, BM_, wm * (MU * 16), m0 + wm * (MU * 16), n0 + wn * 64, lane);
         __syncthreads();
         tile_logprob_join<2, BM_>(p, sums, tn, m0, tid);
     } else if (EPI == EPI_PARTIAL) {

@@ -152,26 +152,18 @@ __device__ __forceinline__ Stats piece_stats(const float (&v)[PER_WAVE][8], int 
     return wave_stats(v, m);
 }
 
-// Pieces of rows: a wavefront each.  at (may be null): the logit of token tokens[row], where the piece holds it.
+// Pieces of rows: a wavefront each.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256, 6) logprob_pieces_kernel(const T* __restrict__ logits, int64_t ld, int V, int pieces, int64_t total,
-                                                                Stats* __restrict__ stats, int64_t stats_ld, float* __restrict__ chunk_max, int chunks,
-                                                                const int32_t* __restrict__ tokens, int first_token, float* __restrict__ at) {
+                                                                Stats* __restrict__ stats, float* __restrict__ chunk_max, int chunks) {
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (w >= total) return;
     const int64_t r = w / pieces;
-    const int p = (int)(w - r * pieces), i0 = p * PIECE;
-    const T* row = logits + r * ld;
+    const int p = (int)(w - r * pieces);
     float v[PER_WAVE][8];
-    load_piece<T, VEC>(row, p, V, v);
+    load_piece<T, VEC>(logits + r * ld, p, V, v);
     const Stats st = piece_stats(v, p, chunk_max ? chunk_max + r * chunks : nullptr, chunks);
-    if ((threadIdx.x & 63) == 0) {
-        stats[r * stats_ld + p] = st;
-        if (at) {
-            const int64_t t = (int64_t)tokens[r] - first_token;
-            if (t >= i0 && t < i0 + PIECE && t < V) at[r] = to_f32(row[t]);
-        }
-    }
+    if ((threadIdx.x & 63) == 0) stats[w] = st;
 }
 
 // what joins pieces: their m, S, T relative to a common maximum
@@ -458,7 +450,7 @@ void run(const T* logits, int64_t ld, int64_t rows, int V, const RowAnswer& a, v
     float* cm = a.top ? (float*)(stats + rows * pieces) : nullptr;
     const int64_t total = rows * pieces;
     hipLaunchKernelGGL((logprob_pieces_kernel<T, VEC>), dim3((unsigned)((total + 3) / 4)), dim3(256), 0, s, logits, ld, V, pieces, total, stats,
-                       (int64_t)pieces, cm, chunks, (const int32_t*)nullptr, 0, (float*)nullptr);
+                       cm, chunks);
     hipLaunchKernelGGL((logprob_rows_kernel<T, VEC>), dim3((unsigned)rows), dim3(256), lds, s, logits, ld, V, pieces, chunks, stats, cm, a);
 }
 
@@ -482,12 +474,8 @@ void launch_token_logprobs(int dtype, const void* logits, int64_t ld, int64_t ro
 }
 
 // ------------------------------------------------------------------ through the LM head
-// bf16: the product leaves (m, S, T) of blocks of 256 or 128 columns (launch_gemm_logprob).  float32: logits in panels of columns in scratch,
-// each reduced to its pieces' (m, S, T) before the next.
+// The product leaves (m, S, T) of blocks of 256 or 128 columns (launch_gemm_logprob, launch_head_logprob_f32).
 namespace {
-
-// columns of a panel: what stays in the memory-side cache (256 MiB of logits), at least a piece
-inline int64_t panel_width(int64_t rows, int V) { return std::min(std::max<int64_t>(1, ((int64_t)1 << 26) / rows / PIECE) * PIECE, round_up64(V, PIECE)); }
 
 __device__ __forceinline__ void head_answer(const Sums& sum, float m, float at, const int32_t* tokens, int V, int64_t r, float* logprobs, float* entropy) {
     const double log_s = log(sum.s);
@@ -498,27 +486,7 @@ __device__ __forceinline__ void head_answer(const Sums& sum, float m, float at, 
     }
 }
 
-// a row's answer from its pieces: a wavefront each
-__global__ void __launch_bounds__(256) head_rows_kernel(const Stats* __restrict__ stats, int pieces, const float* __restrict__ at,
-                                                        const int32_t* __restrict__ tokens, int V, int64_t rows, float* __restrict__ logprobs,
-                                                        float* __restrict__ entropy) {
-    const int lane = threadIdx.x & 63;
-    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (r >= rows) return;
-    const Stats* st = stats + r * pieces;
-    float m = -INFINITY;
-    for (int i = lane; i < pieces; i += 64) m = fmaxf(m, st[i].m);
-    m = wave_max(m);
-    Sums sum = {0.0, 0.0};
-    for (int i = lane; i < pieces; i += 64) join(st[i], m, sum);
-    for (int off = 32; off > 0; off >>= 1) {
-        sum.s += __shfl_xor(sum.s, off);
-        sum.t += __shfl_xor(sum.t, off);
-    }
-    if (lane == 0) head_answer(sum, m, logprobs ? at[r] : 0.f, tokens, V, r, logprobs, entropy);
-}
-
-// ... from its blocks' planes [blocks][rows]: R rows (a power of two) side by side in a workgroup, 256 / R threads a row (one row of 1002 blocks 5 us,
+// a row's answer from its blocks' planes [blocks][rows]: R rows (a power of two) side by side in a workgroup, 256 / R threads a row (one row of 1002 blocks 5 us,
 // 150 of 1188 10, 4001 of 501 20)
 __global__ void __launch_bounds__(256) head_blocks_kernel(const float* __restrict__ stats, int64_t plane, int blocks, int R, const float* __restrict__ at,
                                                           const int32_t* __restrict__ tokens, int V, int64_t rows, float* __restrict__ logprobs,
@@ -569,39 +537,22 @@ __global__ void __launch_bounds__(256) head_blocks_kernel(const float* __restric
 
 }  // namespace
 
-size_t head_logprobs_scratch(int dtype, int64_t rows, int V, int d) {
-    if (dtype != 0) return (size_t)rows * ((size_t)gemm_logprob_blocks(rows, V, d) * 12 + 4);
-    return (size_t)rows * ((size_t)panel_width(rows, V) * 4 + (size_t)pieces_of(V) * sizeof(Stats) + 4);
-}
+static int head_blocks(int dtype, int64_t rows, int V, int d) { return dtype == 0 ? head_logprob_f32_blocks(V) : gemm_logprob_blocks(rows, V, d); }
+
+size_t head_logprobs_scratch(int dtype, int64_t rows, int V, int d) { return (size_t)rows * ((size_t)head_blocks(dtype, rows, V, d) * 12 + 4); }
 
 void launch_head_logprobs(int dtype, const void* x, const void* w, int64_t rows, int V, int d, const int32_t* tokens, float* logprobs,
                           float* entropy, void* scratch, hipStream_t s) {
-    if (dtype != 0) {
-        const int blocks = gemm_logprob_blocks(rows, V, d);
-        const int64_t plane = (int64_t)blocks * rows;
-        float* stats = (float*)scratch;
-        float* at = stats + 3 * plane;
-        launch_gemm_logprob((const bf16_t*)x, d, (const bf16_t*)w, d, stats, tokens, at, rows, V, d, s);
-        // (as many workgroups as fill the card, before whole lines of a plane; us with R 1 / 16: 1 row 5.3 / 26, 150 rows 10 / 38, 4001 rows 39 / 20)
-        int R = 1;
-        while (R < 16 && rows >= 800 * R) R *= 2;
-        hipLaunchKernelGGL(head_blocks_kernel, dim3((unsigned)((rows + R - 1) / R)), dim3(256), 0, s, stats, plane, blocks, R, at, tokens, V, rows, logprobs,
-                           entropy);
-        return;
-    }
-    const int64_t width = panel_width(rows, V);
-    const int pieces = pieces_of(V);
-    float* panel = (float*)scratch;
-    Stats* stats = (Stats*)(panel + rows * width);
-    float* at = (float*)(stats + rows * pieces);
-    for (int v0 = 0; v0 < V; v0 += (int)width) {
-        const int n = (int)std::min<int64_t>(width, V - v0), p = pieces_of(n);
-        launch_gemm_basic(0, x, d, (const float*)w + (int64_t)v0 * d, d, panel, width, nullptr, nullptr, 0, rows, n, d, s);
-        const int64_t total = rows * p;
-        hipLaunchKernelGGL((logprob_pieces_kernel<float, true>), dim3((unsigned)((total + 3) / 4)), dim3(256), 0, s, panel, width, n, p, total,
-                           stats + v0 / PIECE, (int64_t)pieces, (float*)nullptr, 0, tokens, v0, tokens ? at : nullptr);
-    }
-    hipLaunchKernelGGL(head_rows_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, stats, pieces, at, tokens, V, rows, logprobs, entropy);
+    const int blocks = head_blocks(dtype, rows, V, d);
+    const int64_t plane = (int64_t)blocks * rows;
+    float* stats = (float*)scratch;
+    float* at = stats + 3 * plane;
+    if (dtype == 0) launch_head_logprob_f32((const float*)x, (const float*)w, stats, tokens, at, rows, V, d, s);
+    else launch_gemm_logprob((const bf16_t*)x, d, (const bf16_t*)w, d, stats, tokens, at, rows, V, d, s);
+    // (as many workgroups as fill the card, before whole lines of a plane; us with R 1 / 16: 1 row 5.3 / 26, 150 rows 10 / 38, 4001 rows 39 / 20)
+    int R = 1;
+    while (R < 16 && rows >= 800 * R) R *= 2;
+    hipLaunchKernelGGL(head_blocks_kernel, dim3((unsigned)((rows + R - 1) / R)), dim3(256), 0, s, stats, plane, blocks, R, at, tokens, V, rows, logprobs, entropy);
 }
 
 }  // namespace po

@@ -1877,7 +1877,7 @@ static po_status head_shape(int32_t dtype, int64_t rows, int32_t V, int32_t d) {
     if (bad_dtype(dtype) || rows <= 0 || V <= 0 || d <= 0) return PO_ERR_INVALID_ARG;
     if (d % (dtype == PO_F32 ? 4 : 64)) return PO_ERR_BAD_CONFIG;
     // (tiles of both operands are addressed with 32-bit offsets)
-    return rows > 1 << 20 || V > 1 << 24 || d > 1 << 16 || !token_logprobs_fits(rows, V) ? PO_ERR_TOO_LONG : PO_OK;
+    return rows > 1 << 20 || V > 1 << 24 || d > 1 << 16 || ((rows + 63) / 64) * ((V + 127) / 128) > MAX_WORKGROUPS_256 - 8 ? PO_ERR_TOO_LONG : PO_OK;
 }
 
 po_status po_lm_head_logprobs_bytes(int32_t dtype, int64_t rows, int32_t V, int32_t d, size_t* scratch_bytes) {
