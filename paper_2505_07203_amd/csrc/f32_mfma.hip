@@ -789,41 +789,44 @@ bool launch_gemm_f32_qkv_rope(const float* A, int64_t lda, const float* W, int64
 }
 
 // ---------------------------------------------------------------- log-probabilities behind the LM head
-// Logits as by the GEMM above, bit for bit (elements 8 g .. 8 g + 7 of a slice of 32 in lane group g, one per MFMA), of which a block of 128 columns
-// leaves (m, S, T) of each row (tile_logprob).  A workgroup is 16 MU rows x 128 columns, 32 a wavefront, K in slices of 32 through a ring of D
-// positions, one barrier a slice: behind it slice s has landed and everybody has read slice s - 1, whose place slice s + D - 1 takes.  Two
-// workgroups a compute unit, one's products beside the other's waits.
-// What bounds it: up to 32 rows the weights from memory, beyond them the matrix pipe.
+// Logits as by the GEMM above, bit for bit (elements 8 g .. 8 g + 7 of a slice of 32 in lane group g, one per MFMA), of which a block of columns
+// leaves (m, S, T) of each row (tile_logprob).  Four wavefronts, WM x 4 / WM, a patch of 16 MU rows x 16 CT columns each; K in slices of 32 through a
+// ring of D positions, one barrier a slice: it hands over slice s + 1, whose fragments are read while slice s is multiplied, and frees the place of
+// slice s for s + D.  Two workgroups a compute unit.  What bounds it: up to 32 rows the weights from memory (one row of 128256 x 4096 375 us, 5.6
+// TB/s), beyond them the matrix pipe (1000 rows 7860 us, 134 TFLOP/s).
 using namespace gemm;
 
-template <int MU> struct HeadF32 {
-    static constexpr int NA = MU <= 2 ? 1 : 2, AU = NA * 4096, UNIT = AU + 128 * 128;        // a wavefront's loads of x, 8 rows each; bytes of a slice
-    static constexpr int D = NA == 1 ? 4 : 3;
-    static_assert(D * UNIT <= 80 * 1024, "two workgroups per compute unit");
+template <int MU, int CT, int WM> struct HeadF32 {
+    static constexpr int BM = 16 * MU * WM, BN = 16 * CT * (4 / WM);
+    static constexpr int NA = BM <= 32 ? 1 : 2, NW = BN / 32;                              // a wavefront's loads of x and of W, 8 rows each
+    static constexpr int AU = NA * 4096, UNIT = AU + NW * 4096;                            // bytes of a slice
+    static constexpr int D = CT == 1 ? 8 : NA == 1 ? 4 : 3;
+    static_assert(BM <= NA * 32 && D * UNIT <= 80 * 1024, "two workgroups per compute unit");
 };
 constexpr int HEAD_GROUP = 8;                    // row tiles that one XCD takes beside each other, with the same weights
 
-template <int MU>
+template <int MU, int CT, int WM>
 __global__ void __launch_bounds__(256, 2) head_logprob_f32_kernel(const GemmParams p) {
-    typedef HeadF32<MU> L;
-    constexpr int D = L::D, NA = L::NA, BM = 16 * MU, BN = 128;
+    typedef HeadF32<MU, CT, WM> L;
+    constexpr int D = L::D, NA = L::NA, NW = L::NW, BM = L::BM, BN = L::BN;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int total = p.mt * p.nt, per_xcd = (total + 7) >> 3, local = blockIdx.x >> 3, li = (blockIdx.x & 7) * per_xcd + local;
     if (local >= per_xcd || li >= total) return;
     const int group = li / (HEAD_GROUP * p.nt), within = li - group * (HEAD_GROUP * p.nt), beside = min(HEAD_GROUP, p.mt - group * HEAD_GROUP);
     const int tn = within / beside, m0 = (group * HEAD_GROUP + within - tn * beside) * BM, n0 = tn * BN;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l15 = lane & 15, l4 = lane >> 4;
+    const int wm = wave / (4 / WM), wn = wave % (4 / WM);
     const uint32_t pitch = (uint32_t)p.K * 4u;
     const uint32_t a_bytes = (uint32_t)min(BM, p.M - m0) * pitch, w_bytes = (uint32_t)min(BN, p.N - n0) * pitch;
     void* const pa_ = (void*)((const float*)p.A + (int64_t)m0 * p.K);
     void* const pw_ = (void*)((const float*)p.W + (int64_t)n0 * p.K);
     const int KT = (p.K + 31) / 32;
-    // loads of 8 rows each: NA of x, then 4 of W.  (Rows that are not there read as zero, and so do columns of the last slice beyond K, by the lane's
+    // loads of 8 rows each: NA of x, then NW of W.  (Rows that are not there read as zero, and so do columns of the last slice beyond K, by the lane's
     // offset, and slices past the end, by an empty descriptor.)
-    uint32_t vo[8], tail = 0;                    // (NA + 4 entries used; bit i: load i of the last slice lies beyond K for this lane)
+    uint32_t vo[8], tail = 0;                    // (NA + NW entries used; bit i: load i of the last slice lies beyond K for this lane)
 #pragma unroll
-    for (int i = 0; i < NA + 4; ++i) {
-        const int row = (i < NA ? wave * NA + i : wave * 4 + i - NA) * 8 + (lane >> 3), seg = (lane & 7) ^ ((row >> 1) & 7);
+    for (int i = 0; i < NA + NW; ++i) {
+        const int row = (i < NA ? wave * NA + i : wave * NW + i - NA) * 8 + (lane >> 3), seg = (lane & 7) ^ ((row >> 1) & 7);
         vo[i] = (uint32_t)row * pitch + seg * 16;
         if ((KT - 1) * 32 + seg * 4 >= p.K) tail |= 1u << i;
     }
@@ -837,74 +840,100 @@ __global__ void __launch_bounds__(256, 2) head_logprob_f32_kernel(const GemmPara
         _Pragma("unroll") for (int i = 0; i < NA; ++i)                                                                                      \
             __builtin_amdgcn_raw_ptr_buffer_load_lds(ra_, (__attribute__((address_space(3))) void*)(u_ + (wave * NA + i) * 1024), 16,       \
                                                      vo[i] + ((past_ >> i & 1) << 31), wa_.offset, 0, 0);                                   \
-        _Pragma("unroll") for (int i = 0; i < 4; ++i)                                                                                       \
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rw_, (__attribute__((address_space(3))) void*)(u_ + L::AU + (wave * 4 + i) * 1024), 16, \
+        _Pragma("unroll") for (int i = 0; i < NW; ++i)                                                                                      \
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rw_, (__attribute__((address_space(3))) void*)(u_ + L::AU + (wave * NW + i) * 1024), 16, \
                                                      vo[NA + i] + ((past_ >> (NA + i) & 1) << 31), ww_.offset, 0, 0);                       \
     }
     int fo[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) fo[h] = l15 * 128 + (((2 * l4 + h) ^ ((l15 >> 1) & 7)) << 4);
-    f32x4 acc[MU][2];
+    f32x4 acc[MU][CT];
 #pragma unroll
-    for (int u = 0; u < MU; ++u) acc[u][0] = acc[u][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < MU; ++u)
 #pragma unroll
-    for (int s = 0; s < D - 1; ++s) PO_FETCH(s, s)
-    int pos = 0, next = D - 1;
-    for (int s = 0; s < KT; ++s) {
-        PO_WAIT_BARRIER((D - 2) * (NA + 4));
-        PO_FETCH(s + D - 1, next)
-        const unsigned char* const u = smem + pos * L::UNIT;
-        f32x4 a[2][MU], w[2][2];
+        for (int t = 0; t < CT; ++t) acc[u][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+    for (int s = 0; s < D; ++s) PO_FETCH(s, s)
+    PO_WAIT_BARRIER((D - 1) * (NA + NW));          // slice 0 has landed
+    struct Frags { f32x4 a[2][MU], w[2][CT]; } f0, f1;
+    auto read = [&](Frags& f, int at, int h) {
+        const unsigned char* const u = smem + at * L::UNIT;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) w[h][t] = *(const f32x4*)(u + L::AU + (wave * 32 + t * 16) * 128 + fo[h]);
+        for (int t = 0; t < CT; ++t) f.w[h][t] = *(const f32x4*)(u + L::AU + (wn * CT + t) * 2048 + fo[h]);
 #pragma unroll
-            for (int j = 0; j < MU; ++j) a[h][j] = *(const f32x4*)(u + j * 2048 + fo[h]);
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int j = 0; j < MU; ++j)
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[h][t][e], a[h][j][e], acc[j][t], 0, 0, 0);
-        next = pos;
-        pos = pos + 1 == D ? 0 : pos + 1;
+        for (int j = 0; j < MU; ++j) f.a[h][j] = *(const f32x4*)(u + (wm * MU + j) * 2048 + fo[h]);
+    };
+    read(f0, 0, 0);
+    read(f0, 0, 1);
+    int s = 0, pos = 0;
+#define PO_SLICE(F, G)                                                                                                              \
+    {                                                                                                                               \
+        PO_WAIT_BARRIER((D - 2) * (NA + NW));                                                                                       \
+        const int pos1 = pos + 1 == D ? 0 : pos + 1;                                                                                \
+        _Pragma("unroll") for (int h = 0; h < 2; ++h) _Pragma("unroll") for (int e = 0; e < 4; ++e) {                               \
+            _Pragma("unroll") for (int j = 0; j < MU; ++j) _Pragma("unroll") for (int t = 0; t < CT; ++t)                           \
+                acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(F.w[h][t][e], F.a[h][j][e], acc[j][t], 0, 0, 0);                   \
+            __builtin_amdgcn_sched_barrier(0);                                                                                      \
+            if (h == 0 && e == 0) PO_FETCH(s + D, pos)                                                                              \
+            if (h == 0 && e == 1) read(G, pos1, 0);                                                                                 \
+            if (h == 0 && e == 3) read(G, pos1, 1);                                                                                 \
+            __builtin_amdgcn_sched_barrier(0);                                                                                      \
+        }                                                                                                                           \
+        pos = pos1;                                                                                                                 \
+        ++s;                                                                                                                        \
     }
+    while (s + 2 <= KT) {
+        PO_SLICE(f0, f1)
+        PO_SLICE(f1, f0)
+    }
+    if (s < KT) PO_SLICE(f0, f1)
+#undef PO_SLICE
 #undef PO_FETCH
     PO_WAIT_BARRIER(0);
-    float* const sums = (float*)smem;            // [4][3][BM]
-    tile_logprob(p, acc, sums + wave * 3 * BM, BM, 0, m0, n0 + wave * 32, lane);
+    float* const sums = (float*)smem;            // [4 / WM][3][BM]
+    tile_logprob(p, acc, sums + wn * 3 * BM, BM, wm * MU * 16, m0 + wm * MU * 16, n0 + wn * CT * 16, lane);
     __syncthreads();
-    tile_logprob_join<4, BM>(p, sums, tn, m0, (int)threadIdx.x);
+    tile_logprob_join<4 / WM, BM>(p, sums, tn, m0, (int)threadIdx.x);
 }
 
-template <int MU>
+template <int MU, int CT, int WM>
 static void launch_head_f32(GemmParams p, hipStream_t s) {
-    constexpr int SMEM = HeadF32<MU>::D * HeadF32<MU>::UNIT;
+    typedef HeadF32<MU, CT, WM> L;
+    constexpr int SMEM = L::D * L::UNIT;
     static OncePerDevice once;
-    once.run(current_device(), [] { allow_dynamic_lds((const void*)(head_logprob_f32_kernel<MU>), SMEM); });
-    p.mt = (p.M + 16 * MU - 1) / (16 * MU);
-    hipLaunchKernelGGL(head_logprob_f32_kernel<MU>, dim3((unsigned)((p.mt * p.nt + 7) / 8 * 8)), dim3(256), SMEM, s, p);
+    once.run(current_device(), [] { allow_dynamic_lds((const void*)(head_logprob_f32_kernel<MU, CT, WM>), SMEM); });
+    p.mt = (p.M + L::BM - 1) / L::BM;
+    p.nt = (p.N + L::BN - 1) / L::BN;
+    p.ldr = (int64_t)p.nt * p.M;
+    hipLaunchKernelGGL((head_logprob_f32_kernel<MU, CT, WM>), dim3((unsigned)((p.mt * p.nt + 7) / 8 * 8)), dim3(256), SMEM, s, p);
 }
 
-int head_logprob_f32_blocks(int N) { return (N + 127) / 128; }
+// Which tile, by expected time: a round of 256 tiles, one a compute unit, costs this many us per slice.  Of 128 columns and as few row tiles as
+// there can be (each reads all weights) of as few times 16 rows as these need; of 32 x 32 (0).  K 4096, us with 128 columns / 32 x 32: 1 row V 1000
+// 53 / 32, 64 rows V 8000 141 / 51, 1000 rows V 1000 147 / 100; 40 rows V 32000 124 / 186, 1000 rows V 4000 280 / 349, 130 rows V 128256 1187
+// and 1723 by way of logits in memory.
+static int head_f32_units(int64_t M, int N) {
+    constexpr double us[5] = {0.175, 0.37, 0.58, 0.82, 1.05};
+    const int64_t tiles = (M + 63) / 64;
+    const int units = (int)(((M + tiles - 1) / tiles + 15) / 16);
+    auto rounds = [](int64_t m, int64_t n) { return (double)((m * n + 255) / 256); };
+    return rounds((M + 31) / 32, ((int64_t)N + 31) / 32) * us[0] < rounds(tiles, ((int64_t)N + 127) / 128) * us[units] ? 0 : units;
+}
+
+int head_logprob_f32_blocks(int64_t M, int N) { return head_f32_units(M, N) == 0 ? (N + 31) / 32 : (N + 127) / 128; }
 
 void launch_head_logprob_f32(const float* A, const float* W, float* stats, const int32_t* tok, float* at, int64_t M, int N, int K, hipStream_t s) {
     GemmParams p;
     memset(&p, 0, sizeof(p));
     p.A = (const bf16_t*)A; p.W = (const bf16_t*)W; p.dst = (bf16_t*)stats; p.tok = tok; p.at = at;
     p.M = (int)M; p.N = N; p.K = K;
-    p.nt = head_logprob_f32_blocks(N);
-    p.ldr = (int64_t)p.nt * M;
-    // as few row tiles as there can be (each reads all weights), of as few rows as these need
-    const int tiles = (p.M + 63) / 64, units = ((p.M + tiles - 1) / tiles + 15) / 16;
-    if (units == 1) launch_head_f32<1>(p, s);
-    else if (units == 2) launch_head_f32<2>(p, s);
-    else if (units == 3) launch_head_f32<3>(p, s);
-    else launch_head_f32<4>(p, s);
+    switch (head_f32_units(M, N)) {
+        case 0: launch_head_f32<1, 1, 2>(p, s); break;
+        case 1: launch_head_f32<1, 2, 1>(p, s); break;
+        case 2: launch_head_f32<2, 2, 1>(p, s); break;
+        case 3: launch_head_f32<3, 2, 1>(p, s); break;
+        default: launch_head_f32<4, 2, 1>(p, s); break;
+    }
 }
 
 }  // namespace po

@@ -537,7 +537,7 @@ __global__ void __launch_bounds__(256) head_blocks_kernel(const float* __restric
 
 }  // namespace
 
-static int head_blocks(int dtype, int64_t rows, int V, int d) { return dtype == 0 ? head_logprob_f32_blocks(V) : gemm_logprob_blocks(rows, V, d); }
+static int head_blocks(int dtype, int64_t rows, int V, int d) { return dtype == 0 ? head_logprob_f32_blocks(rows, V) : gemm_logprob_blocks(rows, V, d); }
 
 size_t head_logprobs_scratch(int dtype, int64_t rows, int V, int d) { return (size_t)rows * ((size_t)head_blocks(dtype, rows, V, d) * 12 + 4); }
 

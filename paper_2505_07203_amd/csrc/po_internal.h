@@ -254,7 +254,7 @@ int gemm_logprob_blocks(int64_t M, int N, int K);
 void launch_gemm_logprob(const bf16_t* A, int64_t lda, const bf16_t* W, int64_t ldw, float* stats, const int32_t* tok, float* at, int64_t M, int N,
                          int K, hipStream_t s);
 // ... of float32 rows (K % 4 == 0), pitch K
-int head_logprob_f32_blocks(int N);
+int head_logprob_f32_blocks(int64_t M, int N);
 void launch_head_logprob_f32(const float* A, const float* W, float* stats, const int32_t* tok, float* at, int64_t M, int N, int K, hipStream_t s);
 
 // ---- micro-peaks (measurement only)

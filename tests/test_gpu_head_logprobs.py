@@ -160,3 +160,18 @@ def test_logits_further_apart_than_float32(dtype, rows, V):
     assert bool(((lp.double() + want).abs() <= 2.0 ** -21 * want).all()) and bool(((ent.double() - want).abs() <= 2.0 ** -21 * want).all())
     lp, _ = B.po_op_lm_head_logprobs(x, w, t + 1)
     assert bool((lp < -3e38).all())
+
+
+@pytest.mark.parametrize("rows,V,d", [(1, 40000, 260), (31, 33001, 100), (33, 32129, 64), (48, 33000, 4), (64, 32900, 292), (65, 33000, 96), (700, 6001, 132), (17, 31, 1028)])
+def test_float32_tiles(rows, V, d):
+    """every tile, odd columns and ends of K, rows up to and beyond a tile's"""
+    x, w, t = inputs(rows, V, d, rows + V + d, torch.float32)
+    got = B.po_op_lm_head_logprobs(x, w, t)
+    check(x, w, t, *got)
+    again = B.po_op_lm_head_logprobs(x, w, t)
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+    x2 = x.clone()
+    x2[0], x2[-1, 1] = float("nan"), float("inf")
+    keep = slice(1, rows - 1)
+    other = B.po_op_lm_head_logprobs(x2, w, t)
+    assert torch.equal(other[0][keep], got[0][keep]) and torch.equal(other[1][keep], got[1][keep])
