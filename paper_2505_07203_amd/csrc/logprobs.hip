@@ -241,8 +241,8 @@ __device__ __forceinline__ void largest(unsigned long long* keys, int n, int top
 struct RowShared {
     double red_s[4], red_t[4];
     unsigned long long best[MAX_TOP];
-    float red_m[4];
-    int count, ranks[256];
+    float red_m[4], group_max[256];
+    int chunk_count, count, ranks[256];
 };
 struct RowAnswer {
     const int32_t* tokens;
@@ -253,8 +253,33 @@ struct RowAnswer {
     float* top_logprobs;
 };
 
-// A row's answer, by a workgroup of which 256 threads work, from its pieces' sums and its chunks' largest logits.  What bounds it is the way of its
-// loads, one after another: pieces and chunks; the chunks that hold the answer.  keys: RUNS + 32, only where top > 0.
+// A number that at least `top` of 256 (64) disjoint groups of logits reach, from their largest, as large as 16 bits of it allow; 0: fewer groups have
+// weight.  As an order key's upper half.
+__device__ __forceinline__ uint32_t reached(const float (&largest_of)[256], int top) {
+    uint32_t u[4], t = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = (uint32_t)(order_key(largest_of[i * 64 + (threadIdx.x & 63)], 0) >> 32);
+    const bool few = top <= 32;                  // (then of 64 groups: four in one)
+    if (few) u[0] = max(max(u[0], u[1]), max(u[2], u[3]));
+#pragma unroll
+    for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
+        int n = __popcll(__ballot(u[0] >= (t | bit)));
+        if (!few) {
+#pragma unroll
+            for (int i = 1; i < 4; ++i) n += __popcll(__ballot(u[i] >= (t | bit)));
+        }
+        if (n >= top) t |= bit;
+    }
+    return t;
+}
+// ... as a logit, at least `lowest`.  (Cut to 16 bits it may lie below -infinity, where no logit is.)
+__device__ __forceinline__ float reached_logit(uint32_t t, float lowest) {
+    return t > 0x007fffffu ? fmaxf(key_logit((unsigned long long)t << 32), lowest) : lowest;
+}
+
+// A row's answer, by a workgroup of which 256 threads work, from its pieces' sums and its chunks' largest logits.  What bounds it is a chain: the
+// loads of pieces and chunks' maxima; a floor under the answer from those; the loads of the chunks that reach it, and beside them the sums; the
+// order of the few elements that do.  Only rows with more than LIST of those go through the exact way by keys.  keys: RUNS + 32, only where top > 0.
 template <typename T, bool VEC>
 __device__ __forceinline__ void answer_row(const T* row, int64_t r, int V, int pieces, int chunks, const Stats* st, const float* cm, const RowAnswer& a,
                                            unsigned long long* keys, RowShared& sh) {
@@ -262,6 +287,7 @@ __device__ __forceinline__ void answer_row(const T* row, int64_t r, int V, int p
     float(&red_m)[4] = sh.red_m;
     unsigned long long(&best)[MAX_TOP] = sh.best;
     int &count = sh.count, (&ranks)[256] = sh.ranks;
+    int* const near = (int*)(keys + 2 * LIST);                         // chunks that reach the floor
     const int n_tokens = a.n_tokens, top = a.top, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int tid = threadIdx.x < 256 ? (int)threadIdx.x : 1 << 30;    // (the others only wait)
     // (first turn of each list and the first token: asked for together)
@@ -282,36 +308,96 @@ __device__ __forceinline__ void answer_row(const T* row, int64_t r, int V, int p
     for (int i = tid + 256; i < pieces; i += 256) m = fmaxf(m, st[i].m);
     m = wave_max(m);
     if (lane == 0 && wave < 4) red_m[wave] = m;
+    if (top && wave < 4) {
+        float own = fmaxf(cm0[0], cm0[1]);
+        for (int i = tid + 512; i < chunks; i += 256) own = fmaxf(own, cm[i]);
+        sh.group_max[tid] = own;
+    }
     if (tid < MAX_TOP) best[tid] = 0;
-    if (tid == 0) count = 0;
+    if (tid == 0) sh.chunk_count = count = 0;
     __syncthreads();
     m = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
-    Sums sum = {0.0, 0.0};
-    join(first, m, sum);
-    for (int i = tid + 256; i < pieces; i += 256) join(st[i], m, sum);
-    for (int off = 32; off > 0; off >>= 1) {
-        sum.s += __shfl_xor(sum.s, off);
-        sum.t += __shfl_xor(sum.t, off);
-    }
-    if (lane == 0 && wave < 4) { red_s[wave] = sum.s; red_t[wave] = sum.t; }
     const float lowest = m == INFINITY ? INFINITY : -INFINITY;         // of a logit with weight
-    // the chunks that hold the first tokens, as keys of (largest logit, chunk).  (More than a list holds: in turns, the best so far among them.)
+    float floor_logit = lowest;
+    bool few_groups = false;
     if (top) {
-        for (int c0 = 0; c0 < chunks; c0 += RUNS - MAX_TOP) {
-            const int n = min(chunks - c0, RUNS - MAX_TOP), more = c0 ? MAX_TOP : 0;
-            if (c0) __syncthreads();
-            for (int i = tid; i < n; i += 256) {
-                const float c = c0 || i >= 512 ? cm[c0 + i] : i < 256 ? cm0[0] : cm0[1];
-                keys[i] = c >= lowest ? order_key(c, c0 + i) : 0;
+        const uint32_t t = reached(sh.group_max, top);
+        few_groups = t == 0;
+        floor_logit = reached_logit(t, lowest);
+        for (int i = tid; i < chunks; i += 256) {
+            const float c = i < 256 ? cm0[0] : i < 512 ? cm0[1] : cm[i];
+            if (c >= floor_logit && c > -INFINITY) {
+                const int slot = atomicAdd(&sh.chunk_count, 1);
+                if (slot < LIST) near[slot] = i;
             }
-            if (tid < more) keys[n + tid] = best[tid];
-            __syncthreads();
-            if (tid < more) best[tid] = 0;
-            largest(keys, n + more, top, best, ranks);
         }
+        __syncthreads();
     }
+    const int n_near = sh.chunk_count;
+    // f(logits, index of the first) of every run of 8 of n_chunks chunks, four at a time a thread; between: what is done while the first ones come
+    auto runs = [&](int n_chunks, auto chunk_of, auto between, auto f) {
+        const int n = n_chunks * (CHUNK / 8);
+        bool once = true;
+        for (int i0 = tid; once || i0 < n; i0 += 1024) {
+            float v[4][8];
+            int at[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * 256;
+                at[u] = V;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[u][e] = -INFINITY;
+                if (i < n) {
+                    at[u] = chunk_of(i / (CHUNK / 8)) * CHUNK + (i % (CHUNK / 8)) * 8;
+                    load8<T, VEC>(row, at[u], V, v[u]);
+                }
+            }
+            if (once) between();
+            once = false;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) f(v[u], at[u]);
+        }
+    };
+    auto push = [&](const float (&v)[8], int at) {
+        int n = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) n += v[e] >= floor_logit && v[e] > -INFINITY;
+        if (n) {
+            int slot = atomicAdd(&count, n);                   // (their order in the list changes nothing: the keys are ranked)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (v[e] >= floor_logit && v[e] > -INFINITY) {
+                    if (slot < LIST) keys[slot] = order_key(v[e], at + e);
+                    ++slot;
+                }
+        }
+    };
+    auto nothing = [] {};
+    auto sums = [&] {
+        Sums sum = {0.0, 0.0};
+        join(first, m, sum);
+        for (int i = tid + 256; i < pieces; i += 256) join(st[i], m, sum);
+        for (int off = 32; off > 0; off >>= 1) {
+            sum.s += __shfl_xor(sum.s, off);
+            sum.t += __shfl_xor(sum.t, off);
+        }
+        if (lane == 0 && wave < 4) { red_s[wave] = sum.s; red_t[wave] = sum.t; }
+    };
+    const bool listed = n_near <= LIST;
+    auto near_chunk = [&](int i) { return near[i]; };
+    if (few_groups && listed && n_near == chunks && n_near * CHUNK > LIST) {       // (short rows: a floor from their elements)
+        float own = -INFINITY;
+        runs(n_near, near_chunk, nothing, [&](const float (&v)[8], int) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) own = fmaxf(own, v[e]);
+        });
+        if (wave < 4) sh.group_max[tid] = own;
+        __syncthreads();
+        floor_logit = reached_logit(reached(sh.group_max, top), lowest);
+    }
+    runs(listed ? n_near : 0, near_chunk, sums, push);
     __syncthreads();
-    sum = {red_s[0] + red_s[1] + red_s[2] + red_s[3], red_t[0] + red_t[1] + red_t[2] + red_t[3]};
+    const Sums sum = {red_s[0] + red_s[1] + red_s[2] + red_s[3], red_t[0] + red_t[1] + red_t[2] + red_t[3]};
     const double log_s = log(sum.s);
     if (tid < n_tokens) a.logprobs[r * n_tokens + tid] = logprob_of(given, m, log_s);
     for (int i = tid + 256; i < n_tokens; i += 256) {
@@ -321,73 +407,65 @@ __device__ __forceinline__ void answer_row(const T* row, int64_t r, int V, int p
     if (tid == 0 && a.entropy) a.entropy[r] = m > -INFINITY ? (float)fmax(0.0, log_s - sum.t / sum.s) : 0.f;
     if (top == 0) return;
 
-    const int n_chunks = __popcll(__ballot(lane < top && best[lane] != 0));
-    // (as many elements as tokens are wanted are as large as this)
-    const float floor_logit = n_chunks == top ? key_logit(best[top - 1]) : lowest;
-    // their elements that reach as far: mostly a few more than are wanted
-    const int runs_in = n_chunks * (CHUNK / 8);
-    for (int i0 = tid; i0 < runs_in; i0 += 1024) {
-        float v[4][8];
-        int at[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = i0 + u * 256;
-            at[u] = i < runs_in ? (int)(uint32_t)~best[i / (CHUNK / 8)] * CHUNK + (i % (CHUNK / 8)) * 8 : V;
-            load8<T, VEC>(row, at[u], V, v[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            int n = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) n += v[u][e] >= floor_logit && v[u][e] > -INFINITY;
-            if (n) {
-                int slot = atomicAdd(&count, n);                   // (their order in the list changes nothing: the keys are ranked)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (v[u][e] >= floor_logit && v[u][e] > -INFINITY) {
-                        if (slot < LIST) keys[slot] = order_key(v[u][e], at[u] + e);
-                        ++slot;
-                    }
-            }
-        }
-    }
-    __syncthreads();
     int n = count;
-    if (n > LIST) {
-        // many as large as that: first the runs of 8 that hold the answer, by their first and largest element
-        __syncthreads();
-        if (tid == 0) count = 0;
-        __syncthreads();
-        for (int i = tid; i < runs_in; i += 256) {
-            const int at = (int)(uint32_t)~best[i / (CHUNK / 8)] * CHUNK + (i % (CHUNK / 8)) * 8;
-            float v[8];
-            load8<T, VEC>(row, at, V, v);
-            unsigned long long k = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const unsigned long long ke = v[e] >= floor_logit ? order_key(v[e], at + e) : 0;
-                k = ke > k ? ke : k;
+    if (!listed || n > LIST) {
+        // exactly: the chunks that hold the first tokens, as keys of (largest logit, chunk).  (More than a list holds: in turns, the best so far among
+        // them.)
+        for (int c0 = 0; c0 < chunks; c0 += RUNS - MAX_TOP) {
+            const int in = min(chunks - c0, RUNS - MAX_TOP), more = c0 ? MAX_TOP : 0;
+            __syncthreads();
+            for (int i = tid; i < in; i += 256) {
+                const float c = cm[c0 + i];
+                keys[i] = c >= lowest ? order_key(c, c0 + i) : 0;
             }
-            if (k) keys[atomicAdd(&count, 1)] = k;
+            if (tid < more) keys[in + tid] = best[tid];
+            __syncthreads();
+            if (tid < more) best[tid] = 0;
+            largest(keys, in + more, top, best, ranks);
         }
-        __syncthreads();
-        const int runs = count;
-        if (tid < MAX_TOP) best[tid] = 0;
-        largest(keys, runs, top, best, ranks);
         __syncthreads();
         if (tid == 0) count = 0;
+        const int n_chunks = __popcll(__ballot(lane < top && best[lane] != 0));
+        // (as many elements as tokens are wanted are as large as this)
+        floor_logit = n_chunks == top ? key_logit(best[top - 1]) : lowest;
+        auto best_chunk = [&](int i) { return (int)(uint32_t)~best[i]; };
         __syncthreads();
-        for (int i = tid; i < top * 8; i += 256) {
-            if (!best[i >> 3]) continue;
-            const int at = (int)((uint32_t)~best[i >> 3] & ~7u) + (i & 7);
-            const float l = at < V ? to_f32(row[at]) : -INFINITY;
-            const unsigned long long k = l >= floor_logit ? order_key(l, at) : 0;
-            if (k) keys[atomicAdd(&count, 1)] = k;
-        }
+        runs(n_chunks, best_chunk, nothing, push);
         __syncthreads();
         n = count;
+        if (n > LIST) {
+            // many as large as that: first the runs of 8 that hold the answer, by their first and largest element
+            __syncthreads();
+            if (tid == 0) count = 0;
+            __syncthreads();
+            runs(n_chunks, best_chunk, nothing, [&](const float (&v)[8], int at) {
+                unsigned long long k = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const unsigned long long ke = v[e] >= floor_logit ? order_key(v[e], at + e) : 0;
+                    k = ke > k ? ke : k;
+                }
+                if (k) keys[atomicAdd(&count, 1)] = k;
+            });
+            __syncthreads();
+            const int n_runs = count;
+            if (tid < MAX_TOP) best[tid] = 0;
+            largest(keys, n_runs, top, best, ranks);
+            __syncthreads();
+            if (tid == 0) count = 0;
+            __syncthreads();
+            for (int i = tid; i < top * 8; i += 256) {
+                if (!best[i >> 3]) continue;
+                const int at = (int)((uint32_t)~best[i >> 3] & ~7u) + (i & 7);
+                const float l = at < V ? to_f32(row[at]) : -INFINITY;
+                const unsigned long long k = l >= floor_logit ? order_key(l, at) : 0;
+                if (k) keys[atomicAdd(&count, 1)] = k;
+            }
+            __syncthreads();
+            n = count;
+        }
+        if (tid < MAX_TOP) best[tid] = 0;
     }
-    if (tid < MAX_TOP) best[tid] = 0;
     largest(keys, n, top, best, ranks);
     __syncthreads();
     if (tid < top) {

@@ -230,3 +230,22 @@ def test_refusals():
         B.po_op_token_logprobs(z, tk, top=65)
     with pytest.raises(B.PoError):
         B.po_op_token_logprobs(z, tk, top=3, scratch=torch.empty(B.po_token_logprobs_bytes(4, 300, 3) - 1, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [40, 1500, 20_000, 131_073, 300_001])
+@pytest.mark.parametrize("top", [1, 7, 32, 33, 64])
+def test_where_the_answer_lies(V, top, dtype):
+    """in few chunks or many, among few elements as large or thousands, at the ends of what the type holds"""
+    lowest, inf = torch.finfo(dtype).min, float("inf")
+    i = torch.arange(V, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(V + top)
+    rows = [i / V, -i / V, (i % 2) * 3.0, (i % 511 == 17) * 2.0 - 50, torch.full((V,), lowest, device="cuda"), -1e-3 - (i // 9) * 1e-5,
+            torch.where(i % 3 == 0, 0.0, -0.0), torch.where(i % 5 == 0, 1e-39, -1e-39), torch.where(i < V - 9, -inf, i / V), torch.where(i % 97 == 5, -1e30, -inf)]
+    for n in (top - 1, top, top + 1):
+        few = torch.full((V,), -inf, device="cuda")
+        few[torch.randperm(V, device="cuda", generator=g)[:n]] = torch.randn(min(n, V), device="cuda", generator=g)
+        rows.append(few)
+    rows.append(torch.where(i % 1024 < 600, 5.0, torch.randn(V, device="cuda", generator=g)))
+    z = torch.stack([r.float() for r in rows]).to(dtype)
+    check(z, torch.randint(0, V, (len(rows), 2), dtype=torch.int32, device="cuda", generator=g), top)
