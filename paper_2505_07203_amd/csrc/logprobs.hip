@@ -52,28 +52,53 @@ __device__ __forceinline__ void load8(const T* row, int i, int V, float (&v)[8])
     for (int c = 0; c < 8; ++c) v[c] = i + c < V ? to_f32(row[i + c]) : -INFINITY;
 }
 
-// Over a wavefront, all lanes get it: rotations within rows of 16 lanes on the vector ALU, then the four rows (the same by way of LDS,
-// six exchanges for each of seven reductions a piece, took 11 us of LDS in 256 rows of 152064).
+// Over a wavefront, all lanes get it, on the vector ALU: within rows of 16 lanes, then the four rows (the same by way of LDS, six exchanges for
+// each of seven reductions a piece, took 11 us of LDS in 256 rows of 152064).
 template <int CTRL>
-__device__ __forceinline__ float rotated(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true)); }
-__device__ __forceinline__ float of_row(float v, int row) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), row * 16)); }
-__device__ __forceinline__ float wave_max(float v) {
-    v = fmaxf(v, rotated<0x128>(v));
-    v = fmaxf(v, rotated<0x124>(v));
-    v = fmaxf(v, rotated<0x122>(v));
-    v = fmaxf(v, rotated<0x121>(v));
-    return fmaxf(fmaxf(of_row(v, 0), of_row(v, 1)), fmaxf(of_row(v, 2), of_row(v, 3)));
+__device__ __forceinline__ float moved_lanes(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true)); }
+constexpr int ROR8 = 0x128, HALF_MIRROR = 0x141, QUAD_1032 = 0xb1, QUAD_2301 = 0x4e;       // lane ^ 8; 7 - lane in each 8; lane ^ 1; lane ^ 2
+__device__ __forceinline__ float max_quads(float v) {
+    v = fmaxf(v, moved_lanes<QUAD_1032>(v));
+    return fmaxf(v, moved_lanes<QUAD_2301>(v));
 }
-__device__ __forceinline__ float wave_sum(float v) {
-    v += rotated<0x128>(v);
-    v += rotated<0x124>(v);
-    v += rotated<0x122>(v);
-    v += rotated<0x121>(v);
-    return (of_row(v, 0) + of_row(v, 1)) + (of_row(v, 2) + of_row(v, 3));
+__device__ __forceinline__ float sum_quads(float v) {
+    v += moved_lanes<QUAD_1032>(v);
+    return v + moved_lanes<QUAD_2301>(v);
+}
+template <typename F>
+__device__ __forceinline__ float over_rows(float v, F f) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);       // (a row beside the next one)
+    v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float added(float a, float b) { return a + b; }
+__device__ __forceinline__ float first_lane(float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); }
+__device__ __forceinline__ float wave_max(float v) {
+    v = fmaxf(v, moved_lanes<ROR8>(v));
+    v = fmaxf(v, moved_lanes<HALF_MIRROR>(v));
+    return first_lane(over_rows(max_quads(v), larger));
+}
+// Four maxima together: each exchange halves how many values a lane still holds.  Lane 4 q gets number (q & 1) * 2 + (q >> 1 & 1).
+__device__ __forceinline__ float wave_max4(const float (&v)[4]) {
+    const bool b3 = threadIdx.x & 8, b2 = threadIdx.x & 4;
+    const float p = fmaxf(b3 ? v[1] : v[0], moved_lanes<ROR8>(b3 ? v[0] : v[1])), q = fmaxf(b3 ? v[3] : v[2], moved_lanes<ROR8>(b3 ? v[2] : v[3]));
+    return over_rows(max_quads(fmaxf(b2 ? q : p, moved_lanes<HALF_MIRROR>(b2 ? p : q))), larger);
+}
+// ... and two sums
+__device__ __forceinline__ void wave_sum2(float& s, float& t) {
+    const bool b3 = threadIdx.x & 8;
+    float p = (b3 ? t : s) + moved_lanes<ROR8>(b3 ? s : t);
+    p += moved_lanes<HALF_MIRROR>(p);
+    p = over_rows(sum_quads(p), added);
+    s = first_lane(p);
+    t = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(p), 8));
 }
 
-// S and T of the wavefront's values with maximum m, in powers of 2 (T log2(e)).  -infinity and NaN make T NaN; then once more with
-// every distance held to where a term is 0 in float32 (fmaxf turns NaN into its other operand).
+// S and T of the wavefront's values with maximum m, in powers of 2 (T log2(e)).  A distance is one fma, v log2(e) - c with c = m log2(e) rounded: what
+// that rounding adds to all of them, delta, is taken out of the sums.  -infinity, NaN and a product beyond float32 leave T no finite number; then,
+// and where m is so large that delta is not small, every distance held to where a term is 0 in float32 (fmaxf turns NaN into its other operand).
 __device__ __forceinline__ Stats wave_stats(const float (&x)[PER_WAVE][8], float m) {
     constexpr int N = PER_WAVE * 8;
     const float(&v)[N] = *(const float(*)[N])&x;
@@ -82,16 +107,23 @@ __device__ __forceinline__ Stats wave_stats(const float (&x)[PER_WAVE][8], float
     if (m == INFINITY) {
 #pragma unroll
         for (int i = 0; i < N; ++i) r.s += v[i] == INFINITY ? 1.f : 0.f;
-        r.s = wave_sum(r.s);
+        wave_sum2(r.s, r.t);
     } else if (m > -INFINITY) {
+        bool done = fabsf(m) < 0x1p20f;          // (delta is below 0.1)
+        if (done) {
+            const float c = m * LOG2E, delta = fmaf(m, LOG2E, -c), back = __builtin_amdgcn_exp2f(-delta);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float d = (v[i] - m) * LOG2E, e = __builtin_amdgcn_exp2f(d);
-            r.s += e;
-            r.t = fmaf(d, e, r.t);
+            for (int i = 0; i < N; ++i) {
+                const float d = fmaf(v[i], LOG2E, -c), e = __builtin_amdgcn_exp2f(d);
+                r.s += e;
+                r.t = fmaf(d, e, r.t);
+            }
+            wave_sum2(r.s, r.t);
+            done = fabsf(r.t) < INFINITY;
+            r.t = fmaf(-delta, r.s, r.t) * back;
+            r.s *= back;
         }
-        r.t = wave_sum(r.t);
-        if (!(r.t > -INFINITY)) {
+        if (!done) {
             r.s = r.t = 0.f;
             asm volatile("" : "+v"(m));          // (else the compiler keeps the first pass's 32 distances for this one)
 #pragma unroll
@@ -100,9 +132,8 @@ __device__ __forceinline__ Stats wave_stats(const float (&x)[PER_WAVE][8], float
                 r.s += e;
                 r.t = fmaf(d, e, r.t);
             }
-            r.t = wave_sum(r.t);
+            wave_sum2(r.s, r.t);
         }
-        r.s = wave_sum(r.s);
         r.t *= LN2;
     }
     return r;
@@ -138,12 +169,11 @@ __device__ __forceinline__ Stats piece_stats(const float (&v)[PER_WAVE][8], int 
     }
     float m = -INFINITY;
     if (chunk_max) {
-#pragma unroll
-        for (int c = 0; c < PER_WAVE; ++c) {
-            cm[c] = wave_max(cm[c]);
-            m = fmaxf(m, cm[c]);
-            if ((threadIdx.x & 63) == 0 && p * PER_WAVE + c < chunks) chunk_max[p * PER_WAVE + c] = cm[c];
-        }
+        const float one = wave_max4(cm);
+        const int lane = threadIdx.x & 63, c = (lane >> 2 & 1) * 2 + (lane >> 3 & 1);
+        if (lane < 16 && (lane & 3) == 0 && p * PER_WAVE + c < chunks) chunk_max[p * PER_WAVE + c] = one;
+        m = fmaxf(one, moved_lanes<ROR8>(one));
+        m = first_lane(fmaxf(m, moved_lanes<HALF_MIRROR>(m)));
     } else {
 #pragma unroll
         for (int c = 0; c < PER_WAVE; ++c) m = fmaxf(m, cm[c]);

@@ -249,3 +249,11 @@ def test_where_the_answer_lies(V, top, dtype):
     rows.append(torch.where(i % 1024 < 600, 5.0, torch.randn(V, device="cuda", generator=g)))
     z = torch.stack([r.float() for r in rows]).to(dtype)
     check(z, torch.randint(0, V, (len(rows), 2), dtype=torch.int32, device="cuda", generator=g), top)
+
+
+@pytest.mark.parametrize("at", [0.0, 37.7, -911.3, 65_000.3, 1.04e6, -1.05e6, 3e7, -7e30])
+def test_far_from_zero(at):
+    """logits around a large one: distances are exact differences of float32 numbers whatever their size"""
+    g = torch.Generator(device="cuda").manual_seed(7)
+    z = at + torch.randn(5, 9000, device="cuda", generator=g) * max(3.0, abs(at) * 2.0 ** -22)
+    check(z, torch.randint(0, 9000, (5, 3), dtype=torch.int32, device="cuda", generator=g), 9)
