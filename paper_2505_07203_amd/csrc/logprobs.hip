@@ -8,9 +8,9 @@
 // ascending).  They lie in the chunks whose largest logits come first in that order, as many chunks as tokens: an element of any
 // other chunk has the largest elements of all of those before it.  The same holds for the runs of 8 within those chunks, so
 // at most 8 elements a token are ordered in the end, whatever the row holds, and no more than `top` chunks are read again.
-// What bounds it: many rows, reading them (1024 float32 rows of 128256: pieces 93 us, 5.7 TB/s; 256 of 152064 in bf16 18.5, 4.2: five
-// operations and an exponential a logit), then the answers, 11 to 18 us a launch whatever the rows, a chain of loads, exchanges and rankings;
-// one row, that chain (4.9 + 11.4 us).
+// What bounds it: many rows, reading them (1024 float32 rows of 128256 in one launch 97 us, 5.4 TB/s; pieces of 256 bf16 rows of 152064 17, 4.6: four
+// operations and an exponential a logit), then the answers, 7.4 us for 256 rows' five tokens and 23 for 64, a chain of loads, exchanges and
+// rankings; one row, that chain (4.7 + 8.8 us for twenty tokens).
 // NaN counts as -infinity; -infinity has no weight; with +infinity among the logits only those have, the same each.
 #include "po_internal.h"
 
@@ -514,12 +514,16 @@ __global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__
     answer_row<T, VEC>(logits + r * ld, r, V, pieces, chunks, stats + r * pieces, chunk_max + r * chunks, a, keys, sh);
 }
 
-// Many long rows: pieces and answer of a row by one workgroup, sums and largest logits in LDS, one launch, so that the next row's logits are read
-// while one is answered.  The same arithmetic in the same order as by the two kernels.  Float32 rows of 128256, five alternatives, us
-// against the two kernels: 256 rows 31 / 31, 1024 103 / 106, 2048 186 / 207; 1024 rows of 2048 logits 33 / 26 (half of the wavefronts only wait
-// during the answer).
+// Pieces and answer of a row by one workgroup, sums and largest logits in LDS, one launch; the same arithmetic in the same order as by the two
+// kernels.  For rows of up to 2^16 logits that all run at once, two a compute unit: a launch less; and for so many long rows of float32 that the next
+// row's logits are read while one is answered.  Five alternatives, us against the two kernels: 512 rows of 1000 12.2 / 15.8, of 65536
+// (bf16) 21.5 / 20.7, 700 rows of 1000 19.5 / 15.6 (half of the wavefronts only wait during the answer), 64 of 128256 20.2 / 15.8; float32 rows of
+// 128256: 512 54 / 54, 768 75.7 / 77.6, 2048 181 / 198; of 65536: 1024 55.5 / 53.8, 1536 76 / 83; 2048 bf16 rows of 152064 128 / 125.
 constexpr int WHOLE_WAVES = 8, WHOLE_CHUNKS = 1024;            // (rows of up to 2^19 logits)
-inline bool whole_rows(int64_t rows, int pieces, int chunks) { return rows >= 768 && pieces >= 32 && chunks <= WHOLE_CHUNKS; }
+template <typename T>
+inline bool whole_rows(int64_t rows, int pieces, int chunks) {
+    return (pieces <= 32 && rows <= 512) || (sizeof(T) == 4 && pieces >= 32 && rows * pieces >= 48000 && chunks <= WHOLE_CHUNKS);
+}
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(64 * WHOLE_WAVES, 4) logprob_whole_kernel(const T* __restrict__ logits, int64_t ld, int V, int pieces, int chunks, const RowAnswer a) {
     extern __shared__ unsigned long long keys[];
@@ -550,7 +554,7 @@ inline int chunks_of(int V) { return (V + CHUNK - 1) / CHUNK; }
 template <typename T, bool VEC>
 void run(const T* logits, int64_t ld, int64_t rows, int V, const RowAnswer& a, void* scratch, hipStream_t s) {
     const int pieces = pieces_of(V), chunks = chunks_of(V), lds = a.top ? (RUNS + 32) * 8 : 0;
-    if (whole_rows(rows, pieces, chunks)) {
+    if (whole_rows<T>(rows, pieces, chunks)) {
         hipLaunchKernelGGL((logprob_whole_kernel<T, VEC>), dim3((unsigned)rows), dim3(64 * WHOLE_WAVES), lds, s, logits, ld, V, pieces, chunks, a);
         return;
     }
