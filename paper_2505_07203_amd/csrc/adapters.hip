@@ -114,9 +114,8 @@ __device__ __forceinline__ void keep(Frag<float>& f, int n) {
 // groups of rows in LDS, a load covering whole lines of two rows (four); 16-byte segments are XOR-swizzled with the row on the global side, so
 // that a fragment's 16 rows meet 16 different banks.  The wavefronts' sums meet in LDS.  A lane of a product of 16 ranks and 16 rows holds row
 // lane & 15 and ranks 4 (lane >> 4) .. + 3.
-// What bounds it: x from memory.  16584 rows of K 14336, rank 64, 120 us (4.0 TB/s), of which the loads alone, with nothing done between them, take
-// 104 to 114; the fragments straight from memory to registers, 64 bytes of a line each, 161 where this took 149 (runs of rows of another
-// length).  7394 rows of K 4096 in 41 requests 26: one round of workgroups, each of which waits for A first.  64 single tokens 7.4.
+// What bounds it: x from memory.  16584 rows of K 14336, rank 64, 99 us (4.8 TB/s; 120 where x passes through the caches, ONCE false); the
+// fragments straight from memory to registers, 64 bytes of a line each, 161 where this took 149 (runs of rows of another length).  7394 rows of K 4096 in 41 requests 26: one round of workgroups, each of which waits for A first.  64 single tokens 7.4.
 // (LDS is read as vectors of bf16 or float: as uint4 the compiler, which cannot tell them from what the loads write, waits for all loads.)
 constexpr int DOWN_WAVES = 8;
 template <typename T, int NR> struct Down {
@@ -128,7 +127,7 @@ template <typename T, int NR> struct Down {
     static_assert(DOWN_WAVES * WAVE <= 160 * 1024, "LDS of a compute unit");
 };
 
-template <typename T, int NR>
+template <typename T, int NR, bool ONCE>
 __global__ void __launch_bounds__(64 * DOWN_WAVES, 2) adapter_down_kernel(const AdapterParams p, const Table tab) {
     typedef Down<T, NR> L;
     constexpr int C = L::C, D = L::D, ROWB = L::ROWB, SEGS = ROWB / 16, RPL = 1024 / ROWB;
@@ -163,7 +162,7 @@ __global__ void __launch_bounds__(64 * DOWN_WAVES, 2) adapter_down_kernel(const 
             (void*)(xbase + (int64_t)(bytes_ ? at_ : g0) * 16 * pitch), 0, (int)bytes_, 0x00020000);                   \
         _Pragma("unroll") for (int i = 0; i < L::NL; ++i)                                                              \
             __builtin_amdgcn_raw_ptr_buffer_load_lds(                                                                  \
-                rs_, (__attribute__((address_space(3))) void*)(ring + (pos_) * L::GROUP + i * 1024), 16, vo[i], 0, 0, 0); \
+                rs_, (__attribute__((address_space(3))) void*)(ring + (pos_) * L::GROUP + i * 1024), 16, vo[i], 0, 0, ONCE ? LOAD_ONCE : 0); \
     }
 #pragma unroll
     for (int d = 0; d < D; ++d) PO_FETCH(g0 + d, d)
@@ -590,15 +589,22 @@ void for_launches(const int32_t* ranks, const float* scales, bool in_place, int 
     flush();
 }
 
+template <typename T, int NR, bool ONCE>
+void run_down(const AdapterParams& p, const Launch& l, hipStream_t s) {
+    constexpr int WAVE = Down<T, NR>::WAVE;
+    static OncePerDevice once;
+    once.run(current_device(), [] { allow_dynamic_lds((const void*)(adapter_down_kernel<T, NR, ONCE>), DOWN_WAVES * WAVE); });
+    const int waves = std::min(DOWN_WAVES, k_slices(NR, sizeof(T), p.K));
+    hipLaunchKernelGGL((adapter_down_kernel<T, NR, ONCE>), dim3((unsigned)l.tab.down0[l.tab.n], (unsigned)p.pieces), dim3(64 * waves), waves * WAVE, s, p, l.tab);
+}
+
 template <typename T, int NR>
 void run_t(const AdapterParams& p, const Launch& l, hipStream_t s) {
     constexpr int KS = ks_of(NR), H = UpCols<T, KS>::H;
     if (l.rank) {
-        constexpr int WAVE = Down<T, NR>::WAVE;
-        static OncePerDevice once;
-        once.run(current_device(), [] { allow_dynamic_lds((const void*)(adapter_down_kernel<T, NR>), DOWN_WAVES * WAVE); });
-        const int waves = std::min(DOWN_WAVES, k_slices(NR, sizeof(T), p.K));
-        hipLaunchKernelGGL((adapter_down_kernel<T, NR>), dim3((unsigned)l.tab.down0[l.tab.n], (unsigned)p.pieces), dim3(64 * waves), waves * WAVE, s, p, l.tab);
+        // (x past the caches / not, K 14336, N 4096, rank 64, the whole call: 2000 rows 42 / 41 us, 8000 86 / 104, 16000 157 / 178)
+        if ((int64_t)l.total * 16 * ((int64_t)p.K + 2 * p.N) * (int64_t)sizeof(T) >= READ_ONCE_BYTES) run_down<T, NR, true>(p, l, s);
+        else run_down<T, NR, false>(p, l, s);
     }
     if (l.few) {
         hipLaunchKernelGGL((adapter_up_few_kernel<T, KS>), dim3((unsigned)l.tab.n * (unsigned)((p.N + 255) / 256)), dim3(256), 0, s, p, l.tab);

@@ -792,7 +792,7 @@ bool launch_gemm_f32_qkv_rope(const float* A, int64_t lda, const float* W, int64
 // Logits as by the GEMM above, bit for bit (elements 8 g .. 8 g + 7 of a slice of 32 in lane group g, one per MFMA), of which a block of columns
 // leaves (m, S, T) of each row (tile_logprob).  Four wavefronts, WM x 4 / WM, a patch of 16 MU rows x 16 CT columns each; K in slices of 32 through a
 // ring of D positions, one barrier a slice: it hands over slice s + 1, whose fragments are read while slice s is multiplied, and frees the place of
-// slice s for s + D.  Two workgroups a compute unit.  What bounds it: up to 32 rows the weights from memory (one row of 128256 x 4096 375 us, 5.6
+// slice s for s + D.  Two workgroups a compute unit.  What bounds it: up to 32 rows the weights from memory (one row of 128256 x 4096 333 us, 6.3
 // TB/s), beyond them the matrix pipe (1000 rows 7860 us, 134 TFLOP/s).
 using namespace gemm;
 
@@ -805,7 +805,7 @@ template <int MU, int CT, int WM> struct HeadF32 {
 };
 constexpr int HEAD_GROUP = 8;                    // row tiles that one XCD takes beside each other, with the same weights
 
-template <int MU, int CT, int WM>
+template <int MU, int CT, int WM, bool ONCE>
 __global__ void __launch_bounds__(256, 2) head_logprob_f32_kernel(const GemmParams p) {
     typedef HeadF32<MU, CT, WM> L;
     constexpr int D = L::D, NA = L::NA, NW = L::NW, BM = L::BM, BN = L::BN;
@@ -842,7 +842,7 @@ __global__ void __launch_bounds__(256, 2) head_logprob_f32_kernel(const GemmPara
                                                      vo[i] + ((past_ >> i & 1) << 31), wa_.offset, 0, 0);                                   \
         _Pragma("unroll") for (int i = 0; i < NW; ++i)                                                                                      \
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rw_, (__attribute__((address_space(3))) void*)(u_ + L::AU + (wave * NW + i) * 1024), 16, \
-                                                     vo[NA + i] + ((past_ >> (NA + i) & 1) << 31), ww_.offset, 0, 0);                       \
+                                                     vo[NA + i] + ((past_ >> (NA + i) & 1) << 31), ww_.offset, 0, ONCE ? LOAD_ONCE : 0);    \
     }
     int fo[2];
 #pragma unroll
@@ -896,16 +896,22 @@ __global__ void __launch_bounds__(256, 2) head_logprob_f32_kernel(const GemmPara
     tile_logprob_join<4 / WM, BM>(p, sums, tn, m0, (int)threadIdx.x);
 }
 
-template <int MU, int CT, int WM>
-static void launch_head_f32(GemmParams p, hipStream_t s) {
+template <int MU, int CT, int WM, bool ONCE>
+static void launch_head_f32_t(GemmParams p, hipStream_t s) {
     typedef HeadF32<MU, CT, WM> L;
     constexpr int SMEM = L::D * L::UNIT;
     static OncePerDevice once;
-    once.run(current_device(), [] { allow_dynamic_lds((const void*)(head_logprob_f32_kernel<MU, CT, WM>), SMEM); });
+    once.run(current_device(), [] { allow_dynamic_lds((const void*)(head_logprob_f32_kernel<MU, CT, WM, ONCE>), SMEM); });
     p.mt = (p.M + L::BM - 1) / L::BM;
     p.nt = (p.N + L::BN - 1) / L::BN;
     p.ldr = (int64_t)p.nt * p.M;
-    hipLaunchKernelGGL((head_logprob_f32_kernel<MU, CT, WM>), dim3((unsigned)((p.mt * p.nt + 7) / 8 * 8)), dim3(256), SMEM, s, p);
+    hipLaunchKernelGGL((head_logprob_f32_kernel<MU, CT, WM, ONCE>), dim3((unsigned)((p.mt * p.nt + 7) / 8 * 8)), dim3(256), SMEM, s, p);
+}
+template <int MU, int CT, int WM>
+static void launch_head_f32(const GemmParams& p, hipStream_t s) {
+    // (past the caches / not, K 4096, us: 1 row of N 16000 52 / 49, 128000 333 / 373, 64 rows of it 567 / 574)
+    if (p.M <= HeadF32<MU, CT, WM>::BM && (int64_t)p.N * p.K * 4 >= READ_ONCE_BYTES) launch_head_f32_t<MU, CT, WM, true>(p, s);
+    else launch_head_f32_t<MU, CT, WM, false>(p, s);
 }
 
 // Which tile, by expected time: a round of 256 tiles, one a compute unit, costs this many us per slice.  Of 128 columns and as few row tiles as

@@ -64,6 +64,8 @@ constexpr int UNIT_BYTES = BM * BK * 2;            // one operand's slice: 256 r
 constexpr int NUNIT = 5;                           // ring of five units: the whole 160 KiB of LDS
 constexpr int SMEM_BYTES = NUNIT * UNIT_BYTES;
 constexpr int NT_BF16 = 512;                       // eight wavefronts
+constexpr bool is_logprob(int epi) { return epi == EPI_LOGPROB || epi == EPI_LOGPROB_ONCE; }
+constexpr int w_policy(int epi) { return epi == EPI_LOGPROB_ONCE ? LOAD_ONCE : 0; }      // of the weights' loads
 
 // MU = 16-row groups per wavefront patch: 8 (the form described above) or 6 (192-row block tile, phases of 12 MFMAs, the A
 // unit three quarters full): the bits are the same, and 3/4 of a tile's time in 3/4 of its rows lets a launch whose 256-row
@@ -113,9 +115,9 @@ __global__ void __launch_bounds__(NT_BF16) gemm_bf16_mfma_kernel(const GemmParam
 #define PO_DMA(is_w_, slice_, pos_, i_)                                                                              \
     {                                                                                                                  \
         unsigned char* d_ = smem + (pos_) * UNIT_BYTES + (wave * ((is_w_) ? 4 : NA) + (i_)) * 1024;                    \
-        __builtin_amdgcn_raw_ptr_buffer_load_lds((is_w_) ? rw : ra, (__attribute__((address_space(3))) void*)d_, 16,   \
-                                                 (is_w_) ? vow[(i_)] : voa[(i_)],                    \
-                                                 min((slice_), KT - 1) * (BK * 2), 0, 0);                              \
+        const int so_ = min((slice_), KT - 1) * (BK * 2);                                                              \
+        if (is_w_) __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (__attribute__((address_space(3))) void*)d_, 16, vow[(i_)], so_, 0, w_policy(EPI)); \
+        else __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (__attribute__((address_space(3))) void*)d_, 16, voa[(i_)], so_, 0, 0); \
     }
     int f_off[2];
 #pragma unroll
@@ -188,7 +190,7 @@ __global__ void __launch_bounds__(NT_BF16) gemm_bf16_mfma_kernel(const GemmParam
 #undef PO_DMA
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
-    if (EPI == EPI_LOGPROB) {
+    if (is_logprob(EPI)) {
         float* const sums = (float*)smem;                  // [4][3][BM_]
         tile_logprob(p, acc, sums + wn * 3 * BM_, BM_, wm * (MU * 16), m0 + wm * (MU * 16), n0 + wn * 64, lane);
         __syncthreads();
@@ -284,7 +286,7 @@ __global__ void __launch_bounds__(256, 2) gemm_bf16_small_kernel(const GemmParam
 #define PO_DMA_W(pos_, i_)                                                                                               \
     __builtin_amdgcn_raw_ptr_buffer_load_lds(                                                                            \
         rw, (__attribute__((address_space(3))) void*)(smem + (D + 1) * AU + (pos_) * WU + (wave * NW + (i_)) * 1024), 16,  \
-        vow[(i_)], so, 0, 0);
+        vow[(i_)], so, 0, w_policy(EPI));
     int f_off[2];
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) f_off[ks] = l15 * 128 + (((ks * 4 + l4) ^ ((l15 >> 1) & 7)) << 4);
@@ -372,7 +374,7 @@ __global__ void __launch_bounds__(256, 2) gemm_bf16_small_kernel(const GemmParam
 #undef PO_DMA_W
 #undef PO_SLICE_RSRC
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (EPI == EPI_LOGPROB) {
+    if (is_logprob(EPI)) {
         float* const sums = (float*)smem;                  // [2][3][BM_]
         tile_logprob(p, acc, sums + wn * 3 * BM_, BM_, wm * (MU * 16), m0 + wm * (MU * 16), n0 + wn * 64, lane);
         __syncthreads();
@@ -719,8 +721,8 @@ void launch_strips(const GemmParams& p, hipStream_t s) {
 
 template <int EPI>
 void launch_form(int form, const GemmParams& p, hipStream_t s, int splits = 1) {
-    if (EPI != EPI_PARTIAL && EPI != EPI_LOGPROB && form == STRIPS) {
-        constexpr int E = EPI == EPI_PARTIAL || EPI == EPI_LOGPROB ? EPI_STORE : EPI;
+    if (EPI != EPI_PARTIAL && !is_logprob(EPI) && form == STRIPS) {
+        constexpr int E = EPI == EPI_PARTIAL || is_logprob(EPI) ? EPI_STORE : EPI;
         if (p.M <= 2) launch_strips<E, 1>(p, s);
         else launch_strips<E, 8>(p, s);
         return;
@@ -800,7 +802,11 @@ void launch_gemm_logprob(const bf16_t* A, int64_t lda, const bf16_t* W, int64_t 
     p.ldr = gemm_logprob_blocks(M, N, K) * M;
     p.tok = tok;
     p.at = at;
-    launch_form<EPI_LOGPROB>(pick_form(TILES, p, 1), p, s);
+    // one row tile reads each weight once (past the caches / not, d 4096, us: 1 row of V 16000 33 / 25, of 32000 alone 57 / 46, in turn with
+    // another head 57 / 63, of 128000 157 / 174; 64 rows of it 168 / 185)
+    const int form = pick_form(TILES, p, 1);
+    if (M <= FORMS[form].bm && (int64_t)N * ldw * 2 >= READ_ONCE_BYTES) launch_form<EPI_LOGPROB_ONCE>(form, p, s);
+    else launch_form<EPI_LOGPROB>(form, p, s);
 }
 
 namespace gemm {

@@ -5,8 +5,8 @@
 // amax = max |y| over a row or over each block of 128 of it.  y is a float32 number throughout: it is rounded once, to the code (and once to bf16
 // where the rows are wanted too), not to bf16 first and then to the code.
 //
-// Bound by memory; a row is read once and stays in the registers of its workgroup.  16384 x 4096 in blocks 85 us (5.5 TB/s read and written;
-// addition, norm and quantisation in three calls 161), 16384 x 8192 177 (5.3), 1931 x 5120 in blocks with the bf16 rows 17 (5.2: one round of
+// Bound by memory; a row is read once and stays in the registers of its workgroup.  16384 x 4096 in blocks 78 us (6.0 TB/s read and written;
+// addition, norm and quantisation in three calls 161), 1931 x 5120 in blocks with the bf16 rows 17 (5.2: one round of
 // workgroups, which read together and write together), one row of 4096 3.7, a launch and two exchanges.
 #include "po_internal.h"
 
@@ -28,6 +28,11 @@ struct NormQuant {
     float eps, inv_d;
 };
 
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+template <bool ONCE>
+__device__ __forceinline__ uint4 load16(const uint4* p) {
+    return ONCE ? __builtin_bit_cast(uint4, __builtin_nontemporal_load((const u32x4*)p)) : *p;
+}
 __device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -79,7 +84,8 @@ __device__ __forceinline__ uint2 encode8(const float (&h)[8], const float (&g)[8
 }
 
 // A workgroup per row, whose values stay in registers: QV vectors of 8 a thread.  BLOCK: a scale per 128 values, which 16 lanes hold.
-template <int QV, bool BLOCK>
+// ONCE: x and delta go past the caches.
+template <int QV, bool BLOCK, bool ONCE>
 __global__ void __launch_bounds__(256) norm_quant_kernel(const NormQuant p) {
     __shared__ float part[4], partm[4], party[4];
     const int64_t row = blockIdx.x, at = row * p.vecs;
@@ -91,10 +97,10 @@ __global__ void __launch_bounds__(256) norm_quant_kernel(const NormQuant p) {
         const int i = threadIdx.x + j * 256;
         if (i < p.vecs) {
             gv[j] = p.g[i];
-            unpack8(p.x[at + i], h[j]);
+            unpack8(load16<ONCE>(p.x + at + i), h[j]);
             if (p.delta) {
                 float a[8];
-                unpack8(p.delta[at + i], a);
+                unpack8(load16<ONCE>(p.delta + at + i), a);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) a[e] += h[j][e];
                 const uint4 v = pack8(a);
@@ -159,14 +165,14 @@ __global__ void __launch_bounds__(256) norm_quant_kernel(const NormQuant p) {
     }
 }
 
-template <bool BLOCK>
+template <bool BLOCK, bool ONCE>
 void run(const NormQuant& p, hipStream_t s) {
     const dim3 grid((unsigned)p.rows), wg(256);
-    if (p.vecs <= 256) hipLaunchKernelGGL((norm_quant_kernel<1, BLOCK>), grid, wg, 0, s, p);
-    else if (p.vecs <= 512) hipLaunchKernelGGL((norm_quant_kernel<2, BLOCK>), grid, wg, 0, s, p);
-    else if (p.vecs <= 768) hipLaunchKernelGGL((norm_quant_kernel<3, BLOCK>), grid, wg, 0, s, p);
-    else if (p.vecs <= 1024) hipLaunchKernelGGL((norm_quant_kernel<4, BLOCK>), grid, wg, 0, s, p);
-    else hipLaunchKernelGGL((norm_quant_kernel<8, BLOCK>), grid, wg, 0, s, p);
+    if (p.vecs <= 256) hipLaunchKernelGGL((norm_quant_kernel<1, BLOCK, ONCE>), grid, wg, 0, s, p);
+    else if (p.vecs <= 512) hipLaunchKernelGGL((norm_quant_kernel<2, BLOCK, ONCE>), grid, wg, 0, s, p);
+    else if (p.vecs <= 768) hipLaunchKernelGGL((norm_quant_kernel<3, BLOCK, ONCE>), grid, wg, 0, s, p);
+    else if (p.vecs <= 1024) hipLaunchKernelGGL((norm_quant_kernel<4, BLOCK, ONCE>), grid, wg, 0, s, p);
+    else hipLaunchKernelGGL((norm_quant_kernel<8, BLOCK, ONCE>), grid, wg, 0, s, p);
 }
 
 }  // namespace
@@ -175,8 +181,10 @@ void launch_add_rmsnorm_quantize(const bf16_t* x, const bf16_t* delta, const bf1
                                  int64_t rows, int d, bool blocks, float eps, hipStream_t s) {
     const NormQuant p = {(const uint4*)x, (const uint4*)delta, (const uint4*)g, (uint4*)h, (uint4*)y, (uint2*)codes, scales, rows, d / 8, eps,
                          1.0f / (float)d};
-    if (blocks) run<true>(p, s);
-    else run<false>(p, s);
+    // (x and delta past the caches / not, rows of 4096 in blocks: 8192 43.6 / 42.4 us, 12288 61 / 67, 16384 78 / 87)
+    const bool once = rows * d * (2 + (delta ? 2 : 0) + (h ? 2 : 0) + (y ? 2 : 0) + (codes ? 1 : 0)) >= READ_ONCE_BYTES;
+    if (blocks) { if (once) run<true, true>(p, s); else run<true, false>(p, s); }
+    else { if (once) run<false, true>(p, s); else run<false, false>(p, s); }
 }
 
 }  // namespace po

@@ -37,6 +37,10 @@ static inline int current_device() {
 // HIP takes fewer than 2^32 threads in a launch's first dimension: so many workgroups of 256
 constexpr int64_t MAX_WORKGROUPS_256 = ((int64_t)1 << 24) - 1;
 
+// Calls that move at least so many bytes (the memory-side cache) read what they read once past the caches: what is written or read beside it stays
+// there.
+constexpr int64_t READ_ONCE_BYTES = (int64_t)256 << 20;
+
 static inline int64_t round_up64(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 // ---- launchers: "basic" kernels, any dtype (dtype: 0 = fp32, 1 = bf16) ----------------
@@ -69,7 +73,7 @@ void launch_pack_gate_up(int dtype, const void* wg, const void* wu, void* wgu, i
                          hipStream_t s);
 
 // ---- launchers: bf16 MFMA kernels ------------------------------------------------------
-enum { EPI_STORE = 0, EPI_RESIDUAL = 1, EPI_SILU_MUL = 2, EPI_QKV_ROPE = 3, EPI_PARTIAL = 4, EPI_LOGPROB = 5 };
+enum { EPI_STORE = 0, EPI_RESIDUAL = 1, EPI_SILU_MUL = 2, EPI_QKV_ROPE = 3, EPI_PARTIAL = 4, EPI_LOGPROB = 5, EPI_LOGPROB_ONCE = 6 };
 // C[M,N] = A[M,K] W[N,K]^T with bf16 MFMA, fp32 accumulation.
 //   EPI_STORE    : C = acc (+ bias[N], bf16)
 //   EPI_RESIDUAL : C = acc + R  (added in fp32; R may alias C)

@@ -19,6 +19,9 @@ constexpr SliceWindow slice_window(int s, int n_slices, unsigned tile_bytes, int
 
 }  // namespace po
 
+// cache policy of a buffer load whose line nobody reads again: first to leave the caches
+constexpr int LOAD_ONCE = 2;
+
 // all but the n_ youngest global->LDS loads and every LDS read done, then the workgroup barrier (n_ a constant
 // expression of template parameters, which the host pass would not take as an asm operand)
 #ifdef __HIP_DEVICE_COMPILE__
