@@ -1,4 +1,4 @@
-// Float32-path kernels on the float32 matrix instruction (gfx950): causal GQA attention and the GEMM.
+// Float32-path kernels on the float32 matrix instruction (gfx950): causal GQA attention, the GEMM, and log-probabilities behind the LM head.
 // Operands, products and sums are float32 throughout (32x32x2 and 16x16x4 MFMAs); nothing is rounded to a narrower
 // type.  The float32 path is the one that is held to 1e-4 against the float64 definition and that stands in for it
 // at configurations no CPU run reaches, so what matters here is that every output is one float32 dot product in a

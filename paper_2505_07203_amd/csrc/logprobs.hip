@@ -3,11 +3,12 @@
 //   m = max_i l_i,  S = sum_i exp(l_i - m),  T = sum_i (l_i - m) exp(l_i - m)
 //   log p(t) = (l_t - m) - log S,   entropy = log S - T / S
 //
-// A row is read once, in pieces by a wavefront each: (m, S, T) of a piece, and the largest logit of each of its chunks of 512.
-// A second kernel, a workgroup per row, joins the pieces and finds the first tokens of the order (logit descending, index
-// ascending).  They lie in the chunks whose largest logits come first in that order, as many chunks as tokens: an element of any
-// other chunk has the largest elements of all of those before it.  The same holds for the runs of 8 within those chunks, so
-// at most 8 elements a token are ordered in the end, whatever the row holds, and no more than `top` chunks are read again.
+// A row is read once, in pieces by a wavefront each: (m, S, T) of a piece, and the largest logit of each of its chunks of 512.  Then a workgroup per
+// row joins the pieces and finds the first tokens of the order (logit descending, index ascending): a number that at least as many
+// disjoint groups of logits reach as tokens are wanted is a floor under them, and the chunks that reach it are read again for the few elements that
+// do.  Where those are more than a list holds: the tokens lie in the chunks whose largest logits come first in that order, as many chunks as
+// tokens (an element of any other chunk has the largest elements of all of those before it), and the same holds for the runs of 8
+// within those chunks, so that at most 8 elements a token are ordered in the end, whatever the row holds.
 // What bounds it: many rows, reading them (1024 float32 rows of 128256 in one launch 97 us, 5.4 TB/s; pieces of 256 bf16 rows of 152064 17, 4.6: four
 // operations and an exponential a logit), then the answers, 7.4 us for 256 rows' five tokens and 23 for 64, a chain of loads, exchanges and
 // rankings; one row, that chain (4.7 + 8.8 us for twenty tokens).
