@@ -10,8 +10,8 @@
 // tokens (an element of any other chunk has the largest elements of all of those before it), and the same holds for the runs of 8
 // within those chunks, so that at most 8 elements a token are ordered in the end, whatever the row holds.
 // What bounds it: many rows, reading them (1024 float32 rows of 128256 in one launch 97 us, 5.4 TB/s; pieces of 256 bf16 rows of 152064 17, 4.6: four
-// operations and an exponential a logit), then the answers, 7.4 us for 256 rows' five tokens and 23 for 64, a chain of loads, exchanges and
-// rankings; one row, that chain (4.7 + 8.8 us for twenty tokens).
+// operations and an exponential a logit), then the answers, 7.2 us for 256 rows' five tokens and 16 for 64, a chain of loads, exchanges and
+// rankings; one row, that chain (4.7 + 7.1 us for twenty tokens).
 // NaN counts as -infinity; -infinity has no weight; with +infinity among the logits only those have, the same each.
 #include "po_internal.h"
 
@@ -233,6 +233,7 @@ __device__ __forceinline__ float key_logit(unsigned long long k) {
 }
 
 constexpr int RUNS = MAX_TOP * (CHUNK / 8);      // of the chunks that are read again
+constexpr int ROW_THREADS = 512;                 // (256: 64 tokens of 256 rows 23 us instead of 16, twenty of one 8.8 instead of 7.1)
 constexpr int LIST = 512;                        // elements that are ordered at once; 8 of each of MAX_TOP runs
 
 // Leaves in out[0 .. min(n, top)) the largest of keys[0 .. n), in order; keys[n .. n + 32) are overwritten.  All different, but for
@@ -308,7 +309,7 @@ __device__ __forceinline__ float reached_logit(uint32_t t, float lowest) {
     return t > 0x007fffffu ? fmaxf(key_logit((unsigned long long)t << 32), lowest) : lowest;
 }
 
-// A row's answer, by a workgroup of which 256 threads work, from its pieces' sums and its chunks' largest logits.  What bounds it is a chain: the
+// A row's answer, by a workgroup of which 256 threads work, all where elements are read, from its pieces' sums and its chunks' largest logits.  What bounds it is a chain: the
 // loads of pieces and chunks' maxima; a floor under the answer from those; the loads of the chunks that reach it, and beside them the sums; the
 // order of the few elements that do.  Only rows with more than LIST of those go through the exact way by keys.  keys: RUNS + 32, only where top > 0.
 template <typename T, bool VEC>
@@ -365,16 +366,17 @@ __device__ __forceinline__ void answer_row(const T* row, int64_t r, int V, int p
         __syncthreads();
     }
     const int n_near = sh.chunk_count;
-    // f(logits, index of the first) of every run of 8 of n_chunks chunks, four at a time a thread; between: what is done while the first ones come
-    auto runs = [&](int n_chunks, auto chunk_of, auto between, auto f) {
+    // f(logits, index of the first) of every run of 8 of n_chunks chunks, four at a time a thread (number t of nt); between: what is done while the
+    // first ones come
+    auto runs_of = [&](int t, int nt, int n_chunks, auto chunk_of, auto between, auto f) {
         const int n = n_chunks * (CHUNK / 8);
         bool once = true;
-        for (int i0 = tid; once || i0 < n; i0 += 1024) {
+        for (int i0 = t; once || i0 < n; i0 += 4 * nt) {
             float v[4][8];
             int at[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int i = i0 + u * 256;
+                const int i = i0 + u * nt;
                 at[u] = V;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[u][e] = -INFINITY;
@@ -389,6 +391,7 @@ __device__ __forceinline__ void answer_row(const T* row, int64_t r, int V, int p
             for (int u = 0; u < 4; ++u) f(v[u], at[u]);
         }
     };
+    auto runs = [&](int n_chunks, auto chunk_of, auto between, auto f) { runs_of((int)threadIdx.x, (int)blockDim.x, n_chunks, chunk_of, between, f); };
     auto push = [&](const float (&v)[8], int at) {
         int n = 0;
 #pragma unroll
@@ -418,7 +421,7 @@ __device__ __forceinline__ void answer_row(const T* row, int64_t r, int V, int p
     auto near_chunk = [&](int i) { return near[i]; };
     if (few_groups && listed && n_near == chunks && n_near * CHUNK > LIST) {       // (short rows: a floor from their elements)
         float own = -INFINITY;
-        runs(n_near, near_chunk, nothing, [&](const float (&v)[8], int) {
+        runs_of(tid, 256, n_near, near_chunk, nothing, [&](const float (&v)[8], int) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) own = fmaxf(own, v[e]);
         });
@@ -507,7 +510,7 @@ __device__ __forceinline__ void answer_row(const T* row, int64_t r, int V, int p
 }
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) logprob_rows_kernel(const T* __restrict__ logits, int64_t ld, int V, int pieces, int chunks,
+__global__ void __launch_bounds__(ROW_THREADS) logprob_rows_kernel(const T* __restrict__ logits, int64_t ld, int V, int pieces, int chunks,
                                                            const Stats* __restrict__ stats, const float* __restrict__ chunk_max, const RowAnswer a) {
     extern __shared__ unsigned long long keys[];
     __shared__ RowShared sh;
@@ -564,7 +567,7 @@ void run(const T* logits, int64_t ld, int64_t rows, int V, const RowAnswer& a, v
     const int64_t total = rows * pieces;
     hipLaunchKernelGGL((logprob_pieces_kernel<T, VEC>), dim3((unsigned)((total + 3) / 4)), dim3(256), 0, s, logits, ld, V, pieces, total, stats,
                        cm, chunks);
-    hipLaunchKernelGGL((logprob_rows_kernel<T, VEC>), dim3((unsigned)rows), dim3(256), lds, s, logits, ld, V, pieces, chunks, stats, cm, a);
+    hipLaunchKernelGGL((logprob_rows_kernel<T, VEC>), dim3((unsigned)rows), dim3(ROW_THREADS), lds, s, logits, ld, V, pieces, chunks, stats, cm, a);
 }
 
 }  // namespace
