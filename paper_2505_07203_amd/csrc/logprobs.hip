@@ -9,7 +9,7 @@
 // do.  Where those are more than a list holds: the tokens lie in the chunks whose largest logits come first in that order, as many chunks as
 // tokens (an element of any other chunk has the largest elements of all of those before it), and the same holds for the runs of 8
 // within those chunks, so that at most 8 elements a token are ordered in the end, whatever the row holds.
-// What bounds it: many rows, reading them (1024 float32 rows of 128256 in one launch 97 us, 5.4 TB/s; pieces of 256 bf16 rows of 152064 17, 4.6: four
+// What bounds it: many rows, reading them (1024 float32 rows of 128256 in one launch 97 us, 5.4 TB/s; pieces of 256 bf16 rows of 152064 17, 4.6: five
 // operations and an exponential a logit), then the answers, 7.2 us for 256 rows' five tokens and 16 for 64, a chain of loads, exchanges and
 // rankings; one row, that chain (4.7 + 7.1 us for twenty tokens).
 // NaN counts as -infinity; -infinity has no weight; with +infinity among the logits only those have, the same each.
@@ -27,19 +27,22 @@ constexpr int MAX_TOP = 64;
 
 struct Stats { float m, s, t, pad; };            // of a piece
 
+// A logit as it is read: the sum quiets a signalling NaN.  (Of a number and a quiet NaN the larger is the number; of a signalling one it is NaN, and
+// of that and the next number the next one: what came before it would be lost.)
+__device__ __forceinline__ float quiet(float v) { return v + 0.0f; }
 // the logits of a lane: 8 from i on; they exist, and lie on 16 bytes
 __device__ __forceinline__ void load8_whole(const float* p, float (&v)[8]) {
     const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    v[0] = quiet(a.x); v[1] = quiet(a.y); v[2] = quiet(a.z); v[3] = quiet(a.w);
+    v[4] = quiet(b.x); v[5] = quiet(b.y); v[6] = quiet(b.z); v[7] = quiet(b.w);
 }
 __device__ __forceinline__ void load8_whole(const bf16_t* p, float (&v)[8]) {
     const uint4 a = *(const uint4*)p;
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-        v[2 * c] = __uint_as_float(w[c] << 16);
-        v[2 * c + 1] = __uint_as_float(w[c] & 0xffff0000u);
+        v[2 * c] = quiet(__uint_as_float(w[c] << 16));
+        v[2 * c + 1] = quiet(__uint_as_float(w[c] & 0xffff0000u));
     }
 }
 // -infinity beyond V
@@ -50,7 +53,7 @@ __device__ __forceinline__ void load8(const T* row, int i, int V, float (&v)[8])
         return;
     }
 #pragma unroll
-    for (int c = 0; c < 8; ++c) v[c] = i + c < V ? to_f32(row[i + c]) : -INFINITY;
+    for (int c = 0; c < 8; ++c) v[c] = i + c < V ? quiet(to_f32(row[i + c])) : -INFINITY;
 }
 
 // Over a wavefront, all lanes get it, on the vector ALU: within rows of 16 lanes, then the four rows (the same by way of LDS, six exchanges for

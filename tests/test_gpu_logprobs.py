@@ -257,3 +257,41 @@ def test_far_from_zero(at):
     g = torch.Generator(device="cuda").manual_seed(7)
     z = at + torch.randn(5, 9000, device="cuda", generator=g) * max(3.0, abs(at) * 2.0 ** -22)
     check(z, torch.randint(0, 9000, (5, 3), dtype=torch.int32, device="cuda", generator=g), 9)
+
+
+SIGNALLING = {torch.float32: (0x7fa00000, -0x600000, 0x7f800001), torch.bfloat16: (0x7fa0, -0x60, 0x7f81)}
+
+
+def signalling(V, dtype, seed):
+    """eight rows: the largest logits with a signalling NaN behind each among a lane's eight (whose larger one would be NaN), as large as others or
+    300 above them; little but such NaNs; random bits"""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    z = logits(8, V, seed, dtype)[0]
+    whole = torch.int32 if dtype is torch.float32 else torch.int16
+    bits = z.view(whole)
+    bits[7] = torch.randint(-(2 ** 31), 2 ** 31, (V,), device="cuda", generator=g).to(whole)
+    bits[6, torch.rand(V, device="cuda", generator=g) < 0.9] = SIGNALLING[dtype][2]
+    for i in range(6):
+        runs = torch.randperm(V // 8, device="cuda", generator=g)[:7] * 8
+        for e in range(len(runs)):
+            z[i, runs[e] + e] = (12.0 if i % 2 else 312.0) + e
+            bits[i, runs[e] + e + 1] = SIGNALLING[dtype][(i + e) % 3]
+    return z, torch.randint(0, V, (8, 3), dtype=torch.int32, device="cuda", generator=g)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [64, 700, 1200, 20_000, 40_003, 70_001, 128_256])
+def test_signalling_nans(V, dtype):
+    """as memory that nobody wrote may hold them: none hides a larger logit, whichever way the rows go"""
+    z, tk = signalling(V, dtype, V)
+    with np.errstate(invalid="ignore"):
+        for top in (0, 1, 7, 40):
+            want = check(z, tk, top)
+            rows = 600 if V < 60_000 else 1500 if dtype is torch.float32 and V < 100_000 else 20
+            pick = torch.arange(rows, device="cuda") * 3 % 8
+            got = B.po_op_token_logprobs(z[pick], tk[pick], top=top)
+            assert all(torch.equal(a, b[pick]) for a, b in zip(got, want))
+        odd = torch.empty(8, V + 5, dtype=dtype, device="cuda")           # rows that are read one by one
+        odd[:, 3:3 + V].view(torch.int32 if dtype is torch.float32 else torch.int16).copy_(z.view(torch.int32 if dtype is torch.float32 else torch.int16))
+        got, want = B.po_op_token_logprobs(odd[:, 3:3 + V], tk, top=9), B.po_op_token_logprobs(z, tk, top=9)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
