@@ -116,7 +116,26 @@ __global__ void __launch_bounds__(256) norm_quant_kernel(const NormQuant p) {
     for (int off = 32; off > 0; off >>= 1) ss += __shfl_xor(ss, off);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = ss;
     __syncthreads();
-    const float mean = (part[0] + part[1] + part[2] + part[3]) * p.inv_d + p.eps;
+    float mean = (part[0] + part[1] + part[2] + part[3]) * p.inv_d + p.eps;
+    if (mean < 0x1p-100f) {                      // (the workgroup together)
+        // Squares below the normal numbers count (each of 16384 may be off by 2^-150): the row times 2^100, exactly, is normed in its place.  Its
+        // values are below 2^57, as mean * d is below 2^-86.
+        ss = 0.f;
+#pragma unroll
+        for (int j = 0; j < QV; ++j)
+            if ((int)threadIdx.x + j * 256 < p.vecs) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    h[j][e] *= 0x1p100f;
+                    ss = fmaf(h[j][e], h[j][e], ss);
+                }
+            }
+        for (int off = 32; off > 0; off >>= 1) ss += __shfl_xor(ss, off);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = ss;
+        __syncthreads();
+        mean = (part[0] + part[1] + part[2] + part[3]) * p.inv_d + p.eps * 0x1p100f * 0x1p100f;
+    }
     const float r = mean > 0.f ? 1.0f / sqrtf(mean) : 0.f;               // (a row of zeros with eps 0: zeros)
     float pm = 0.f, ym = 0.f;                    // (ym: for the rare case alone, but a pass over registers)
 #pragma unroll

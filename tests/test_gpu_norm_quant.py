@@ -157,3 +157,18 @@ def test_zeros_without_eps(block):
     check(x[1:2], None, gain, block, 0.0, h[1:2], c[1:2], (s[:, 1:2] if block else s[1:2]), y[1:2])
     z = torch.tensor([0, 2], device="cuda")
     assert not c[z].any() and not y[z].any() and bool(((s[:, z] if block else s[z]) == 1).all())
+
+
+@pytest.mark.parametrize("rows,d,block", [(6, 8, 0), (9, 2056, 0), (9, 1024, 128), (7, 16384, 128), (7, 8200, 0)])
+def test_tiny_rows(rows, d, block):
+    """rows whose squares leave the range of float32 numbers, without eps or with one as small: the definition holds as for any other"""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    gain = (1 + 0.2 * torch.randn(d, device="cuda", generator=g)).bfloat16()
+    x = torch.randn(rows, d, device="cuda", generator=g).double()
+    x = (x * torch.tensor([2.0 ** -t for t in (90, 64, 75, 49, 110, 126, 2, 60, 132)], device="cuda", dtype=torch.float64)[:rows, None]).float().bfloat16()
+    x[:, ::3] *= 2.0 ** -6
+    for eps in (0.0, 1e-42, 1e-33, 1e-28):
+        for delta in (None, x.flip(1).contiguous()):
+            h, c, s, y = B.po_op_add_rmsnorm_quantize(x, delta, gain, eps, block, normed=True)
+            check(x, delta, gain, block, float(np.float32(eps)), h, c, s, y)
+            assert torch.equal(B.po_op_add_rmsnorm_quantize(x, delta, gain, eps, block, normed=True, codes=False)[3], y)
