@@ -271,6 +271,12 @@ template <typename T> struct Out {
 };
 constexpr uint32_t NONE = 0x80000000u;
 
+// what the sums onto R start with: for rows without an adapter the zero that leaves R's sign alone
+__device__ __forceinline__ f32x4 nothing(int rank) {
+    const float z = rank ? 0.f : -0.f;
+    return f32x4{z, z, z, z};
+}
+
 template <typename T>
 __device__ __forceinline__ void add_out(const f32x4 (&acc)[4], const u32x4 (&r)[Out<T>::PASSES], unsigned char* stg, __amdgpu_buffer_rsrc_t rc, uint32_t vo,
                                         uint32_t pitch, int lane) {
@@ -361,7 +367,7 @@ __global__ void __launch_bounds__(256) adapter_up_few_kernel(const AdapterParams
     for (int i = 0; i < O::PASSES; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rr, vo + (uint32_t)(i * O::RPP) * pitch, 0, 0);
     f32x4 acc[4];
 #pragma unroll
-    for (int h = 0; h < 4; ++h) acc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int h = 0; h < 4; ++h) acc[h] = nothing(rank);
 #pragma unroll
     for (int k = 0; k < KS; ++k)
         if (k * 32 < rank) {
@@ -471,7 +477,7 @@ __global__ void __launch_bounds__(256, 2) adapter_up_kernel(const AdapterParams 
         for (int b = 0; b < SUB; ++b) {
             f32x4 acc[4];
 #pragma unroll
-            for (int h = 0; h < 4; ++h) acc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int h = 0; h < 4; ++h) acc[h] = nothing(rank);
 #pragma unroll
             for (int k = 0; k < KS; ++k)
                 if (k < ks) {

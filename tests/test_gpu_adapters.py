@@ -210,3 +210,16 @@ def test_refusals():
         k = dict(x=x, a=a, b=b, ranks=ranks, scales=scales, segments=seg) | bad
         with pytest.raises(B.PoError):
             B.po_op_adapters(**k)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows", [9, 40])
+def test_rows_without_an_adapter_keep_their_zeros(rows, dtype):
+    """C[r] = R[r] to the sign of a zero, where the residual is not C"""
+    x, a, b, ranks, scales, segments, res = case(rows, 264, 136, [16, 0], 16, [(0, 2, 0), (3, 2, 1), (rows - 2, 1, 0)], dtype)
+    res[:, ::3], res[:, 1::3] = -0.0, 0.0
+    got = B.po_op_adapters(x, a, b, ranks, scales, np.array(segments), residual=res)
+    check(x, a, b, ranks, scales, segments, res, got)
+    kept = torch.tensor([i not in (0, 1, rows - 2) for i in range(rows)], device="cuda")
+    whole = torch.int16 if dtype is torch.bfloat16 else torch.int32
+    assert torch.equal(got[kept].view(whole), res[kept].view(whole))
