@@ -647,8 +647,8 @@ po_status po_op_add_rmsnorm_quantize(const void* dev_x, const void* dev_delta, c
  * NULL (zeros).  R is what the projection left, or the residual that goes into it (po_op_linear, po_op_linear_fp8_block).  Adapters lie in
  * slots of a pool: dev_a [n_slots, width, K], dev_b [n_slots, N, width]; of slot a the first ranks[a] rows of A and columns of B are used, whatever the
  * rest holds (rank 0: an empty slot).  ranks, scales [n_slots] and segments are HOST arrays, read before the call returns (a captured
- * call keeps them).  segments: rows ascending and apart, n_rows may be 0, adapter -1 = none.  The product with A is a float32 number
- * (PO_BF16: the sum of two bf16 numbers, 2^-16 off at most); C is rounded once.
+ * call keeps them).  segments: rows ascending and apart, n_rows may be 0, adapter -1 = none.  The product with A is a float32 number,
+ * also as an operand of the product with B; C is rounded once.
  * N (up to 2^20) and K (up to 2^17) multiples of 8; width a multiple of 8, at most 128; up to 2^23 rows, fewer slots; pointers 16-byte aligned.  x
  * overlaps neither C nor the residual, and those are the same or apart.  Finite inputs; a row that has others may hold anything, the other rows
  * are as if it had none.

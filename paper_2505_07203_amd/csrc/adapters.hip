@@ -219,21 +219,28 @@ __global__ void __launch_bounds__(64 * DOWN_WAVES, 2) adapter_down_kernel(const 
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (nothing is on its way into LDS when the workgroup ends)
 }
 
-// the fragments of T in the second product: bf16 in two parts (the rounding of T and that of what it left, 2^-16 of T together),
-// float32 whole
+// The fragments of T in the second product: float32 whole, in bf16 three numbers, whose sum T is (each takes 8 bits of what the ones before left;
+// what lies below the smallest bf16 number is lost).  Two of them would leave 2^-16 of T out, which shows where the residual takes the rest away, for
+// 2 % of the time of the whole call with rank 64 (posts 64 / 66 us) and 5 % with 128 (two prompts of 4000 rows 81 / 85).
 template <typename T> struct Parts;
-template <> struct Parts<bf16_t> { static constexpr int N = 2; };
+template <> struct Parts<bf16_t> { static constexpr int N = 3; };
 template <> struct Parts<float> { static constexpr int N = 1; };
-__device__ __forceinline__ void split(const float (&v)[8], Frag<bf16_t> (&f)[2]) {
-    uint32_t hi[4], lo[4];
+__device__ __forceinline__ void split(const float (&v)[8], Frag<bf16_t> (&f)[3]) {
+    float left[8];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        const bf16_t h0 = f2bf(v[2 * c]), h1 = f2bf(v[2 * c + 1]);
-        hi[c] = (uint32_t)h0 | ((uint32_t)h1 << 16);
-        lo[c] = (uint32_t)f2bf(v[2 * c] - bf2f(h0)) | ((uint32_t)f2bf(v[2 * c + 1] - bf2f(h1)) << 16);
+    for (int e = 0; e < 8; ++e) left[e] = v[e];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        uint32_t w[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const bf16_t a = f2bf(left[2 * c]), b = f2bf(left[2 * c + 1]);
+            w[c] = (uint32_t)a | ((uint32_t)b << 16);
+            left[2 * c] -= bf2f(a);
+            left[2 * c + 1] -= bf2f(b);
+        }
+        f[i].v = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
     }
-    f[0].v = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-    f[1].v = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
 }
 __device__ __forceinline__ void split(const float (&v)[8], Frag<float> (&f)[1]) {
     f[0].lo = f32x4{v[0], v[1], v[2], v[3]};
@@ -333,7 +340,7 @@ __device__ __forceinline__ void sum_planes(const AdapterParams& p, const float* 
 }
 
 // C of up to 16 rows of a request and 64 columns a wavefront, for batches of requests of up to 16 rows: every wavefront adds the planes of T itself.
-// Its loads are all under way together: this is what a single token waits for (64 of them, N 4096, rank 16: 5.1 us; by the two kernels below
+// Its loads are all under way together: this is what a single token waits for (64 of them, N 4096, rank 16: 5.5 us; by the two kernels below
 // 3.2 + 6.2).
 template <typename T, int KS>
 __global__ void __launch_bounds__(256) adapter_up_few_kernel(const AdapterParams p, const Table tab) {
@@ -387,7 +394,7 @@ __global__ void __launch_bounds__(256) adapter_up_few_kernel(const AdapterParams
 }
 
 // Longer requests: first T as the second product's fragments, in the order of its lanes: [group][step][part][lane] (in scratch behind the planes;
-// 16584 rows, rank 64, seven planes: 9 us) ...
+// 16584 rows, rank 64, seven planes: 9.5 us) ...
 template <typename T>
 __global__ void __launch_bounds__(256) adapter_join_kernel(const AdapterParams p, const Table tab) {
     constexpr int NP = Parts<T>::N;
@@ -409,7 +416,7 @@ __global__ void __launch_bounds__(256) adapter_join_kernel(const AdapterParams p
 
 // ... then C of a run of rows of one request and 4 x 16 H columns, a quarter a wavefront, which holds its part of B in registers for all of
 // them: B is read once a run.  16 rows at a time, the next ones' R and T on their way; wavefronts wait for nobody.  What bounds it: R and C,
-// 16584 x 4096 with rank 64 59 us (4.6 TB/s; a copy of as many bytes 46).  Tiles of 64 rows x 1024 columns that read B and the planes of T
+// 16584 x 4096 with rank 64 63 us (4.3 TB/s; a copy of as many bytes 46).  Tiles of 64 rows x 1024 columns that read B and the planes of T
 // anew took 89: what a compute unit can have under way towards it is the limit there, and reads that caches answer take their places in it.
 template <typename T, int KS> struct UpCols {
     static constexpr int H = 32 / (int)sizeof(T) / (KS == 1 ? 1 : KS / 2);              // 128 registers of B (64 with one step)
@@ -467,12 +474,14 @@ __global__ void __launch_bounds__(256, 2) adapter_up_kernel(const AdapterParams 
 #pragma unroll
         for (int i = 0; i < O::PASSES; ++i) r[b][i] = __builtin_amdgcn_raw_buffer_load_b128(rr, vo[b] + (uint32_t)(i * O::RPP) * pitch, 0, 0);
     };
-    // (the next rows' R go where this one's are no longer needed: B, two of these and of T do not fit the registers)
-    auto turn = [&](const Frag<T> (&t)[KS][NP], Frag<T> (&next)[KS][NP], int g) {
+    // (the next rows' R go where this one's are no longer needed: B, two of these and of T do not fit the registers; nor does another T of twelve
+    // fragments, with which two prompts of 4000 rows and rank 128 took 121 us instead of 85)
+    constexpr bool AHEAD = NP * KS < 12;
+    auto turn = [&](Frag<T> (&t)[KS][NP], Frag<T> (&next)[KS][NP], int g) {
         const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void*)((unsigned char*)p.c + (int64_t)(sg.row + g * 16) * pitch), 0,
                                                                             (int)((uint32_t)min(16, sg.n - g * 16) * pitch), 0x00020000);
         const bool more = g + 1 < g1;
-        if (more) fetch_t(next, g + 1);
+        if (AHEAD && more) fetch_t(next, g + 1);
 #pragma unroll
         for (int b = 0; b < SUB; ++b) {
             f32x4 acc[4];
@@ -486,6 +495,7 @@ __global__ void __launch_bounds__(256, 2) adapter_up_kernel(const AdapterParams 
 #pragma unroll
                         for (int h = 0; h < 4; ++h) acc[h] = mma(w[b * 4 + h][k], t[k][i], acc[h]);
                 }
+            if (!AHEAD && b == SUB - 1 && more) fetch_t(t, g + 1);
             add_out<T>(acc, r[b], stage[wave], rc, vo[b], pitch, lane);
             if (more) fetch_r(b, g + 1);
         }
@@ -496,7 +506,7 @@ __global__ void __launch_bounds__(256, 2) adapter_up_kernel(const AdapterParams 
     for (int b = 0; b < SUB; ++b) fetch_r(b, g0);
     for (int g = g0; g < g1; g += 2) {
         turn(t0, t1, g);
-        if (g + 1 < g1) turn(t1, t0, g + 1);
+        if (g + 1 < g1) turn(AHEAD ? t1 : t0, t0, g + 1);
     }
 }
 
@@ -650,8 +660,8 @@ size_t adapters_scratch(int dtype, const int32_t* ranks, int K, const po_adapter
         rank = std::max(rank, r);
     }
     const int nr = nr_of(rank);
-    // planes of T, and T as fragments (32 ranks a step: of float32, or of two bf16 numbers)
-    return rank ? (size_t)groups * 16 * sizeof(float) * ((size_t)k_pieces(nr, dtype == 0 ? 4 : 2, K) * (16 * nr) + 32 * ks_of(nr)) : 0;
+    // planes of T, and T as fragments (32 ranks a step: of float32, or of three bf16 numbers)
+    return rank ? (size_t)groups * 16 * ((size_t)k_pieces(nr, dtype == 0 ? 4 : 2, K) * (16 * nr) * sizeof(float) + 32 * ks_of(nr) * (dtype == 0 ? sizeof(float) : 3 * sizeof(bf16_t))) : 0;
 }
 
 void launch_adapters(int dtype, const void* x, const void* a, const void* b, const int32_t* ranks, const float* scales, int width, const void* res,

@@ -223,3 +223,18 @@ def test_rows_without_an_adapter_keep_their_zeros(rows, dtype):
     kept = torch.tensor([i not in (0, 1, rows - 2) for i in range(rows)], device="cuda")
     whole = torch.int16 if dtype is torch.bfloat16 else torch.int32
     assert torch.equal(got[kept].view(whole), res[kept].view(whole))
+
+
+@pytest.mark.parametrize("rows", [1, 16, 17, 100])
+@pytest.mark.parametrize("rank", [2, 32, 50, 100, 128])
+def test_product_with_a_is_a_float32_number(rows, rank):
+    """T[0] = 1 + 2^-10 + 2^-20, T[1] = -2^-10 and R = -1: every sum of these is a float32 number, and the result 2^-20"""
+    K, N = 64, 136
+    x, res = torch.zeros(rows, K, device="cuda").bfloat16(), torch.full((rows, N), -1.0, device="cuda").bfloat16()
+    a, b = torch.zeros(1, 128, K, device="cuda").bfloat16(), torch.zeros(1, N, 128, device="cuda").bfloat16()
+    x[:, :3] = 1
+    a[0, 0, :3] = torch.tensor([1.0, 2.0 ** -10, 2.0 ** -20])
+    a[0, rank - 1, 0] = -(2.0 ** -10)
+    b[0, :, 0] = b[0, :, rank - 1] = 1
+    got = B.po_op_adapters(x, a, b, [rank], [1.0], [(0, rows, 0)], residual=res)
+    assert bool((got == 2.0 ** -20).all()), got.double().abs().max()
