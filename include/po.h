@@ -664,7 +664,7 @@ po_status po_op_adapters(int32_t dtype, const void* dev_x, const void* dev_a, co
 /* Log-probabilities of rows of logits [rows][ld] (dtype PO_F32 or PO_BF16; V <= ld of each row used), what a distribution says about given tokens:
  * logprobs [rows][n_tokens] of tokens [rows][n_tokens] (an id outside [0, V): -infinity), entropy [rows] (may be NULL) in nats, and the
  * `top` (0 .. 64) most likely tokens with their log-probs [rows][top], ordered by logit, the largest first, equal ones by index.
- * n_tokens and top may be 0 (their arrays then NULL).  NaN counts as -infinity; tokens of -infinity have no weight (log-prob -infinity) and are no
+ * n_tokens (up to 2^30) and top may be 0 (their arrays then NULL).  NaN counts as -infinity; tokens of -infinity have no weight (log-prob -infinity) and are no
  * alternatives: where a row has fewer than `top` others, the rest are token -1, log-prob -infinity.  With +infinity among the logits only those
  * have weight, the same each.  A row without any weight: entropy 0, every log-prob -infinity.  Exponentials and sums of a piece of
  * 2048 logits are float32, sums of pieces and logarithms float64.  Up to 2^20 rows, V up to 2^24, any rows * V up to 2^36 (PO_ERR_TOO_LONG).  Every

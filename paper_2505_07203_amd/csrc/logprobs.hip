@@ -324,7 +324,7 @@ __device__ __forceinline__ void answer_row(const T* row, int64_t r, int V, int p
     int &count = sh.count, (&ranks)[256] = sh.ranks;
     int* const near = (int*)(keys + 2 * LIST);                         // chunks that reach the floor
     const int n_tokens = a.n_tokens, top = a.top, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int tid = threadIdx.x < 256 ? (int)threadIdx.x : 1 << 30;    // (the others only wait)
+    const int tid = threadIdx.x < 256 ? (int)threadIdx.x : MAX_GIVEN_TOKENS;      // (the others only wait: behind the end of every list)
     // (first turn of each list and the first token: asked for together)
     const Stats none = {-INFINITY, 0.f, 0.f, 0.f};
     const Stats first = tid < pieces ? st[tid] : none;

@@ -1865,6 +1865,7 @@ po_status po_op_token_logprobs(int32_t dtype, const void* logits, int64_t ld, in
     if (bad_dtype(dtype) || !logits || !scratch || ((uintptr_t)scratch & 255) || ld < V || n_tokens < 0) return PO_ERR_INVALID_ARG;
     if ((n_tokens && (!tokens || !logprobs)) || (top && (!top_tokens || !top_logprobs)) || (!n_tokens && !top && !entropy)) return PO_ERR_INVALID_ARG;
     if ((uintptr_t)logits & (dtype == PO_F32 ? 3 : 1)) return PO_ERR_INVALID_ARG;
+    if (n_tokens > MAX_GIVEN_TOKENS) return PO_ERR_TOO_LONG;
     const po_status st = logprob_shape(rows, V, top);
     if (st != PO_OK) return st;
     if (scratch_bytes < token_logprobs_scratch(rows, V, top)) return PO_ERR_WORKSPACE_TOO_SMALL;

@@ -242,7 +242,8 @@ size_t sample_scratch(int64_t rows, int V, bool top_k, bool top_p);
 void launch_add_rmsnorm_quantize(const bf16_t* x, const bf16_t* delta, const bf16_t* g, bf16_t* h, bf16_t* y, unsigned char* codes, float* scales,
                                  int64_t rows, int d, bool blocks, float eps, hipStream_t s);
 
-// log-probs of given tokens, entropy (may be null) and the `top` most likely tokens of each row of logits (row pitch ld)
+// log-probs of given tokens (up to MAX_GIVEN_TOKENS a row), entropy (may be null) and the `top` most likely tokens of each row of logits (row pitch ld)
+constexpr int MAX_GIVEN_TOKENS = 1 << 30;                          // (the kernels count them in 32 bits, 256 at a time)
 bool token_logprobs_fits(int64_t rows, int V);                     // in a launch
 size_t token_logprobs_scratch(int64_t rows, int V, int top);
 void launch_token_logprobs(int dtype, const void* logits, int64_t ld, int64_t rows, int V, const int32_t* tokens, int n_tokens, int top,

@@ -78,3 +78,9 @@ def test_lm_head_logprobs_refusals():
     n = C.c_size_t(7)
     f = B.lib().po_lm_head_logprobs_bytes
     assert f(1, 4, 1000, 128, None) == 1 and f(2, 4, 1000, 128, C.byref(n)) == 1 and f(1, 4, 1000, 100, C.byref(n)) == 2 and n.value == 7
+
+
+def test_token_logprobs_of_too_many_tokens():
+    """a row's tokens are counted in 32 bits, 256 at a time"""
+    ok = [0, P, 1000, 1, 1000, P, 2, 0, P, P, None, None, P, 1 << 30, None]
+    refused(B.lib().po_op_token_logprobs, ok, [(6, (1 << 30) + 1, 4), (6, (1 << 31) - 1, 4), (6, (1 << 31) - 257, 4), (6, 1 << 30, 13, 0, 6)])
