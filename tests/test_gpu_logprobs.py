@@ -295,3 +295,50 @@ def test_signalling_nans(V, dtype):
         odd[:, 3:3 + V].view(torch.int32 if dtype is torch.float32 else torch.int16).copy_(z.view(torch.int32 if dtype is torch.float32 else torch.int16))
         got, want = B.po_op_token_logprobs(odd[:, 3:3 + V], tk, top=9), B.po_op_token_logprobs(z, tk, top=9)
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def kinds(V, dtype):
+    """twelve rows of every kind: ordinary, without weight, with few tokens, equal, infinite, with NaN, in steps"""
+    z, tk = logits(12, V, 12, dtype)
+    z[1] = -float("inf")
+    z[2, 100:] = -float("inf")
+    z[3] = 2.5
+    z[4, [7, V - 300]] = float("inf")
+    z[5, ::3] = float("nan")
+    z[6] = (torch.arange(V, device="cuda") // 700).to(dtype)
+    z[8, V - 1] = 60.0
+    tk[7], tk[8] = torch.tensor([-1, V, 0], dtype=torch.int32), torch.tensor([V - 1, 0, 1], dtype=torch.int32)
+    return z, tk
+
+
+@pytest.mark.parametrize("V,rows", [(66_001, 1500), (524_288, 200), (524_281, 189), (130_000, 750)])
+def test_long_rows_in_one_launch(V, rows):
+    """float32 rows of 33 to 256 pieces, of which 48000 and more are read and answered by a workgroup a row: the bits of the same rows twelve at a time,
+    which are held to the definition; aligned, and with a pitch that is no multiple of 16 bytes"""
+    assert rows * ((V + 2047) // 2048) >= 48000
+    z, tk = kinds(V, torch.float32)
+    pick = torch.arange(rows, device="cuda") * 7 % 12
+    many = z[pick]
+    odd = torch.empty(rows, V + 5, device="cuda")
+    odd[:, 1:V + 1] = many
+    for top in (0, 1, 20, 64):
+        want = check(z, tk, top)
+        for rows_of in (many, odd[:, 1:V + 1]):
+            got = B.po_op_token_logprobs(rows_of, tk[pick], top=top)
+            assert all(torch.equal(a, b[pick]) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,rows", [(900, 513), (1003, 800), (40_000, 600), (65_536, 513), (65_536, 512), (65_537, 512), (70_001, 300)])
+def test_rows_on_either_side_of_one_launch(V, rows, dtype):
+    """short rows, of which more than 512 take two launches; rows above 2^16 logits"""
+    z, tk = kinds(V, dtype)
+    pick = torch.arange(rows, device="cuda") * 5 % 12
+    many = z[pick]
+    odd = torch.empty(rows, V + 5, dtype=dtype, device="cuda")
+    odd[:, 1:V + 1] = many
+    for top in (0, 1, 20, 64):
+        want = check(z, tk, top)
+        for rows_of in (many, odd[:, 1:V + 1]):
+            got = B.po_op_token_logprobs(rows_of, tk[pick], top=top)
+            assert all(torch.equal(a, b[pick]) for a, b in zip(got, want))
