@@ -238,3 +238,18 @@ def test_product_with_a_is_a_float32_number(rows, rank):
     b[0, :, 0] = b[0, :, rank - 1] = 1
     got = B.po_op_adapters(x, a, b, [rank], [1.0], [(0, rows, 0)], residual=res)
     assert bool((got == 2.0 ** -20).all()), got.double().abs().max()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,N,K,ranks", [(8007, 4096, 14336, [64, 40]), (33003, 64, 4104, [8, 16]), (33003, 64, 4104, [24, 32]), (33003, 72, 4104, [128, 3])])
+def test_past_the_caches(rows, N, K, ranks, dtype):
+    """calls that move 256 MiB or more read x past the caches"""
+    rows = rows if dtype is torch.bfloat16 else rows // 2
+    assert rows * (K + 2 * N) * (2 if dtype is torch.bfloat16 else 4) >= 256 << 20
+    segments = [(2, rows // 2, 1), (rows // 2 + 3, rows - rows // 2 - 3, 0)]
+    x, a, b, ranks, scales, segments, res = case(rows, N, K, ranks, (max(ranks) + 7) // 8 * 8, segments, dtype)
+    got = B.po_op_adapters(x, a, b, ranks, scales, np.array(segments), residual=res)
+    check(x, a, b, ranks, scales, segments, res, got)
+    assert torch.equal(B.po_op_adapters(x, a, b, ranks, scales, np.array(segments), residual=res.clone()), got)
+    one = B.po_op_adapters(x, a, b, ranks, scales, np.array(segments), residual=res, out=res)
+    assert one is res and torch.equal(res, got)

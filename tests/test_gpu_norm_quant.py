@@ -172,3 +172,21 @@ def test_tiny_rows(rows, d, block):
             h, c, s, y = B.po_op_add_rmsnorm_quantize(x, delta, gain, eps, block, normed=True)
             check(x, delta, gain, block, float(np.float32(eps)), h, c, s, y)
             assert torch.equal(B.po_op_add_rmsnorm_quantize(x, delta, gain, eps, block, normed=True, codes=False)[3], y)
+
+
+@pytest.mark.parametrize("rows,d,block", [(16385, 4096, 0), (16385, 4096, 128), (19001, 2048, 128), (7501, 5120, 128), (7501, 5120, 0), (4801, 8192, 0), (2403, 16384, 128), (2403, 16376, 0)])
+def test_past_the_caches(rows, d, block):
+    """calls that move 256 MiB or more"""
+    x, delta, gain = inputs(rows, d, rows + d)
+    x[-2], delta[-2] = 0, 0
+    want = B.po_op_add_rmsnorm_quantize(x, delta, gain, 1e-5, block=block, normed=True)
+    assert rows * d * 7 >= 256 << 20
+    for r0 in range(0, rows, 4096):
+        part = slice(r0, r0 + 4096)
+        check(x[part], delta[part], gain, block, 1e-5, want[0][part], want[1][part], want[2][:, part] if block else want[2][part], want[3][part])
+    got = B.po_op_add_rmsnorm_quantize(x, delta, gain, 1e-5, block=block)                         # the codes alone
+    assert all(torch.equal(a, b) for a, b in zip(got[:3], want))
+    got = B.po_op_add_rmsnorm_quantize(x, delta, gain, 1e-5, block=block, normed=True, h=x)       # in place
+    assert got[0] is x and all(torch.equal(a, b) for a, b in zip(got, want))
+    got = B.po_op_add_rmsnorm_quantize(x, None, gain, 1e-5, block=block, normed=True)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
