@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(256) adapter_up_few_kernel(const AdapterParams
 }
 
 // Longer requests: first T as the second product's fragments, in the order of its lanes: [group][step][part][lane] (in scratch behind the planes;
-// 16584 rows, rank 64, seven planes: 9.5 us) ...
+// 16584 rows, rank 64, seven planes: 10 us) ...
 template <typename T>
 __global__ void __launch_bounds__(256) adapter_join_kernel(const AdapterParams p, const Table tab) {
     constexpr int NP = Parts<T>::N;
@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(256) adapter_join_kernel(const AdapterParams p
 
 // ... then C of a run of rows of one request and 4 x 16 H columns, a quarter a wavefront, which holds its part of B in registers for all of
 // them: B is read once a run.  16 rows at a time, the next ones' R and T on their way; wavefronts wait for nobody.  What bounds it: R and C,
-// 16584 x 4096 with rank 64 63 us (4.3 TB/s; a copy of as many bytes 46).  Tiles of 64 rows x 1024 columns that read B and the planes of T
+// 16584 x 4096 with rank 64 65 us (4.2 TB/s; a copy of as many bytes 46).  Tiles of 64 rows x 1024 columns that read B and the planes of T
 // anew took 89: what a compute unit can have under way towards it is the limit there, and reads that caches answer take their places in it.
 template <typename T, int KS> struct UpCols {
     static constexpr int H = 32 / (int)sizeof(T) / (KS == 1 ? 1 : KS / 2);              // 128 registers of B (64 with one step)
@@ -618,7 +618,8 @@ template <typename T, int NR>
 void run_t(const AdapterParams& p, const Launch& l, hipStream_t s) {
     constexpr int KS = ks_of(NR), H = UpCols<T, KS>::H;
     if (l.rank) {
-        // (x past the caches / not, K 14336, N 4096, rank 64, the whole call: 2000 rows 42 / 41 us, 8000 86 / 104, 16000 157 / 178)
+        // (x past the caches / not, us.  K 14336, N 4096, rank 64, the whole call: 2000 rows 42 / 41, 8000 86 / 104, 16000 157 / 178.  Of far more columns
+        // than K, x just written by the norm, whose time is in it, K 4096, N 28672, rank 64: 2300 rows 88 / 91, 4000 138 / 137, 9000 272 / 276)
         if ((int64_t)l.total * 16 * ((int64_t)p.K + 2 * p.N) * (int64_t)sizeof(T) >= READ_ONCE_BYTES) run_down<T, NR, true>(p, l, s);
         else run_down<T, NR, false>(p, l, s);
     }

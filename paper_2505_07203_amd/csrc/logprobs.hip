@@ -523,9 +523,11 @@ __global__ void __launch_bounds__(ROW_THREADS) logprob_rows_kernel(const T* __re
 
 // Pieces and answer of a row by one workgroup, sums and largest logits in LDS, one launch; the same arithmetic in the same order as by the two
 // kernels.  For rows of up to 2^16 logits that all run at once, two a compute unit: a launch less; and for so many long rows of float32 that the next
-// row's logits are read while one is answered.  Five alternatives, us against the two kernels: 512 rows of 1000 12.2 / 15.8, of 65536
-// (bf16) 21.5 / 20.7, 700 rows of 1000 19.5 / 15.6 (half of the wavefronts only wait during the answer), 64 of 128256 20.2 / 15.8; float32 rows of
-// 128256: 512 54 / 54, 768 75.7 / 77.6, 2048 181 / 198; of 65536: 1024 55.5 / 53.8, 1536 76 / 83; 2048 bf16 rows of 152064 128 / 125.
+// row's logits are read while one is answered.  Five alternatives, us against the two kernels, calls from a graph: one row of 1000 9.8 / 11.1, of 8000
+// 8.5 / 9.8, of 32000 9.9 / 10.1, of 65536 11.3 / 8.8 (there the launch saved is no longer what the row's eight wavefronts take longer); bf16 rows: 64 of
+// 32000 10.4 / 10.6, of 65536 12.4 / 9.8, 256 of 32000 11.9 / 13.5, of 65536 14.3 / 15.2, 512 of 32000 16.0 / 17.2, of 65536 20.8 / 20.8; 512 float32
+// rows of 1000 11.4 / 13.8, of 65536 31.3 / 31.8.  By calls: 700 rows of 1000 19.5 / 15.6 (half of the wavefronts only wait during the answer), 64 of
+// 128256 20.2 / 15.8; float32 rows of 128256: 512 54 / 54, 768 75.7 / 77.6, 2048 181 / 198; of 65536: 1024 55.5 / 53.8, 1536 76 / 83; 2048 bf16 rows of 152064 128 / 125.
 constexpr int WHOLE_WAVES = 8, WHOLE_CHUNKS = 1024;            // (rows of up to 2^19 logits)
 template <typename T>
 inline bool whole_rows(int64_t rows, int pieces, int chunks) {

@@ -5,8 +5,8 @@
 // amax = max |y| over a row or over each block of 128 of it.  y is a float32 number throughout: it is rounded once, to the code (and once to bf16
 // where the rows are wanted too), not to bf16 first and then to the code.
 //
-// Bound by memory; a row is read once and stays in the registers of its workgroup.  16384 x 4096 in blocks 78 us (6.0 TB/s read and written;
-// addition, norm and quantisation in three calls 161), 1931 x 5120 in blocks with the bf16 rows 17 (5.2: one round of
+// Bound by memory; a row is read once and stays in the registers of its workgroup.  16384 x 4096 in blocks 78 us, calls of 1 to 12 batches in turn (6.0 TB/s read and
+// written; addition, norm and quantisation in three calls 161), 1931 x 5120 in blocks with the bf16 rows 17 (5.2: one round of
 // workgroups, which read together and write together), one row of 4096 3.7, a launch and two exchanges.
 #include "po_internal.h"
 
