@@ -253,3 +253,16 @@ def test_past_the_caches(rows, N, K, ranks, dtype):
     assert torch.equal(B.po_op_adapters(x, a, b, ranks, scales, np.array(segments), residual=res.clone()), got)
     one = B.po_op_adapters(x, a, b, ranks, scales, np.array(segments), residual=res, out=res)
     assert one is res and torch.equal(res, got)
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_product_with_a_near_the_largest_number(rows):
+    """T = (2 - 2^-7 + 2^-8 + 2^-9) 2^127, which bf16 would round to infinity, B = 2^-126 and R = -4: -2^-8"""
+    K, N = 64, 136
+    x, res = torch.zeros(rows, K, device="cuda").bfloat16(), torch.full((rows, N), -4.0, device="cuda").bfloat16()
+    a, b = torch.zeros(1, 8, K, device="cuda").bfloat16(), torch.zeros(1, N, 8, device="cuda").bfloat16()
+    x[:, :3] = 2.0 ** 64
+    a[0, 0, :3] = torch.tensor([(2 - 2.0 ** -7) * 2.0 ** 63, 2.0 ** 55, 2.0 ** 54])
+    b[0, :, 0] = 2.0 ** -126
+    got = B.po_op_adapters(x, a, b, [1], [1.0], [(0, rows, 0)], residual=res)
+    assert bool((got == -(2.0 ** -8)).all()), got
